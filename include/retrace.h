@@ -423,6 +423,121 @@ retrace_status retrace_verify_noalloc(const void* logits, retrace_dtype dtype, i
                                       int32_t* committed, int32_t* bonus,
                                       int32_t* target_argmax, cudaStream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Around the round: the paged key/value cache, attention over it, sampling.
+ *
+ * What a decoding loop runs before retrace_round: a block's keys and values go
+ * into the cache, its queries attend over the cache, and the drafter's logits
+ * become the draft tokens.  Tokens of a call are packed: q, k and v are
+ * [T, heads, head_dim], and sequence b owns the rows q_start[b] ..
+ * q_start[b+1]-1 (q_start: [B+1] int32 on the device, non-decreasing, from 0 to T;
+ * NULL: T / B tokens each, T a multiple of B).  Token i of sequence b has the
+ * position cache_len[b] + i, where cache_len[b] (device) counts the tokens that
+ * were in the cache before this call's (at most 2^30), whatever the caller then
+ * makes of them: after a round it adds the committed tokens, and the next call
+ * overwrites the rejected ones.
+ * ------------------------------------------------------------------------- */
+
+/* A paged cache as the caller holds it (host struct; the pointers are device
+ * memory).  Element (page, slot, head, i) of k and v lies at
+ * page*page_stride + slot*slot_stride + head*head_stride + i; position p of
+ * sequence b is slot p % page_size of page
+ * page_table[b*table_stride + p / page_size].  A page outside [0, num_pages),
+ * or a position beyond max_pages*page_size, means that the position has no
+ * place: it is neither written nor attended to. */
+typedef struct {
+  void* k;
+  void* v;
+  int64_t page_stride, slot_stride, head_stride; /* elements, the same for k and v */
+  int num_pages, page_size, kv_heads, head_dim;
+  const int32_t* page_table; /* [B, max_pages] */
+  int64_t table_stride;      /* elements, >= max_pages */
+  int max_pages;
+  retrace_dtype dtype;
+} retrace_kv_cache;
+
+/* Appends the keys and values of T tokens to the cache, with the rotary position
+ * rotation of keys and queries on the way (one launch).
+ *   q, k, v     [T, q_heads | kv_heads, head_dim] of the cache's dtype, strides in
+ *               elements (>= 0), head_dim contiguous; they may be parts of one
+ *               projection's output.  q may be NULL (then q_out is not written).
+ *   rope        [rope_positions, rot/2, 2] fp32: cos and sin of position p and pair
+ *               a.  A pair is (i, i + rot/2) of the first `rot` dimensions, or with
+ *               interleaved != 0 (2i, 2i+1); (x, y) becomes
+ *               (x cos - y sin, y cos + x sin), in fp32 and rounded once.
+ *               Dimensions from rot on, and v, are copied.  NULL: no rotation
+ *               (rot and rope_positions are not read).
+ *   q_out       the rotated queries, strides as given; may be q itself.
+ * A token whose position is negative or not below rope_positions caches nothing,
+ * and its row of q_out is zero.  head_dim <= 256, rot even and <= head_dim.
+ * 16-byte loads where every base and stride allows them, and rot / 2 (interleaved:
+ * rot) and head_dim are whole vectors; element loads otherwise. */
+retrace_status retrace_kv_append(const void* q, int64_t q_token_stride, int64_t q_head_stride, int q_heads,
+                                 const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v,
+                                 int64_t v_token_stride, int64_t v_head_stride, const int32_t* q_start,
+                                 const int32_t* cache_len, int B, int T, const float* rope, int rope_positions,
+                                 int rot, int interleaved, const retrace_kv_cache* cache, void* q_out,
+                                 int64_t q_out_token_stride, int64_t q_out_head_stride, cudaStream_t stream);
+
+/* Bytes of workspace that retrace_attend needs, whatever the batch (0 for invalid
+ * arguments).  A workspace of its own, zeroed once with retrace_workspace_init;
+ * retrace_workspace_check reads its status word. */
+size_t retrace_attend_workspace_bytes(int q_heads, int kv_heads, int head_dim, retrace_dtype dtype);
+
+/* Attention of T packed query tokens over the cache (their own keys and values
+ * among it: call retrace_kv_append first, with the same q_start and cache_len).
+ * Query head h reads key/value head h / (q_heads / kv_heads).  The token at
+ * position p sees position j >= 0 iff
+ *     j <= p (causal != 0), or j <= cache_len[b] + n_b - 1 (causal == 0: the
+ *     block's n_b tokens see each other both ways, as a drafter's block does), and
+ *     window <= 0, or j > p - window, or j < sinks (a sliding window, and the
+ *     first `sinks` tokens that stay visible), and
+ *     j has a place in the cache.
+ *   out[t, h] = sum_j softmax_j(scale q.k_j) v_j over the visible j; zero where
+ *   nothing is visible.
+ * What lies at positions that no token of a sequence sees does not matter (slots
+ * never written, pages given away), whatever its bits.
+ *   q, out      [T, q_heads, head_dim], strides in elements, head_dim contiguous.
+ * bf16: products on tensor cores with fp32 accumulation, the softmax in fp32 with
+ * the weights rounded to bf16 before the product with v, out rounded once.  fp32:
+ * FFMA throughout.  Tensor cores need head_dim <= 128 a multiple of 8, 16-byte
+ * aligned bases and strides, page_size a multiple of 8 and at most 128 query heads
+ * per key/value head in whole groups of 8 rows (lcm(8, group) <= 128); other shapes
+ * run on FFMA.  head_dim <= 256.  One stream, no host synchronisation; the same
+ * inputs on the same device give the same bits. */
+retrace_status retrace_attend(const void* q, int64_t q_token_stride, int64_t q_head_stride, int q_heads,
+                              const int32_t* q_start, const int32_t* cache_len, int B, int T, float scale,
+                              int window, int sinks, int causal, const retrace_kv_cache* cache, void* out,
+                              int64_t out_token_stride, int64_t out_head_stride, void* ws, size_t ws_bytes,
+                              cudaStream_t stream);
+
+/* Draws one token per logits row with temperature, top-k, top-p and min-p from the
+ * caller's random numbers.  The settings are per sequence, on the device ([B];
+ * NULL: temperature 1, the filter off).
+ *   logits       [B, R, V], element (b,r,v) at b*batch_stride + r*row_stride + v.
+ *   uniforms     [B, R] fp32 in [0, 1) (values outside are taken as the nearest end;
+ *                NaN as 0).
+ *   temperature  <= 0 (or NaN): greedy, the first maximum, probability 1.
+ *   top_k        keep the top_k first tokens in descending order of logits, the
+ *                lower index first among equal ones; <= 0 or >= V: off.
+ *   top_p        of those, keep a token iff the mass before it is below top_p of
+ *                their whole mass (the first always); >= 1 or NaN: off.
+ *   min_p        of those, keep a token iff its probability is at least min_p times
+ *                the largest; <= 0 or NaN: off, above 1: as 1.
+ *   tokens       [B, R] int32 out: the first token, in index order, at which the
+ *                running sum of the kept probabilities exceeds uniform times their
+ *                sum.  -1 if every logit of the row is -inf.
+ *   probs        [B, R] fp32 out, optional: the token's probability among the kept
+ *                ones (the drafter's q of speculative sampling), 0 with token -1.
+ * A NaN logit counts as -inf; among +inf logits each has the same probability and
+ * the others none.  A token's weight is exp((logit - max) / temperature) in
+ * fp32, taken to 31 binary places, and the sums are whole numbers, so they do not
+ * depend on their order: the same inputs give the same token whatever the batch. */
+retrace_status retrace_sample(const void* logits, retrace_dtype dtype, int B, int R, int V, int64_t row_stride,
+                              int64_t batch_stride, const float* uniforms, const float* temperature,
+                              const int32_t* top_k, const float* top_p, const float* min_p, int32_t* tokens,
+                              float* probs, cudaStream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

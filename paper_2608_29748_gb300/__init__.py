@@ -12,6 +12,7 @@ __version__ = "0.1.0"
 
 def __getattr__(name):
     if name in ("retrace_verify", "retrace_align_refine", "retrace_gate_fuse", "retrace_round",
+                "retrace_kv_append", "retrace_attend", "retrace_sample", "KvCache", "AttendWorkspace",
                 "retrace_workspace_bytes", "retrace_workspace_init", "retrace_workspace_check",
                 "Workspace", "lib", "RetraceError"):
         from . import binding

@@ -62,7 +62,13 @@ def _load() -> ctypes.CDLL:
     lib.retrace_verify_plan.argtypes = [I, I, I, I, I, ctypes.POINTER(ctypes.c_int)]
     lib.retrace_round_sampled.argtypes = [P, I64, I64, P, I64, I64, P, P, F, I, F, P, P, P, I64, I64, P, P, P, F,
                                           I, I, I, I, I, P, P, P, P, P, P, SZ, P, P]
-    for name in ("retrace_workspace_init", "retrace_workspace_check", "retrace_verify",
+    lib.retrace_kv_append.argtypes = [P, I64, I64, I, P, I64, I64, P, I64, I64, P, P, I, I, P, I, I, I, P, P, I64, I64, P]
+    lib.retrace_attend_workspace_bytes.argtypes = [I, I, I, I]
+    lib.retrace_attend_workspace_bytes.restype = SZ
+    lib.retrace_attend.argtypes = [P, I64, I64, I, P, P, I, I, F, I, I, I, P, P, I64, I64, P, SZ, P]
+    lib.retrace_sample.argtypes = [P, I, I, I, I, I64, I64, P, P, P, P, P, P, P, P]
+    for name in ("retrace_kv_append", "retrace_attend", "retrace_sample",
+                 "retrace_workspace_init", "retrace_workspace_check", "retrace_verify",
                  "retrace_align_refine", "retrace_gate_fuse", "retrace_round", "retrace_round_lowrank",
                  "retrace_verify_sampled", "retrace_round_sampled", "retrace_wait_selftest",
                  "retrace_set_verify_schedule", "retrace_verify_plan"):
@@ -117,7 +123,10 @@ class Workspace:
     """Caller-owned device workspace sized for (B, K, V, d, dtype), zeroed once."""
 
     def __init__(self, B, K, V, d, dtype, device=None, stream=None):
-        self.nbytes = retrace_workspace_bytes(B, K, V, d, dtype)
+        self._allocate(retrace_workspace_bytes(B, K, V, d, dtype), device, stream)
+
+    def _allocate(self, nbytes, device, stream):
+        self.nbytes = nbytes
         if self.nbytes == 0:
             raise ValueError("invalid workspace shape")
         self.buf = torch.empty(self.nbytes + 256, dtype=torch.uint8, device=device or "cuda")
@@ -376,3 +385,121 @@ def run_round_sampled(x: dict, s: dict, ws: Workspace, out: RoundBuffers | None 
                           out.committed, out.bonus, out.e_out, ws, n_out=out.n, phase_events=phase_events,
                           stream=stream)
     return out
+
+
+# ---- around the round: paged cache, attention over it, sampling ---------------
+
+
+class _KvCacheStruct(ctypes.Structure):  # retrace_kv_cache (include/retrace.h)
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_stride", ctypes.c_int64),
+                ("slot_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("num_pages", ctypes.c_int),
+                ("page_size", ctypes.c_int), ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
+                ("page_table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("max_pages", ctypes.c_int),
+                ("dtype", ctypes.c_int)]
+
+
+class KvCache:
+    """A paged cache: k and v [num_pages, page_size, kv_heads, head_dim] (any strides,
+    the same for both, head_dim contiguous) and page_table [B, max_pages] int32.  Keeps the
+    tensors; their contents may change between calls."""
+
+    def __init__(self, k, v, page_table):
+        if k.dim() != 4 or v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype or k.stride(3) != 1:
+            raise ValueError("k and v must be [pages, page_size, kv_heads, head_dim] of one dtype and layout, head_dim contiguous")
+        _int32(page_table, "page_table")
+        if page_table.dim() != 2 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+            raise ValueError("page_table must be [B, max_pages], the pages of a sequence contiguous")
+        self.k, self.v, self.page_table = k, v, page_table
+        self.B, self.kv_heads, self.head_dim, self.dtype = page_table.shape[0], k.shape[2], k.shape[3], k.dtype
+        self.struct = _KvCacheStruct(_ptr(k), _ptr(v), k.stride(0), k.stride(1), k.stride(2), k.shape[0], k.shape[1],
+                                     k.shape[2], k.shape[3], _ptr(page_table), max(page_table.stride(0), page_table.shape[1]),
+                                     page_table.shape[1], _dtype_code(k))
+        self.ref = ctypes.addressof(self.struct)
+
+
+def _packed(t, heads, T, cache, name):
+    if t.dim() != 3 or t.shape[0] != T or t.shape[2] != cache.head_dim or t.dtype != cache.dtype or \
+            (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{name} must be [{T}, {heads or 'heads'}, {cache.head_dim}] of the cache's dtype")
+    if t.stride(2) != 1:
+        raise ValueError(f"{name}: head_dim must be contiguous")
+
+
+def _lengths(cache, cache_len, q_start):
+    _int32(cache_len, "cache_len")
+    if cache_len.shape != (cache.B,) or not cache_len.is_contiguous():
+        raise ValueError("cache_len must be a contiguous [B], B the rows of the page table")
+    if q_start is not None:
+        _int32(q_start, "q_start")
+        if q_start.shape != (cache.B + 1,) or not q_start.is_contiguous():
+            raise ValueError("q_start must be a contiguous [B + 1]")
+
+
+def retrace_kv_append(q, k, v, cache: KvCache, cache_len, rope, q_out=None, q_start=None, interleaved=False, stream=None):
+    """Appends k and v [T, kv_heads, head_dim] to the cache, rotating k and q [T, q_heads, head_dim]
+    (optional, into q_out) by rope [positions, rot/2, 2] (None: no rotation) on the way (see
+    include/retrace.h)."""
+    T = k.shape[0]
+    _packed(k, cache.kv_heads, T, cache, "k")
+    _packed(v, cache.kv_heads, T, cache, "v")
+    _lengths(cache, cache_len, q_start)
+    q_heads, qs, os = 0, (0, 0), (0, 0)
+    if q is not None:
+        q_heads = q.shape[1]
+        _packed(q, None, T, cache, "q")
+        _packed(q_out, q_heads, T, cache, "q_out")
+        qs, os = q.stride(), q_out.stride()
+    positions = rot = 0
+    if rope is not None:
+        if rope.dtype != torch.float32 or rope.dim() != 3 or rope.shape[2] != 2 or not rope.is_contiguous():
+            raise ValueError("rope must be a contiguous float32 [positions, rot/2, 2]")
+        positions, rot = rope.shape[0], 2 * rope.shape[1]
+    ks, vs = k.stride(), v.stride()
+    _check(lib.retrace_kv_append(_ptr(q), qs[0], qs[1], q_heads, _ptr(k), ks[0], ks[1], _ptr(v), vs[0], vs[1], _ptr(q_start),
+                                 _ptr(cache_len), cache.B, T, _ptr(rope), positions, rot, int(interleaved), cache.ref,
+                                 _ptr(q_out) if q is not None else None, os[0], os[1], _stream(stream)))
+
+
+class AttendWorkspace(Workspace):
+    """Workspace of retrace_attend: one serves every call of these head counts and size."""
+
+    def __init__(self, q_heads, kv_heads, head_dim, dtype, device=None, stream=None):
+        code = RETRACE_BF16 if dtype == torch.bfloat16 else RETRACE_F32
+        self._allocate(int(lib.retrace_attend_workspace_bytes(q_heads, kv_heads, head_dim, code)), device, stream)
+
+
+def retrace_attend(q, cache: KvCache, cache_len, out, ws: AttendWorkspace, q_start=None, scale=None, window=0, sinks=0,
+                   causal=True, stream=None):
+    """Attention of q [T, q_heads, head_dim] over the cache into out (see include/retrace.h);
+    scale defaults to head_dim ** -0.5."""
+    T, q_heads, D = q.shape
+    _packed(q, None, T, cache, "q")
+    _packed(out, q_heads, T, cache, "out")
+    _lengths(cache, cache_len, q_start)
+    qs, os = q.stride(), out.stride()
+    _check(lib.retrace_attend(_ptr(q), qs[0], qs[1], q_heads, _ptr(q_start), _ptr(cache_len), cache.B, T,
+                              D ** -0.5 if scale is None else float(scale), int(window), int(sinks), int(causal), cache.ref,
+                              _ptr(out), os[0], os[1], ws.ptr, ws.nbytes, _stream(stream)))
+
+
+def _setting(t, B, dtype, name):
+    if t is None:
+        return None
+    if t.dtype != dtype or t.shape != (B,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous [B] {dtype}")
+    return _ptr(t)
+
+
+def retrace_sample(logits, uniforms, tokens, probs=None, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
+    """Draws tokens [B, R] from logits [B, R, V] with the settings of each sequence ([B]) and the
+    given uniforms [B, R] (see include/retrace.h)."""
+    B, R, V = logits.shape
+    if logits.stride(2) != 1:
+        raise ValueError("logits: vocabulary dimension must be contiguous")
+    for t, dtype, name in ((uniforms, torch.float32, "uniforms"), (tokens, torch.int32, "tokens"), (probs, torch.float32, "probs")):
+        if t is not None and (t.dtype != dtype or t.shape != (B, R) or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous [B, R] {dtype}")
+    _check(lib.retrace_sample(_ptr(logits), _dtype_code(logits), B, R, V, logits.stride(1), logits.stride(0), _ptr(uniforms),
+                              _setting(temperature, B, torch.float32, "temperature"), _setting(top_k, B, torch.int32, "top_k"),
+                              _setting(top_p, B, torch.float32, "top_p"), _setting(min_p, B, torch.float32, "min_p"),
+                              _ptr(tokens), _ptr(probs), _stream(stream)))

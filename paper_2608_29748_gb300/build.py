@@ -20,7 +20,8 @@ ROOT = os.path.dirname(PKG)
 INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(PKG, "_build")
 LIB_PATH = os.path.join(PKG, "libretrace.so")
-SOURCES = ["api.cu", "verify.cu", "cond_simt.cu", "cond_tc.cu", "verify_noalloc.cu", "lowrank.cu", "verify_sampled.cu"]
+SOURCES = ["api.cu", "verify.cu", "cond_simt.cu", "cond_tc.cu", "verify_noalloc.cu", "lowrank.cu", "verify_sampled.cu",
+           "serve/serve_api.cu", "serve/kv_append.cu", "serve/attend_simt.cu", "serve/sample.cu"]
 ARCH = "-gencode=arch=compute_103a,code=sm_103a"
 NVCC_FLAGS = [
     "-O3",
@@ -42,7 +43,8 @@ def _nvcc() -> str:
 
 
 def _inputs() -> list[str]:
-    files = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cu", ".cuh", ".h"))]
+    files = [os.path.join(where, f) for where in (CSRC, os.path.join(CSRC, "serve")) for f in os.listdir(where)
+             if f.endswith((".cu", ".cuh", ".h"))]
     files.append(os.path.join(INCLUDE, "retrace.h"))
     files.append(os.path.abspath(__file__))
     return files
@@ -63,7 +65,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     os.makedirs(BUILD_DIR, exist_ok=True)
 
     def compile_one(src: str) -> tuple[str, str]:
-        obj = os.path.join(BUILD_DIR, src.replace(".cu", ".o"))
+        obj = os.path.join(BUILD_DIR, os.path.basename(src).replace(".cu", ".o"))
         cmd = [nvcc, *NVCC_FLAGS, "-I", INCLUDE, "-c", os.path.join(CSRC, src), "-o", obj]
         res = subprocess.run(cmd, capture_output=True, text=True)
         if res.returncode != 0:
