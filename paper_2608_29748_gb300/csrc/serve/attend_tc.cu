@@ -1,0 +1,745 @@
+// Attention over the paged cache on the tensor cores (bf16).
+//
+// A row is a query token under one query head; the rows of a tile (128, a TMEM lane
+// each) share a key/value head.  Per tile of 128 keys a stream computes
+//     S = Q K^T        tcgen05.mma, Q and K from shared memory, S in TMEM (fp32)
+//     m, p, l          one thread per row: running maximum, p = 2^(s - m), running sum
+//     O += P V         tcgen05.mma, P (bf16) from TMEM over S's columns, V from shared
+//                      memory as it lies (keys by head dimension), O in TMEM (fp32)
+// A CTA runs two streams, so that one's matrix products run during the other's softmax:
+// two row tiles over the same key tiles where a unit has more than 128 rows (prompts),
+// or the even and the odd key tiles of one row tile (tokens, blocks), joined at the end.
+// The maximum that the exponents refer to is raised, and O rescaled, only where a row
+// would otherwise pass 2^8 of it: the first tile and few others.
+//
+// Warp 0 copies K and V tiles into a ring with TMA, a box for each run of slots
+// within a page; warp 1 issues the products; warps 4-7 and 8-11 are the streams' softmax.
+// A tile of keys is 4 D 128 bytes of HBM traffic against 2 x 128 x 128 x D products of a
+// tensor core that does 8192 flop a cycle: 1024 of the 2790 cycles that the bytes take
+// at D = 128, so tokens and blocks are bound by HBM, and a row tile that is not full costs
+// nothing.
+#include <math.h>
+
+#include "../tc_pair.cuh"
+#include "attend_plan.cuh"
+#include "serve.h"
+
+namespace retrace {
+namespace {
+
+constexpr int kThreads = 384;
+constexpr int kKeys = 128;  // keys of a tile
+constexpr int kRows = 128;  // rows of a tile
+constexpr int kMasks = 16;  // ring of page masks: more than the tiles between loading and softmax
+
+struct TcParams {
+  AttendArgs a;
+  AttendShape shape;  // unit_tokens = 2 tile_tokens
+  int group;          // query heads of a key/value head
+  int tile_tokens;    // tokens of a row tile
+  int q_box;          // tokens of a Q box
+  int kv_box;         // slots of a K or V box: they lie within a page and divide a tile
+  float scale2;       // |scale| log2(e)
+  int negate;         // scale < 0
+};
+
+template <int DP>
+struct TcShape {
+  static constexpr int kTileBytes = kKeys * DP * 2;
+  static constexpr int kStages = DP == 64 ? 10 : 5;
+  static constexpr int kHalves = DP / 64;              // 128-byte columns of a tile
+  static constexpr int kHalfBytes = kKeys * 128;
+  static constexpr int kQOffset = kStages * kTileBytes;  // after the ring
+  static constexpr int kControl = kQOffset + 2 * kRows * DP * 2;
+  static constexpr int kPartRows = 2 * kRows;
+  static constexpr int kPart = kPartRows * (DP + 2);  // floats of a part
+};
+
+struct Control {
+  uint64_t full[10], empty[10];  // the ring
+  uint64_t q_full, q_empty;
+  uint64_t s_full[2];  // S of a tile ready (and the product before it done), or O complete
+  uint64_t p_full[2];  // P written, O rescaled
+  uint64_t done;       // after an expired wait: the issued products
+  PlanStart plan;
+  long long sum[kThreads / 32];
+  uint32_t tmem;
+  int abort;
+  int last;
+  uint32_t mask[kMasks];  // of a key tile: bit i: box i has a page
+  float2 stat[2][kRows];  // m and l of a stream's rows
+};
+
+// ---- instructions -------------------------------------------------------------
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar)
+      : "memory");
+}
+// D[tmem] (+)= A[tmem] * B[smem], bf16 inputs, fp32 accumulation.
+__device__ __forceinline__ void tc_mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
+                                               uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// 32 consecutive columns of each thread's lane, without waiting for them.
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, float* v) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(v);
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, float (&v)[8]) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7])
+               : "r"(taddr)
+               : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const float (&v)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(taddr), "f"(v[0]), "f"(v[1]),
+               "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+               : "memory");
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// A bounded wait that every lane of the warp polls; all of them agree on the outcome.
+__device__ __forceinline__ bool warp_wait_all(uint64_t* bar, uint32_t parity, volatile int* abort) {
+  const bool ok = mbar_wait_bounded(smem_u32(bar), parity, abort);
+  return __all_sync(0xFFFFFFFFu, ok);
+}
+__device__ __forceinline__ void named_barrier(int id, int threads) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+
+// Descriptor of V [keys, 64-element columns] as the MN-major operand: rows of 128
+// bytes with the 128-byte swizzle; 64-element blocks of the head dimension 16 KB apart
+// (leading offset), groups of 8 keys 1024 bytes apart (stride offset).
+__device__ __forceinline__ uint64_t sw128_mnmajor_desc(uint32_t saddr) {
+  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)((kKeys * 128) >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 |
+         (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+constexpr uint32_t kMajorB = 1u << 16;  // instruction descriptor: B is MN-major
+
+// The key tiles of a piece in the order in which the products take them from the ring:
+// with two row tiles K0 V0 K1 V1 ..., with one K0 K1 V0 K2 V1 ... .
+__device__ __forceinline__ int v_position(int j, int tiles, bool two) {
+  return two ? 2 * j + 1 : (j + 1 < tiles ? 2 * j + 2 : 2 * j + 1);
+}
+
+// Bits c of a word of 32 keys: key c is visible iff c <= hi and (c >= lo or c < sinks).
+__device__ __forceinline__ uint32_t seen_word(int hi, int lo, int sinks) {
+  const uint32_t h = hi < 0 ? 0u : hi >= 31 ? ~0u : (2u << hi) - 1u;
+  const uint32_t l = lo <= 0 ? ~0u : lo >= 32 ? 0u : ~0u << lo;
+  const uint32_t k = sinks <= 0 ? 0u : sinks >= 32 ? ~0u : (1u << sinks) - 1u;
+  return h & (l | k);
+}
+// Bits of the keys of word w that have a page, from a bit per box of `box` keys.
+__device__ __forceinline__ uint32_t page_word(uint32_t boxes, int box, int w) {
+  if (box >= 32) return boxes >> (w * 32 / box) & 1u ? ~0u : 0u;
+  uint32_t x = 0;
+  const uint32_t ones = (1u << box) - 1u;
+  for (int i = 0; i < 32 / box; ++i)
+    if (boxes >> (w * (32 / box) + i) & 1u) x |= ones << (i * box);
+  return x;
+}
+__device__ __forceinline__ uint32_t boxes_mask(int boxes) { return (1u << boxes) - 1u; }
+
+template <int DP>
+__global__ void __launch_bounds__(kThreads, 1)
+    attend_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
+                     const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ TcParams P) {
+  using Sh = TcShape<DP>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  Control& ct = *reinterpret_cast<Control*>(smem + Sh::kControl);
+  volatile int* abort = &ct.abort;
+  const uint32_t base = smem_u32(smem);
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+  const AttendArgs& a = P.a;
+
+  if (tid == 0) {
+    ct.abort = 0;
+    for (int s = 0; s < Sh::kStages; ++s) {
+      mbar_init(smem_u32(&ct.full[s]), 1);
+      mbar_init(smem_u32(&ct.empty[s]), 1);
+    }
+    mbar_init(smem_u32(&ct.q_full), 1);
+    mbar_init(smem_u32(&ct.q_empty), 1);
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(smem_u32(&ct.s_full[s]), 1);
+      mbar_init(smem_u32(&ct.p_full[s]), 4);  // one arrival per warp of the stream
+    }
+    mbar_init(smem_u32(&ct.done), 1);
+    fence_mbar_init();
+    tma_prefetch_desc(&tm_q);
+    tma_prefetch_desc(&tm_k);
+    tma_prefetch_desc(&tm_v);
+  }
+  if (warp == 2) {
+    tmem_alloc(smem_u32(&ct.tmem), 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = ct.tmem;
+  pdl_wait();
+  plan_start<kThreads>(P.shape, gridDim.x, 2, &ct.plan, ct.sum);
+  const PlanStart& plan = ct.plan;
+  PieceWalk walk;
+  walk.start(plan);
+  Piece pc;
+
+  if (warp == 0) {
+    // ---- copies: lane (half, box) loads one box of a tile ----
+    const int boxes = kKeys / P.kv_box, half = lane / 16, box = lane % 16;
+    const bool active = box < boxes && half < Sh::kHalves;
+    const int page_size = a.cache.page_size;
+    uint32_t it = 0, pieces = 0, tiles = 0;
+    bool ok = true;
+    while (ok && walk.next(P.shape, plan, &pc)) {
+      const int nt = pc.k1 - pc.k0;
+      if (nt == 0) continue;
+      const int tokens = pc.i1 - pc.i0;
+      const bool two = tokens > P.tile_tokens;
+      auto page_at = [&](int k) {  // of this lane's box of the piece's tile k
+        if (!active || k >= nt) return -1;
+        const int j = pc.keys.tile(pc.k0 + k) * kKeys + box * P.kv_box;
+        return page_of(a.cache, pc.b, j / page_size);
+      };
+      auto load = [&](const CUtensorMap* map, int k, int page, bool keys) {
+        const uint32_t slot = it % Sh::kStages, phase = (it / Sh::kStages) & 1u;
+        if (!warp_wait_all(&ct.empty[slot], phase ^ 1u, abort)) return false;
+        const uint32_t bar = smem_u32(&ct.full[slot]);
+        const uint32_t placed = __ballot_sync(0xFFFFFFFFu, active && half == 0 && page >= 0);
+        if (lane == 0) {
+          if (keys) ct.mask[tiles % kMasks] = placed;
+          mbar_arrive_expect_tx(bar, Sh::kTileBytes);
+        }
+        __syncwarp();
+        if (active) {
+          const int j = pc.keys.tile(pc.k0 + k) * kKeys + box * P.kv_box;
+          // a box without a page lies outside the tensor: zeros
+          tma_load_4d(base + slot * Sh::kTileBytes + half * Sh::kHalfBytes + box * P.kv_box * 128, map, half * 64, pc.head,
+                      j % page_size, page >= 0 ? page : a.cache.num_pages, bar);
+        }
+        ++it;
+        if (keys) ++tiles;
+        return true;
+      };
+      int page = page_at(0);
+      ok = warp_wait_all(&ct.q_empty, (pieces & 1u) ^ 1u, abort);
+      if (!ok) break;
+      ++pieces;
+      // Q: boxes of q_box tokens times the head group, rows in order
+      const int b0 = (min(tokens, P.tile_tokens) + P.q_box - 1) / P.q_box;
+      const int b1 = two ? (tokens - P.tile_tokens + P.q_box - 1) / P.q_box : 0;
+      const int box_rows = P.q_box * P.group;
+      if (lane == 0) mbar_arrive_expect_tx(smem_u32(&ct.q_full), (b0 + b1) * Sh::kHalves * box_rows * 128);
+      __syncwarp();
+      for (int i = lane; i < (b0 + b1) * Sh::kHalves; i += 32) {
+        const int h = i % Sh::kHalves, x = i / Sh::kHalves, tile = x >= b0, n = tile ? x - b0 : x;
+        tma_load_3d(base + Sh::kQOffset + tile * (kRows * DP * 2) + h * Sh::kHalfBytes + n * box_rows * 128, &tm_q, h * 64,
+                    pc.head * P.group, pc.row0 + pc.i0 + tile * P.tile_tokens + n * P.q_box, smem_u32(&ct.q_full));
+      }
+      if (two) {
+        for (int k = 0; k < nt && ok; ++k) {
+          const int next = page_at(k + 1);
+          ok = load(&tm_k, k, page, true) && load(&tm_v, k, page, false);
+          page = next;
+        }
+      } else {
+        ok = load(&tm_k, 0, page, true);
+        for (int k = 0; k < nt && ok; ++k) {
+          const int next = page_at(k + 1);
+          if (k + 1 < nt) ok = load(&tm_k, k + 1, next, true);
+          ok = ok && load(&tm_v, k, page, false);
+          page = next;
+        }
+      }
+    }
+    if (!ok) {
+      if (lane == 0) raise_abort(abort, a.status);
+      volatile int never = 0;  // this CTA's copies in flight
+      const uint32_t first = it > Sh::kStages ? it - Sh::kStages : 0;
+      for (uint32_t k = first; k < it; ++k)
+        mbar_wait_bounded(smem_u32(&ct.full[k % Sh::kStages]), (k / Sh::kStages) & 1u, &never);
+      if (pieces) mbar_wait_bounded(smem_u32(&ct.q_full), (pieces - 1) & 1u, &never);
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    // ---- products ----
+    constexpr uint32_t kS = idesc_bf16_f32(kRows, kKeys), kPV = idesc_bf16_f32(kRows, DP) | kMajorB;
+    uint32_t it = 0, pieces = 0, np[2] = {0, 0};
+    bool ok = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      ok = ok && warp_wait_all(bar, parity, abort);
+      return ok;
+    };
+    auto wait_tile = [&](uint32_t n) { return wait(&ct.full[n % Sh::kStages], (n / Sh::kStages) & 1u); };
+    auto tile = [&](uint32_t n) { return base + n % Sh::kStages * Sh::kTileBytes; };
+    auto scores = [&](int s, int q, uint32_t k_tile) {
+      if (elect_one()) {
+        const uint64_t qd = sw128_kmajor_desc(base + Sh::kQOffset + q * (kRows * DP * 2)), kd = sw128_kmajor_desc(k_tile);
+#pragma unroll
+        for (int h = 0; h < Sh::kHalves; ++h)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            tc_mma_bf16(tmem + s * 128, qd + h * (Sh::kHalfBytes >> 4) + 2 * k, kd + h * (Sh::kHalfBytes >> 4) + 2 * k, kS,
+                        h + k > 0);
+      }
+      __syncwarp();
+    };
+    auto values = [&](int s, uint32_t v_tile, bool first) {
+      if (elect_one()) {
+        const uint64_t vd = sw128_mnmajor_desc(v_tile);
+#pragma unroll
+        for (int k = 0; k < kKeys / 16; ++k)
+          tc_mma_bf16_ts(tmem + 256 + s * 128, tmem + s * 128 + k * 8, vd + k * (2048 >> 4), kPV, !(first && k == 0));
+      }
+      __syncwarp();
+    };
+    auto commit = [&](uint64_t* bar) {
+      if (elect_one()) tc_commit(smem_u32(bar));
+      __syncwarp();
+    };
+    while (ok && walk.next(P.shape, plan, &pc)) {
+      const int nt = pc.k1 - pc.k0;
+      if (nt == 0) continue;
+      const bool two = pc.i1 - pc.i0 > P.tile_tokens;
+      if (!wait(&ct.q_full, pieces & 1u)) break;
+      ++pieces;
+      tc_fence_after();
+      if (two) {
+        for (int j = 0; j <= nt && ok; ++j) {  // the products of tile j - 1 with V, then the scores of tile j
+          const uint32_t v = it + 2 * (j - 1) + 1, k = it + 2 * j;
+          if (j > 0 && !wait_tile(v)) break;
+          if (j < nt && !wait_tile(k)) break;
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            if (j > 0) {
+              if (!wait(&ct.p_full[s], np[s]++ & 1u)) break;
+              tc_fence_after();
+              values(s, tile(v), j == 1);
+              if (s == 1) commit(&ct.empty[v % Sh::kStages]);
+            }
+            if (j < nt) scores(s, s, tile(k));
+            commit(&ct.s_full[s]);
+          }
+          if (j < nt && ok) commit(&ct.empty[k % Sh::kStages]);
+          if (j == nt - 1) commit(&ct.q_empty);
+        }
+      } else {
+        for (int j = 0; j < nt + 2 && ok; ++j) {
+          const int s = j & 1;
+          if (j >= 2) {
+            const uint32_t v = it + v_position(j - 2, nt, false);
+            if (!wait_tile(v) || !wait(&ct.p_full[s], np[s]++ & 1u)) break;
+            tc_fence_after();
+            values(s, tile(v), j < 4);
+            commit(&ct.empty[v % Sh::kStages]);
+          }
+          if (j < nt) {
+            const uint32_t k = it + (j == 0 ? 0 : 2 * j - 1);
+            if (!wait_tile(k)) break;
+            tc_fence_after();
+            scores(s, 0, tile(k));
+            commit(&ct.empty[k % Sh::kStages]);
+            if (j == nt - 1) commit(&ct.q_empty);
+          }
+          if (j >= 2 || j < nt) commit(&ct.s_full[s]);
+        }
+      }
+      it += 2 * nt;
+    }
+    if (!ok) {
+      if (lane == 0) raise_abort(abort, a.status);
+      volatile int never = 0;
+      commit(&ct.done);
+      mbar_wait_bounded(smem_u32(&ct.done), 0, &never);
+    }
+    __syncwarp();
+  } else if (warp >= 4) {
+    // ---- softmax: stream s, one thread per row ----
+    const int s = warp >= 8, row = tid & 127;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const uint32_t t_s = tmem + lanes + s * 128, t_o = tmem + lanes + 256 + s * 128;
+    const int G = P.group, D = a.cache.head_dim;
+    const float sl = P.scale2;
+    uint32_t it = 0, ns = 0, tiles = 0;
+    bool ok = true;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      if (ok && !warp_wait_all(bar, parity, abort)) {
+        ok = false;
+        if (lane == 0) raise_abort(abort, a.status);
+      }
+    };
+    while (walk.next(P.shape, plan, &pc)) {
+      const int nt = pc.k1 - pc.k0, tokens = pc.i1 - pc.i0;
+      const bool two = tokens > P.tile_tokens;
+      const int t0 = two ? s * P.tile_tokens : 0;                                       // first token of this stream's tile
+      const int rows = (two && s == 1 ? tokens - P.tile_tokens : min(tokens, P.tile_tokens)) * G;
+      const bool valid = row < rows, busy = (row & ~31) < rows;                          // this row, this warp
+      const int p = pc.c + pc.i0 + t0 + row / G;
+      const int hi = !valid ? -1 : a.causal ? p : pc.c + pc.n - 1, lo = a.window > 0 ? p - a.window + 1 : 0;
+      const long long at = (long long)(pc.row0 + pc.i0 + t0 + row / G) * a.out_token + (pc.head * G + row % G) * (long long)a.out_head;
+      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + at;
+      if (nt == 0) {  // nothing is visible
+        if (valid && (two || s == 0) && ok)
+          for (int c = 0; c < D; c += 8) *reinterpret_cast<uint4*>(out + c) = make_uint4(0u, 0u, 0u, 0u);
+        continue;
+      }
+      float m = -INFINITY, l = 0.f;  // of the raw scores; the sum of 2^((score - m) sl)
+      int done = 0;
+      for (int j = two ? 0 : s; j < nt; j += two ? 1 : 2) {
+        const int tile = pc.keys.tile(pc.k0 + j), j0 = tile * kKeys;
+        wait(&ct.s_full[s], ns++ & 1u);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t pages = ct.mask[(tiles + j) % kMasks];
+        // A row of V that no row of the unit sees holds anything, and 0 times that need not
+        // be 0: cleared before the product.
+        if (j0 < pc.keys.lo || j0 + kKeys - 1 > pc.keys.hi) {
+          const uint32_t v = it + v_position(j, nt, two), slot = v % Sh::kStages;
+          wait(&ct.full[slot], (v / Sh::kStages) & 1u);
+          if (!ok) break;
+          const int key = j0 + row;
+          if (key > pc.keys.hi || (key < pc.keys.lo && key >= a.sinks)) {
+#pragma unroll
+            for (int h = 0; h < Sh::kHalves; ++h)
+#pragma unroll
+              for (int c = 0; c < 8; ++c)
+                *reinterpret_cast<uint4*>(smem + slot * Sh::kTileBytes + h * Sh::kHalfBytes + row * 128 + c * 16) =
+                    make_uint4(0u, 0u, 0u, 0u);
+          }
+          fence_proxy_async_shared();
+        }
+        if (busy) {
+          float v[kKeys];
+#pragma unroll
+          for (int c = 0; c < kKeys; c += 32) tmem_ld32(t_s + c, v + c);
+          tmem_wait_ld();
+          if (P.negate) {
+#pragma unroll
+            for (int c = 0; c < kKeys; ++c) v[c] = -v[c];
+          }
+          const uint32_t all = boxes_mask(kKeys / P.kv_box);
+          const bool whole = j0 + kKeys - 1 <= hi && (j0 >= lo || j0 + kKeys <= a.sinks) && pages == all;
+          if (!__all_sync(0xFFFFFFFFu, whole)) {
+#pragma unroll
+            for (int w = 0; w < kKeys / 32; ++w) {
+              const uint32_t see = seen_word(hi - j0 - 32 * w, lo - j0 - 32 * w, a.sinks - j0 - 32 * w) &
+                                   page_word(pages, P.kv_box, w);
+#pragma unroll
+              for (int c = 0; c < 32; ++c)
+                if (!(see >> c & 1u)) v[32 * w + c] = -INFINITY;
+            }
+          }
+          float top = v[0];
+#pragma unroll
+          for (int c = 1; c < kKeys; ++c) top = fmaxf(top, v[c]);
+          if (done == 0) {
+            m = top;
+          } else {
+            const bool raise = (top - m) * sl > 8.f;
+            if (__any_sync(0xFFFFFFFFu, raise)) {
+              const float up = fmaxf(m, top), f = raise ? exp2_fast((m - up) * sl) : 1.f;
+              if (raise) m = up;
+              l *= f;
+#pragma unroll
+              for (int c = 0; c < DP; c += 8) {
+                float o[8];
+                tmem_ld8(t_o + c, o);
+                tmem_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] *= f;
+                tmem_st8(t_o + c, o);
+              }
+            }
+          }
+          const float ref = m == -INFINITY ? 0.f : m * sl;
+          float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int c = 0; c < kKeys; c += 32) {
+            uint32_t w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float x = exp2_fast(fmaf(v[c + 2 * i], sl, -ref)), y = exp2_fast(fmaf(v[c + 2 * i + 1], sl, -ref));
+              sum[i & 1] += x;
+              sum[2 + (i & 1)] += y;
+              w[i] = pack_bf16x2(x, y);
+            }
+            tmem_st16(t_s + c / 2, w);
+          }
+          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+          tmem_wait_st();
+        }
+        ++done;
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&ct.p_full[s]));
+      }
+      if (done && ok) {
+        wait(&ct.s_full[s], ns++ & 1u);  // O is complete
+        tc_fence_after();
+      }
+      it += 2 * nt;
+      tiles += nt;
+
+      const bool whole = pc.pieces == 1;
+      float* part = a.partials + ((long long)blockIdx.x * 2 + (pc.k0 == 0 ? 1 : 0)) * Sh::kPart;
+      // Columns [c0, c1) of this thread's row: into the output, or into the part.
+      auto put = [&](int c, const float (&o)[32], float inv) {
+        if (!valid || !ok) return;
+        if (whole) {
+#pragma unroll
+          for (int i = 0; i < 32; i += 8) {
+            if (c + i >= D) break;
+            uint4 x;
+            x.x = pack_bf16x2(o[i] * inv, o[i + 1] * inv);
+            x.y = pack_bf16x2(o[i + 2] * inv, o[i + 3] * inv);
+            x.z = pack_bf16x2(o[i + 4] * inv, o[i + 5] * inv);
+            x.w = pack_bf16x2(o[i + 6] * inv, o[i + 7] * inv);
+            *reinterpret_cast<uint4*>(out + c + i) = x;
+          }
+        } else {
+          float* to = part + ((two ? s * kRows : 0) + row) * DP + c;
+#pragma unroll
+          for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(to + i) = make_float4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+        }
+      };
+      auto put_stat = [&](float mm, float ll) {
+        if (valid && !whole && ok)
+          *reinterpret_cast<float2*>(part + Sh::kPartRows * DP + ((two ? s * kRows : 0) + row) * 2) = make_float2(mm * sl, ll);
+      };
+      if (two) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        if (busy && ok) {
+#pragma unroll
+          for (int c = 0; c < DP; c += 32) {
+            float o[32];
+            tmem_ld32(t_o + c, o);
+            tmem_wait_ld();
+            put(c, o, inv);
+          }
+        }
+        put_stat(m, l);
+      } else {
+        // The two streams hold parts of the same rows: each joins half of the columns.
+        ct.stat[s][row] = make_float2(done ? m : -INFINITY, l);
+        tc_fence_before();
+        named_barrier(1, 256);
+        tc_fence_after();
+        const float2 x0 = ct.stat[0][row], x1 = ct.stat[1][row];
+        const float top = fmaxf(x0.x, x1.x);
+        const float f0 = x0.x == -INFINITY ? 0.f : exp2_fast((x0.x - top) * sl);
+        const float f1 = x1.x == -INFINITY ? 0.f : exp2_fast((x1.x - top) * sl);
+        const float sum = x0.y * f0 + x1.y * f1, inv = sum == 0.f ? 0.f : 1.f / sum;
+        if (busy && ok) {
+#pragma unroll
+          for (int c = 0; c < DP / 2; c += 32) {
+            const int col = s * (DP / 2) + c;
+            float o[32], y[32];
+            tmem_ld32(tmem + lanes + 256 + col, o);
+            if (nt > 1) tmem_ld32(tmem + lanes + 384 + col, y);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = nt > 1 ? o[i] * f0 + y[i] * f1 : o[i] * f0;
+            put(col, o, inv);
+          }
+        }
+        if (s == 0) put_stat(top, sum);
+        tc_fence_before();
+        named_barrier(1, 256);  // both are through with O and the statistics
+        tc_fence_after();
+      }
+      if (whole) continue;
+
+      // The last of the CTAs that share the unit joins their parts, in the order of their
+      // ranges.
+      __threadfence();
+      named_barrier(1, 256);
+      if (tid == 128) ct.last = !*abort && atomicAdd(a.tickets + pc.first_cta, 1u) == (uint32_t)(pc.pieces - 1);
+      named_barrier(1, 256);
+      const bool last = ct.last;
+      named_barrier(1, 256);  // `last` is read before the next piece writes it
+      if (!last) continue;
+      __threadfence();
+      if (tid == 128) a.tickets[pc.first_cta] = 0u;
+      constexpr int kLanes = DP / 4;  // threads of a row
+      const int first_rows = min(tokens, P.tile_tokens) * G, all_rows = tokens * G;
+      const int col = (tid - 128) % kLanes * 4;
+      for (int r = (tid - 128) / kLanes; r < all_rows; r += 256 / kLanes) {
+        const int tile = r >= first_rows, tr = tile ? r - first_rows : r, slot = tile * kRows + tr;
+        float top = -INFINITY, sum = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int x = 0; x < pc.pieces; ++x) {
+          const float* from = a.partials + ((long long)(pc.first_cta + x) * 2 + (x == 0 ? 1 : 0)) * Sh::kPart;
+          const float2 st = __ldcg(reinterpret_cast<const float2*>(from + Sh::kPartRows * DP + slot * 2));
+          const float4 y = __ldcg(reinterpret_cast<const float4*>(from + slot * DP + col));
+          if (st.x == -INFINITY) continue;
+          const float up = fmaxf(top, st.x), f = exp2_fast(top - up), g = exp2_fast(st.x - up);
+          top = up;
+          sum = sum * f + st.y * g;
+          o.x = o.x * f + y.x * g;
+          o.y = o.y * f + y.y * g;
+          o.z = o.z * f + y.z * g;
+          o.w = o.w * f + y.w * g;
+        }
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        const int token = pc.row0 + pc.i0 + r / G;  // rows run on over the tiles: tile_tokens * G of the first
+        if (col < D)
+          *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + (long long)token * a.out_token +
+                                    (pc.head * G + r % G) * (long long)a.out_head + col) =
+              make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 2) tmem_dealloc(tmem, 512);
+}
+
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                             const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                             CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeFn encode_fn() {
+  static std::atomic<EncodeFn> fn{nullptr};
+  EncodeFn f = fn.load(std::memory_order_acquire);
+  if (!f) {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &q) == cudaSuccess &&
+        q == cudaDriverEntryPointSuccess) {
+      f = reinterpret_cast<EncodeFn>(p);
+      fn.store(f, std::memory_order_release);
+    }
+  }
+  return f;
+}
+
+// A bf16 tensor with `rank` dimensions, strides (elements) of all but the first; boxes
+// with the 128-byte swizzle.
+bool encode(CUtensorMap* map, const void* base, int rank, const long long* dims, const long long* strides, const int* box) {
+  EncodeFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t d[4], st[3];
+  cuuint32_t b[4], one[4];
+  for (int i = 0; i < rank; ++i) {
+    d[i] = (cuuint64_t)dims[i];
+    b[i] = (cuuint32_t)box[i];
+    one[i] = 1;
+    if (i > 0) st[i - 1] = dims[i] > 1 ? (cuuint64_t)strides[i] * 2 : 16;  // the stride of a single one is not used
+  }
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), d, st, b, one,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int gcd(int a, int b) { return b ? gcd(b, a % b) : a; }
+
+template <int DP>
+cudaError_t launch(TcParams& p, cudaStream_t stream) {
+  using Sh = TcShape<DP>;
+  const AttendArgs& a = p.a;
+  const retrace_kv_cache& c = a.cache;
+  CUtensorMap mq, mk, mv;
+  {
+    const long long dims[3] = {c.head_dim, a.q_heads, a.T}, strides[3] = {1, a.q_head, a.q_token};
+    const int box[3] = {64, p.group, p.q_box};
+    if (!encode(&mq, a.q, 3, dims, strides, box)) return cudaErrorInvalidValue;
+  }
+  {
+    const long long dims[4] = {c.head_dim, c.kv_heads, c.page_size, c.num_pages};
+    const long long strides[4] = {1, c.head_stride, c.slot_stride, c.page_stride};
+    const int box[4] = {64, 1, p.kv_box, 1};
+    if (!encode(&mk, c.k, 4, dims, strides, box) || !encode(&mv, c.v, 4, dims, strides, box)) return cudaErrorInvalidValue;
+  }
+  constexpr size_t smem = Sh::kControl + sizeof(Control);
+  static_assert(smem <= 227 * 1024, "shared memory of a CTA");
+  cudaError_t e = cudaFuncSetAttribute(attend_tc_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  DeviceInfo dev;
+  if ((e = device_info(&dev)) != cudaSuccess) return e;
+  const int grid = dev.sm_count < kAttendMaxTcCtas ? dev.sm_count : kAttendMaxTcCtas;
+  return launch_dependent(attend_tc_kernel<DP>, dim3(grid), dim3(kThreads), smem, stream, 1u, mq, mk, mv, p);
+}
+
+}  // namespace
+
+bool attend_tc_supported(const AttendArgs& a) {
+  const retrace_kv_cache& c = a.cache;
+  const int G = a.q_heads / c.kv_heads;
+  auto whole = [](long long x) { return x % 8 == 0; };
+  auto stride = [&](long long x, int extent) { return extent <= 1 || (x > 0 && whole(x)); };
+  return c.dtype == RETRACE_BF16 && c.head_dim <= 128 && c.head_dim % 8 == 0 && c.page_size % 8 == 0 && c.num_pages > 0 &&
+         G * (8 / gcd(G, 8)) <= kRows && stride(a.q_token, a.T) && stride(a.q_head, a.q_heads) &&
+         stride(c.page_stride, c.num_pages) && stride(c.slot_stride, c.page_size) && stride(c.head_stride, c.kv_heads) &&
+         whole(a.out_token) && whole(a.out_head) &&
+         (((uintptr_t)a.q | (uintptr_t)a.out | (uintptr_t)c.k | (uintptr_t)c.v) & 15u) == 0;
+}
+
+size_t attend_tc_partial_bytes(int head_dim) {
+  if (head_dim > 128) return 0;
+  return (size_t)kAttendMaxTcCtas * 2 * (head_dim <= 64 ? TcShape<64>::kPart : TcShape<128>::kPart) * 4;
+}
+
+cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t stream) {
+  TcParams p{};
+  p.a = a;
+  const retrace_kv_cache& c = a.cache;
+  p.group = a.q_heads / c.kv_heads;
+  p.q_box = 8 / gcd(p.group, 8);  // boxes of whole 8-row groups of the swizzle
+  p.tile_tokens = kRows / (p.group * p.q_box) * p.q_box;
+  p.kv_box = gcd(c.page_size, kKeys);
+  const float s = a.scale == 0.f ? 1e-30f : a.scale;  // 2^(1e-30 s) is 1, and -inf stays -inf
+  p.scale2 = fabsf(s) * 1.4426950408889634f;
+  p.negate = s < 0.f;
+  p.shape.q_start = a.q_start;
+  p.shape.cache_len = a.cache_len;
+  p.shape.B = a.B;
+  p.shape.T = a.T;
+  p.shape.kv_heads = c.kv_heads;
+  p.shape.causal = a.causal;
+  p.shape.window = a.window;
+  p.shape.sinks = a.sinks;
+  p.shape.places = c.max_pages * c.page_size;
+  p.shape.unit_tokens = 2 * p.tile_tokens;
+  p.shape.key_tile = kKeys;
+  return c.head_dim <= 64 ? launch<64>(p, stream) : launch<128>(p, stream);
+}
+
+}  // namespace retrace

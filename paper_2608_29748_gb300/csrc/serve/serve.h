@@ -31,7 +31,8 @@ cudaError_t launch_kv_append(const AppendArgs& a, cudaStream_t stream);
 // then two partial results per CTA (a CTA's range of work begins and ends inside
 // a unit at most): fp32 rows and their maximum and sum.  It does not depend on
 // the batch, so one workspace serves every call of its head size.
-constexpr int kAttendMaxCtas = 512;
+constexpr int kAttendMaxCtas = 512;    // of the CUDA-core kernel
+constexpr int kAttendMaxTcCtas = 192;  // of the tensor-core kernel
 constexpr size_t kAttendTickets = 256;
 constexpr size_t kAttendPartials = kAttendTickets + kAttendMaxCtas * 4;
 
@@ -53,6 +54,9 @@ struct AttendArgs {
 };
 cudaError_t launch_attend_simt(const AttendArgs& a, cudaStream_t stream);
 size_t attend_simt_partial_bytes(int head_dim);
+cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t stream);
+size_t attend_tc_partial_bytes(int head_dim);
+bool attend_tc_supported(const AttendArgs& a);
 
 struct SampleArgs {
   const void* logits;

@@ -102,7 +102,8 @@ retrace_status retrace_kv_append(const void* q, int64_t q_token_stride, int64_t 
 size_t retrace_attend_workspace_bytes(int q_heads, int kv_heads, int head_dim, retrace_dtype dtype) {
   if (kv_heads < 1 || q_heads < 1 || q_heads % kv_heads || head_dim < 1 || head_dim > kMaxHeadDim || !dtype_ok(dtype))
     return 0;
-  return kAttendPartials + attend_simt_partial_bytes(head_dim);
+  const size_t tc = dtype == RETRACE_BF16 ? attend_tc_partial_bytes(head_dim) : 0;
+  return kAttendPartials + std::max(attend_simt_partial_bytes(head_dim), tc);
 }
 
 retrace_status retrace_attend(const void* q, int64_t q_token_stride, int64_t q_head_stride, int q_heads,
@@ -145,7 +146,7 @@ retrace_status retrace_attend(const void* q, int64_t q_token_stride, int64_t q_h
   a.status = reinterpret_cast<uint32_t*>(w);
   a.tickets = reinterpret_cast<uint32_t*>(w + kAttendTickets);
   a.partials = reinterpret_cast<float*>(w + kAttendPartials);
-  const cudaError_t e = launch_attend_simt(a, stream);
+  const cudaError_t e = attend_tc_supported(a) ? launch_attend_tc(a, stream) : launch_attend_simt(a, stream);
   return e == cudaSuccess ? RETRACE_OK : cuda_fail(e, "attention kernel launch");
 }
 
