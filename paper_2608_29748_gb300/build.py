@@ -21,7 +21,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(PKG, "_build")
 LIB_PATH = os.path.join(PKG, "libretrace.so")
 SOURCES = ["api.cu", "verify.cu", "cond_simt.cu", "cond_tc.cu", "verify_noalloc.cu", "lowrank.cu", "verify_sampled.cu",
-           "serve/serve_api.cu", "serve/kv_append.cu", "serve/attend_simt.cu", "serve/attend_tc.cu", "serve/sample.cu"]
+           "serve/serve_api.cu", "serve/kv_append.cu", "serve/attend_simt.cu", "serve/attend_tc.cu", "serve/attend_join.cu", "serve/sample.cu"]
 ARCH = "-gencode=arch=compute_103a,code=sm_103a"
 NVCC_FLAGS = [
     "-O3",

@@ -3,12 +3,11 @@
 // A unit is the rows of `unit_tokens` consecutive tokens of a sequence under one
 // key/value head (G query heads each), its cost the number of key tiles that any
 // of its rows sees, at least one (an empty unit writes zeros).  The units follow
-// one another by sequence, head, token; CTA i of n takes the costs
-// [total i / n, total (i+1) / n) of that row, so every CTA has the same number of
-// key tiles whatever the lengths are, and a long context is split over as many CTAs
-// as it fills.  The lengths are device data, so every CTA finds its own range: one
-// scan over the sequences.  A unit that several CTAs share is joined by the last
-// of them to finish.
+// one another by sequence, head, token; CTA i takes the costs [i share, (i+1) share) of
+// that row, so the CTAs have the same number of key tiles whatever the lengths are, and
+// a long context is split over as many CTAs as it fills.  The lengths are device data,
+// so every CTA finds its own range: one scan over the sequences.  A unit that several
+// CTAs share is joined by a second kernel.
 #pragma once
 
 #include "tokens.cuh"
@@ -23,10 +22,9 @@ struct AttendShape {
   int causal, window, sinks;
   int places;       // positions a sequence has places for: max_pages * page_size
   int unit_tokens;  // tokens of a unit
-  int key_tile;     // keys of a tile
 };
 
-// The key tiles of a unit: `sink_tiles` from 0, then those from `first` on.
+// The tiles of kKeys keys of a unit: `sink_tiles` from 0, then those from `first` on.
 struct UnitKeys {
   int lo, hi;  // any row sees at most [lo, hi] and the sinks
   int sink_tiles, first, count;
@@ -34,26 +32,29 @@ struct UnitKeys {
 };
 
 // Tokens [i0, i1) of a sequence of n tokens after c cached ones.
+template <int kKeys>
 __device__ __forceinline__ UnitKeys unit_keys(const AttendShape& s, int c, int n, int i0, int i1) {
   UnitKeys u;
   u.hi = min(c + (s.causal ? i1 : n) - 1, s.places - 1);
   u.lo = s.window > 0 ? max(0, c + i0 - s.window + 1) : 0;
   const int sinks = min(s.sinks, u.hi + 1);
-  const int end = u.hi < u.lo ? 0 : u.hi / s.key_tile + 1;
-  u.first = u.lo / s.key_tile;
+  const int end = u.hi < u.lo ? 0 : u.hi / kKeys + 1;
+  u.first = u.lo / kKeys;
   if (end == 0) u.first = 0x3FFFFFFF;  // only sinks, if any
-  u.sink_tiles = sinks > 0 ? min((sinks + s.key_tile - 1) / s.key_tile, u.first) : 0;
+  u.sink_tiles = sinks > 0 ? min((sinks + kKeys - 1) / kKeys, u.first) : 0;
   u.count = u.sink_tiles + max(0, end - u.first);
   return u;
 }
 
 __device__ __forceinline__ int units_of(const AttendShape& s, int n) { return (n + s.unit_tokens - 1) / s.unit_tokens; }
+template <int kKeys>
 __device__ __forceinline__ int unit_cost(const AttendShape& s, int c, int n, int u) {
-  return max(1, unit_keys(s, c, n, u * s.unit_tokens, min(n, (u + 1) * s.unit_tokens)).count);
+  return max(1, unit_keys<kKeys>(s, c, n, u * s.unit_tokens, min(n, (u + 1) * s.unit_tokens)).count);
 }
 
 // Cost of one head of sequence b.  Called by whole warps: the sequences with many
 // units (prompts) are summed by all lanes, one after another.
+template <int kKeys>
 __device__ __forceinline__ long long head_cost(const AttendShape& s, int b, bool valid) {
   constexpr int kAlone = 4;
   SeqTokens q{0, 0};
@@ -64,7 +65,7 @@ __device__ __forceinline__ long long head_cost(const AttendShape& s, int b, bool
     c = cached_tokens(s.cache_len, b);
     units = units_of(s, q.n);
     if (units <= kAlone)
-      for (int u = 0; u < units; ++u) cost += unit_cost(s, c, q.n, u);
+      for (int u = 0; u < units; ++u) cost += unit_cost<kKeys>(s, c, q.n, u);
   }
   unsigned many = __ballot_sync(0xFFFFFFFFu, units > kAlone);
   while (many) {
@@ -73,7 +74,7 @@ __device__ __forceinline__ long long head_cost(const AttendShape& s, int b, bool
     const int cl = __shfl_sync(0xFFFFFFFFu, c, l), nl = __shfl_sync(0xFFFFFFFFu, q.n, l);
     const int ul = __shfl_sync(0xFFFFFFFFu, units, l);
     long long part = 0;
-    for (int u = threadIdx.x & 31; u < ul; u += 32) part += unit_cost(s, cl, nl, u);
+    for (int u = threadIdx.x & 31; u < ul; u += 32) part += unit_cost<kKeys>(s, cl, nl, u);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) part += __shfl_xor_sync(0xFFFFFFFFu, part, o);
     if ((int)(threadIdx.x & 31) == l) cost = part;
@@ -86,7 +87,7 @@ struct PlanStart {
   long long total;       // cost of the call
   long long begin, end;  // this CTA's range of it
   long long unit_begin;  // where the first unit begins
-  int ctas;              // CTAs that have work
+  long long share;       // cost of a CTA's range (the last may be shorter)
   int b, head, unit;     // the first unit
 };
 
@@ -100,8 +101,9 @@ struct Piece {
   int first_cta, pieces;  // the CTAs that share the unit
 };
 
-__device__ __forceinline__ int cta_at(long long x, long long total, int ctas) {
-  return (int)(((x + 1) * ctas - 1) / total);
+// x / y; a division of 64 bits takes many instructions, and costs rarely need them.
+__device__ __forceinline__ long long quotient(long long x, long long y) {
+  return ((x | y) >> 32) == 0 ? (long long)((uint32_t)x / (uint32_t)y) : x / y;
 }
 
 // Walks a CTA's pieces; every role of the CTA walks them for itself.
@@ -117,6 +119,7 @@ struct PieceWalk {
     unit = p.unit;
   }
   // The piece at `at`, and on to the next one.  False at the end of the range.
+  template <int kKeys>
   __device__ __forceinline__ bool next(const AttendShape& s, const PlanStart& p, Piece* out) {
     if (at >= p.end) return false;
     for (;;) {
@@ -130,7 +133,7 @@ struct PieceWalk {
         out->c = cached_tokens(s.cache_len, b);
         out->i0 = unit * s.unit_tokens;
         out->i1 = min(q.n, out->i0 + s.unit_tokens);
-        out->keys = unit_keys(s, out->c, q.n, out->i0, out->i1);
+        out->keys = unit_keys<kKeys>(s, out->c, q.n, out->i0, out->i1);
         break;
       }
       // past the sequence's last unit: the next head, or the next sequence
@@ -145,8 +148,8 @@ struct PieceWalk {
     const int cost = max(1, out->keys.count);
     const long long k0 = at - unit_begin, left = p.end - unit_begin;
     const int k1 = left < cost ? (int)left : cost;
-    out->first_cta = cta_at(unit_begin, p.total, p.ctas);
-    out->pieces = cta_at(unit_begin + cost - 1, p.total, p.ctas) - out->first_cta + 1;
+    out->first_cta = (int)quotient(unit_begin, p.share);
+    out->pieces = (int)quotient(unit_begin + cost - 1, p.share) - out->first_cta + 1;
     out->k0 = out->keys.count ? (int)k0 : 0;
     out->k1 = out->keys.count ? k1 : 0;
     at = unit_begin + k1;
@@ -159,8 +162,8 @@ struct PieceWalk {
 };
 
 // Finds this CTA's share; all kThreads threads of the CTA call it.  `s_sum` has
-// one entry per thread.  At least `least` key tiles to a CTA.
-template <int kThreads>
+// one entry per warp.  At least `least` key tiles to a CTA.
+template <int kThreads, int kKeys>
 __device__ __forceinline__ void plan_start(const AttendShape& s, int grid, int least, PlanStart* s_plan, long long* s_sum) {
   static_assert(kThreads % 32 == 0, "whole warps");
   const int tid = threadIdx.x;
@@ -169,7 +172,7 @@ __device__ __forceinline__ void plan_start(const AttendShape& s, int grid, int l
   long long mine = 0;
   for (int i = 0; i < per; ++i) {
     const int b = tid * per + i;
-    mine += head_cost(s, b, b < s.B) * s.kv_heads;
+    mine += head_cost<kKeys>(s, b, b < s.B) * s.kv_heads;
   }
   // Inclusive scan over the threads: warps, then their sums.
   long long x = mine;
@@ -191,11 +194,10 @@ __device__ __forceinline__ void plan_start(const AttendShape& s, int grid, int l
     __syncthreads();
     return;
   }
-  const long long most = (total + least - 1) / least;
-  const int ctas = most < grid ? (int)most : grid;
-  const long long begin = total * blockIdx.x / ctas, end = total * (blockIdx.x + 1ll) / ctas;
-  if ((int)blockIdx.x >= ctas) {
-    if (tid == 0) *s_plan = PlanStart{total, 0, 0, 0, ctas, 0, 0, 0};
+  const long long even = quotient(total + grid - 1, grid), share = even > least ? even : least;
+  const long long begin = share * blockIdx.x, end = begin + share < total ? begin + share : total;
+  if (begin >= total) {
+    if (tid == 0) *s_plan = PlanStart{total, 0, 0, 0, share, 0, 0, 0};
   } else if (from <= begin && begin < upto) {  // one thread: its sequences hold the start
     long long at = from;
     for (int i = 0; i < per; ++i) {
@@ -204,17 +206,17 @@ __device__ __forceinline__ void plan_start(const AttendShape& s, int grid, int l
       const SeqTokens q = seq_tokens(s.q_start, s.B, s.T, b);
       const int c = cached_tokens(s.cache_len, b), units = units_of(s, q.n);
       long long one = 0;
-      for (int u = 0; u < units; ++u) one += unit_cost(s, c, q.n, u);
+      for (int u = 0; u < units; ++u) one += unit_cost<kKeys>(s, c, q.n, u);
       if (begin < at + one * s.kv_heads) {
-        const int head = (int)((begin - at) / one);
+        const int head = (int)quotient(begin - at, one);
         at += head * one;
         int u = 0;
         for (;; ++u) {
-          const int cost = unit_cost(s, c, q.n, u);
+          const int cost = unit_cost<kKeys>(s, c, q.n, u);
           if (begin < at + cost) break;
           at += cost;
         }
-        *s_plan = PlanStart{total, begin, end, at, ctas, b, head, u};
+        *s_plan = PlanStart{total, begin, end, at, share, b, head, u};
         break;
       }
       at += one * s.kv_heads;

@@ -45,7 +45,6 @@ struct SimtShared {
   long long off[2][kKeys];  // a key's place in the cache, -1: none, or seen by no row
   long long sum[kThreads / 32];
   PlanStart plan;
-  int last;
 };
 
 // Rows of D elements as fp32, zero beyond D, into rows of shared memory.
@@ -81,7 +80,7 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(const __grid_cons
   const AttendArgs& a = P.a;
   const retrace_kv_cache& cache = a.cache;
   const int tid = threadIdx.x, D = cache.head_dim;
-  plan_start<kThreads>(P.shape, gridDim.x, 1, &sm.plan, sm.sum);
+  plan_start<kThreads, kKeys>(P.shape, gridDim.x, 1, &sm.plan, sm.sum);
   const PlanStart plan = sm.plan;
   PieceWalk walk;
   walk.start(plan);
@@ -93,8 +92,9 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(const __grid_cons
   constexpr int kColVec = kCols >= 4 ? 4 : 1, kColSteps = kCols / kColVec;
   const int rg = tid / kLanes, lane = tid % kLanes;
 
+  JoinUnit unit{};
   Piece pc;
-  while (walk.next(P.shape, plan, &pc)) {
+  while (walk.next<kKeys>(P.shape, plan, &pc)) {
     const int kv_head = pc.head / P.splits, part = pc.head % P.splits;
     const int G_all = a.q_heads / cache.kv_heads;
     const int G = min(P.group, G_all - part * P.group), h0 = kv_head * G_all + part * P.group;
@@ -266,43 +266,17 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(const __grid_cons
       }
       continue;
     }
-    // A part of a unit: rows, maxima and sums to the workspace; the last of the CTAs
-    // that share the unit joins them, in the order of their ranges.
+    // A part of a unit: rows, maxima and sums to the workspace.
     constexpr int kPart = R * (DP + 2);
-    auto part_of = [&](int cta, bool begins) { return a.partials + ((long long)cta * 2 + (begins ? 1 : 0)) * kPart; };
-    {
-      float* to = part_of(blockIdx.x, pc.k0 == 0);
+    float* to = a.partials + ((long long)blockIdx.x * 2 + (pc.k0 == 0 ? 1 : 0)) * kPart;
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
+    for (int r = 0; r < 4; ++r)
 #pragma unroll
-        for (int c = 0; c < kCols; ++c) to[(rg * 4 + r) * DP + column(c)] = acc[r][c];
-      if (tid < R) {
-        to[R * DP + tid] = sm.m[tid];
-        to[R * DP + R + tid] = sm.l[tid];
-      }
-    }
-    __threadfence();
-    __syncthreads();
-    if (tid == 0) sm.last = atomicAdd(a.tickets + pc.first_cta, 1u) == (uint32_t)(pc.pieces - 1);
-    __syncthreads();
-    if (!sm.last) continue;
-    __threadfence();
-    if (tid == 0) a.tickets[pc.first_cta] = 0u;
-    for (int i = tid; i < rows * D; i += kThreads) {
-      const int row = i / D, col = i % D;
-      float top = -INFINITY;
-      for (int x = 0; x < pc.pieces; ++x) top = fmaxf(top, __ldcg(part_of(pc.first_cta + x, x == 0) + R * DP + row));
-      const float ref = top == -INFINITY ? 0.f : top;
-      float o = 0.f, l = 0.f;
-      for (int x = 0; x < pc.pieces; ++x) {
-        const float* from = part_of(pc.first_cta + x, x == 0);
-        const float w = expf(__ldcg(from + R * DP + row) - ref);
-        o = fmaf(w, __ldcg(from + row * DP + col), o);
-        l = fmaf(w, __ldcg(from + R * DP + R + row), l);
-      }
-      put(row, col, l == 0.f ? 0.f : o / l);
-    }
+      for (int c = 0; c < kCols; ++c) to[(rg * 4 + r) * DP + column(c)] = acc[r][c];
+    if (tid < R) *reinterpret_cast<float2*>(to + R * DP + tid * 2) = make_float2(sm.m[tid], sm.l[tid]);
+    if (pc.k0 == 0) unit = JoinUnit{pc.pieces, rows, rows, pc.row0 + pc.i0, h0, G, {0, 0}};
   }
+  if (tid == 0) a.units[blockIdx.x] = unit;
 }
 
 template <typename T, int DP, int R>
@@ -320,9 +294,9 @@ cudaError_t launch(SimtParams& p, cudaStream_t stream) {
   p.group = (p.a.q_heads / p.a.cache.kv_heads + p.splits - 1) / p.splits;
   p.shape.kv_heads = p.a.cache.kv_heads * p.splits;
   p.shape.unit_tokens = R / p.group;
-  p.shape.key_tile = kKeys;
   kernel<<<grid, kThreads, smem, stream>>>(p);
-  return cudaGetLastError();
+  if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  return launch_attend_join(p.a, PartShape{R, DP, 0}, grid, stream);
 }
 
 template <typename T, int DP>

@@ -65,7 +65,6 @@ struct Control {
   long long sum[kThreads / 32];
   uint32_t tmem;
   int abort;
-  int last;
   uint32_t mask[kMasks];  // of a key tile: bit i: box i has a page
   float2 stat[2][kRows];  // m and l of a stream's rows
 };
@@ -215,8 +214,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = ct.tmem;
+  pdl_launch_dependents();
   pdl_wait();
-  plan_start<kThreads>(P.shape, gridDim.x, 2, &ct.plan, ct.sum);
+  plan_start<kThreads, kKeys>(P.shape, gridDim.x, 2, &ct.plan, ct.sum);
   const PlanStart& plan = ct.plan;
   PieceWalk walk;
   walk.start(plan);
@@ -229,7 +229,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int page_size = a.cache.page_size;
     uint32_t it = 0, pieces = 0, tiles = 0;
     bool ok = true;
-    while (ok && walk.next(P.shape, plan, &pc)) {
+    while (ok && walk.next<kKeys>(P.shape, plan, &pc)) {
       const int nt = pc.k1 - pc.k0;
       if (nt == 0) continue;
       const int tokens = pc.i1 - pc.i0;
@@ -335,7 +335,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (elect_one()) tc_commit(smem_u32(bar));
       __syncwarp();
     };
-    while (ok && walk.next(P.shape, plan, &pc)) {
+    while (ok && walk.next<kKeys>(P.shape, plan, &pc)) {
       const int nt = pc.k1 - pc.k0;
       if (nt == 0) continue;
       const bool two = pc.i1 - pc.i0 > P.tile_tokens;
@@ -399,6 +399,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int G = P.group, D = a.cache.head_dim;
     const float sl = P.scale2;
     uint32_t it = 0, ns = 0, tiles = 0;
+    JoinUnit unit{};
     bool ok = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
       if (ok && !warp_wait_all(bar, parity, abort)) {
@@ -406,7 +407,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) raise_abort(abort, a.status);
       }
     };
-    while (walk.next(P.shape, plan, &pc)) {
+    while (walk.next<kKeys>(P.shape, plan, &pc)) {
       const int nt = pc.k1 - pc.k0, tokens = pc.i1 - pc.i0;
       const bool two = tokens > P.tile_tokens;
       const int t0 = two ? s * P.tile_tokens : 0;                                       // first token of this stream's tile
@@ -447,29 +448,55 @@ __global__ void __launch_bounds__(kThreads, 1)
           fence_proxy_async_shared();
         }
         if (busy) {
-          float v[kKeys];
-#pragma unroll
-          for (int c = 0; c < kKeys; c += 32) tmem_ld32(t_s + c, v + c);
-          tmem_wait_ld();
-          if (P.negate) {
-#pragma unroll
-            for (int c = 0; c < kKeys; ++c) v[c] = -v[c];
-          }
           const uint32_t all = boxes_mask(kKeys / P.kv_box);
           const bool whole = j0 + kKeys - 1 <= hi && (j0 >= lo || j0 + kKeys <= a.sinks) && pages == all;
-          if (!__all_sync(0xFFFFFFFFu, whole)) {
+          const bool masked = !__all_sync(0xFFFFFFFFu, whole);
+          uint32_t see[kKeys / 32];
+          if (masked) {
 #pragma unroll
-            for (int w = 0; w < kKeys / 32; ++w) {
-              const uint32_t see = seen_word(hi - j0 - 32 * w, lo - j0 - 32 * w, a.sinks - j0 - 32 * w) &
-                                   page_word(pages, P.kv_box, w);
+            for (int w = 0; w < kKeys / 32; ++w)
+              see[w] = seen_word(hi - j0 - 32 * w, lo - j0 - 32 * w, a.sinks - j0 - 32 * w) & page_word(pages, P.kv_box, w);
+          }
+          // The row is read twice, 32 scores at a time, so that it needs no more registers: for
+          // its maximum, then for its weights.
+          float va[32], vb[32];
+          auto scores_of = [&](int w, float* v) {
+            if (P.negate) {
+#pragma unroll
+              for (int c = 0; c < 32; ++c) v[c] = -v[c];
+            }
+            if (masked) {
 #pragma unroll
               for (int c = 0; c < 32; ++c)
-                if (!(see >> c & 1u)) v[32 * w + c] = -INFINITY;
+                if (!(see[w] >> c & 1u)) v[c] = -INFINITY;
             }
-          }
-          float top = v[0];
+          };
+          auto top_of = [&](const float* v) {
+            float t[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-          for (int c = 1; c < kKeys; ++c) top = fmaxf(top, v[c]);
+            for (int c = 4; c < 32; c += 4)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) t[i] = fmaxf(t[i], v[c + i]);
+            return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+          };
+          tmem_ld32(t_s, va);
+          tmem_wait_ld();
+          tmem_ld32(t_s + 32, vb);
+          scores_of(0, va);
+          float top = top_of(va);
+          tmem_wait_ld();
+          tmem_ld32(t_s + 64, va);
+          scores_of(1, vb);
+          top = fmaxf(top, top_of(vb));
+          tmem_wait_ld();
+          tmem_ld32(t_s + 96, vb);
+          scores_of(2, va);
+          top = fmaxf(top, top_of(va));
+          tmem_wait_ld();
+          tmem_ld32(t_s, va);
+          scores_of(3, vb);
+          top = fmaxf(top, top_of(vb));
+          tmem_wait_ld();
           if (done == 0) {
             m = top;
           } else {
@@ -491,18 +518,29 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           const float ref = m == -INFINITY ? 0.f : m * sl;
           float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int c = 0; c < kKeys; c += 32) {
-            uint32_t w[16];
+          // P takes the columns of scores that are read already
+          auto weights_of = [&](int w, float* v) {
+            scores_of(w, v);
+            uint32_t x[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const float x = exp2_fast(fmaf(v[c + 2 * i], sl, -ref)), y = exp2_fast(fmaf(v[c + 2 * i + 1], sl, -ref));
-              sum[i & 1] += x;
-              sum[2 + (i & 1)] += y;
-              w[i] = pack_bf16x2(x, y);
+              const float y = exp2_fast(fmaf(v[2 * i], sl, -ref)), z = exp2_fast(fmaf(v[2 * i + 1], sl, -ref));
+              sum[i & 1] += y;
+              sum[2 + (i & 1)] += z;
+              x[i] = pack_bf16x2(y, z);
             }
-            tmem_st16(t_s + c / 2, w);
-          }
+            tmem_st16(t_s + 16 * w, x);
+          };
+          tmem_ld32(t_s + 32, vb);
+          weights_of(0, va);
+          tmem_wait_ld();
+          tmem_ld32(t_s + 64, va);
+          weights_of(1, vb);
+          tmem_wait_ld();
+          tmem_ld32(t_s + 96, vb);
+          weights_of(2, va);
+          tmem_wait_ld();
+          weights_of(3, vb);
           l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
           tmem_wait_st();
         }
@@ -587,45 +625,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (whole) continue;
 
-      // The last of the CTAs that share the unit joins their parts, in the order of their
-      // ranges.
-      __threadfence();
-      named_barrier(1, 256);
-      if (tid == 128) ct.last = !*abort && atomicAdd(a.tickets + pc.first_cta, 1u) == (uint32_t)(pc.pieces - 1);
-      named_barrier(1, 256);
-      const bool last = ct.last;
-      named_barrier(1, 256);  // `last` is read before the next piece writes it
-      if (!last) continue;
-      __threadfence();
-      if (tid == 128) a.tickets[pc.first_cta] = 0u;
-      constexpr int kLanes = DP / 4;  // threads of a row
-      const int first_rows = min(tokens, P.tile_tokens) * G, all_rows = tokens * G;
-      const int col = (tid - 128) % kLanes * 4;
-      for (int r = (tid - 128) / kLanes; r < all_rows; r += 256 / kLanes) {
-        const int tile = r >= first_rows, tr = tile ? r - first_rows : r, slot = tile * kRows + tr;
-        float top = -INFINITY, sum = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int x = 0; x < pc.pieces; ++x) {
-          const float* from = a.partials + ((long long)(pc.first_cta + x) * 2 + (x == 0 ? 1 : 0)) * Sh::kPart;
-          const float2 st = __ldcg(reinterpret_cast<const float2*>(from + Sh::kPartRows * DP + slot * 2));
-          const float4 y = __ldcg(reinterpret_cast<const float4*>(from + slot * DP + col));
-          if (st.x == -INFINITY) continue;
-          const float up = fmaxf(top, st.x), f = exp2_fast(top - up), g = exp2_fast(st.x - up);
-          top = up;
-          sum = sum * f + st.y * g;
-          o.x = o.x * f + y.x * g;
-          o.y = o.y * f + y.y * g;
-          o.z = o.z * f + y.z * g;
-          o.w = o.w * f + y.w * g;
-        }
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        const int token = pc.row0 + pc.i0 + r / G;  // rows run on over the tiles: tile_tokens * G of the first
-        if (col < D)
-          *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + (long long)token * a.out_token +
-                                    (pc.head * G + r % G) * (long long)a.out_head + col) =
-              make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
-      }
+      if (pc.k0 == 0)
+        unit = JoinUnit{pc.pieces, tokens * G, min(tokens, P.tile_tokens) * G, pc.row0 + pc.i0, pc.head * G, G, {0, 0}};
     }
+    if (tid == 128) a.units[blockIdx.x] = unit;
   }
   tc_fence_before();
   __syncthreads();
@@ -695,7 +698,9 @@ cudaError_t launch(TcParams& p, cudaStream_t stream) {
   DeviceInfo dev;
   if ((e = device_info(&dev)) != cudaSuccess) return e;
   const int grid = dev.sm_count < kAttendMaxTcCtas ? dev.sm_count : kAttendMaxTcCtas;
-  return launch_dependent(attend_tc_kernel<DP>, dim3(grid), dim3(kThreads), smem, stream, 1u, mq, mk, mv, p);
+  e = launch_dependent(attend_tc_kernel<DP>, dim3(grid), dim3(kThreads), smem, stream, 1u, mq, mk, mv, p);
+  if (e != cudaSuccess) return e;
+  return launch_attend_join(a, PartShape{Sh::kPartRows, DP, 1}, grid, stream);
 }
 
 }  // namespace
@@ -738,7 +743,6 @@ cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t stream) {
   p.shape.sinks = a.sinks;
   p.shape.places = c.max_pages * c.page_size;
   p.shape.unit_tokens = 2 * p.tile_tokens;
-  p.shape.key_tile = kKeys;
   return c.head_dim <= 64 ? launch<64>(p, stream) : launch<128>(p, stream);
 }
 

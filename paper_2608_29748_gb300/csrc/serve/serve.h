@@ -27,14 +27,24 @@ struct AppendArgs {
 };
 cudaError_t launch_kv_append(const AppendArgs& a, cudaStream_t stream);
 
-// Workspace of retrace_attend: the status word (256 bytes), one ticket per CTA,
-// then two partial results per CTA (a CTA's range of work begins and ends inside
-// a unit at most): fp32 rows and their maximum and sum.  It does not depend on
-// the batch, so one workspace serves every call of its head size.
+// Workspace of retrace_attend: the status word (256 bytes), a JoinUnit per CTA, then
+// two partial results per CTA (a CTA's range of work begins and ends inside a unit at
+// most): fp32 rows, and the maximum and sum of each.  Nothing in it outlives a call but
+// the status word, and its size does not depend on the batch, so one workspace serves
+// every call of its head size.
 constexpr int kAttendMaxCtas = 512;    // of the CUDA-core kernel
 constexpr int kAttendMaxTcCtas = 192;  // of the tensor-core kernel
-constexpr size_t kAttendTickets = 256;
-constexpr size_t kAttendPartials = kAttendTickets + kAttendMaxCtas * 4;
+
+// A unit that several CTAs shared: its first rows are `part_rows` apart from the next
+// ones in a part; row r is the query head head + r % group of token + r / group.
+struct JoinUnit {
+  int pieces;  // CTAs, from the one whose entry this is; 0: none
+  int rows, first_rows;
+  int token, head, group;
+  int unused[2];
+};
+constexpr size_t kAttendUnits = 256;
+constexpr size_t kAttendPartials = kAttendUnits + kAttendMaxCtas * sizeof(JoinUnit);
 
 struct AttendArgs {
   const void* q;
@@ -49,9 +59,15 @@ struct AttendArgs {
   void* out;
   long long out_token, out_head;
   uint32_t* status;
-  uint32_t* tickets;
+  JoinUnit* units;
   float* partials;
 };
+// A part: `rows` rows of `cols` floats, then their (maximum, sum).
+struct PartShape {
+  int rows, cols;
+  int base2;  // the maxima are binary exponents (else natural)
+};
+cudaError_t launch_attend_join(const AttendArgs& a, PartShape part, int ctas, cudaStream_t stream);
 cudaError_t launch_attend_simt(const AttendArgs& a, cudaStream_t stream);
 size_t attend_simt_partial_bytes(int head_dim);
 cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t stream);
