@@ -12,8 +12,10 @@
 // The maximum that the exponents refer to is raised, and O rescaled, only where a row
 // would otherwise pass 2^8 of it: the first tile and few others.
 //
-// Warp 0 copies K and V tiles into a ring with TMA, a box for each run of slots
-// within a page; warp 1 issues the products; warps 4-7 and 8-11 are the streams' softmax.
+// Warps 0 and 2 copy the K and the V tiles into a ring with TMA, a box for each run of
+// slots within a page (a warp issues a box in about 120 cycles, so one warp for both was
+// the bound with pages of 16), warp 3 copies Q; warp 1 issues the products; warps 4-7 and
+// 8-11 are the streams' softmax.
 // A tile of keys is 4 D 128 bytes of HBM traffic against 2 x 128 x 128 x D products of a
 // tensor core that does 8192 flop a cycle: 1024 of the 2790 cycles that the bytes take
 // at D = 128, so tokens and blocks are bound by HBM, and a row tile that is not full costs
@@ -65,6 +67,9 @@ struct Control {
   long long sum[kThreads / 32];
   uint32_t tmem;
   int abort;
+  int more[2];
+  PieceWalk walk[2];  // of the softmax streams
+  Piece piece[2];
   uint32_t mask[kMasks];  // of a key tile: bit i: box i has a page
   float2 stat[2][kRows];  // m and l of a stream's rows
 };
@@ -134,13 +139,26 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// Moves registers from the warpgroup of the copies and products to those of the softmax:
+// 128 x 88 + 256 x 208 are the 384 x 168 of the launch.
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 88;"); }
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 208;"); }
 // A bounded wait that every lane of the warp polls; all of them agree on the outcome.
 __device__ __forceinline__ bool warp_wait_all(uint64_t* bar, uint32_t parity, volatile int* abort) {
   const bool ok = mbar_wait_bounded(smem_u32(bar), parity, abort);
   return __all_sync(0xFFFFFFFFu, ok);
 }
-__device__ __forceinline__ void named_barrier(int id, int threads) {
-  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+template <int id, int threads>
+__device__ __forceinline__ void named_barrier() {
+  asm volatile("bar.sync %0, %1;" ::"n"(id), "n"(threads) : "memory");
+}
+
+// The four warps of a stream.
+__device__ __forceinline__ void stream_barrier(int s) {
+  if (s == 0)
+    named_barrier<2, kRows>();
+  else
+    named_barrier<3, kRows>();
 }
 
 // Descriptor of V [keys, 64-element columns] as the MN-major operand: rows of 128
@@ -154,6 +172,7 @@ constexpr uint32_t kMajorB = 1u << 16;  // instruction descriptor: B is MN-major
 
 // The key tiles of a piece in the order in which the products take them from the ring:
 // with two row tiles K0 V0 K1 V1 ..., with one K0 K1 V0 K2 V1 ... .
+__device__ __forceinline__ int k_position(int j, bool two) { return two ? 2 * j : (j == 0 ? 0 : 2 * j - 1); }
 __device__ __forceinline__ int v_position(int j, int tiles, bool two) {
   return two ? 2 * j + 1 : (j + 1 < tiles ? 2 * j + 2 : 2 * j + 1);
 }
@@ -218,180 +237,189 @@ __global__ void __launch_bounds__(kThreads, 1)
   pdl_wait();
   plan_start<kThreads, kKeys>(P.shape, gridDim.x, 2, &ct.plan, ct.sum);
   const PlanStart& plan = ct.plan;
-  PieceWalk walk;
-  walk.start(plan);
-  Piece pc;
-
-  if (warp == 0) {
-    // ---- copies: lane (half, box) loads one box of a tile ----
-    const int boxes = kKeys / P.kv_box, half = lane / 16, box = lane % 16;
-    const bool active = box < boxes && half < Sh::kHalves;
-    const int page_size = a.cache.page_size;
-    uint32_t it = 0, pieces = 0, tiles = 0;
-    bool ok = true;
-    while (ok && walk.next<kKeys>(P.shape, plan, &pc)) {
-      const int nt = pc.k1 - pc.k0;
-      if (nt == 0) continue;
-      const int tokens = pc.i1 - pc.i0;
-      const bool two = tokens > P.tile_tokens;
-      auto page_at = [&](int k) {  // of this lane's box of the piece's tile k
-        if (!active || k >= nt) return -1;
-        const int j = pc.keys.tile(pc.k0 + k) * kKeys + box * P.kv_box;
-        return page_of(a.cache, pc.b, j / page_size);
+  if (warp < 4) {
+    fewer_registers();
+    PieceWalk walk;
+    walk.start(plan);
+    Piece pc;
+    if (warp == 0 || warp == 2) {
+      // ---- copies of K (warp 0) and V (warp 2): lane (half, box) loads one box of a tile ----
+      const bool keys = warp == 0;
+      const CUtensorMap* map = keys ? &tm_k : &tm_v;
+      const int boxes = kKeys / P.kv_box, half = lane / 16, box = lane % 16;
+      const bool active = box < boxes && half < Sh::kHalves;
+      const int page_size = a.cache.page_size;
+      uint32_t it = 0, tiles = 0, issued = 0, parity = 0;
+      bool ok = true;
+      while (ok && walk.next<kKeys>(P.shape, plan, &pc)) {
+        const int nt = pc.k1 - pc.k0;
+        const bool two = pc.i1 - pc.i0 > P.tile_tokens;
+        struct Place {
+          int page, slot;
+        };
+        auto place_of = [&](int k) {  // of this lane's box of the piece's tile k
+          Place x{a.cache.num_pages, 0};  // a box without a page lies outside the tensor: zeros
+          if (active && k < nt) {
+            const int j = pc.keys.tile(pc.k0 + k) * kKeys + box * P.kv_box, i = j / page_size;
+            const int page = page_of(a.cache, pc.b, i);
+            if (page >= 0) x = Place{page, j - i * page_size};
+          }
+          return x;
+        };
+        // looked up two tiles ahead of their copies
+        Place now = place_of(0), next = place_of(1);
+        for (int k = 0; k < nt; ++k) {
+          const Place after = place_of(k + 2);
+          const uint32_t n = it + (keys ? k_position(k, two) : v_position(k, nt, two));
+          const uint32_t slot = n % Sh::kStages, phase = (n / Sh::kStages) & 1u;
+          ok = warp_wait_all(&ct.empty[slot], phase ^ 1u, abort);
+          if (!ok) break;
+          const uint32_t bar = smem_u32(&ct.full[slot]);
+          const uint32_t placed = __ballot_sync(0xFFFFFFFFu, active && half == 0 && now.page < a.cache.num_pages);
+          if (lane == 0) {
+            if (keys) ct.mask[tiles % kMasks] = placed;
+            mbar_arrive_expect_tx(bar, Sh::kTileBytes);
+          }
+          __syncwarp();
+          if (active)
+            tma_load_4d(base + slot * Sh::kTileBytes + half * Sh::kHalfBytes + box * P.kv_box * 128, map, half * 64, pc.head,
+                        now.slot, now.page, bar);
+          issued |= 1u << slot;
+          parity = (parity & ~(1u << slot)) | phase << slot;
+          ++tiles;
+          now = next;
+          next = after;
+        }
+        it += 2 * nt;
+      }
+      if (!ok) {
+        if (lane == 0) raise_abort(abort, a.status);
+        volatile int never = 0;  // this warp's copies in flight
+        for (int slot = 0; slot < Sh::kStages; ++slot)
+          if (issued >> slot & 1u) mbar_wait_bounded(smem_u32(&ct.full[slot]), parity >> slot & 1u, &never);
+      }
+    } else if (warp == 3) {
+      // ---- copies of Q: boxes of q_box tokens times the head group, rows in order ----
+      const int box_rows = P.q_box * P.group;
+      uint32_t pieces = 0;
+      bool ok = true;
+      while (ok && walk.next<kKeys>(P.shape, plan, &pc)) {
+        if (pc.k1 == pc.k0) continue;
+        const int tokens = pc.i1 - pc.i0;
+        const bool two = tokens > P.tile_tokens;
+        const int b0 = (min(tokens, P.tile_tokens) + P.q_box - 1) / P.q_box;
+        const int b1 = two ? (tokens - P.tile_tokens + P.q_box - 1) / P.q_box : 0;
+        ok = warp_wait_all(&ct.q_empty, (pieces & 1u) ^ 1u, abort);
+        if (!ok) break;
+        ++pieces;
+        if (lane == 0) mbar_arrive_expect_tx(smem_u32(&ct.q_full), (b0 + b1) * Sh::kHalves * box_rows * 128);
+        __syncwarp();
+        for (int i = lane; i < (b0 + b1) * Sh::kHalves; i += 32) {
+          const int h = i % Sh::kHalves, x = i / Sh::kHalves, tile = x >= b0, n = tile ? x - b0 : x;
+          tma_load_3d(base + Sh::kQOffset + tile * (kRows * DP * 2) + h * Sh::kHalfBytes + n * box_rows * 128, &tm_q, h * 64,
+                      pc.head * P.group, pc.row0 + pc.i0 + tile * P.tile_tokens + n * P.q_box, smem_u32(&ct.q_full));
+        }
+      }
+      if (!ok) {
+        if (lane == 0) raise_abort(abort, a.status);
+        volatile int never = 0;
+        if (pieces) mbar_wait_bounded(smem_u32(&ct.q_full), (pieces - 1) & 1u, &never);
+      }
+    } else if (warp == 1) {
+      // ---- products ----
+      constexpr uint32_t kS = idesc_bf16_f32(kRows, kKeys), kPV = idesc_bf16_f32(kRows, DP) | kMajorB;
+      uint32_t it = 0, pieces = 0, np[2] = {0, 0};
+      bool ok = true;
+      auto wait = [&](uint64_t* bar, uint32_t parity) {
+        ok = ok && warp_wait_all(bar, parity, abort);
+        return ok;
       };
-      auto load = [&](const CUtensorMap* map, int k, int page, bool keys) {
-        const uint32_t slot = it % Sh::kStages, phase = (it / Sh::kStages) & 1u;
-        if (!warp_wait_all(&ct.empty[slot], phase ^ 1u, abort)) return false;
-        const uint32_t bar = smem_u32(&ct.full[slot]);
-        const uint32_t placed = __ballot_sync(0xFFFFFFFFu, active && half == 0 && page >= 0);
-        if (lane == 0) {
-          if (keys) ct.mask[tiles % kMasks] = placed;
-          mbar_arrive_expect_tx(bar, Sh::kTileBytes);
+      auto wait_tile = [&](uint32_t n) { return wait(&ct.full[n % Sh::kStages], (n / Sh::kStages) & 1u); };
+      auto tile = [&](uint32_t n) { return base + n % Sh::kStages * Sh::kTileBytes; };
+      auto scores = [&](int s, int q, uint32_t k_tile) {
+        if (elect_one()) {
+          const uint64_t qd = sw128_kmajor_desc(base + Sh::kQOffset + q * (kRows * DP * 2)), kd = sw128_kmajor_desc(k_tile);
+#pragma unroll
+          for (int h = 0; h < Sh::kHalves; ++h)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              tc_mma_bf16(tmem + s * 128, qd + h * (Sh::kHalfBytes >> 4) + 2 * k, kd + h * (Sh::kHalfBytes >> 4) + 2 * k, kS,
+                          h + k > 0);
         }
         __syncwarp();
-        if (active) {
-          const int j = pc.keys.tile(pc.k0 + k) * kKeys + box * P.kv_box;
-          // a box without a page lies outside the tensor: zeros
-          tma_load_4d(base + slot * Sh::kTileBytes + half * Sh::kHalfBytes + box * P.kv_box * 128, map, half * 64, pc.head,
-                      j % page_size, page >= 0 ? page : a.cache.num_pages, bar);
-        }
-        ++it;
-        if (keys) ++tiles;
-        return true;
       };
-      int page = page_at(0);
-      ok = warp_wait_all(&ct.q_empty, (pieces & 1u) ^ 1u, abort);
-      if (!ok) break;
-      ++pieces;
-      // Q: boxes of q_box tokens times the head group, rows in order
-      const int b0 = (min(tokens, P.tile_tokens) + P.q_box - 1) / P.q_box;
-      const int b1 = two ? (tokens - P.tile_tokens + P.q_box - 1) / P.q_box : 0;
-      const int box_rows = P.q_box * P.group;
-      if (lane == 0) mbar_arrive_expect_tx(smem_u32(&ct.q_full), (b0 + b1) * Sh::kHalves * box_rows * 128);
-      __syncwarp();
-      for (int i = lane; i < (b0 + b1) * Sh::kHalves; i += 32) {
-        const int h = i % Sh::kHalves, x = i / Sh::kHalves, tile = x >= b0, n = tile ? x - b0 : x;
-        tma_load_3d(base + Sh::kQOffset + tile * (kRows * DP * 2) + h * Sh::kHalfBytes + n * box_rows * 128, &tm_q, h * 64,
-                    pc.head * P.group, pc.row0 + pc.i0 + tile * P.tile_tokens + n * P.q_box, smem_u32(&ct.q_full));
-      }
-      if (two) {
-        for (int k = 0; k < nt && ok; ++k) {
-          const int next = page_at(k + 1);
-          ok = load(&tm_k, k, page, true) && load(&tm_v, k, page, false);
-          page = next;
+      auto values = [&](int s, uint32_t v_tile, bool first) {
+        if (elect_one()) {
+          const uint64_t vd = sw128_mnmajor_desc(v_tile);
+#pragma unroll
+          for (int k = 0; k < kKeys / 16; ++k)
+            tc_mma_bf16_ts(tmem + 256 + s * 128, tmem + s * 128 + k * 8, vd + k * (2048 >> 4), kPV, !(first && k == 0));
         }
-      } else {
-        ok = load(&tm_k, 0, page, true);
-        for (int k = 0; k < nt && ok; ++k) {
-          const int next = page_at(k + 1);
-          if (k + 1 < nt) ok = load(&tm_k, k + 1, next, true);
-          ok = ok && load(&tm_v, k, page, false);
-          page = next;
-        }
-      }
-    }
-    if (!ok) {
-      if (lane == 0) raise_abort(abort, a.status);
-      volatile int never = 0;  // this CTA's copies in flight
-      const uint32_t first = it > Sh::kStages ? it - Sh::kStages : 0;
-      for (uint32_t k = first; k < it; ++k)
-        mbar_wait_bounded(smem_u32(&ct.full[k % Sh::kStages]), (k / Sh::kStages) & 1u, &never);
-      if (pieces) mbar_wait_bounded(smem_u32(&ct.q_full), (pieces - 1) & 1u, &never);
-    }
-    __syncwarp();
-  } else if (warp == 1) {
-    // ---- products ----
-    constexpr uint32_t kS = idesc_bf16_f32(kRows, kKeys), kPV = idesc_bf16_f32(kRows, DP) | kMajorB;
-    uint32_t it = 0, pieces = 0, np[2] = {0, 0};
-    bool ok = true;
-    auto wait = [&](uint64_t* bar, uint32_t parity) {
-      ok = ok && warp_wait_all(bar, parity, abort);
-      return ok;
-    };
-    auto wait_tile = [&](uint32_t n) { return wait(&ct.full[n % Sh::kStages], (n / Sh::kStages) & 1u); };
-    auto tile = [&](uint32_t n) { return base + n % Sh::kStages * Sh::kTileBytes; };
-    auto scores = [&](int s, int q, uint32_t k_tile) {
-      if (elect_one()) {
-        const uint64_t qd = sw128_kmajor_desc(base + Sh::kQOffset + q * (kRows * DP * 2)), kd = sw128_kmajor_desc(k_tile);
+        __syncwarp();
+      };
+      auto commit = [&](uint64_t* bar) {
+        if (elect_one()) tc_commit(smem_u32(bar));
+        __syncwarp();
+      };
+      while (ok && walk.next<kKeys>(P.shape, plan, &pc)) {
+        const int nt = pc.k1 - pc.k0;
+        if (nt == 0) continue;
+        const bool two = pc.i1 - pc.i0 > P.tile_tokens;
+        if (!wait(&ct.q_full, pieces & 1u)) break;
+        ++pieces;
+        tc_fence_after();
+        if (two) {
+          for (int j = 0; j <= nt && ok; ++j) {  // the products of tile j - 1 with V, then the scores of tile j
+            const uint32_t v = it + v_position(j - 1, nt, true), k = it + k_position(j, true);
+            if (j > 0 && !wait_tile(v)) break;
+            if (j < nt && !wait_tile(k)) break;
 #pragma unroll
-        for (int h = 0; h < Sh::kHalves; ++h)
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            tc_mma_bf16(tmem + s * 128, qd + h * (Sh::kHalfBytes >> 4) + 2 * k, kd + h * (Sh::kHalfBytes >> 4) + 2 * k, kS,
-                        h + k > 0);
-      }
-      __syncwarp();
-    };
-    auto values = [&](int s, uint32_t v_tile, bool first) {
-      if (elect_one()) {
-        const uint64_t vd = sw128_mnmajor_desc(v_tile);
-#pragma unroll
-        for (int k = 0; k < kKeys / 16; ++k)
-          tc_mma_bf16_ts(tmem + 256 + s * 128, tmem + s * 128 + k * 8, vd + k * (2048 >> 4), kPV, !(first && k == 0));
-      }
-      __syncwarp();
-    };
-    auto commit = [&](uint64_t* bar) {
-      if (elect_one()) tc_commit(smem_u32(bar));
-      __syncwarp();
-    };
-    while (ok && walk.next<kKeys>(P.shape, plan, &pc)) {
-      const int nt = pc.k1 - pc.k0;
-      if (nt == 0) continue;
-      const bool two = pc.i1 - pc.i0 > P.tile_tokens;
-      if (!wait(&ct.q_full, pieces & 1u)) break;
-      ++pieces;
-      tc_fence_after();
-      if (two) {
-        for (int j = 0; j <= nt && ok; ++j) {  // the products of tile j - 1 with V, then the scores of tile j
-          const uint32_t v = it + 2 * (j - 1) + 1, k = it + 2 * j;
-          if (j > 0 && !wait_tile(v)) break;
-          if (j < nt && !wait_tile(k)) break;
-#pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            if (j > 0) {
-              if (!wait(&ct.p_full[s], np[s]++ & 1u)) break;
-              tc_fence_after();
-              values(s, tile(v), j == 1);
-              if (s == 1) commit(&ct.empty[v % Sh::kStages]);
+            for (int s = 0; s < 2; ++s) {
+              if (j > 0) {
+                if (!wait(&ct.p_full[s], np[s]++ & 1u)) break;
+                tc_fence_after();
+                values(s, tile(v), j == 1);
+                if (s == 1) commit(&ct.empty[v % Sh::kStages]);
+              }
+              if (j < nt) scores(s, s, tile(k));
+              commit(&ct.s_full[s]);
             }
-            if (j < nt) scores(s, s, tile(k));
-            commit(&ct.s_full[s]);
-          }
-          if (j < nt && ok) commit(&ct.empty[k % Sh::kStages]);
-          if (j == nt - 1) commit(&ct.q_empty);
-        }
-      } else {
-        for (int j = 0; j < nt + 2 && ok; ++j) {
-          const int s = j & 1;
-          if (j >= 2) {
-            const uint32_t v = it + v_position(j - 2, nt, false);
-            if (!wait_tile(v) || !wait(&ct.p_full[s], np[s]++ & 1u)) break;
-            tc_fence_after();
-            values(s, tile(v), j < 4);
-            commit(&ct.empty[v % Sh::kStages]);
-          }
-          if (j < nt) {
-            const uint32_t k = it + (j == 0 ? 0 : 2 * j - 1);
-            if (!wait_tile(k)) break;
-            tc_fence_after();
-            scores(s, 0, tile(k));
-            commit(&ct.empty[k % Sh::kStages]);
+            if (j < nt && ok) commit(&ct.empty[k % Sh::kStages]);
             if (j == nt - 1) commit(&ct.q_empty);
           }
-          if (j >= 2 || j < nt) commit(&ct.s_full[s]);
+        } else {
+          for (int j = 0; j < nt + 2 && ok; ++j) {
+            const int s = j & 1;
+            if (j >= 2) {
+              const uint32_t v = it + v_position(j - 2, nt, false);
+              if (!wait_tile(v) || !wait(&ct.p_full[s], np[s]++ & 1u)) break;
+              tc_fence_after();
+              values(s, tile(v), j < 4);
+              commit(&ct.empty[v % Sh::kStages]);
+            }
+            if (j < nt) {
+              const uint32_t k = it + k_position(j, false);
+              if (!wait_tile(k)) break;
+              tc_fence_after();
+              scores(s, 0, tile(k));
+              commit(&ct.empty[k % Sh::kStages]);
+              if (j == nt - 1) commit(&ct.q_empty);
+            }
+            if (j >= 2 || j < nt) commit(&ct.s_full[s]);
+          }
         }
+        it += 2 * nt;
       }
-      it += 2 * nt;
+      if (!ok) {
+        if (lane == 0) raise_abort(abort, a.status);
+        volatile int never = 0;
+        commit(&ct.done);
+        mbar_wait_bounded(smem_u32(&ct.done), 0, &never);
+      }
+      __syncwarp();
     }
-    if (!ok) {
-      if (lane == 0) raise_abort(abort, a.status);
-      volatile int never = 0;
-      commit(&ct.done);
-      mbar_wait_bounded(smem_u32(&ct.done), 0, &never);
-    }
-    __syncwarp();
-  } else if (warp >= 4) {
+  } else {
+    more_registers();
     // ---- softmax: stream s, one thread per row ----
     const int s = warp >= 8, row = tid & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
@@ -407,7 +435,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) raise_abort(abort, a.status);
       }
     };
-    while (walk.next<kKeys>(P.shape, plan, &pc)) {
+    // One thread of the stream walks; the piece stays in shared memory, since the scores of a
+    // tile take most of the registers.
+    const Piece& pc = ct.piece[s];
+    if (row == 0) ct.walk[s].start(plan);
+    for (;;) {
+      stream_barrier(s);
+      if (row == 0) ct.more[s] = ct.walk[s].next<kKeys>(P.shape, plan, &ct.piece[s]);
+      stream_barrier(s);
+      if (!ct.more[s]) break;
       const int nt = pc.k1 - pc.k0, tokens = pc.i1 - pc.i0;
       const bool two = tokens > P.tile_tokens;
       const int t0 = two ? s * P.tile_tokens : 0;                                       // first token of this stream's tile
@@ -448,59 +484,40 @@ __global__ void __launch_bounds__(kThreads, 1)
           fence_proxy_async_shared();
         }
         if (busy) {
-          const uint32_t all = boxes_mask(kKeys / P.kv_box);
-          const bool whole = j0 + kKeys - 1 <= hi && (j0 >= lo || j0 + kKeys <= a.sinks) && pages == all;
+          float v[kKeys];
+#pragma unroll
+          for (int c = 0; c < kKeys; c += 32) tmem_ld32(t_s + c, v + c);
+          // A row of the tile that holds no token is left as it is: nothing reads what it gives.
+          const bool whole = !valid || (j0 + kKeys - 1 <= hi && (j0 >= lo || j0 + kKeys <= a.sinks) &&
+                                        pages == boxes_mask(kKeys / P.kv_box));
           const bool masked = !__all_sync(0xFFFFFFFFu, whole);
-          uint32_t see[kKeys / 32];
+          tmem_wait_ld();
+          if (P.negate) {
+#pragma unroll
+            for (int c = 0; c < kKeys; ++c) v[c] = -v[c];
+          }
           if (masked) {
 #pragma unroll
-            for (int w = 0; w < kKeys / 32; ++w)
-              see[w] = seen_word(hi - j0 - 32 * w, lo - j0 - 32 * w, a.sinks - j0 - 32 * w) & page_word(pages, P.kv_box, w);
-          }
-          // The row is read twice, 32 scores at a time, so that it needs no more registers: for
-          // its maximum, then for its weights.
-          float va[32], vb[32];
-          auto scores_of = [&](int w, float* v) {
-            if (P.negate) {
-#pragma unroll
-              for (int c = 0; c < 32; ++c) v[c] = -v[c];
-            }
-            if (masked) {
+            for (int w = 0; w < kKeys / 32; ++w) {
+              const uint32_t see = seen_word(hi - j0 - 32 * w, lo - j0 - 32 * w, a.sinks - j0 - 32 * w) &
+                                   page_word(pages, P.kv_box, w);
 #pragma unroll
               for (int c = 0; c < 32; ++c)
-                if (!(see[w] >> c & 1u)) v[c] = -INFINITY;
+                if (!(see >> c & 1u)) v[32 * w + c] = -INFINITY;
             }
-          };
-          auto top_of = [&](const float* v) {
-            float t[4] = {v[0], v[1], v[2], v[3]};
+          }
+          float t[8];
 #pragma unroll
-            for (int c = 4; c < 32; c += 4)
+          for (int i = 0; i < 8; ++i) t[i] = v[i];
 #pragma unroll
-              for (int i = 0; i < 4; ++i) t[i] = fmaxf(t[i], v[c + i]);
-            return fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
-          };
-          tmem_ld32(t_s, va);
-          tmem_wait_ld();
-          tmem_ld32(t_s + 32, vb);
-          scores_of(0, va);
-          float top = top_of(va);
-          tmem_wait_ld();
-          tmem_ld32(t_s + 64, va);
-          scores_of(1, vb);
-          top = fmaxf(top, top_of(vb));
-          tmem_wait_ld();
-          tmem_ld32(t_s + 96, vb);
-          scores_of(2, va);
-          top = fmaxf(top, top_of(va));
-          tmem_wait_ld();
-          tmem_ld32(t_s, va);
-          scores_of(3, vb);
-          top = fmaxf(top, top_of(vb));
-          tmem_wait_ld();
+          for (int c = 8; c < kKeys; c += 8)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t[i] = fmaxf(t[i], v[c + i]);
+          const float top = fmaxf(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])), fmaxf(fmaxf(t[4], t[5]), fmaxf(t[6], t[7])));
           if (done == 0) {
             m = top;
           } else {
-            const bool raise = (top - m) * sl > 8.f;
+            const bool raise = valid && (top - m) * sl > 8.f;
             if (__any_sync(0xFFFFFFFFu, raise)) {
               const float up = fmaxf(m, top), f = raise ? exp2_fast((m - up) * sl) : 1.f;
               if (raise) m = up;
@@ -518,29 +535,18 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           const float ref = m == -INFINITY ? 0.f : m * sl;
           float sum[4] = {0.f, 0.f, 0.f, 0.f};
-          // P takes the columns of scores that are read already
-          auto weights_of = [&](int w, float* v) {
-            scores_of(w, v);
+#pragma unroll
+          for (int c = 0; c < kKeys; c += 32) {
             uint32_t x[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const float y = exp2_fast(fmaf(v[2 * i], sl, -ref)), z = exp2_fast(fmaf(v[2 * i + 1], sl, -ref));
+              const float y = exp2_fast(fmaf(v[c + 2 * i], sl, -ref)), z = exp2_fast(fmaf(v[c + 2 * i + 1], sl, -ref));
               sum[i & 1] += y;
               sum[2 + (i & 1)] += z;
               x[i] = pack_bf16x2(y, z);
             }
-            tmem_st16(t_s + 16 * w, x);
-          };
-          tmem_ld32(t_s + 32, vb);
-          weights_of(0, va);
-          tmem_wait_ld();
-          tmem_ld32(t_s + 64, va);
-          weights_of(1, vb);
-          tmem_wait_ld();
-          tmem_ld32(t_s + 96, vb);
-          weights_of(2, va);
-          tmem_wait_ld();
-          weights_of(3, vb);
+            tmem_st16(t_s + c / 2, x);
+          }
           l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
           tmem_wait_st();
         }
@@ -598,7 +604,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         // The two streams hold parts of the same rows: each joins half of the columns.
         ct.stat[s][row] = make_float2(done ? m : -INFINITY, l);
         tc_fence_before();
-        named_barrier(1, 256);
+        named_barrier<1, 256>();
         tc_fence_after();
         const float2 x0 = ct.stat[0][row], x1 = ct.stat[1][row];
         const float top = fmaxf(x0.x, x1.x);
@@ -620,7 +626,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         if (s == 0) put_stat(top, sum);
         tc_fence_before();
-        named_barrier(1, 256);  // both are through with O and the statistics
+        named_barrier<1, 256>();  // both are through with O and the statistics
         tc_fence_after();
       }
       if (whole) continue;
