@@ -93,12 +93,12 @@ struct PlanStart {
 
 // One piece: key tiles [k0, k1) of a unit.
 struct Piece {
-  int b, head, unit;
+  int b, head;
   int row0, n, c;  // first packed row of the sequence, its tokens, its cached tokens
   int i0, i1;      // tokens of the unit
   UnitKeys keys;
-  int k0, k1;             // of keys.count (an empty unit: 0, 0)
-  int first_cta, pieces;  // the CTAs that share the unit
+  int k0, k1;  // of keys.count (an empty unit: 0, 0)
+  int pieces;  // the CTAs that share the unit
 };
 
 // x / y; a division of 64 bits takes many instructions, and costs rarely need them.
@@ -127,7 +127,6 @@ struct PieceWalk {
       if (unit * (long long)s.unit_tokens < q.n) {
         out->b = b;
         out->head = head;
-        out->unit = unit;
         out->row0 = q.first;
         out->n = q.n;
         out->c = cached_tokens(s.cache_len, b);
@@ -148,8 +147,7 @@ struct PieceWalk {
     const int cost = max(1, out->keys.count);
     const long long k0 = at - unit_begin, left = p.end - unit_begin;
     const int k1 = left < cost ? (int)left : cost;
-    out->first_cta = (int)quotient(unit_begin, p.share);
-    out->pieces = (int)quotient(unit_begin + cost - 1, p.share) - out->first_cta + 1;
+    out->pieces = (int)(quotient(unit_begin + cost - 1, p.share) - quotient(unit_begin, p.share)) + 1;
     out->k0 = out->keys.count ? (int)k0 : 0;
     out->k1 = out->keys.count ? k1 : 0;
     at = unit_begin + k1;

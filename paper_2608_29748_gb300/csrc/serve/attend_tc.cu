@@ -9,13 +9,13 @@
 // A CTA runs two streams, so that one's matrix products run during the other's softmax:
 // two row tiles over the same key tiles where a unit has more than 128 rows (prompts),
 // or the even and the odd key tiles of one row tile (tokens, blocks), joined at the end.
-// The maximum that the exponents refer to is raised, and O rescaled, only where a row
-// would otherwise pass 2^8 of it: the first tile and few others.
+// The maximum that the exponents refer to is the first tile's, and is raised, and O rescaled,
+// only where the weights of a row in a tile pass 2^14.
 //
 // Warps 0 and 2 copy the K and the V tiles into a ring with TMA, a box for each run of
 // slots within a page (a warp issues a box in about 120 cycles, so one warp for both was
-// the bound with pages of 16), warp 3 copies Q; warp 1 issues the products; warps 4-7 and
-// 8-11 are the streams' softmax.
+// the bound with pages of 16); warps 1 and 3 issue the streams' products; warps 4-7 and
+// 8-11 are their softmax.
 // A tile of keys is 4 D 128 bytes of HBM traffic against 2 x 128 x 128 x D products of a
 // tensor core that does 8192 flop a cycle: 1024 of the 2790 cycles that the bytes take
 // at D = 128, so tokens and blocks are bound by HBM, and a row tile that is not full costs
@@ -32,6 +32,7 @@ namespace {
 constexpr int kThreads = 384;
 constexpr int kKeys = 128;  // keys of a tile
 constexpr int kRows = 128;  // rows of a tile
+constexpr unsigned long long kDrainNs = 20ull * 1000ull * 1000ull;
 constexpr int kMasks = 16;  // ring of page masks: more than the tiles between loading and softmax
 
 struct TcParams {
@@ -48,28 +49,36 @@ struct TcParams {
 template <int DP>
 struct TcShape {
   static constexpr int kTileBytes = kKeys * DP * 2;
-  static constexpr int kStages = DP == 64 ? 10 : 5;
+  // K and V tiles have rings of their own, each filled by one warp.  A tile of K is free after
+  // its scores, one of V only after the softmax, so V has the odd one.
+  static constexpr int kRingK = DP == 64 ? 5 : 2, kRingV = DP == 64 ? 5 : 3;
   static constexpr int kHalves = DP / 64;              // 128-byte columns of a tile
   static constexpr int kHalfBytes = kKeys * 128;
-  static constexpr int kQOffset = kStages * kTileBytes;  // after the ring
+  static constexpr int kVOffset = kRingK * kTileBytes, kQOffset = kVOffset + kRingV * kTileBytes;
   static constexpr int kControl = kQOffset + 2 * kRows * DP * 2;
   static constexpr int kPartRows = 2 * kRows;
   static constexpr int kPart = kPartRows * (DP + 2);  // floats of a part
 };
 
 struct Control {
-  uint64_t full[10], empty[10];  // the ring
-  uint64_t q_full, q_empty;
-  uint64_t s_full[2];  // S of a tile ready (and the product before it done), or O complete
+  // A ring's slots.  A wait for a phase by its parity is right only for one who has seen the
+  // phase before, so a slot has a `full` barrier per class of tiles (of stream 0, of stream
+  // 1, of both), every use of which its waiters see.
+  struct Ring {
+    uint64_t full[3][5], empty[5];
+  } ring[2];  // K, V
+  uint64_t q_full[2], q_empty[2];
+  uint64_t s_full[2];  // of a stream: S ready and the product with V before it done
   uint64_t p_full[2];  // P written, O rescaled
-  uint64_t done;       // after an expired wait: the issued products
+  uint64_t issued[2];  // two row tiles: a stream's products of a tile are on their way
+  uint64_t done[2];    // after an expired wait: the issued products
   PlanStart plan;
   long long sum[kThreads / 32];
   uint32_t tmem;
   int abort;
-  int more[2];
   PieceWalk walk[2];  // of the softmax streams
-  Piece piece[2];
+  Piece piece[2][2];  // this one and the next
+  int more[2][2];
   uint32_t mask[kMasks];  // of a key tile: bit i: box i has a page
   float2 stat[2][kRows];  // m and l of a stream's rows
 };
@@ -139,6 +148,32 @@ __device__ __forceinline__ float exp2_fast(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+// Two fp32 operations as one instruction.
+__device__ __forceinline__ uint64_t bits2(float2 v) {
+  uint64_t x;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(v.x), "f"(v.y));
+  return x;
+}
+__device__ __forceinline__ float2 floats2(uint64_t x) {
+  float2 v;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(x));
+  return v;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  uint64_t y;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
+  return floats2(y);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  uint64_t y;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(bits2(a)), "l"(bits2(b)));
+  return floats2(y);
+}
 // Moves registers from the warpgroup of the copies and products to those of the softmax:
 // 128 x 88 + 256 x 208 are the 384 x 168 of the launch.
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 88;"); }
@@ -169,13 +204,6 @@ __device__ __forceinline__ uint64_t sw128_mnmajor_desc(uint32_t saddr) {
          (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
 constexpr uint32_t kMajorB = 1u << 16;  // instruction descriptor: B is MN-major
-
-// The key tiles of a piece in the order in which the products take them from the ring:
-// with two row tiles K0 V0 K1 V1 ..., with one K0 K1 V0 K2 V1 ... .
-__device__ __forceinline__ int k_position(int j, bool two) { return two ? 2 * j : (j == 0 ? 0 : 2 * j - 1); }
-__device__ __forceinline__ int v_position(int j, int tiles, bool two) {
-  return two ? 2 * j + 1 : (j + 1 < tiles ? 2 * j + 2 : 2 * j + 1);
-}
 
 // Bits c of a word of 32 keys: key c is visible iff c <= hi and (c >= lo or c < sinks).
 __device__ __forceinline__ uint32_t seen_word(int hi, int lo, int sinks) {
@@ -209,17 +237,21 @@ __global__ void __launch_bounds__(kThreads, 1)
 
   if (tid == 0) {
     ct.abort = 0;
-    for (int s = 0; s < Sh::kStages; ++s) {
-      mbar_init(smem_u32(&ct.full[s]), 1);
-      mbar_init(smem_u32(&ct.empty[s]), 1);
-    }
-    mbar_init(smem_u32(&ct.q_full), 1);
-    mbar_init(smem_u32(&ct.q_empty), 1);
+    // A tile of a ring is free when both streams are through with it; where only one of them
+    // uses it, the copying warp counts for the other.
+    for (int r = 0; r < 2; ++r)
+      for (int s = 0; s < 5; ++s) {
+        for (int c = 0; c < 3; ++c) mbar_init(smem_u32(&ct.ring[r].full[c][s]), 1);
+        mbar_init(smem_u32(&ct.ring[r].empty[s]), 2);
+      }
     for (int s = 0; s < 2; ++s) {
+      mbar_init(smem_u32(&ct.q_full[s]), 1);
+      mbar_init(smem_u32(&ct.q_empty[s]), 2);  // both streams
       mbar_init(smem_u32(&ct.s_full[s]), 1);
       mbar_init(smem_u32(&ct.p_full[s]), 4);  // one arrival per warp of the stream
+      mbar_init(smem_u32(&ct.issued[s]), 1);
+      mbar_init(smem_u32(&ct.done[s]), 1);
     }
-    mbar_init(smem_u32(&ct.done), 1);
     fence_mbar_init();
     tma_prefetch_desc(&tm_q);
     tma_prefetch_desc(&tm_k);
@@ -242,18 +274,24 @@ __global__ void __launch_bounds__(kThreads, 1)
     PieceWalk walk;
     walk.start(plan);
     Piece pc;
+    bool drain = false;
     if (warp == 0 || warp == 2) {
-      // ---- copies of K (warp 0) and V (warp 2): lane (half, box) loads one box of a tile ----
+      // ---- copies of K (warp 0), and of Q and V (warp 2) ----
       const bool keys = warp == 0;
       const CUtensorMap* map = keys ? &tm_k : &tm_v;
+      // lane (half, box) loads one box of a tile
       const int boxes = kKeys / P.kv_box, half = lane / 16, box = lane % 16;
       const bool active = box < boxes && half < Sh::kHalves;
-      const int page_size = a.cache.page_size;
-      uint32_t it = 0, tiles = 0, issued = 0, parity = 0;
+      const int page_size = a.cache.page_size, box_rows = P.q_box * P.group;
+      Control::Ring& ring = ct.ring[keys ? 0 : 1];
+      const uint32_t slots = keys ? Sh::kRingK : Sh::kRingV, tiles_at = base + (keys ? 0 : Sh::kVOffset);
+      uint32_t tiles = 0, slot = 0, phase = 0, used[2] = {0, 0};
+      int turn = 0;
       bool ok = true;
       while (ok && walk.next<kKeys>(P.shape, plan, &pc)) {
-        const int nt = pc.k1 - pc.k0;
-        const bool two = pc.i1 - pc.i0 > P.tile_tokens;
+        const int nt = pc.k1 - pc.k0, tokens = pc.i1 - pc.i0;
+        if (nt == 0) continue;
+        const bool two = tokens > P.tile_tokens;
         struct Place {
           int page, slot;
         };
@@ -268,156 +306,180 @@ __global__ void __launch_bounds__(kThreads, 1)
         };
         // looked up two tiles ahead of their copies
         Place now = place_of(0), next = place_of(1);
-        for (int k = 0; k < nt; ++k) {
+        if (!keys) {
+          // Q: boxes of q_box tokens times the head group, rows in order.  A unit of two row
+          // tiles takes both buffers, one of one tile the other one than before.
+#pragma unroll
+          for (int q = 0; q < 2; ++q) {
+            if (!ok || (!two && q != turn)) continue;
+            const int t0 = two ? q * P.tile_tokens : 0, n = min(tokens - t0, P.tile_tokens);
+            const int q_boxes = (n + P.q_box - 1) / P.q_box;
+            ok = warp_wait_all(&ct.q_empty[q], (used[q] & 1u) ^ 1u, abort);
+            if (!ok) continue;
+            ++used[q];
+            const uint32_t bar = smem_u32(&ct.q_full[q]);
+            if (lane == 0) mbar_arrive_expect_tx(bar, q_boxes * Sh::kHalves * box_rows * 128);
+            __syncwarp();
+            for (int i = lane; i < q_boxes * Sh::kHalves; i += 32) {
+              const int h = i % Sh::kHalves, x = i / Sh::kHalves;
+              tma_load_3d(base + Sh::kQOffset + q * (kRows * DP * 2) + h * Sh::kHalfBytes + x * box_rows * 128, &tm_q, h * 64,
+                          pc.head * P.group, pc.row0 + pc.i0 + t0 + x * P.q_box, bar);
+            }
+          }
+          if (!two) turn ^= 1;
+        }
+        for (int k = 0; k < nt && ok; ++k) {
           const Place after = place_of(k + 2);
-          const uint32_t n = it + (keys ? k_position(k, two) : v_position(k, nt, two));
-          const uint32_t slot = n % Sh::kStages, phase = (n / Sh::kStages) & 1u;
-          ok = warp_wait_all(&ct.empty[slot], phase ^ 1u, abort);
+          ok = warp_wait_all(&ring.empty[slot], phase ^ 1u, abort);
           if (!ok) break;
-          const uint32_t bar = smem_u32(&ct.full[slot]);
+          const uint32_t bar = smem_u32(&ring.full[two ? 2 : k & 1][slot]);
           const uint32_t placed = __ballot_sync(0xFFFFFFFFu, active && half == 0 && now.page < a.cache.num_pages);
           if (lane == 0) {
+            if (!two) mbar_arrive(smem_u32(&ring.empty[slot]));
             if (keys) ct.mask[tiles % kMasks] = placed;
             mbar_arrive_expect_tx(bar, Sh::kTileBytes);
           }
           __syncwarp();
           if (active)
-            tma_load_4d(base + slot * Sh::kTileBytes + half * Sh::kHalfBytes + box * P.kv_box * 128, map, half * 64, pc.head,
+            tma_load_4d(tiles_at + slot * Sh::kTileBytes + half * Sh::kHalfBytes + box * P.kv_box * 128, map, half * 64, pc.head,
                         now.slot, now.page, bar);
-          issued |= 1u << slot;
-          parity = (parity & ~(1u << slot)) | phase << slot;
+          if (++slot == slots) {
+            slot = 0;
+            phase ^= 1u;
+          }
           ++tiles;
           now = next;
           next = after;
         }
-        it += 2 * nt;
       }
       if (!ok) {
         if (lane == 0) raise_abort(abort, a.status);
-        volatile int never = 0;  // this warp's copies in flight
-        for (int slot = 0; slot < Sh::kStages; ++slot)
-          if (issued >> slot & 1u) mbar_wait_bounded(smem_u32(&ct.full[slot]), parity >> slot & 1u, &never);
+        drain = true;
       }
-    } else if (warp == 3) {
-      // ---- copies of Q: boxes of q_box tokens times the head group, rows in order ----
-      const int box_rows = P.q_box * P.group;
-      uint32_t pieces = 0;
-      bool ok = true;
-      while (ok && walk.next<kKeys>(P.shape, plan, &pc)) {
-        if (pc.k1 == pc.k0) continue;
-        const int tokens = pc.i1 - pc.i0;
-        const bool two = tokens > P.tile_tokens;
-        const int b0 = (min(tokens, P.tile_tokens) + P.q_box - 1) / P.q_box;
-        const int b1 = two ? (tokens - P.tile_tokens + P.q_box - 1) / P.q_box : 0;
-        ok = warp_wait_all(&ct.q_empty, (pieces & 1u) ^ 1u, abort);
-        if (!ok) break;
-        ++pieces;
-        if (lane == 0) mbar_arrive_expect_tx(smem_u32(&ct.q_full), (b0 + b1) * Sh::kHalves * box_rows * 128);
-        __syncwarp();
-        for (int i = lane; i < (b0 + b1) * Sh::kHalves; i += 32) {
-          const int h = i % Sh::kHalves, x = i / Sh::kHalves, tile = x >= b0, n = tile ? x - b0 : x;
-          tma_load_3d(base + Sh::kQOffset + tile * (kRows * DP * 2) + h * Sh::kHalfBytes + n * box_rows * 128, &tm_q, h * 64,
-                      pc.head * P.group, pc.row0 + pc.i0 + tile * P.tile_tokens + n * P.q_box, smem_u32(&ct.q_full));
-        }
-      }
-      if (!ok) {
-        if (lane == 0) raise_abort(abort, a.status);
-        volatile int never = 0;
-        if (pieces) mbar_wait_bounded(smem_u32(&ct.q_full), (pieces - 1) & 1u, &never);
-      }
-    } else if (warp == 1) {
-      // ---- products ----
+    } else {
+      // ---- products of stream s (warps 1 and 3) ----
       constexpr uint32_t kS = idesc_bf16_f32(kRows, kKeys), kPV = idesc_bf16_f32(kRows, DP) | kMajorB;
-      uint32_t it = 0, pieces = 0, np[2] = {0, 0};
+      const int s = warp >> 1;
+      const uint32_t t_s = tmem + s * 128, t_o = tmem + 256 + s * 128;
+      uint32_t tiles = 0, used[2] = {0, 0}, np = 0;
+      int turn = 0;
       bool ok = true;
       auto wait = [&](uint64_t* bar, uint32_t parity) {
         ok = ok && warp_wait_all(bar, parity, abort);
         return ok;
       };
-      auto wait_tile = [&](uint32_t n) { return wait(&ct.full[n % Sh::kStages], (n / Sh::kStages) & 1u); };
-      auto tile = [&](uint32_t n) { return base + n % Sh::kStages * Sh::kTileBytes; };
-      auto scores = [&](int s, int q, uint32_t k_tile) {
-        if (elect_one()) {
-          const uint64_t qd = sw128_kmajor_desc(base + Sh::kQOffset + q * (kRows * DP * 2)), kd = sw128_kmajor_desc(k_tile);
-#pragma unroll
-          for (int h = 0; h < Sh::kHalves; ++h)
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              tc_mma_bf16(tmem + s * 128, qd + h * (Sh::kHalfBytes >> 4) + 2 * k, kd + h * (Sh::kHalfBytes >> 4) + 2 * k, kS,
-                          h + k > 0);
-        }
-        __syncwarp();
-      };
-      auto values = [&](int s, uint32_t v_tile, bool first) {
-        if (elect_one()) {
-          const uint64_t vd = sw128_mnmajor_desc(v_tile);
-#pragma unroll
-          for (int k = 0; k < kKeys / 16; ++k)
-            tc_mma_bf16_ts(tmem + 256 + s * 128, tmem + s * 128 + k * 8, vd + k * (2048 >> 4), kPV, !(first && k == 0));
-        }
-        __syncwarp();
+      uint32_t phases = 0;  // a bit per slot, tiles of this stream or of both, ring
+      auto wait_tile = [&](int ring, uint32_t slot, bool two) {
+        const uint32_t bit = 1u << (ring * 16 + two * 8 + slot);
+        const bool landed = wait(&ct.ring[ring].full[two ? 2 : s][slot], (phases & bit) != 0);
+        phases ^= bit;
+        return landed;
       };
       auto commit = [&](uint64_t* bar) {
         if (elect_one()) tc_commit(smem_u32(bar));
         __syncwarp();
       };
-      while (ok && walk.next<kKeys>(P.shape, plan, &pc)) {
-        const int nt = pc.k1 - pc.k0;
-        if (nt == 0) continue;
-        const bool two = pc.i1 - pc.i0 > P.tile_tokens;
-        if (!wait(&ct.q_full, pieces & 1u)) break;
-        ++pieces;
-        tc_fence_after();
-        if (two) {
-          for (int j = 0; j <= nt && ok; ++j) {  // the products of tile j - 1 with V, then the scores of tile j
-            const uint32_t v = it + v_position(j - 1, nt, true), k = it + k_position(j, true);
-            if (j > 0 && !wait_tile(v)) break;
-            if (j < nt && !wait_tile(k)) break;
+      auto scores = [&](int q, uint32_t slot) {
+        if (elect_one()) {
+          const uint64_t qd = sw128_kmajor_desc(base + Sh::kQOffset + q * (kRows * DP * 2));
+          const uint64_t kd = sw128_kmajor_desc(base + slot * Sh::kTileBytes);
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-              if (j > 0) {
-                if (!wait(&ct.p_full[s], np[s]++ & 1u)) break;
-                tc_fence_after();
-                values(s, tile(v), j == 1);
-                if (s == 1) commit(&ct.empty[v % Sh::kStages]);
-              }
-              if (j < nt) scores(s, s, tile(k));
-              commit(&ct.s_full[s]);
-            }
-            if (j < nt && ok) commit(&ct.empty[k % Sh::kStages]);
-            if (j == nt - 1) commit(&ct.q_empty);
-          }
-        } else {
-          for (int j = 0; j < nt + 2 && ok; ++j) {
-            const int s = j & 1;
-            if (j >= 2) {
-              const uint32_t v = it + v_position(j - 2, nt, false);
-              if (!wait_tile(v) || !wait(&ct.p_full[s], np[s]++ & 1u)) break;
-              tc_fence_after();
-              values(s, tile(v), j < 4);
-              commit(&ct.empty[v % Sh::kStages]);
-            }
-            if (j < nt) {
-              const uint32_t k = it + k_position(j, false);
-              if (!wait_tile(k)) break;
-              tc_fence_after();
-              scores(s, 0, tile(k));
-              commit(&ct.empty[k % Sh::kStages]);
-              if (j == nt - 1) commit(&ct.q_empty);
-            }
-            if (j >= 2 || j < nt) commit(&ct.s_full[s]);
-          }
+          for (int h = 0; h < Sh::kHalves; ++h)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              tc_mma_bf16(t_s, qd + h * (Sh::kHalfBytes >> 4) + 2 * k, kd + h * (Sh::kHalfBytes >> 4) + 2 * k, kS, h + k > 0);
         }
-        it += 2 * nt;
+        __syncwarp();
+      };
+      // The product of P with a tile of V, which is free after it.
+      auto values = [&](uint32_t slot, bool first) {
+        tc_fence_after();
+        if (elect_one()) {
+          const uint64_t vd = sw128_mnmajor_desc(base + Sh::kVOffset + slot * Sh::kTileBytes);
+#pragma unroll
+          for (int k = 0; k < kKeys / 16; ++k)
+            tc_mma_bf16_ts(t_o, t_s + k * 8, vd + k * (2048 >> 4), kPV, !(first && k == 0));
+        }
+        __syncwarp();
+        commit(&ct.ring[1].empty[slot]);
+      };
+      struct Work {  // of a piece: what the products need of it, looked up a piece ahead
+        int nt, two, k0;
+        UnitKeys keys;
+      };
+      bool more = true;
+      auto next_work = [&]() {
+        Work w{};
+        do {
+          more = walk.next<kKeys>(P.shape, plan, &pc);
+          if (more) w = Work{pc.k1 - pc.k0, pc.i1 - pc.i0 > P.tile_tokens, pc.k0, pc.keys};
+        } while (more && w.nt == 0);
+        return w;
+      };
+      uint32_t batches = 0;
+      Work next = next_work();
+      while (ok && more) {
+        const Work w = next;
+        const int nt = w.nt;
+        const bool two = w.two;
+        const int q = two ? s : turn, step = two ? 1 : 2;
+        const int first = two ? 0 : s;  // of this stream's tiles: first, first + step, ...
+        if (!wait(&ct.q_full[q], used[q]++ & 1u)) break;
+        if (two && !wait(&ct.q_full[q ^ 1], used[q ^ 1]++ & 1u)) break;
+        if (two && lane == 0) mbar_arrive(smem_u32(&ct.q_empty[q ^ 1]));  // the other stream's
+        if (!two) turn ^= 1;
+        tc_fence_after();
+        int j = first;
+        bool landed = false;  // V of the tile before
+        for (; j < nt; j += step) {
+          const uint32_t k = (tiles + j) % Sh::kRingK, v = (tiles + j) % Sh::kRingV, before = (tiles + j - step) % Sh::kRingV;
+          if (!wait_tile(0, k, two)) break;
+          if (j > first && ((!landed && !wait_tile(1, before, two)) || !wait(&ct.p_full[s], np++ & 1u))) break;
+          // With two row tiles the streams issue in turn: products that are issued together
+          // share the tensor core and end together, and then it waits for both softmaxes.
+          if (two && (s == 1 || batches > 0) && !wait(&ct.issued[s ^ 1], (s == 1 ? batches : batches - 1) & 1u)) break;
+          if (j > first) values(before, j == first + step);
+          // V of a tile at the edge of what the unit sees is there before its scores are: the
+          // softmax clears rows of it
+          const int j0 = w.keys.tile(w.k0 + j) * kKeys;
+          landed = j0 < w.keys.lo || j0 + kKeys - 1 > w.keys.hi;
+          if (landed && !wait_tile(1, v, two)) break;
+          tc_fence_after();
+          scores(q, k);
+          if (two) {
+            if (lane == 0) mbar_arrive(smem_u32(&ct.issued[s]));
+            ++batches;
+          }
+          commit(&ct.s_full[s]);
+          commit(&ct.ring[0].empty[k]);
+          if (j == first) next = next_work();
+        }
+        if (!ok) break;
+        if (j > first) {
+          commit(&ct.q_empty[q]);
+          const uint32_t before = (tiles + j - step) % Sh::kRingV;
+          if ((!landed && !wait_tile(1, before, two)) || !wait(&ct.p_full[s], np++ & 1u)) break;
+          values(before, j == first + step);
+          commit(&ct.s_full[s]);
+        } else {
+          if (lane == 0) mbar_arrive(smem_u32(&ct.q_empty[q]));  // no tile for this stream
+          next = next_work();
+        }
+        tiles += nt;
       }
       if (!ok) {
         if (lane == 0) raise_abort(abort, a.status);
         volatile int never = 0;
-        commit(&ct.done);
-        mbar_wait_bounded(smem_u32(&ct.done), 0, &never);
+        commit(&ct.done[s]);
+        mbar_wait_bounded(smem_u32(&ct.done[s]), 0, &never);
       }
-      __syncwarp();
     }
+    // After an expired wait: time for this CTA's copies in flight to land.
+    if (drain) {
+      const unsigned long long t0 = global_ns();
+      while (global_ns() - t0 < kDrainNs) __nanosleep(1000);
+    }
+    __syncwarp();
   } else {
     more_registers();
     // ---- softmax: stream s, one thread per row ----
@@ -426,7 +488,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t t_s = tmem + lanes + s * 128, t_o = tmem + lanes + 256 + s * 128;
     const int G = P.group, D = a.cache.head_dim;
     const float sl = P.scale2;
-    uint32_t it = 0, ns = 0, tiles = 0;
+    uint32_t ns = 0, tiles = 0;
     JoinUnit unit{};
     bool ok = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
@@ -435,15 +497,17 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) raise_abort(abort, a.status);
       }
     };
-    // One thread of the stream walks; the piece stays in shared memory, since the scores of a
-    // tile take most of the registers.
-    const Piece& pc = ct.piece[s];
-    if (row == 0) ct.walk[s].start(plan);
-    for (;;) {
+    // One thread of the stream walks, a piece ahead; the pieces stay in shared memory.
+    const bool walker = row == kRows - 32;
+    if (walker) {
+      ct.walk[s].start(plan);
+      ct.more[s][0] = ct.walk[s].next<kKeys>(P.shape, plan, &ct.piece[s][0]);
+    }
+    for (int np = 0;; np ^= 1) {
       stream_barrier(s);
-      if (row == 0) ct.more[s] = ct.walk[s].next<kKeys>(P.shape, plan, &ct.piece[s]);
-      stream_barrier(s);
-      if (!ct.more[s]) break;
+      if (!ct.more[s][np]) break;
+      if (walker) ct.more[s][np ^ 1] = ct.walk[s].next<kKeys>(P.shape, plan, &ct.piece[s][np ^ 1]);
+      const Piece& pc = ct.piece[s][np];
       const int nt = pc.k1 - pc.k0, tokens = pc.i1 - pc.i0;
       const bool two = tokens > P.tile_tokens;
       const int t0 = two ? s * P.tile_tokens : 0;                                       // first token of this stream's tile
@@ -458,7 +522,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int c = 0; c < D; c += 8) *reinterpret_cast<uint4*>(out + c) = make_uint4(0u, 0u, 0u, 0u);
         continue;
       }
-      float m = -INFINITY, l = 0.f;  // of the raw scores; the sum of 2^((score - m) sl)
+      float m = -INFINITY;                // of the raw scores
+      float2 l = make_float2(0.f, 0.f);  // the sum of 2^((score - m) sl), in two parts
       int done = 0;
       for (int j = two ? 0 : s; j < nt; j += two ? 1 : 2) {
         const int tile = pc.keys.tile(pc.k0 + j), j0 = tile * kKeys;
@@ -467,30 +532,29 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc_fence_after();
         const uint32_t pages = ct.mask[(tiles + j) % kMasks];
         // A row of V that no row of the unit sees holds anything, and 0 times that need not
-        // be 0: cleared before the product.
+        // be 0: cleared before the product (V of such a tile landed before its scores were
+        // issued).
         if (j0 < pc.keys.lo || j0 + kKeys - 1 > pc.keys.hi) {
-          const uint32_t v = it + v_position(j, nt, two), slot = v % Sh::kStages;
-          wait(&ct.full[slot], (v / Sh::kStages) & 1u);
-          if (!ok) break;
+          const uint32_t slot = (tiles + j) % Sh::kRingV;
           const int key = j0 + row;
           if (key > pc.keys.hi || (key < pc.keys.lo && key >= a.sinks)) {
 #pragma unroll
             for (int h = 0; h < Sh::kHalves; ++h)
 #pragma unroll
-              for (int c = 0; c < 8; ++c)
-                *reinterpret_cast<uint4*>(smem + slot * Sh::kTileBytes + h * Sh::kHalfBytes + row * 128 + c * 16) =
+              for (int c = 0; c < 8; ++c)  // the lanes of a warp begin at different banks
+                *reinterpret_cast<uint4*>(smem + Sh::kVOffset + slot * Sh::kTileBytes + h * Sh::kHalfBytes + row * 128 + ((c + row) & 7) * 16) =
                     make_uint4(0u, 0u, 0u, 0u);
           }
           fence_proxy_async_shared();
         }
+        // A row of the tile that holds no token is left as it is: nothing reads what it gives.
+        const bool whole = !valid || (j0 + kKeys - 1 <= hi && (j0 >= lo || j0 + kKeys <= a.sinks) &&
+                                      pages == boxes_mask(kKeys / P.kv_box));
+        const bool masked = !__all_sync(0xFFFFFFFFu, whole);
         if (busy) {
           float v[kKeys];
 #pragma unroll
           for (int c = 0; c < kKeys; c += 32) tmem_ld32(t_s + c, v + c);
-          // A row of the tile that holds no token is left as it is: nothing reads what it gives.
-          const bool whole = !valid || (j0 + kKeys - 1 <= hi && (j0 >= lo || j0 + kKeys <= a.sinks) &&
-                                        pages == boxes_mask(kKeys / P.kv_box));
-          const bool masked = !__all_sync(0xFFFFFFFFu, whole);
           tmem_wait_ld();
           if (P.negate) {
 #pragma unroll
@@ -499,29 +563,60 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (masked) {
 #pragma unroll
             for (int w = 0; w < kKeys / 32; ++w) {
-              const uint32_t see = seen_word(hi - j0 - 32 * w, lo - j0 - 32 * w, a.sinks - j0 - 32 * w) &
-                                   page_word(pages, P.kv_box, w);
+              const int k0 = j0 + 32 * w;
+              const uint32_t see = seen_word(hi - k0, lo - k0, a.sinks - k0) & page_word(pages, P.kv_box, w);
+              if (__all_sync(0xFFFFFFFFu, !valid || see == ~0u)) continue;
 #pragma unroll
               for (int c = 0; c < 32; ++c)
                 if (!(see >> c & 1u)) v[32 * w + c] = -INFINITY;
             }
           }
-          float t[8];
+          auto top_of = [&]() {
+            float t[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) t[i] = v[i];
+            for (int i = 0; i < 8; ++i) t[i] = max3(v[i], v[8 + i], v[16 + i]);
 #pragma unroll
-          for (int c = 8; c < kKeys; c += 8)
+            for (int c = 24; c < 120; c += 16)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) t[i] = fmaxf(t[i], v[c + i]);
-          const float top = fmaxf(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])), fmaxf(fmaxf(t[4], t[5]), fmaxf(t[6], t[7])));
-          if (done == 0) {
-            m = top;
-          } else {
-            const bool raise = valid && (top - m) * sl > 8.f;
-            if (__any_sync(0xFFFFFFFFu, raise)) {
-              const float up = fmaxf(m, top), f = raise ? exp2_fast((m - up) * sl) : 1.f;
-              if (raise) m = up;
-              l *= f;
+              for (int i = 0; i < 8; ++i) t[i] = max3(t[i], v[c + i], v[c + 8 + i]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t[i] = fmaxf(t[i], v[120 + i]);
+            return max3(max3(t[0], t[1], t[2]), max3(t[3], t[4], t[5]), fmaxf(t[6], t[7]));
+          };
+          if (__any_sync(0xFFFFFFFFu, valid && m == -INFINITY)) {  // the first tile, or nothing seen so far
+            const float top = top_of();
+            if (m == -INFINITY) m = top;
+          }
+          // The weights refer to a maximum of before, without looking for this tile's.  Where their
+          // sum in a row shows that one may have grown past 2^14, and only there, the maximum is
+          // taken, O rescaled, and the tile done again.
+          float2 sum[2];
+          for (;;) {
+            const float ref = m == -INFINITY ? 0.f : -m * sl;
+            const float2 sl2 = make_float2(sl, sl), ref2 = make_float2(ref, ref);
+            sum[0] = sum[1] = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int c = 0; c < kKeys; c += 32) {
+              uint32_t x[16];
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                float2 y = fma2(make_float2(v[c + 2 * i], v[c + 2 * i + 1]), sl2, ref2);
+                y.x = exp2_fast(y.x);
+                y.y = exp2_fast(y.y);
+                sum[i & 1] = add2(sum[i & 1], y);
+                x[i] = pack_bf16x2(y.x, y.y);
+              }
+              tmem_st16(t_s + c / 2, x);
+            }
+            const float2 both = add2(sum[0], sum[1]);
+            const bool raise = valid && both.x + both.y > 16384.f;
+            tmem_wait_st();
+            if (!__any_sync(0xFFFFFFFFu, raise)) break;
+            const float up = raise ? fmaxf(m, top_of()) : m, f = raise ? exp2_fast((m - up) * sl) : 1.f;
+            m = up;
+            l.x *= f;
+            l.y *= f;
+            if (done > 0) {
 #pragma unroll
               for (int c = 0; c < DP; c += 8) {
                 float o[8];
@@ -533,35 +628,20 @@ __global__ void __launch_bounds__(kThreads, 1)
               }
             }
           }
-          const float ref = m == -INFINITY ? 0.f : m * sl;
-          float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int c = 0; c < kKeys; c += 32) {
-            uint32_t x[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const float y = exp2_fast(fmaf(v[c + 2 * i], sl, -ref)), z = exp2_fast(fmaf(v[c + 2 * i + 1], sl, -ref));
-              sum[i & 1] += y;
-              sum[2 + (i & 1)] += z;
-              x[i] = pack_bf16x2(y, z);
-            }
-            tmem_st16(t_s + c / 2, x);
-          }
-          l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-          tmem_wait_st();
+          l = add2(l, add2(sum[0], sum[1]));
         }
         ++done;
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&ct.p_full[s]));
       }
-      if (done && ok) {
-        wait(&ct.s_full[s], ns++ & 1u);  // O is complete
+      if (done && ok) {  // O is complete
+        wait(&ct.s_full[s], ns++ & 1u);
         tc_fence_after();
       }
-      it += 2 * nt;
       tiles += nt;
 
+      const float sum_l = l.x + l.y;
       const bool whole = pc.pieces == 1;
       float* part = a.partials + ((long long)blockIdx.x * 2 + (pc.k0 == 0 ? 1 : 0)) * Sh::kPart;
       // Columns [c0, c1) of this thread's row: into the output, or into the part.
@@ -589,7 +669,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           *reinterpret_cast<float2*>(part + Sh::kPartRows * DP + ((two ? s * kRows : 0) + row) * 2) = make_float2(mm * sl, ll);
       };
       if (two) {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
+        const float inv = sum_l == 0.f ? 0.f : 1.f / sum_l;
         if (busy && ok) {
 #pragma unroll
           for (int c = 0; c < DP; c += 32) {
@@ -599,10 +679,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             put(c, o, inv);
           }
         }
-        put_stat(m, l);
+        put_stat(m, sum_l);
       } else {
         // The two streams hold parts of the same rows: each joins half of the columns.
-        ct.stat[s][row] = make_float2(done ? m : -INFINITY, l);
+        ct.stat[s][row] = make_float2(done ? m : -INFINITY, sum_l);
         tc_fence_before();
         named_barrier<1, 256>();
         tc_fence_after();
