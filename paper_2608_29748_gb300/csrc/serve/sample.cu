@@ -8,18 +8,22 @@
 // weight at least min_p times the first one's.  The token is then the first one in
 // index order at which the running sum of the kept weights exceeds floor(u W).
 //
-// sample_cluster_kernel: a row lies in the registers of a cluster of CTAs (read once,
-// in 16-byte vectors), so that every pass over it is arithmetic.  Sorting it would
-// cost far more than reading it, and so would a histogram of every token in shared
-// memory (its atomics).  Instead a sample of the row gives a logit that about enough
-// tokens reach; these few are collected and sorted, and where they hold all that the
-// filters keep, which is the rule with top-k, or with top-p over a peaked
-// distribution, the rest is done among them.  Otherwise the place where a count or a
-// mass is reached is found by two histograms, the second within a bin of the first,
+// Sorting a row would cost far more than reading it, and so would a histogram of all of
+// its tokens in shared memory (its atomics).  Instead a sample of the row gives a logit
+// that about enough tokens reach; these few are collected and sorted, and where they
+// hold all that the filters keep, which is the rule with top-k, or with top-p over a
+// peaked distribution, the rest is done among them.  Otherwise the place where a count
+// or a mass is reached is found by two histograms, the second within a bin of the first,
 // and an exact sum.  Whatever does not fit (thousands of tokens with one logit) goes to
-// sample_row, which needs no memory for the row: radix selection over the 32-bit keys
-// of the logits, also for rows that no cluster holds.
+// sample_row: radix selection over the 32-bit keys of the logits.
+//
+// With many rows a CTA takes one and streams it (Stream), three or more of them to an SM,
+// and later passes over the row, where needed, find it in L2: 4096 rows are 46 MB at a
+// time.  With few rows a cluster of up to eight CTAs holds one in registers (Held), so
+// that every later pass is arithmetic.
 #include <math.h>
+
+#include <type_traits>
 
 #include "../tc_pair.cuh"
 #include "serve.h"
@@ -250,28 +254,152 @@ __device__ void sample_row(const SampleArgs& a, int r, RowShared& sm) {
 }
 
 
-constexpr int kRowThreads = 1024;
-template <typename T>
-__global__ void __launch_bounds__(kRowThreads) sample_row_kernel(SampleArgs a) {
-  __shared__ RowShared sm;
-  sample_row<T, kRowThreads>(a, blockIdx.x, sm);
-}
-
-// ---- a row in the registers of a cluster ---------------------------------------
+// ---- rows as the kernel below reads them ----------------------------------------
 constexpr int kThreads = 512;
 constexpr int kWarps = kThreads / 32;
-constexpr int kList = 4096;       // collected tokens
-constexpr int kBins = 256;        // of the first histogram, and of the sample's
-constexpr int kFineBins = 1024;   // of the second
+constexpr int kList = 4096;           // collected tokens
+constexpr int kBins = 256;            // of the first histogram, and of the sample's
+constexpr int kFineBins = 1024;       // of the second
 constexpr float kBinsPerNat = 11.5f;  // so that a token past the last bin (22.26 nats) weighs 0
-constexpr int kListTopK = 1024;   // largest top_k for which the list is tried
-constexpr int kListTopP = 400;    // tokens that the list aims at without top_k
+constexpr int kListTopK = 1024;       // largest top_k for which the list is tried
+constexpr int kListTopP = 400;        // tokens that the list aims at without top_k
 constexpr int kMaxCluster = 8;
+
+template <typename T>
+struct Vec {  // 16 bytes of a row
+  static constexpr int E = 16 / sizeof(T);
+  __device__ __forceinline__ static float value(const uint4& q, int e) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    if constexpr (E == 8) return e & 1 ? bf16_hi(w[e >> 1]) : bf16_lo(w[e >> 1]);
+    return __uint_as_float(w[e & 3]);
+  }
+  __device__ __forceinline__ static uint4 none() {
+    const uint32_t w = E == 8 ? 0xFF80FF80u : 0xFF800000u;  // -inf
+    return make_uint4(w, w, w, w);
+  }
+  // The largest of the 16 bytes' values; NaN where all of them are.
+  __device__ __forceinline__ static float top(const uint4& q) {
+    if constexpr (E == 8) {
+      const __nv_bfloat162* v = reinterpret_cast<const __nv_bfloat162*>(&q);
+      const __nv_bfloat162 m = __hmax2(__hmax2(v[0], v[1]), __hmax2(v[2], v[3]));
+      return fmaxf(__low2float(m), __high2float(m));
+    }
+    return fmaxf(fmaxf(value(q, 0), value(q, 1)), fmaxf(value(q, 2), value(q, 3)));
+  }
+};
+
+// What both forms of a row share: its vectors, and the elements before and after them.
+template <typename T>
+struct RowParts {
+  static constexpr int E = Vec<T>::E;
+  const T* p;
+  const uint4* q;
+  int V, head, vecs;
+  float edge;   // this thread's element before or after the vectors
+  int edge_at;  // its index; past the row where there is none
+  float top, inv_t, ys;
+
+  __device__ __forceinline__ void find(const SampleArgs& a, int r, bool edges) {
+    p = static_cast<const T*>(a.logits) + (r / a.R) * a.batch_stride + (r % a.R) * a.row_stride;
+    V = a.V;
+    head = min(V, (int)((16u - ((uintptr_t)p & 15u)) % 16u / sizeof(T)));
+    vecs = (V - head) / E;
+    q = reinterpret_cast<const uint4*>(p + head);
+    edge = -INFINITY;
+    edge_at = 0x7FFFFFFF;
+    const int t = threadIdx.x, tail = V - head - vecs * E;
+    if (edges && t < head + tail) {
+      edge_at = t < head ? t : head + vecs * E + t - head;
+      edge = logit(p, edge_at);
+    }
+  }
+  __device__ __forceinline__ int index(int vec) const { return head + vec * E; }
+  // How far below the maximum, in bins; 256 or more, or NaN: of no weight.
+  __device__ __forceinline__ float depth(float v) const { return v == top ? 0.f : (top - v) * ys; }
+  __device__ __forceinline__ uint32_t mass(float v) const { return whole_weight(weight(v, top, inv_t)); }
+};
+
+// A row in the registers of a cluster: vector `(rank NV + i) kThreads + tid` is x[i].
+template <typename T, int NV>
+struct Held : RowParts<T> {
+  static constexpr int kSegments = NV * kWarps;
+  uint4 x[NV];
+  int first;  // vector of x[0]
+
+  __device__ __forceinline__ void load(const SampleArgs& a, int r, int rank) {
+    this->find(a, r, rank == 0);
+    first = rank * NV * kThreads + threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      x[i] = first + i * kThreads < this->vecs ? __ldcs(this->q + first + i * kThreads) : Vec<T>::none();
+  }
+  // f(vector, index of its first element); past the row: -inf.
+  template <typename F>
+  __device__ __forceinline__ void vectors(F f) const {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) f(x[i], this->index(first + i * kThreads));
+  }
+  // Some vectors; the share of the row that they are.
+  template <typename F>
+  __device__ __forceinline__ float sample(F f) const {
+#pragma unroll
+    for (int i = 0; i < NV; i += kStep) f(x[i]);
+    return (float)((NV + kStep - 1) / kStep) / (float)NV;
+  }
+  static constexpr int kStep = NV >= 5 ? 5 : 1;
+  // The row in index order: segment s of warp w.  f(vector, index) of this thread's part.
+  __device__ __forceinline__ int segments() const { return NV; }
+  template <typename F>
+  __device__ __forceinline__ void segment(int s, F f) const {
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (i == s) f(x[i], this->index(first + i * kThreads));
+  }
+};
+
+// A row that a CTA streams.
+template <typename T>
+struct Stream : RowParts<T> {
+  static constexpr int kSegments = kWarps;
+  static constexpr int kAhead = 4;  // loads in flight per thread
+  __device__ __forceinline__ void load(const SampleArgs& a, int r, int) { this->find(a, r, true); }
+  template <typename F>
+  __device__ __forceinline__ void vectors(F f) const {
+    int v = threadIdx.x;
+    for (; v + (kAhead - 1) * kThreads < this->vecs; v += kAhead * kThreads) {
+      uint4 x[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) x[i] = __ldg(this->q + v + i * kThreads);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) f(x[i], this->index(v + i * kThreads));
+    }
+    for (; v < this->vecs; v += kThreads) f(__ldg(this->q + v), this->index(v));
+  }
+  // 32 runs of 32 vectors, spread over the row.
+  template <typename F>
+  __device__ __forceinline__ float sample(F f) const {
+    const int runs = this->vecs / 32, taken = runs < 32 ? runs : 32;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    for (int j = warp; j < taken; j += kWarps) f(__ldg(this->q + (long long)j * runs / taken * 32 + lane));
+    return (float)taken * 32.f / (float)(this->vecs > 0 ? this->vecs : 1);
+  }
+  // Warp w has the vectors [w per, (w + 1) per), 32 at a time.
+  __device__ __forceinline__ int per() const { return ((this->vecs + kWarps - 1) / kWarps + 31) / 32 * 32; }
+  __device__ __forceinline__ int segments() const { return 1; }
+  template <typename F>
+  __device__ __forceinline__ void run(F f) const {  // f(vector or none, index), whole warps
+    const int w = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const int end = min(this->vecs, (w + 1) * per());
+    for (int v = w * per(); v < end; v += 32)
+      if (!f(v + lane < end ? __ldg(this->q + v + lane) : Vec<T>::none(), this->index(v + lane))) break;
+  }
+};
 
 struct ClusterShared {
   union {
     struct {
       u64 list[kList];
+      u64 spare[kList / 4];  // of sort_list
       union {
         float mass[kFineBins];
         uint32_t count[kFineBins];
@@ -279,92 +407,23 @@ struct ClusterShared {
     };
     RowShared row;
   };
-  u64 seg[16 * kWarps + 2];  // kept mass by vector number and warp, before and after them
+  u64 seg[5 * kWarps + 2];  // kept mass of the segments, of what is before and after the vectors
   u64 part[kWarps];
   float wtop[kWarps];
+  int bin[2];
+  int entries;  // of the list that are kept
   // written by this CTA, read by the others of the cluster
   float top;
-  int first;       // index of its first maximum
-  int listed;      // tokens in its list
-  u64 sum;         // exact sums of a pass
-  // results that a CTA works out for itself
-  int bin[2];
-  u64 before;
+  int listed;  // tokens in its list
+  u64 sum[2];  // exact sums of a pass, in turn
   // written by CTA 0, read by all
-  u64 key;         // the last kept token, as an argmax key
+  u64 key;     // the last kept token
   int state;
-  int pick;
 };
-
-// States of a row after its list: done, or the general way.
-enum : int { kDone = 0, kGeneral = 1, kSlow = 2 };
-
-template <typename T, int NV>
-struct Row {
-  static constexpr int E = 16 / sizeof(T);
-  uint4 x[NV];  // this thread's vectors, rank * NV * kThreads + i * kThreads + tid
-  float edge;   // and an element before or after the row's vectors
-  int edge_at;  // its index, past the row where there is none
-  int head;     // elements before the vectors
-  int v0;       // index of the first element of vector 0 of this thread
-  int V;
-  float top, inv_t, ys;
-
-  __device__ __forceinline__ float value(const uint4& q, int e) const {
-    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-    if constexpr (E == 8) return e & 1 ? bf16_hi(w[e >> 1]) : bf16_lo(w[e >> 1]);
-    return __uint_as_float(w[e & 3]);
-  }
-  // f(logit, index) for every element of this thread; past the row: -inf, an index >= V.
-  template <typename F>
-  __device__ __forceinline__ void each(F f) const {
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int e = 0; e < E; ++e) f(value(x[i], e), v0 + i * kThreads * E + e);
-    f(edge, edge_at);
-  }
-  // How far below the maximum, in bins; 256 or more: of no weight.
-  __device__ __forceinline__ float depth(float v) const { return v == top ? 0.f : (top - v) * ys; }
-  __device__ __forceinline__ uint32_t mass(float v) const { return whole_weight(weight(v, top, inv_t)); }
-};
-
-__device__ __forceinline__ float4 no_nan(float4 v) {
-  v.x = v.x == v.x ? v.x : -INFINITY;
-  v.y = v.y == v.y ? v.y : -INFINITY;
-  v.z = v.z == v.z ? v.z : -INFINITY;
-  v.w = v.w == v.w ? v.w : -INFINITY;
-  return v;
-}
-// Two bf16 values with NaN replaced by -inf.
-__device__ __forceinline__ uint32_t no_nan2(uint32_t w) {
-  const uint32_t lo = (w & 0x7FFFu) > 0x7F80u ? 0xFF80u : w & 0xFFFFu;
-  const uint32_t hi = (w & 0x7FFF0000u) > 0x7F800000u ? 0xFF800000u : w & 0xFFFF0000u;
-  return lo | hi;
-}
-
-// Sorts the first `n` of the list (n at most kList) in descending order.
-__device__ void sort_list(u64* list, int n) {
-  int size = 1;
-  while (size < n) size <<= 1;
-  for (int i = n + threadIdx.x; i < size; i += kThreads) list[i] = 0;
-  __syncthreads();
-  for (int k = 2; k <= size; k <<= 1)
-    for (int j = k >> 1; j > 0; j >>= 1) {
-      for (int t = threadIdx.x; t < size / 2; t += kThreads) {
-        const int i = 2 * t - (t & (j - 1)), o = i + j;
-        const u64 a = list[i], b = list[o];
-        if ((a < b) == ((i & k) == 0)) {
-          list[i] = b;
-          list[o] = a;
-        }
-      }
-      __syncthreads();
-    }
-}
+enum : int { kDone = 0, kGeneral = 1, kSlow = 2 };  // what is left to do for a row after its list
 
 // Exclusive prefix of x over the block; *total the whole sum.
-__device__ u64 block_scan(u64 x, u64* part, u64* total) {
+__device__ __forceinline__ u64 block_scan(u64 x, u64* part, u64* total) {
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   u64 upto = x;
 #pragma unroll
@@ -378,11 +437,80 @@ __device__ u64 block_scan(u64 x, u64* part, u64* total) {
   u64 before = 0, sum = 0;
 #pragma unroll
   for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) before += part[w];
-    sum += part[w];
+    const u64 y = part[w];
+    if (w < warp) before += y;
+    sum += y;
   }
   *total = sum;
   return before + upto - x;
+}
+
+// Sorts the first n (at most kList) of the list in descending order, in place.  Up to a
+// quarter of the list: into bins by the depth of a logit below the maximum, then by counting
+// the larger ones within a bin, few where the logits differ.  More: bitonic.
+__device__ __noinline__ void sort_list(ClusterShared& sm, int n, float top, float scale) {
+  const int tid = threadIdx.x;
+  u64* list = sm.list;
+  if (n <= kList / 4) {
+    constexpr int kEach = kList / 4 / kThreads;
+    auto bin_of = [&](u64 key) {
+      const float v = key_value(key), y = v == top ? 0.f : (top - v) * scale;
+      return y < (float)kFineBins ? max(0, (int)y) : kFineBins - 1;
+    };
+    // sm.count is zero here
+    u64 key[kEach];
+    int place[kEach], bin[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int e = tid + i * kThreads;
+      if (e < n) {
+        key[i] = list[e];
+        bin[i] = bin_of(key[i]);
+        place[i] = (int)atomicAdd(&sm.count[bin[i]], 1u);
+      }
+    }
+    __syncthreads();
+    const uint32_t c0 = sm.count[2 * tid], c1 = sm.count[2 * tid + 1];
+    u64 all;
+    const uint32_t start = (uint32_t)block_scan(c0 + c1, sm.part, &all);
+    // start of a bin in the low half, its size in the high half
+    sm.count[2 * tid] = start | c0 << 16;
+    sm.count[2 * tid + 1] = (start + c0) | c1 << 16;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (tid + i * kThreads < n) sm.spare[(sm.count[bin[i]] & 0xFFFFu) + place[i]] = key[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+      if (tid + i * kThreads < n) {
+        const int from = (int)(sm.count[bin[i]] & 0xFFFFu), size = (int)(sm.count[bin[i]] >> 16);
+        int larger = 0;
+        for (int e = from; e < from + size; ++e) larger += sm.spare[e] > key[i];
+        list[from + larger] = key[i];
+      }
+    __syncthreads();
+    sm.count[2 * tid] = 0;
+    sm.count[2 * tid + 1] = 0;
+    __syncthreads();
+    return;
+  }
+  int size = 1;
+  while (size < n) size <<= 1;
+  for (int i = n + tid; i < size; i += kThreads) list[i] = 0;
+  __syncthreads();
+  for (int k = 2; k <= size; k <<= 1)
+    for (int j = k >> 1; j > 0; j >>= 1) {
+      for (int t = tid; t < size / 2; t += kThreads) {
+        const int i = 2 * t - (t & (j - 1)), o = i + j;
+        const u64 x = list[i], y = list[o];
+        if ((x < y) == ((i & k) == 0)) {
+          list[i] = y;
+          list[o] = x;
+        }
+      }
+      __syncthreads();
+    }
 }
 
 // The random number's place among `sum`.
@@ -395,285 +523,365 @@ __device__ __forceinline__ u64 top_p_target(float p, u64 total) {
   const double want = ceil((double)p * (double)total);
   return want < 1.0 ? 1ull : (u64)want;
 }
+__device__ __forceinline__ void write_token(const SampleArgs& a, int r, int token, float e, u64 sum) {
+  a.tokens[r] = token;
+  if (a.probs) a.probs[r] = (float)((double)e * (double)kUnit / (double)sum);
+}
 
-// CTA 0, with the sorted list of the row's first n tokens: what the filters keep, and the
-// token.  `total` is the row's mass (top_k off); `all`: every token of any weight is in
-// the list.  False where the list does not hold all that is kept.
+// One CTA, with the sorted list of the row's first n tokens: what the filters keep, and the
+// token.  `total` is the row's mass (read with top-p and without top-k); `all`: every token
+// of any weight is in the list.  False where the list does not hold all that is kept.
 __device__ __noinline__ bool finish_list(const SampleArgs& a, int r, const Filter& f, ClusterShared& sm, float top, int n,
                                          u64 total, bool all) {
   const int tid = threadIdx.x;
-  constexpr int kEach = kList / kThreads;
   if (f.top_k < a.V && f.top_k > n && !all) return false;
-  const int k = min(f.top_k, n);
-  // thread t: entries [t per, (t + 1) per)
-  const int per = (n + kThreads - 1) / kThreads;
-  uint32_t w[kEach];
+  if (f.top_k >= a.V && f.top_p >= 1.f && !all) return false;
+  const int k = min(f.top_k, n), per = (k + kThreads - 1) / kThreads;  // thread t: entries [t per, (t + 1) per)
+  if (tid == 0) sm.entries = k;
   u64 mine = 0;
-  int heavy = 0;  // entries that min-p keeps
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    const int at = tid * per + i;
-    w[i] = 0;
-    if (i < per && at < k) {
-      const float x = key_value(sm.list[at]), e = weight(x, top, f.inv_t);
-      w[i] = whole_weight(e);
-      heavy += x == top || !(e < f.min_p);
-      mine += w[i];
-    }
-  }
+  for (int i = 0; i < per; ++i)
+    if (tid * per + i < k) mine += whole_weight(weight(key_value(sm.list[tid * per + i]), top, f.inv_t));
   u64 listed;
   const u64 before = block_scan(mine, sm.part, &listed);
   if (f.top_k < a.V || all) total = listed;
-  u64 target = ~0ull;
-  if (f.top_p < 1.f) {
-    target = top_p_target(f.top_p, total);
-    if (target > listed) return false;
+  const u64 target = f.top_p < 1.f ? top_p_target(f.top_p, total) : ~0ull;
+  if (f.top_p < 1.f && target > listed) return false;
+  // the first entry that a filter does not keep ends the list
+  u64 run = before;
+  for (int i = 0; i < per; ++i) {
+    const int e = tid * per + i;
+    if (e >= k) break;
+    const float x = key_value(sm.list[e]), w = weight(x, top, f.inv_t);
+    if (run >= target || (x != top && w < f.min_p)) {
+      atomicMin(&sm.entries, e);
+      break;
+    }
+    run += whole_weight(w);
   }
-  // kept: the first ones, as many as top-p and min-p both keep
-  int kept = 0;
-  u64 upto = before;
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) {
-    if (i < per && tid * per + i < k) kept += upto < target;
-    upto += w[i];
-  }
-  u64 all_kept, all_heavy;
-  block_scan((u64)kept, sm.part, &all_kept);
-  block_scan((u64)heavy, sm.part, &all_heavy);
-  const int K = (int)(all_kept < all_heavy ? all_kept : all_heavy);
   __syncthreads();
-  // in index order: (index, entry) ascending is ~(...) descending
-  u64 sum = 0;
-#pragma unroll
-  for (int i = 0; i < kEach; ++i)
-    if (i < per && tid * per + i < K) sum += w[i];
-  block_scan(sum, sm.part, &sum);
-  const u64 at = place_of(a.uniforms[r], sum);
-  if (K == 1) {
-    if (tid == 0) {
-      a.tokens[r] = (int)key_index(sm.list[0]);
-      if (a.probs) a.probs[r] = 1.f;
+  const int K = sm.entries;
+  // the kept mass: what is before entry K
+  run = before;
+  for (int i = 0; i < per; ++i) {
+    const int e = tid * per + i;
+    if (e >= k) break;
+    run += whole_weight(weight(key_value(sm.list[e]), top, f.inv_t));
+    if (e == K - 1) sm.key = run;
+  }
+  __syncthreads();
+  const u64 sum = sm.key, at = place_of(a.uniforms[r], sum);
+  if (K <= kThreads) {
+    // an entry's place in index order: the mass of the entries of lower indices
+    if (tid < K) sm.spare[tid] = (u64)whole_weight(weight(key_value(sm.list[tid]), top, f.inv_t));
+    __syncthreads();
+    if (tid < K) {
+      const uint32_t index = key_index(sm.list[tid]);
+      u64 below = 0;
+      for (int e = 0; e < K; ++e)
+        if (key_index(sm.list[e]) < index) below += sm.spare[e];
+      if (below <= at && at < below + sm.spare[tid])
+        write_token(a, r, (int)index, weight(key_value(sm.list[tid]), top, f.inv_t), sum);
     }
     return true;
   }
-  // weights with their order: the low half of a key is ~index, so that is sorted on
-  u64 key[kEach];
-#pragma unroll
-  for (int i = 0; i < kEach; ++i)
-    if (i < per && tid * per + i < K) key[i] = sm.list[tid * per + i];
+  // many: sorted by ~index, the low half of a key, its halves exchanged
+  for (int e = tid; e < K; e += kThreads) sm.list[e] = sm.list[e] << 32 | sm.list[e] >> 32;
   __syncthreads();
-#pragma unroll
-  for (int i = 0; i < kEach; ++i)
-    if (i < per && tid * per + i < K) sm.list[tid * per + i] = key[i] << 32 | key[i] >> 32;
+  int size = 1;
+  while (size < K) size <<= 1;
+  for (int e = K + tid; e < size; e += kThreads) sm.list[e] = 0;
   __syncthreads();
-  sort_list(sm.list, K);
+  for (int kk = 2; kk <= size; kk <<= 1)
+    for (int j = kk >> 1; j > 0; j >>= 1) {
+      for (int t = tid; t < size / 2; t += kThreads) {
+        const int i = 2 * t - (t & (j - 1)), o = i + j;
+        const u64 x = sm.list[i], y = sm.list[o];
+        if ((x < y) == ((i & kk) == 0)) {
+          sm.list[i] = y;
+          sm.list[o] = x;
+        }
+      }
+      __syncthreads();
+    }
   const int each = (K + kThreads - 1) / kThreads;
   mine = 0;
-  for (int i = 0; i < each; ++i) {
-    const int e = tid * each + i;
-    if (e < K) mine += whole_weight(weight(key_value(sm.list[e] << 32), top, f.inv_t));
-  }
-  u64 unused, run = block_scan(mine, sm.part, &unused);
-  if (run <= at && at < run + mine) {
+  for (int i = 0; i < each; ++i)
+    if (tid * each + i < K) mine += whole_weight(weight(key_value(sm.list[tid * each + i] << 32), top, f.inv_t));
+  u64 unused;
+  run = block_scan(mine, sm.part, &unused);
+  if (run <= at && at < run + mine)
     for (int i = 0; i < each; ++i) {
-      const u64 q = sm.list[tid * each + i];
-      const float e = weight(key_value(q << 32), top, f.inv_t);
-      run += whole_weight(e);
+      const u64 x = sm.list[tid * each + i];
+      const float w = weight(key_value(x << 32), top, f.inv_t);
+      run += whole_weight(w);
       if (run > at) {
-        a.tokens[r] = (int)(0xFFFFFFFFu - (uint32_t)(q >> 32));
-        if (a.probs) a.probs[r] = (float)((double)e * (double)kUnit / (double)sum);
+        write_token(a, r, (int)(0xFFFFFFFFu - (uint32_t)(x >> 32)), w, sum);
         break;
       }
     }
-  }
   return true;
 }
 
-template <typename T, int NV>
-__global__ void __launch_bounds__(kThreads, 2) sample_cluster_kernel(SampleArgs a, int C) {
-  extern __shared__ __align__(16) unsigned char raw[];
-  ClusterShared& sm = *reinterpret_cast<ClusterShared*>(raw);
-  constexpr int E = Row<T, NV>::E;
+// One row by one CTA (Stream, C = 1) or a cluster of C (Held).
+template <typename T, typename Src>
+__device__ __forceinline__ void sample_by(const SampleArgs& a, int C, ClusterShared& sm) {
+  constexpr int E = Vec<T>::E;
+  constexpr bool kHeld = !std::is_same<Src, Stream<T>>::value;
   const int tid = threadIdx.x, lane = tid % 32, warp = tid / 32, V = a.V;
-  const int rank = C > 1 ? (int)cluster_rank() : 0, r = blockIdx.x / C, b = r / a.R;
+  const int rank = kHeld && C > 1 ? (int)cluster_rank() : 0, r = kHeld ? blockIdx.x / C : blockIdx.x;
+  const bool many = kHeld && C > 1;
   auto sync = [&]() {
-    if (C > 1)
+    if (many)
       cluster_sync_all();
     else
       __syncthreads();
   };
   auto remote = [&](const void* p, int cta) { return map_rank(smem_u32(p), (uint32_t)cta); };
 
-  pdl_wait();
-  // ---- the row ----
-  Row<T, NV> row;
-  row.V = V;
-  {
-    const T* p = static_cast<const T*>(a.logits) + b * a.batch_stride + (r % a.R) * a.row_stride;
-    const int head = min(V, (int)((16u - ((uintptr_t)p & 15u)) % 16u / sizeof(T)));
-    const int vecs = (V - head) / E, tail = V - head - vecs * E;
-    const uint4* q = reinterpret_cast<const uint4*>(p + head);
-    const int first = rank * NV * kThreads + tid;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const uint32_t none = E == 8 ? 0xFF80FF80u : 0xFF800000u;  // -inf
-      row.x[i] = first + i * kThreads < vecs ? __ldcs(q + first + i * kThreads) : make_uint4(none, none, none, none);
-    }
-    row.head = head;
-    row.v0 = head + first * E;
-    row.edge = -INFINITY;
-    row.edge_at = 0x7FFFFFFF;
-    if (rank == 0 && tid < head + tail) {
-      row.edge_at = tid < head ? tid : head + vecs * E + tid - head;
-      row.edge = logit(p, row.edge_at);
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      if constexpr (E == 8)
-        row.x[i] = make_uint4(no_nan2(row.x[i].x), no_nan2(row.x[i].y), no_nan2(row.x[i].z), no_nan2(row.x[i].w));
-      else
-        *reinterpret_cast<float4*>(&row.x[i]) = no_nan(*reinterpret_cast<const float4*>(&row.x[i]));
-    }
-  }
-  const Filter f = row_filter(a, b);
+  Src row;
+  row.load(a, r, rank);
+  const Filter f = row_filter(a, r / a.R);
+  row.inv_t = f.inv_t;
+  row.ys = f.inv_t * kBinsPerNat;
+  const bool by_k = f.top_k < V;
+  const bool listing = (by_k && f.top_k <= kListTopK) || (!by_k && f.top_p < 1.f);
 
-  // ---- the maximum ----
-  {
-    float top = -INFINITY;
-    row.each([&](float v, int) { top = fmaxf(top, v); });
+  // Sum over the cluster of a value per thread, to every thread.
+  int turn = 0;
+  auto cluster_sum = [&](u64 x) {
+    const u64 mine = block_sum<kThreads>(x, sm.part);
+    if (!many) return mine;
+    turn ^= 1;  // the sum before this one may still be read
+    if (tid == 0) sm.sum[turn] = mine;
+    sync();
+    u64 all = 0;
+#pragma unroll
+    for (int c = 0; c < kMaxCluster; ++c)
+      if (c < C) all += ld_cluster_u64(remote(&sm.sum[turn], c));
+    return all;
+  };
+  // Maximum over the block.
+  auto block_top = [&](float top) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
     if (lane == 0) sm.wtop[warp] = top;
-    for (int i = tid; i < kFineBins; i += kThreads) sm.mass[i] = 0.f;
-    if (tid == 0) sm.listed = 0;
     __syncthreads();
-    if (warp == 0) {
-      top = lane < kWarps ? sm.wtop[lane] : -INFINITY;
+    top = sm.wtop[lane % kWarps];
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-      if (lane == 0) sm.top = top;
-    }
-    sync();
-    top = -INFINITY;
-    for (int c = 0; c < C; ++c) top = fmaxf(top, C > 1 ? ld_cluster_f1(remote(&sm.top, c)) : sm.top);
-    row.top = top;
-  }
-  row.inv_t = f.inv_t;
-  row.ys = f.inv_t * kBinsPerNat;
-  if (row.top == -INFINITY || f.top_k == 1) {
-    // no token, or the first maximum
-    int at = 0x7FFFFFFF;
-    if (row.top != -INFINITY) row.each([&](float v, int i) { at = v == row.top ? min(at, i) : at; });
-    at = __reduce_min_sync(0xFFFFFFFFu, at);
-    if (lane == 0) sm.part[warp] = (u64)at;
-    __syncthreads();
-    if (tid == 0) {
-      for (int w = 0; w < kWarps; ++w) at = min(at, (int)sm.part[w]);
-      sm.first = at;
-    }
-    sync();
-    if (rank == 0 && tid == 0) {
-      for (int c = 0; c < C; ++c) at = min(at, C > 1 ? ld_cluster_s32(remote(&sm.first, c)) : sm.first);
-      a.tokens[r] = row.top == -INFINITY ? -1 : at;
-      if (a.probs) a.probs[r] = row.top == -INFINITY ? 0.f : 1.f;
-    }
-    sync();  // CTA 0 has read the others
-    return;
-  }
-
-  // Sum over the cluster of a value per thread, to every thread.
-  auto cluster_sum = [&](u64 x) {
-    const u64 mine = block_sum<kThreads>(x, sm.part);
-    if (C == 1) return mine;
-    if (tid == 0) sm.sum = mine;
-    sync();
-    u64 all = 0;
-    for (int c = 0; c < C; ++c) all += ld_cluster_u64(remote(&sm.sum, c));
-    sync();  // `sum` is read before it is written again
-    return all;
+    for (int o = kWarps / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+    return top;
   };
   // Two bins of a histogram over the cluster (in sm.mass, or sm.count): the first at
-  // which the running sum reaches `lo`, and the first at which it reaches `hi` (the last bin
-  // where none does); the histogram is cleared.
+  // which the running sum reaches `lo` (positive), and the first at which it reaches `hi`
+  // (the last bin where none does); the histogram is cleared.
   auto find_bins = [&](int bins, bool counts, double lo, double hi) {
+    if (tid < 2) sm.bin[tid] = bins - 1;
     sync();
-    // thread t sums bins 2t and 2t + 1 over the CTAs
-    double x[2] = {0.0, 0.0};
+    // thread t sums bins 4t to 4t + 3 over the CTAs
+    double x[4] = {0.0, 0.0, 0.0, 0.0};
+    if (4 * tid < bins) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int at = 2 * tid + i;
-      if (at < bins)
-        for (int c = 0; c < C; ++c) {
-          if (counts)
-            x[i] += (double)(C > 1 ? (uint32_t)ld_cluster_s32(remote(&sm.count[at], c)) : sm.count[at]);
-          else
-            x[i] += (double)(C > 1 ? ld_cluster_f1(remote(&sm.mass[at], c)) : sm.mass[at]);
-        }
+      for (int c = 0; c < kMaxCluster; ++c) {
+        if (c >= C) break;
+        const float4 y = many ? ld_cluster_f4(remote(&sm.mass[4 * tid], c)) : *reinterpret_cast<const float4*>(&sm.mass[4 * tid]);
+        const float v[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] += counts ? (double)__float_as_uint(v[i]) : (double)v[i];
+      }
     }
-    double upto = x[0] + x[1];
+    double upto = (x[0] + x[1]) + (x[2] + x[3]);
+    const double mine = upto;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const double y = __shfl_up_sync(0xFFFFFFFFu, upto, o);
       if (lane >= o) upto += y;
     }
-    __syncthreads();
     if (lane == 31) sm.part[warp] = (u64)__double_as_longlong(upto);
-    if (tid < 2) sm.bin[tid] = bins - 1;
     __syncthreads();
-    double before = upto - x[0] - x[1];
+    double before = upto - mine;
     for (int w = 0; w < warp; ++w) before += __longlong_as_double((long long)sm.part[w]);
+    if (4 * tid < bins) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int at = 2 * tid + i;
-      if (at < bins) {
-        if (before < lo && before + x[i] >= lo) atomicMin(&sm.bin[0], at);  // lo > 0
-        if (before < hi && before + x[i] >= hi) atomicMin(&sm.bin[1], at);
+      for (int i = 0; i < 4; ++i) {
+        if (before < lo && before + x[i] >= lo) atomicMin(&sm.bin[0], 4 * tid + i);
+        if (before < hi && before + x[i] >= hi) atomicMin(&sm.bin[1], 4 * tid + i);
+        before += x[i];
       }
-      before += x[i];
     }
     sync();  // every CTA has read the histograms
-    for (int i = tid; i < kFineBins; i += kThreads) sm.mass[i] = 0.f;
+    if (4 * tid < kFineBins) *reinterpret_cast<float4*>(&sm.mass[4 * tid]) = make_float4(0.f, 0.f, 0.f, 0.f);
     const int2 found = make_int2(sm.bin[0], sm.bin[1]);
     __syncthreads();
     return found;
   };
-  // Collects the tokens for which take(logit, index) holds.
-  auto collect = [&](auto take) {
-    row.each([&](float v, int i) {
-      if (take(v, i)) {
-        const int at = atomicAdd(&sm.listed, 1);
-        if (at < kList) sm.list[at] = make_key(v, (uint32_t)i);
-      }
+  auto each = [&](auto take) {  // take(logit, index)
+    row.vectors([&](const uint4& q, int index) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) take(Vec<T>::value(q, e), index + e);
     });
+    take(row.edge, row.edge_at);
+  };
+  auto append = [&](float v, int i) {
+    const int at = atomicAdd(&sm.listed, 1);
+    if (at < kList) sm.list[at] = make_key(v, (uint32_t)i);
+  };
+  // The tokens that reach `floor` into the list.
+  auto collect = [&](const uint4& q, int index, float floor, float top) {
+    if (top >= floor) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float v = Vec<T>::value(q, e);
+        if (v >= floor && index + e < V) append(v, index + e);
+      }
+    }
   };
   // CTA 0: the others' lists after its own; -1 where they are too long.  All CTAs call it.
   auto gather_lists = [&]() {
     sync();
     int n = sm.listed;
-    if (rank == 0 && C > 1) {
-      int all = 0;
-      for (int c = 0; c < C; ++c) all += ld_cluster_s32(remote(&sm.listed, c));
+    if (rank == 0 && many) {
+      int m[kMaxCluster], all = 0;
+#pragma unroll
+      for (int c = 0; c < kMaxCluster; ++c) {
+        m[c] = c < C ? ld_cluster_s32(remote(&sm.listed, c)) : 0;
+        all += m[c];
+      }
       if (all <= kList) {
-        for (int c = 1; c < C; ++c) {
-          const int m = ld_cluster_s32(remote(&sm.listed, c));
-          for (int i = tid; i < m; i += kThreads) sm.list[n + i] = ld_cluster_u64(remote(&sm.list[i], c));
-          n += m;
+#pragma unroll
+        for (int c = 1; c < kMaxCluster; ++c) {
+          for (int i = tid; i < m[c]; i += kThreads) sm.list[n + i] = ld_cluster_u64(remote(&sm.list[i], c));
+          n += m[c];
         }
       } else {
         n = kList + 1;
       }
+      __syncthreads();
     }
-    __syncthreads();
     return n <= kList ? n : -1;
   };
-  // The last token of the prefix in which `metric` reaches `target`, as a key (0 where it was
+
+  // ---- the maximum, and the sample ----
+  if (tid == 0) sm.listed = 0;
+  if (4 * tid < kFineBins) *reinterpret_cast<float4*>(&sm.mass[4 * tid]) = make_float4(0.f, 0.f, 0.f, 0.f);
+  float top = -INFINITY;
+  float share = 1.f;
+  if constexpr (kHeld) {
+    row.vectors([&](const uint4& q, int) { top = fmaxf(top, Vec<T>::top(q)); });
+    top = block_top(fmaxf(top, row.edge));
+    if (many) {
+      if (tid == 0) sm.top = top;
+      sync();
+#pragma unroll
+      for (int c = 0; c < kMaxCluster; ++c)
+        if (c < C) top = fmaxf(top, ld_cluster_f1(remote(&sm.top, c)));
+    }
+  } else {
+    share = row.sample([&](const uint4& q) { top = fmaxf(top, Vec<T>::top(q)); });
+    top = block_top(top);  // of the sample
+  }
+  row.top = top;
+  // A logit that about enough tokens reach; where there are fewer of any weight, one that
+  // all of these reach, at least the lowest finite one.
+  constexpr float kLowest = -3.402823466e38f;
+  float floor = kLowest;
+  if (listing && top != -INFINITY) {
+    share = row.sample([&](const uint4& q) {
+#pragma unroll
+      for (int e = 0; e < E; e += 2) {  // half of the elements
+        const float y = row.depth(Vec<T>::value(q, e));
+        if (y < (float)kBins) atomicAdd(&sm.count[(int)y], 1u);
+      }
+    });
+    const float want = (float)(by_k ? f.top_k : kListTopP) * share * 0.5f;
+    const double reach = f.top_k == 1 ? 1.0 : (double)(want + 4.f * sqrtf(want) + 4.f);
+    const int bin = find_bins(kBins, true, reach, reach).x;
+    floor = fmaxf(kLowest, top - (bin < kBins - 1 ? (float)(bin + 1) : kBins + 1.f) / row.ys);
+  } else {
+    __syncthreads();
+  }
+  // ---- the list ----
+  int state = kGeneral;
+  if constexpr (!kHeld) {
+    // the row's first reading: its maximum, and the list
+    const float least = listing ? floor : INFINITY;
+    row.vectors([&](const uint4& q, int index) {
+      const float t = Vec<T>::top(q);
+      top = fmaxf(top, t);
+      collect(q, index, least, t);
+    });
+    top = fmaxf(top, row.edge);
+    if (row.edge >= least && row.edge_at < V) append(row.edge, row.edge_at);
+    top = block_top(top);
+    row.top = top;
+  } else if (listing) {
+    row.vectors([&](const uint4& q, int index) { collect(q, index, floor, Vec<T>::top(q)); });
+    if (row.edge >= floor && row.edge_at < V) append(row.edge, row.edge_at);
+  }
+  if (row.top == -INFINITY) {
+    if (rank == 0 && tid == 0) {
+      a.tokens[r] = -1;
+      if (a.probs) a.probs[r] = 0.f;
+    }
+    sync();  // nobody reads this CTA's shared memory any more
+    return;
+  }
+  u64 total = 0;  // the row's mass
+  if (!by_k && f.top_p < 1.f) {
+    u64 mine = 0;
+    each([&](float v, int) { mine += row.mass(v); });
+    total = cluster_sum(mine);
+  }
+  if (listing) {
+    // whether what does not reach the floor has no weight
+    const bool all = floor == kLowest || row.depth(floor) >= (float)kBins;
+    const int n = gather_lists();
+    if (rank == 0) {
+      int st = kGeneral;
+      if (n > 0) {
+        if (f.top_k == 1) {
+          u64 best = 0;
+          for (int e = tid; e < n; e += kThreads) best = umax64(best, sm.list[e]);
+          best = warp_max_key(best);
+          if (lane == 0) sm.part[warp] = best;
+          __syncthreads();
+          if (tid == 0) {
+            for (int w = 0; w < kWarps; ++w) best = umax64(best, sm.part[w]);
+            a.tokens[r] = (int)key_index(best);
+            if (a.probs) a.probs[r] = 1.f;
+          }
+          st = kDone;
+        } else {
+          const float deep = fminf(fmaxf(row.depth(floor), 1.f), (float)kBins);
+          sort_list(sm, n, row.top, row.ys * ((float)kFineBins / deep));
+          if (finish_list(a, r, f, sm, row.top, n, total, all)) st = kDone;
+        }
+      }
+      state = st;
+      if (many) {
+        __syncthreads();
+        if (tid == 0) sm.state = st;
+      }
+    }
+    if (many) {
+      sync();
+      state = ld_cluster_s32(remote(&sm.state, 0));
+    }
+    if (state == kDone) {
+      if (many) sync();  // CTA 0's state has been read
+      return;
+    }
+    __syncthreads();
+  }
+
+  // ---- the general way: the last kept token, then the draw over the row ----
+  // The last token of the prefix in which a count or the mass reaches `target`, as a key (0:
   // not found this way).
   auto find_key = [&](u64 target, bool counts) -> u64 {
     auto metric = [&](float v) -> u64 { return counts ? 1u : row.mass(v); };
     const double slack = counts ? 0.0 : 1e-3 * (double)target;  // the masses in a histogram are fp32
-    row.each([&](float v, int i) {
+    each([&](float v, int i) {
       const float y = row.depth(v);
-      if (i < V && y < (float)kBins) {
+      if (y < (float)kBins) {
         if (counts)
           atomicAdd(&sm.count[(int)y], 1u);
         else
@@ -681,55 +889,52 @@ __global__ void __launch_bounds__(kThreads, 2) sample_cluster_kernel(SampleArgs 
       }
     });
     const int2 coarse = find_bins(kBins, counts, (double)target - slack, (double)target + slack);
-    // a fine bin is 2^-shift of a coarse one, whole coarse bins together at most kFineBins
+    // a fine bin is 2^-shift of a coarse one, the coarse bins together at most kFineBins
     int shift = 10;
-    while (((coarse.y - coarse.x + 1) << shift) > kFineBins && shift > 0) --shift;
+    while (((coarse.y - coarse.x + 1) << shift) > kFineBins) --shift;
     const float lo = (float)coarse.x, hi = (float)(coarse.y + 1), per = (float)(1 << shift);
-    u64 above = 0;
-    row.each([&](float v, int i) {
-      const float y = row.depth(v);
-      if (i < V && y < hi) {
-        if (y < lo) {
-          above += metric(v);
-        } else if (counts) {
-          atomicAdd(&sm.count[min(kFineBins - 1, (int)((y - lo) * per))], 1u);
-        } else {
-          atomicAdd(&sm.mass[min(kFineBins - 1, (int)((y - lo) * per))], (float)row.mass(v));
-        }
-      }
-    });
-    above = cluster_sum(above);
-    if (above >= target) return 0;
-    const double left = (double)(target - above);
-    const int2 fine = find_bins(kFineBins, counts, fmax(left - slack, 0.5), left + slack);
-    auto fine_bin = [&](float v) {
+    auto fine_bin = [&](float v) {  // -1 before them, kFineBins after them
       const float y = row.depth(v);
       return y < lo ? -1 : y < hi ? min(kFineBins - 1, (int)((y - lo) * per)) : kFineBins;
     };
+    u64 above = 0;
+    each([&](float v, int) {
+      const int bin = fine_bin(v);
+      if (bin < 0)
+        above += metric(v);
+      else if (bin < kFineBins) {
+        if (counts)
+          atomicAdd(&sm.count[bin], 1u);
+        else
+          atomicAdd(&sm.mass[bin], (float)row.mass(v));
+      }
+    });
+    above = cluster_sum(above);
+    const double left = above < target ? (double)(target - above) : 0.0;
+    const int2 fine = find_bins(kFineBins, counts, fmax(left - slack, 0.5), left + slack);
+    if (above >= target) return 0;  // the same in every thread
     if (tid == 0) sm.listed = 0;
     __syncthreads();
     above = 0;
-    row.each([&](float v, int i) {
-      const int bin = i < V ? fine_bin(v) : kFineBins;
-      if (bin < fine.x) above += metric(v);
-    });
-    collect([&](float v, int i) {
-      const int bin = i < V ? fine_bin(v) : kFineBins;
-      return bin >= fine.x && bin <= fine.y;
+    each([&](float v, int i) {
+      const int bin = fine_bin(v);
+      if (bin < fine.x)
+        above += metric(v);
+      else if (bin <= fine.y && bin < kFineBins && i < V)
+        append(v, i);
     });
     above = cluster_sum(above);
     const int n = gather_lists();
     if (rank == 0) {
       if (tid == 0) sm.key = 0;
+      __syncthreads();
       if (n > 0 && above < target) {
-        sort_list(sm.list, n);
+        sort_list(sm, n, row.top - lo / row.ys, row.ys * per);
         const int per_thread = (n + kThreads - 1) / kThreads;
         u64 mine = 0;
-        for (int i = 0; i < per_thread; ++i) {
-          const int e = tid * per_thread + i;
-          if (e < n) mine += metric(key_value(sm.list[e]));
-        }
-        u64 all, run = above + block_scan(mine, sm.part, &all);
+        for (int i = 0; i < per_thread; ++i)
+          if (tid * per_thread + i < n) mine += metric(key_value(sm.list[tid * per_thread + i]));
+        u64 unused, run = above + block_scan(mine, sm.part, &unused);
         if (run < target && run + mine >= target)
           for (int i = 0; i < per_thread; ++i) {
             run += metric(key_value(sm.list[tid * per_thread + i]));
@@ -741,63 +946,22 @@ __global__ void __launch_bounds__(kThreads, 2) sample_cluster_kernel(SampleArgs 
       }
     }
     sync();
-    const u64 key = C > 1 ? ld_cluster_u64(remote(&sm.key, 0)) : sm.key;
+    const u64 key = many ? ld_cluster_u64(remote(&sm.key, 0)) : sm.key;
     sync();
     return key;
   };
 
-  const bool by_k = f.top_k < V;
-  u64 total = 0;  // the row's mass
-  int state = kGeneral;
-  if (!by_k && f.top_p < 1.f) {
-    u64 mine = 0;
-    row.each([&](float v, int) { mine += row.mass(v); });
-    total = cluster_sum(mine);
-  }
-  if ((by_k && f.top_k <= kListTopK) || (!by_k && f.top_p < 1.f)) {
-    // ---- the list ----
-    // A quarter of the vectors, half their elements, are the sample.
-    constexpr int kStep = NV >= 4 ? 4 : 1;
-#pragma unroll
-    for (int i = 0; i < NV; i += kStep)
-#pragma unroll
-      for (int e = 0; e < E; e += 2) {
-        const float y = row.depth(row.value(row.x[i], e));
-        if (y < (float)kBins) atomicAdd(&sm.count[(int)y], 1u);
-      }
-    const float share = (float)((NV + kStep - 1) / kStep) / (float)(2 * NV);
-    const float want = (float)(by_k ? f.top_k : kListTopP) * share;
-    const double reach = (double)(want + 4.f * sqrtf(want) + 4.f);
-    const int bin = find_bins(kBins, true, reach, reach).x;
-    collect([&](float v, int) { return row.depth(v) < (float)(bin + 1); });
-    const int n = gather_lists();
-    if (rank == 0) {
-      int st = kGeneral;
-      if (n > 0) {
-        sort_list(sm.list, n);
-        if (finish_list(a, r, f, sm, row.top, n, total, bin == kBins - 1)) st = kDone;
-      }
-      __syncthreads();
-      if (tid == 0) sm.state = st;
-    }
-    sync();
-    state = C > 1 ? ld_cluster_s32(remote(&sm.state, 0)) : sm.state;
-    sync();
-    if (state == kDone) return;
-  }
-
-  // ---- the general way: the last kept token, then the draw over the row ----
   u64 last = 0;  // keys from this one on are kept
   if (by_k) {
     u64 heavy = 0;  // tokens of any weight; no other one is drawn
-    row.each([&](float v, int) { heavy += row.depth(v) < (float)kBins; });
+    each([&](float v, int) { heavy += row.depth(v) < (float)kBins; });
     if (cluster_sum(heavy) > (u64)f.top_k) {
       last = find_key((u64)f.top_k, true);
       if (last == 0) state = kSlow;
     }
     if (state != kSlow && f.top_p < 1.f) {
       u64 mine = 0;
-      row.each([&](float v, int i) {
+      each([&](float v, int i) {
         if (make_key(v, (uint32_t)i) >= last) mine += row.mass(v);
       });
       total = cluster_sum(mine);
@@ -811,7 +975,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_cluster_kernel(SampleArgs 
       last = key;
   }
   if (state == kSlow) {
-    sync();  // nobody reads CTA 0's lists any more
+    sync();  // nobody reads the others' shared memory any more
     if (rank == 0) sample_row<T, kThreads>(a, r, sm.row);
     return;
   }
@@ -820,122 +984,149 @@ __global__ void __launch_bounds__(kThreads, 2) sample_cluster_kernel(SampleArgs 
     const float e = weight(v, row.top, f.inv_t);
     return v == row.top || !(e < f.min_p) ? whole_weight(e) : 0;
   };
-  // In index order: the elements before the vectors, vectors i = 0, 1, ... of warps 0, 1,
-  // ... of the CTAs in turn, the elements after them.
-  u64 mine = 0;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) {
+  auto kept_of = [&](const uint4& q, int index) {
     u64 x = 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) x += kept(row.value(row.x[i], e), row.v0 + i * kThreads * E + e);
-    x = warp_sum(x);
-    if (lane == 0) sm.seg[1 + i * kWarps + warp] = x;
-    mine += x;
+    for (int e = 0; e < E; ++e) x += kept(Vec<T>::value(q, e), index + e);
+    return x;
+  };
+  // In index order: the elements before the vectors, the segments (of warps 0, 1, ..., then
+  // those of the next number), CTA by CTA, the elements after the vectors.
+  u64 mine = 0;
+  if constexpr (kHeld) {
+#pragma unroll
+    for (int i = 0; i < Src::kSegments / kWarps; ++i) {
+      u64 x = 0;
+      row.segment(i, [&](const uint4& q, int index) { x = kept_of(q, index); });
+      x = warp_sum(x);
+      if (lane == 0) sm.seg[1 + i * kWarps + warp] = x;
+      mine += x;
+    }
+  } else {
+    row.run([&](const uint4& q, int index) {
+      mine += kept_of(q, index);
+      return true;
+    });
+    mine = warp_sum(mine);
+    if (lane == 0) sm.seg[1 + warp] = mine;
   }
+  const bool early = row.edge_at < row.head;
   if (warp == 0) {
     const u64 x = kept(row.edge, row.edge_at);
-    const bool early = row.edge_at < row.head;
     const u64 head = warp_sum(early ? x : 0), tail = warp_sum(early ? 0 : x);
     if (lane == 0) {
       sm.seg[0] = head;
-      sm.seg[1 + NV * kWarps] = tail;
+      sm.seg[1 + Src::kSegments] = tail;
     }
     mine += head;  // the tail follows the last CTA
   }
   const u64 whole = block_sum<kThreads>(lane == 0 ? mine : 0, sm.part);
-  if (tid == 0) sm.sum = whole;
-  sync();
-  u64 before = 0, sum = 0;
-  for (int c = 0; c < C; ++c) {
-    if (c == rank) before = sum;
-    sum += C > 1 ? ld_cluster_u64(remote(&sm.sum, c)) : sm.sum;
+  u64 before = 0, sum = whole, tail = sm.seg[1 + Src::kSegments];
+  if (many) {
+    turn ^= 1;
+    if (tid == 0) sm.sum[turn] = whole;
+    sync();
+    sum = 0;
+    for (int c = 0; c < C; ++c) {
+      if (c == rank) before = sum;
+      sum += ld_cluster_u64(remote(&sm.sum[turn], c));
+    }
+    tail = ld_cluster_u64(remote(&sm.seg[1 + Src::kSegments], 0));
   }
-  const u64 body = sum, tail = C > 1 ? ld_cluster_u64(remote(&sm.seg[1 + NV * kWarps], 0)) : sm.seg[1 + NV * kWarps];
+  const u64 body = sum;
   sum += tail;
   const u64 at = place_of(a.uniforms[r], sum);
-  auto take = [&](float v, int i) {
-    a.tokens[r] = i;
-    if (a.probs) a.probs[r] = (float)((double)weight(v, row.top, f.inv_t) * (double)kUnit / (double)sum);
-  };
-  // A warp whose segment holds the place looks through its lanes.
-  auto look = [&](u64 x, u64 run, auto each_of_lane) {
+  // A warp's elements with `run` before them: the one that holds the place, if any.
+  auto look = [&](u64 x, u64 run, auto found) {
     u64 upto = x;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const u64 y = __shfl_up_sync(0xFFFFFFFFu, upto, o);
       if (lane >= o) upto += y;
     }
-    if (run + upto > at && run + upto - x <= at) each_of_lane(run + upto - x);
+    if (run + upto > at && run + upto - x <= at) found(run + upto - x);
+    return run + __shfl_sync(0xFFFFFFFFu, upto, 31);
+  };
+  auto look_vector = [&](const uint4& q, int index, u64 run) {
+    return look(kept_of(q, index), run, [&](u64 s) {
+      bool done = false;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float v = Vec<T>::value(q, e);
+        s += kept(v, index + e);
+        if (!done && s > at) {
+          done = true;
+          write_token(a, r, index + e, weight(v, row.top, f.inv_t), sum);
+        }
+      }
+    });
   };
   if (rank == 0 && warp == 0) {
     const u64 x = kept(row.edge, row.edge_at);
-    const bool early = row.edge_at < row.head;
-    if (at < sm.seg[0]) look(early ? x : 0, 0, [&](u64) { take(row.edge, row.edge_at); });
-    if (at >= body) look(early ? 0 : x, body, [&](u64) { take(row.edge, row.edge_at); });
+    auto take = [&](u64) { write_token(a, r, row.edge_at, weight(row.edge, row.top, f.inv_t), sum); };
+    if (at < sm.seg[0]) look(early ? x : 0, 0, take);
+    if (at >= body) look(early ? 0 : x, body, take);
   }
-  // this CTA's segments
-  u64 run = before + sm.seg[0];
-  if (rank != 0) run = before;
+  u64 run = before + (rank == 0 ? sm.seg[0] : 0);
   if (run <= at && at < before + whole) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
+    for (int i = 0; i < Src::kSegments / kWarps; ++i) {
       u64 start = run;
       for (int w = 0; w < warp; ++w) start += sm.seg[1 + i * kWarps + w];
       if (start <= at && at < start + sm.seg[1 + i * kWarps + warp]) {
-        u64 x = 0;
-#pragma unroll
-        for (int e = 0; e < E; ++e) x += kept(row.value(row.x[i], e), row.v0 + i * kThreads * E + e);
-        look(x, start, [&](u64 s) {
-          bool found = false;
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const float v = row.value(row.x[i], e);
-            const int index = row.v0 + i * kThreads * E + e;
-            s += kept(v, index);
-            if (!found && s > at) {
-              found = true;
-              take(v, index);
-            }
-          }
-        });
+        if constexpr (kHeld) {
+          row.segment(i, [&](const uint4& q, int index) { look_vector(q, index, start); });
+        } else {
+          row.run([&](const uint4& q, int index) {
+            start = look_vector(q, index, start);
+            return start <= at;
+          });
+        }
       }
       for (int w = 0; w < kWarps; ++w) run += sm.seg[1 + i * kWarps + w];
     }
   }
-  sync();  // the others have read this CTA's sums
+  if (many) sync();  // the others have read this CTA's sums
 }
 
 template <typename T, int NV>
-cudaError_t launch_cluster_rows(const SampleArgs& a, int C, cudaStream_t stream) {
-  auto kernel = sample_cluster_kernel<T, NV>;
+__global__ void __launch_bounds__(kThreads, 1) sample_cluster_kernel(SampleArgs a, int C) {
+  extern __shared__ __align__(16) unsigned char raw[];
+  pdl_wait();
+  sample_by<T, Held<T, NV>>(a, C, *reinterpret_cast<ClusterShared*>(raw));
+}
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 3) sample_stream_kernel(SampleArgs a) {
+  extern __shared__ __align__(16) unsigned char raw[];
+  pdl_wait();
+  sample_by<T, Stream<T>>(a, 1, *reinterpret_cast<ClusterShared*>(raw));
+}
+
+template <typename K, typename... Args>
+cudaError_t launch_rows(K kernel, const SampleArgs& a, int C, cudaStream_t stream, Args... args) {
   constexpr size_t smem = sizeof(ClusterShared);
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
-  return launch_dependent(kernel, dim3((unsigned)(a.B * a.R) * C), dim3(kThreads), smem, stream, (unsigned)C, a, C);
+  return launch_dependent(kernel, dim3((unsigned)(a.B * a.R) * C), dim3(kThreads), smem, stream, (unsigned)C, a, args...);
 }
 
 template <typename T>
 cudaError_t launch_typed(const SampleArgs& a, cudaStream_t stream) {
-  constexpr int E = 16 / sizeof(T);
-  const int rows = a.B * a.R;
+  constexpr int E = Vec<T>::E;
+  const long long rows = (long long)a.B * a.R, vecs = (a.V + E - 1) / E;
   DeviceInfo dev;
-  cudaError_t e = device_info(&dev);
+  const cudaError_t e = device_info(&dev);
   if (e != cudaSuccess) return e;
-  const long long vecs = (a.V + E - 1) / E;
   auto need = [&](int C) { return (int)((vecs + (long long)C * kThreads - 1) / ((long long)C * kThreads)); };
-  // The fewest CTAs that hold a row; more of them while they are idle otherwise.
+  // A cluster for a row while the device has CTAs enough for all rows at once, as large as
+  // that allows and the row fills.
   int C = 1;
-  while (C < kMaxCluster && need(C) > 10) C *= 2;
-  if (need(C) > 10 || (long long)rows * kMaxCluster > (1ll << 31) - 1) {
-    sample_row_kernel<T><<<rows, kRowThreads, 0, stream>>>(a);
-    return cudaGetLastError();
-  }
-  while (C < kMaxCluster && need(C) > 1 && (long long)rows * C * 2 <= dev.sm_count) C *= 2;
+  while (C < kMaxCluster && need(C) > 1 && rows * C * 2 <= dev.sm_count) C *= 2;
   const int n = need(C);
-  if (n <= 1) return launch_cluster_rows<T, 1>(a, C, stream);
-  if (n <= 2) return launch_cluster_rows<T, 2>(a, C, stream);
-  if (n <= 5) return launch_cluster_rows<T, 5>(a, C, stream);
-  return launch_cluster_rows<T, 10>(a, C, stream);
+  if (rows * C > dev.sm_count || n > 5) return launch_rows(sample_stream_kernel<T>, a, 1, stream);
+  if (n <= 1) return launch_rows(sample_cluster_kernel<T, 1>, a, C, stream, C);
+  if (n <= 2) return launch_rows(sample_cluster_kernel<T, 2>, a, C, stream, C);
+  return launch_rows(sample_cluster_kernel<T, 5>, a, C, stream, C);
 }
 
 }  // namespace
