@@ -17,7 +17,7 @@
 // and an exact sum.  Whatever does not fit (thousands of tokens with one logit) goes to
 // sample_row: radix selection over the 32-bit keys of the logits.
 //
-// With many rows a CTA takes one and streams it (Stream), three or more of them to an SM,
+// With many rows a CTA takes one and streams it (Stream), four of them to an SM,
 // and later passes over the row, where needed, find it in L2: 4096 rows are 46 MB at a
 // time.  With few rows a cluster of up to eight CTAs holds one in registers (Held), so
 // that every later pass is arithmetic.
@@ -60,6 +60,42 @@ __device__ __forceinline__ float weight(float x, float top, float inv_t) {
   return x == top ? 1.f : expf(__fmul_rn(x - top, inv_t));
 }
 __device__ __forceinline__ uint32_t whole_weight(float e) { return __float2uint_rn(e * kUnit); }
+
+// x n for a float x in [0, 1] and n < 2^53, rounded to 53 bits as their product in fp64
+// is, in whole numbers (fp64 arithmetic is slow here): its floor, or its ceiling.
+__device__ __forceinline__ u64 scaled(float x, u64 n, bool up) {
+  const uint32_t bits = __float_as_uint(x);
+  if (n == 0 || bits == 0) return 0;
+  const int exponent = (int)(bits >> 23);
+  const u64 m = (bits & 0x7FFFFFu) | (exponent ? 0x800000u : 0u);
+  int drop = 150 - (exponent ? exponent : 1);  // x = m 2^-drop
+  u64 hi = __umul64hi(m, n), lo = m * n;
+  // to 53 bits, nearest, ties to even
+  const int length = hi ? 128 - __clzll((long long)hi) : 64 - __clzll((long long)lo);
+  if (length > 53) {
+    const int cut = length - 53;  // at most 24
+    const u64 rest = lo & ((1ull << cut) - 1), half = 1ull << (cut - 1);
+    lo = lo >> cut | hi << (64 - cut);
+    lo += rest > half || (rest == half && (lo & 1));
+    drop -= cut;
+  }
+  if (drop <= 0) return lo << -drop;
+  if (drop > 63) return up ? 1 : 0;
+  return (lo >> drop) + (up && (lo & ((1ull << drop) - 1)) ? 1 : 0);
+}
+// The random number's place among `sum`.
+__device__ __forceinline__ u64 place_of(float u, u64 sum) {
+  if (!(u > 0.f)) return 0;
+  const u64 at = u < 1.f ? scaled(u, sum, false) : sum;
+  return at >= sum ? sum - 1 : at;
+}
+// The mass that top-p wants of `total`, p < 1.
+__device__ __forceinline__ u64 top_p_target(float p, u64 total) {
+  const u64 want = p > 0.f ? scaled(p, total, true) : 0;
+  return want < 1 ? 1 : want;
+}
+// e of a weight among the sum of whole weights.
+__device__ __forceinline__ float probability(float e, u64 sum) { return __fdiv_rn(e * kUnit, (float)sum); }
 
 template <typename T>
 __device__ __forceinline__ float logit(const T* row, int v) {
@@ -173,8 +209,7 @@ __device__ void sample_row(const SampleArgs& a, int r, RowShared& sm) {
     total = block_sum<kThreads>(sum, sm.part);
   }
   if (f.top_p < 1.f) {
-    const double want = ceil((double)f.top_p * (double)total);
-    const u64 target = want < 1.0 ? 1ull : (u64)want;
+    const u64 target = top_p_target(f.top_p, total);
     u64 above;
     t = select_key<T, kThreads>(row, V, target, mass, sm, &above);
     const u64 one = mass(key_value((u64)t << 32));
@@ -226,9 +261,7 @@ __device__ void sample_row(const SampleArgs& a, int r, RowShared& sm) {
     if (w < warp) before += sm.part[w];
     sum += sm.part[w];
   }
-  const float u0 = a.uniforms[r], u = u0 > 0.f ? u0 : 0.f;
-  u64 at = (u64)floor((double)u * (double)sum);
-  if (u >= 1.f || at >= sum) at = sum - 1;
+  const u64 at = place_of(a.uniforms[r], sum);
   if (before <= at && at < before + mine) {
     u64 run = before;
     for (int v = v0; v < v1; v += 32) {
@@ -244,7 +277,7 @@ __device__ void sample_row(const SampleArgs& a, int r, RowShared& sm) {
       if (m) {
         if (lane == __ffs(m) - 1) {
           a.tokens[r] = v + lane;
-          if (a.probs) a.probs[r] = (float)((double)weight(x, top, f.inv_t) * (double)kUnit / (double)sum);
+          if (a.probs) a.probs[r] = probability(weight(x, top, f.inv_t), sum);
         }
         break;
       }
@@ -255,7 +288,7 @@ __device__ void sample_row(const SampleArgs& a, int r, RowShared& sm) {
 
 
 // ---- rows as the kernel below reads them ----------------------------------------
-constexpr int kThreads = 512;
+constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kList = 4096;           // collected tokens
 constexpr int kBins = 256;            // of the first histogram, and of the sample's
@@ -361,7 +394,8 @@ struct Held : RowParts<T> {
 template <typename T>
 struct Stream : RowParts<T> {
   static constexpr int kSegments = kWarps;
-  static constexpr int kAhead = 4;  // loads in flight per thread
+  static constexpr int kRuns = 64;
+  static constexpr int kAhead = 8;  // loads in flight per thread
   __device__ __forceinline__ void load(const SampleArgs& a, int r, int) { this->find(a, r, true); }
   template <typename F>
   __device__ __forceinline__ void vectors(F f) const {
@@ -375,12 +409,13 @@ struct Stream : RowParts<T> {
     }
     for (; v < this->vecs; v += kThreads) f(__ldg(this->q + v), this->index(v));
   }
-  // 32 runs of 32 vectors, spread over the row.
+  // 64 runs of 32 vectors, spread over the row.
   template <typename F>
   __device__ __forceinline__ float sample(F f) const {
-    const int runs = this->vecs / 32, taken = runs < 32 ? runs : 32;
+    const int runs = this->vecs / 32, taken = runs < kRuns ? runs : kRuns;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    for (int j = warp; j < taken; j += kWarps) f(__ldg(this->q + (long long)j * runs / taken * 32 + lane));
+#pragma unroll 4
+    for (int j = warp; j < taken; j += kWarps) f(__ldg(this->q + (j * runs / taken) * 32 + lane));
     return (float)taken * 32.f / (float)(this->vecs > 0 ? this->vecs : 1);
   }
   // Warp w has the vectors [w per, (w + 1) per), 32 at a time.
@@ -390,8 +425,14 @@ struct Stream : RowParts<T> {
   __device__ __forceinline__ void run(F f) const {  // f(vector or none, index), whole warps
     const int w = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int end = min(this->vecs, (w + 1) * per());
-    for (int v = w * per(); v < end; v += 32)
-      if (!f(v + lane < end ? __ldg(this->q + v + lane) : Vec<T>::none(), this->index(v + lane))) break;
+    for (int v = w * per() + lane; v - lane < end; v += 4 * 32) {
+      uint4 x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = v + i * 32 < end ? __ldg(this->q + v + i * 32) : Vec<T>::none();
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (!f(x[i], this->index(v + i * 32))) return;
+    }
   }
 };
 
@@ -400,17 +441,15 @@ struct ClusterShared {
     struct {
       u64 list[kList];
       u64 spare[kList / 4];  // of sort_list
-      union {
-        float mass[kFineBins];
-        uint32_t count[kFineBins];
-      };
+      uint32_t count[kFineBins];
     };
     RowShared row;
   };
-  u64 seg[5 * kWarps + 2];  // kept mass of the segments, of what is before and after the vectors
+  u64 seg[10 * kWarps + 2];  // kept mass of the segments, of what is before and after the vectors
   u64 part[kWarps];
   float wtop[kWarps];
   int bin[2];
+  float before;
   int entries;  // of the list that are kept
   // written by this CTA, read by the others of the cluster
   float top;
@@ -470,12 +509,18 @@ __device__ __noinline__ void sort_list(ClusterShared& sm, int n, float top, floa
       }
     }
     __syncthreads();
-    const uint32_t c0 = sm.count[2 * tid], c1 = sm.count[2 * tid + 1];
+    constexpr int kBinsEach = kFineBins / kThreads;
+    uint32_t size[kBinsEach], sum = 0;
+#pragma unroll
+    for (int i = 0; i < kBinsEach; ++i) sum += size[i] = sm.count[kBinsEach * tid + i];
     u64 all;
-    const uint32_t start = (uint32_t)block_scan(c0 + c1, sm.part, &all);
+    uint32_t start = (uint32_t)block_scan(sum, sm.part, &all);
     // start of a bin in the low half, its size in the high half
-    sm.count[2 * tid] = start | c0 << 16;
-    sm.count[2 * tid + 1] = (start + c0) | c1 << 16;
+#pragma unroll
+    for (int i = 0; i < kBinsEach; ++i) {
+      sm.count[kBinsEach * tid + i] = start | size[i] << 16;
+      start += size[i];
+    }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kEach; ++i)
@@ -490,8 +535,8 @@ __device__ __noinline__ void sort_list(ClusterShared& sm, int n, float top, floa
         list[from + larger] = key[i];
       }
     __syncthreads();
-    sm.count[2 * tid] = 0;
-    sm.count[2 * tid + 1] = 0;
+#pragma unroll
+    for (int i = 0; i < kBinsEach; ++i) sm.count[kBinsEach * tid + i] = 0;
     __syncthreads();
     return;
   }
@@ -513,19 +558,9 @@ __device__ __noinline__ void sort_list(ClusterShared& sm, int n, float top, floa
     }
 }
 
-// The random number's place among `sum`.
-__device__ __forceinline__ u64 place_of(float u0, u64 sum) {
-  const float u = u0 > 0.f ? u0 : 0.f;
-  const u64 at = (u64)floor((double)u * (double)sum);
-  return u >= 1.f || at >= sum ? sum - 1 : at;
-}
-__device__ __forceinline__ u64 top_p_target(float p, u64 total) {
-  const double want = ceil((double)p * (double)total);
-  return want < 1.0 ? 1ull : (u64)want;
-}
 __device__ __forceinline__ void write_token(const SampleArgs& a, int r, int token, float e, u64 sum) {
   a.tokens[r] = token;
-  if (a.probs) a.probs[r] = (float)((double)e * (double)kUnit / (double)sum);
+  if (a.probs) a.probs[r] = probability(e, sum);
 }
 
 // One CTA, with the sorted list of the row's first n tokens: what the filters keep, and the
@@ -544,7 +579,8 @@ __device__ __noinline__ bool finish_list(const SampleArgs& a, int r, const Filte
   u64 listed;
   const u64 before = block_scan(mine, sm.part, &listed);
   if (f.top_k < a.V || all) total = listed;
-  const u64 target = f.top_p < 1.f ? top_p_target(f.top_p, total) : ~0ull;
+  u64 target = ~0ull;
+  if (f.top_p < 1.f) target = top_p_target(f.top_p, total);
   if (f.top_p < 1.f && target > listed) return false;
   // the first entry that a filter does not keep ends the list
   u64 run = before;
@@ -671,46 +707,58 @@ __device__ __forceinline__ void sample_by(const SampleArgs& a, int C, ClusterSha
     for (int o = kWarps / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
     return top;
   };
-  // Two bins of a histogram over the cluster (in sm.mass, or sm.count): the first at
-  // which the running sum reaches `lo` (positive), and the first at which it reaches `hi`
-  // (the last bin where none does); the histogram is cleared.
-  auto find_bins = [&](int bins, bool counts, double lo, double hi) {
+  // Of a histogram over the cluster (sm.count): the first bin at which the running sum
+  // reaches `lo` (positive), the first at which it reaches `hi` (the last bin where none
+  // does), and what is before the former; the histogram is cleared.  In fp32, which holds
+  // counts of at most 2^24 exactly (fp64 would take several times as long here).
+  struct Bins {
+    int x, y;
+    float before;
+  };
+  auto find_bins = [&](int bins, float lo, float hi) {
     if (tid < 2) sm.bin[tid] = bins - 1;
+    if (tid == 0) sm.before = 0.f;
     sync();
     // thread t sums bins 4t to 4t + 3 over the CTAs
-    double x[4] = {0.0, 0.0, 0.0, 0.0};
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
     if (4 * tid < bins) {
 #pragma unroll
       for (int c = 0; c < kMaxCluster; ++c) {
         if (c >= C) break;
-        const float4 y = many ? ld_cluster_f4(remote(&sm.mass[4 * tid], c)) : *reinterpret_cast<const float4*>(&sm.mass[4 * tid]);
-        const float v[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] += counts ? (double)__float_as_uint(v[i]) : (double)v[i];
+        const float4 y = many ? ld_cluster_f4(remote(&sm.count[4 * tid], c)) : *reinterpret_cast<const float4*>(&sm.count[4 * tid]);
+        x[0] += (float)__float_as_uint(y.x);
+        x[1] += (float)__float_as_uint(y.y);
+        x[2] += (float)__float_as_uint(y.z);
+        x[3] += (float)__float_as_uint(y.w);
       }
     }
-    double upto = (x[0] + x[1]) + (x[2] + x[3]);
-    const double mine = upto;
+    const float mine = (x[0] + x[1]) + (x[2] + x[3]);
+    float upto = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const double y = __shfl_up_sync(0xFFFFFFFFu, upto, o);
+      const float y = __shfl_up_sync(0xFFFFFFFFu, upto, o);
       if (lane >= o) upto += y;
     }
-    if (lane == 31) sm.part[warp] = (u64)__double_as_longlong(upto);
+    if (lane == 31) sm.wtop[warp] = upto;
     __syncthreads();
-    double before = upto - mine;
-    for (int w = 0; w < warp; ++w) before += __longlong_as_double((long long)sm.part[w]);
+    float before = upto - mine;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w)
+      if (w < warp) before += sm.wtop[w];
     if (4 * tid < bins) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (before < lo && before + x[i] >= lo) atomicMin(&sm.bin[0], 4 * tid + i);
+        if (before < lo && before + x[i] >= lo) {
+          atomicMin(&sm.bin[0], 4 * tid + i);
+          sm.before = before;
+        }
         if (before < hi && before + x[i] >= hi) atomicMin(&sm.bin[1], 4 * tid + i);
         before += x[i];
       }
     }
     sync();  // every CTA has read the histograms
-    if (4 * tid < kFineBins) *reinterpret_cast<float4*>(&sm.mass[4 * tid]) = make_float4(0.f, 0.f, 0.f, 0.f);
-    const int2 found = make_int2(sm.bin[0], sm.bin[1]);
+    if (4 * tid < kFineBins) *reinterpret_cast<uint4*>(&sm.count[4 * tid]) = make_uint4(0u, 0u, 0u, 0u);
+    const Bins found{sm.bin[0], sm.bin[1], sm.before};
     __syncthreads();
     return found;
   };
@@ -728,10 +776,18 @@ __device__ __forceinline__ void sample_by(const SampleArgs& a, int C, ClusterSha
   // The tokens that reach `floor` into the list.
   auto collect = [&](const uint4& q, int index, float floor, float top) {
     if (top >= floor) {
+      uint32_t hits = 0;
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float v = Vec<T>::value(q, e);
-        if (v >= floor && index + e < V) append(v, index + e);
+      for (int e = 0; e < E; ++e) hits |= (uint32_t)(Vec<T>::value(q, e) >= floor) << e;
+      const int n = __popc(hits);
+      int at = atomicAdd(&sm.listed, n);
+      if (at + n > kList) hits = 0;
+      for (; hits; hits &= hits - 1) {
+        const int e = __ffs(hits) - 1;
+        float v = Vec<T>::value(q, 0);
+#pragma unroll
+        for (int i = 1; i < E; ++i) v = e == i ? Vec<T>::value(q, i) : v;
+        sm.list[at++] = make_key(v, (uint32_t)(index + e));
       }
     }
   };
@@ -762,7 +818,7 @@ __device__ __forceinline__ void sample_by(const SampleArgs& a, int C, ClusterSha
 
   // ---- the maximum, and the sample ----
   if (tid == 0) sm.listed = 0;
-  if (4 * tid < kFineBins) *reinterpret_cast<float4*>(&sm.mass[4 * tid]) = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (4 * tid < kFineBins) *reinterpret_cast<uint4*>(&sm.count[4 * tid]) = make_uint4(0u, 0u, 0u, 0u);
   float top = -INFINITY;
   float share = 1.f;
   if constexpr (kHeld) {
@@ -787,14 +843,14 @@ __device__ __forceinline__ void sample_by(const SampleArgs& a, int C, ClusterSha
   if (listing && top != -INFINITY) {
     share = row.sample([&](const uint4& q) {
 #pragma unroll
-      for (int e = 0; e < E; e += 2) {  // half of the elements
+      for (int e = 0; e < E; ++e) {
         const float y = row.depth(Vec<T>::value(q, e));
         if (y < (float)kBins) atomicAdd(&sm.count[(int)y], 1u);
       }
     });
-    const float want = (float)(by_k ? f.top_k : kListTopP) * share * 0.5f;
-    const double reach = f.top_k == 1 ? 1.0 : (double)(want + 4.f * sqrtf(want) + 4.f);
-    const int bin = find_bins(kBins, true, reach, reach).x;
+    const float want = (float)(by_k ? f.top_k : kListTopP) * share;
+    const float reach = f.top_k == 1 ? 1.f : want + 4.f * sqrtf(want) + 4.f;
+    const int bin = find_bins(kBins, reach, reach).x;
     floor = fmaxf(kLowest, top - (bin < kBins - 1 ? (float)(bin + 1) : kBins + 1.f) / row.ys);
   } else {
     __syncthreads();
@@ -874,21 +930,24 @@ __device__ __forceinline__ void sample_by(const SampleArgs& a, int C, ClusterSha
   }
 
   // ---- the general way: the last kept token, then the draw over the row ----
-  // The last token of the prefix in which a count or the mass reaches `target`, as a key (0:
-  // not found this way).
-  auto find_key = [&](u64 target, bool counts) -> u64 {
+  // The last token of the prefix of the row in which a count or the mass reaches `target`,
+  // as a key (0: not found this way).  `whole`: the count or mass of all of it; only keys
+  // from `from` on are looked at.
+  auto find_key = [&](u64 target, u64 whole, bool counts, u64 from) -> u64 {
+    const float from_v = from ? key_value(from) : -INFINITY;
+    const int from_i = (int)key_index(from);
+    auto in = [&](float v, int i) { return v > from_v || (v == from_v && (uint32_t)i <= (uint32_t)from_i); };
     auto metric = [&](float v) -> u64 { return counts ? 1u : row.mass(v); };
-    const double slack = counts ? 0.0 : 1e-3 * (double)target;  // the masses in a histogram are fp32
+    // The histograms hold counts, or masses without their low bits, so that they fit 32:
+    // what these lack is at most a bit per token, far below the slack.
+    const int bits = 64 - __clzll((long long)whole), low = !counts && bits > 32 ? bits - 32 : 0;
+    const float unit = 1.f / (float)(1ull << low), goal = (float)target * unit, slack = counts ? 0.f : 1e-3f * goal + 1.f;
+    auto add = [&](int bin, float v) { atomicAdd(&sm.count[bin], counts ? 1u : row.mass(v) >> low); };
     each([&](float v, int i) {
       const float y = row.depth(v);
-      if (y < (float)kBins) {
-        if (counts)
-          atomicAdd(&sm.count[(int)y], 1u);
-        else
-          atomicAdd(&sm.mass[(int)y], (float)row.mass(v));
-      }
+      if (y < (float)kBins && in(v, i)) add((int)y, v);
     });
-    const int2 coarse = find_bins(kBins, counts, (double)target - slack, (double)target + slack);
+    const Bins coarse = find_bins(kBins, fmaxf(goal - slack, 0.5f), goal + slack);
     // a fine bin is 2^-shift of a coarse one, the coarse bins together at most kFineBins
     int shift = 10;
     while (((coarse.y - coarse.x + 1) << shift) > kFineBins) --shift;
@@ -897,22 +956,13 @@ __device__ __forceinline__ void sample_by(const SampleArgs& a, int C, ClusterSha
       const float y = row.depth(v);
       return y < lo ? -1 : y < hi ? min(kFineBins - 1, (int)((y - lo) * per)) : kFineBins;
     };
-    u64 above = 0;
-    each([&](float v, int) {
+    each([&](float v, int i) {
       const int bin = fine_bin(v);
-      if (bin < 0)
-        above += metric(v);
-      else if (bin < kFineBins) {
-        if (counts)
-          atomicAdd(&sm.count[bin], 1u);
-        else
-          atomicAdd(&sm.mass[bin], (float)row.mass(v));
-      }
+      if (bin >= 0 && bin < kFineBins && in(v, i)) add(bin, v);
     });
-    above = cluster_sum(above);
-    const double left = above < target ? (double)(target - above) : 0.0;
-    const int2 fine = find_bins(kFineBins, counts, fmax(left - slack, 0.5), left + slack);
-    if (above >= target) return 0;  // the same in every thread
+    const float left = goal - coarse.before;
+    const Bins fine = find_bins(kFineBins, fmaxf(left - slack, 0.5f), left + slack);
+    u64 above;
     if (tid == 0) sm.listed = 0;
     __syncthreads();
     above = 0;
@@ -920,7 +970,7 @@ __device__ __forceinline__ void sample_by(const SampleArgs& a, int C, ClusterSha
       const int bin = fine_bin(v);
       if (bin < fine.x)
         above += metric(v);
-      else if (bin <= fine.y && bin < kFineBins && i < V)
+      else if (bin <= fine.y && bin < kFineBins && i < V && in(v, i))
         append(v, i);
     });
     above = cluster_sum(above);
@@ -955,8 +1005,9 @@ __device__ __forceinline__ void sample_by(const SampleArgs& a, int C, ClusterSha
   if (by_k) {
     u64 heavy = 0;  // tokens of any weight; no other one is drawn
     each([&](float v, int) { heavy += row.depth(v) < (float)kBins; });
-    if (cluster_sum(heavy) > (u64)f.top_k) {
-      last = find_key((u64)f.top_k, true);
+    heavy = cluster_sum(heavy);
+    if (heavy > (u64)f.top_k) {
+      last = find_key((u64)f.top_k, heavy, true, 0);
       if (last == 0) state = kSlow;
     }
     if (state != kSlow && f.top_p < 1.f) {
@@ -968,7 +1019,8 @@ __device__ __forceinline__ void sample_by(const SampleArgs& a, int C, ClusterSha
     }
   }
   if (state != kSlow && f.top_p < 1.f) {
-    const u64 key = find_key(top_p_target(f.top_p, total), false);
+    const u64 target = top_p_target(f.top_p, total);
+    const u64 key = find_key(target, total, false, last);
     if (key == 0)
       state = kSlow;
     else
@@ -979,8 +1031,10 @@ __device__ __forceinline__ void sample_by(const SampleArgs& a, int C, ClusterSha
     if (rank == 0) sample_row<T, kThreads>(a, r, sm.row);
     return;
   }
+  const float last_v = last ? key_value(last) : -INFINITY;
+  const int last_i = last ? (int)key_index(last) : V - 1;
   auto kept = [&](float v, int i) -> u64 {
-    if (i >= V || make_key(v, (uint32_t)i) < last) return 0;
+    if (!(v > last_v || (v == last_v && i <= last_i))) return 0;
     const float e = weight(v, row.top, f.inv_t);
     return v == row.top || !(e < f.min_p) ? whole_weight(e) : 0;
   };
@@ -1096,7 +1150,7 @@ __global__ void __launch_bounds__(kThreads, 1) sample_cluster_kernel(SampleArgs 
   sample_by<T, Held<T, NV>>(a, C, *reinterpret_cast<ClusterShared*>(raw));
 }
 template <typename T>
-__global__ void __launch_bounds__(kThreads, 3) sample_stream_kernel(SampleArgs a) {
+__global__ void __launch_bounds__(kThreads, 4) sample_stream_kernel(SampleArgs a) {
   extern __shared__ __align__(16) unsigned char raw[];
   pdl_wait();
   sample_by<T, Stream<T>>(a, 1, *reinterpret_cast<ClusterShared*>(raw));
@@ -1123,10 +1177,11 @@ cudaError_t launch_typed(const SampleArgs& a, cudaStream_t stream) {
   int C = 1;
   while (C < kMaxCluster && need(C) > 1 && rows * C * 2 <= dev.sm_count) C *= 2;
   const int n = need(C);
-  if (rows * C > dev.sm_count || n > 5) return launch_rows(sample_stream_kernel<T>, a, 1, stream);
+  if (rows * C > dev.sm_count || n > 10) return launch_rows(sample_stream_kernel<T>, a, 1, stream);
   if (n <= 1) return launch_rows(sample_cluster_kernel<T, 1>, a, C, stream, C);
   if (n <= 2) return launch_rows(sample_cluster_kernel<T, 2>, a, C, stream, C);
-  return launch_rows(sample_cluster_kernel<T, 5>, a, C, stream, C);
+  if (n <= 5) return launch_rows(sample_cluster_kernel<T, 5>, a, C, stream, C);
+  return launch_rows(sample_cluster_kernel<T, 10>, a, C, stream, C);
 }
 
 }  // namespace
