@@ -449,7 +449,7 @@ struct ClusterShared {
   u64 part[kWarps];
   float wtop[kWarps];
   int bin[2];
-  float before;
+  float before, upto;
   int entries;  // of the list that are kept
   // written by this CTA, read by the others of the cluster
   float top;
@@ -713,11 +713,11 @@ __device__ __forceinline__ void sample_by(const SampleArgs& a, int C, ClusterSha
   // counts of at most 2^24 exactly (fp64 would take several times as long here).
   struct Bins {
     int x, y;
-    float before;
+    float before, inside;  // of bin x; of bins x to y
   };
   auto find_bins = [&](int bins, float lo, float hi) {
     if (tid < 2) sm.bin[tid] = bins - 1;
-    if (tid == 0) sm.before = 0.f;
+    if (tid == 0) sm.before = sm.upto = 0.f;
     sync();
     // thread t sums bins 4t to 4t + 3 over the CTAs
     float x[4] = {0.f, 0.f, 0.f, 0.f};
@@ -752,13 +752,16 @@ __device__ __forceinline__ void sample_by(const SampleArgs& a, int C, ClusterSha
           atomicMin(&sm.bin[0], 4 * tid + i);
           sm.before = before;
         }
-        if (before < hi && before + x[i] >= hi) atomicMin(&sm.bin[1], 4 * tid + i);
+        if (before < hi && before + x[i] >= hi) {
+          atomicMin(&sm.bin[1], 4 * tid + i);
+          sm.upto = before + x[i];
+        }
         before += x[i];
       }
     }
     sync();  // every CTA has read the histograms
     if (4 * tid < kFineBins) *reinterpret_cast<uint4*>(&sm.count[4 * tid]) = make_uint4(0u, 0u, 0u, 0u);
-    const Bins found{sm.bin[0], sm.bin[1], sm.before};
+    const Bins found{sm.bin[0], sm.bin[1], sm.before, sm.upto - sm.before};
     __syncthreads();
     return found;
   };
@@ -942,36 +945,38 @@ __device__ __forceinline__ void sample_by(const SampleArgs& a, int C, ClusterSha
     // what these lack is at most a bit per token, far below the slack.
     const int bits = 64 - __clzll((long long)whole), low = !counts && bits > 32 ? bits - 32 : 0;
     const float unit = 1.f / (float)(1ull << low), goal = (float)target * unit, slack = counts ? 0.f : 1e-3f * goal + 1.f;
-    auto add = [&](int bin, float v) { atomicAdd(&sm.count[bin], counts ? 1u : row.mass(v) >> low); };
+    constexpr float kSplit = (float)(kFineBins / kBins);
     each([&](float v, int i) {
-      const float y = row.depth(v);
-      if (y < (float)kBins && in(v, i)) add((int)y, v);
+      const float y = row.depth(v) * kSplit;
+      const uint32_t w = counts ? 1u : row.mass(v) >> low;
+      if (y < (float)kFineBins && in(v, i)) atomicAdd(&sm.count[(int)y], w);
     });
-    const Bins coarse = find_bins(kBins, fmaxf(goal - slack, 0.5f), goal + slack);
-    // a fine bin is 2^-shift of a coarse one, the coarse bins together at most kFineBins
-    int shift = 10;
-    while (((coarse.y - coarse.x + 1) << shift) > kFineBins) --shift;
-    const float lo = (float)coarse.x, hi = (float)(coarse.y + 1), per = (float)(1 << shift);
-    auto fine_bin = [&](float v) {  // -1 before them, kFineBins after them
-      const float y = row.depth(v);
-      return y < lo ? -1 : y < hi ? min(kFineBins - 1, (int)((y - lo) * per)) : kFineBins;
-    };
-    each([&](float v, int i) {
-      const int bin = fine_bin(v);
-      if (bin >= 0 && bin < kFineBins && in(v, i)) add(bin, v);
-    });
-    const float left = goal - coarse.before;
-    const Bins fine = find_bins(kFineBins, fmaxf(left - slack, 0.5f), left + slack);
-    u64 above;
+    const Bins coarse = find_bins(kFineBins, fmaxf(goal - slack, 0.5f), goal + slack);
+    float lo = (float)coarse.x / kSplit, hi = (float)(coarse.y + 1) / kSplit;
+    // About how many tokens these bins hold, from their mass and the weight there: where that
+    // is more than the list takes, a second histogram within them.
+    const float each_w = counts ? 1.f : fmaxf(1.f, kUnit * unit * expf(-hi / kBinsPerNat));
+    if (coarse.inside > each_w * (float)(kList / 2)) {
+      const float from_y = lo, per = (float)kFineBins / (hi - lo) * 0.999f;
+      each([&](float v, int i) {
+        const float y = row.depth(v);
+        const uint32_t w = counts ? 1u : row.mass(v) >> low;
+        if (y >= from_y && y < hi && in(v, i)) atomicAdd(&sm.count[(int)((y - from_y) * per)], w);
+      });
+      const float left = goal - coarse.before;
+      const Bins fine = find_bins(kFineBins, fmaxf(left - slack, 0.5f), left + slack);
+      // the bins' limits, moved apart by more than their rounding
+      lo = from_y + ((float)fine.x / per) * 0.9999f - 1e-5f * from_y;
+      hi = from_y + ((float)(fine.y + 1) / per) * 1.0001f + 1e-5f * from_y;
+    }
+    u64 above = 0;
     if (tid == 0) sm.listed = 0;
     __syncthreads();
-    above = 0;
     each([&](float v, int i) {
-      const int bin = fine_bin(v);
-      if (bin < fine.x)
-        above += metric(v);
-      else if (bin <= fine.y && bin < kFineBins && i < V && in(v, i))
-        append(v, i);
+      const float y = row.depth(v);
+      const uint32_t w = counts ? 1u : row.mass(v);
+      above += y < lo ? w : 0u;
+      if (y >= lo && y < hi && i < V && in(v, i)) append(v, i);
     });
     above = cluster_sum(above);
     const int n = gather_lists();
@@ -979,7 +984,7 @@ __device__ __forceinline__ void sample_by(const SampleArgs& a, int C, ClusterSha
       if (tid == 0) sm.key = 0;
       __syncthreads();
       if (n > 0 && above < target) {
-        sort_list(sm, n, row.top - lo / row.ys, row.ys * per);
+        sort_list(sm, n, row.top - lo / row.ys, row.ys * ((float)kFineBins / (hi - lo)));
         const int per_thread = (n + kThreads - 1) / kThreads;
         u64 mine = 0;
         for (int i = 0; i < per_thread; ++i)
@@ -1034,9 +1039,9 @@ __device__ __forceinline__ void sample_by(const SampleArgs& a, int C, ClusterSha
   const float last_v = last ? key_value(last) : -INFINITY;
   const int last_i = last ? (int)key_index(last) : V - 1;
   auto kept = [&](float v, int i) -> u64 {
-    if (!(v > last_v || (v == last_v && i <= last_i))) return 0;
     const float e = weight(v, row.top, f.inv_t);
-    return v == row.top || !(e < f.min_p) ? whole_weight(e) : 0;
+    const uint32_t w = whole_weight(e);
+    return (v > last_v || (v == last_v && i <= last_i)) && (v == row.top || !(e < f.min_p)) ? w : 0u;
   };
   auto kept_of = [&](const uint4& q, int index) {
     u64 x = 0;
