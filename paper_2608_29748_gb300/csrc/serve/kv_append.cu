@@ -12,6 +12,8 @@ namespace retrace {
 namespace {
 
 constexpr int kAppendThreads = 256;
+constexpr int kCtasPerSm = 4;
+constexpr int kHeadsEach = 3;  // heads whose loads a thread has in flight
 
 template <typename T, int N>
 struct Chunk {  // N elements, loaded and stored as one access
@@ -38,61 +40,16 @@ struct AppendShape {
 };
 
 template <typename T, int N>
-__global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(AppendArgs a, AppendShape s) {
+__global__ void __launch_bounds__(kAppendThreads, kCtasPerSm) kv_append_kernel(const __grid_constant__ AppendArgs a, AppendShape s) {
   __shared__ int s_seq[kAppendThreads], s_pos[kAppendThreads];
+  pdl_wait();
   const int tokens = s.groups / s.per_token;  // tokens of this CTA
-  const int t0 = blockIdx.x * tokens;
-  // Which sequence a token belongs to: without a list by division, else by one
-  // warp's search, 32 starts at a time.
-  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  for (int i = warp; i < tokens; i += kAppendThreads / 32) {
-    const int t = t0 + i;
-    if (t >= a.T) break;
-    int b = -1, first = 0;
-    if (!a.q_start) {
-      const int n = a.T / a.B;
-      b = t / n;
-      first = b * n;
-    } else {
-      int lo = 0, n = a.B;  // the last start <= t lies in [lo, lo + n), if any
-      while (n > 32) {
-        const int step = (n + 31) / 32;
-        const int at = lo + lane * step;
-        const bool below = at < lo + n && a.q_start[at] <= t;
-        const int k = __popc(__ballot_sync(0xFFFFFFFFu, below));
-        if (k == 0) break;
-        const int end = lo + n;
-        lo += (k - 1) * step;
-        n = min(step, end - lo);
-      }
-      const bool below = lane < n && lane < 32 && a.q_start[lo + lane] <= t;
-      const int k = __popc(__ballot_sync(0xFFFFFFFFu, below));
-      if (k > 0) {
-        b = lo + k - 1;
-        first = a.q_start[b];
-        if (t >= a.q_start[b + 1] || first < 0) b = -1;  // a token of no sequence
-      }
-    }
-    if (lane == 0) {
-      s_seq[i] = b;
-      s_pos[i] = b < 0 ? -1 : cached_tokens(a.cache_len, b) + (t - first);
-    }
-  }
-  __syncthreads();
-
   const int group = threadIdx.x / s.lanes, i = threadIdx.x % s.lanes;
-  if (group >= s.groups) return;
-  const int tl = group / s.per_token, t = t0 + tl;
-  if (tl >= tokens || t >= a.T) return;
-  const int b = s_seq[tl];
-  if (b < 0) return;
-  const int pos = s_pos[tl];
-  const bool placed = pos >= 0 && (!a.rope || pos < a.rope_positions);
+  const int tl = group / s.per_token, first_head = group % s.per_token;
+  const int uniform = a.q_start ? 0 : a.T / a.B;  // tokens of a sequence
   const int D = a.cache.head_dim;
-  const int page = placed ? page_of(a.cache, b, pos / a.cache.page_size) : -1;
-  const long long slot = page < 0 ? 0 : page * a.cache.page_stride + (pos % a.cache.page_size) * a.cache.slot_stride;
 
-  // This lane's chunk of a rotated head, its partner, and their cosines and sines.
+  // This lane's chunk of a rotated head, and whether it has a partner or pairs inside.
   const bool pair = i < s.pairs, inside = !pair && i < s.pairs + s.inside;
   int at;
   if (pair)
@@ -101,78 +58,132 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(AppendArgs a,
     at = (i - s.pairs) * N;
   else
     at = a.rot + (i - s.pairs - s.inside) * N;
-  constexpr int kLoad = N > 1 ? 4 : 2;
-  float cs[2 * N];
-  if (placed && (pair || inside)) {
-    const float* r = a.rope + (long long)pos * a.rot + (inside ? at : i * 2 * N);
-    const int n = inside ? N : 2 * N;
-#pragma unroll
-    for (int k = 0; k < 2 * N; k += kLoad) {
-      if (k >= n) break;
-      if constexpr (kLoad == 4) {
-        *reinterpret_cast<float4*>(cs + k) = *reinterpret_cast<const float4*>(r + k);
-      } else {
-        cs[0] = r[0];
-        cs[1] = r[1];
-      }
-    }
-  }
 
+  // The heads of this group, kHeadsEach at a time; what is read does not depend on where the token
+  // goes, so the first ones are on their way while that is found out.
   const int rotated = a.q_heads + a.cache.kv_heads, heads = rotated + a.cache.kv_heads;
-  for (int h = group % s.per_token; h < heads; h += s.per_token) {
-    if (h >= rotated) {  // a value head: every chunk is copied
-      if (page < 0) continue;
-      const int kh = h - rotated;
-      const T* src = static_cast<const T*>(a.v) + (long long)t * a.v_token + kh * a.v_head;
-      T* dst = static_cast<T*>(a.cache.v) + slot + kh * a.cache.head_stride;
-      Chunk<T, N> x, y;
-      const int c0 = i * N, c1 = (i + s.lanes) * N;
-      const bool one = c0 < D, two = c1 < D;
-      if (one) x.load(src + c0);
-      if (two) y.load(src + c1);
-      if (one) x.store(dst + c0);
-      if (two) y.store(dst + c1);
-      continue;
-    }
-    const bool query = h < a.q_heads;
-    const int kh = h - a.q_heads;
-    if (!query && page < 0) continue;
-    const T* src = query ? static_cast<const T*>(a.q) + (long long)t * a.q_token + h * a.q_head
-                         : static_cast<const T*>(a.k) + (long long)t * a.k_token + kh * a.k_head;
-    T* dst = query ? static_cast<T*>(a.q_out) + (long long)t * a.qo_token + h * a.qo_head
-                   : static_cast<T*>(a.cache.k) + slot + kh * a.cache.head_stride;
-    Chunk<T, N> x, y;
-    if (!placed) {  // a query without a place among the angles
+  Chunk<T, N> x[kHeadsEach], y[kHeadsEach];
+  auto load = [&](int t, int h0) {
 #pragma unroll
-      for (int k = 0; k < N; ++k) x.e[k] = from_f32<T>(0.f);
-      x.store(dst + at);
-      if (pair) x.store(dst + at + s.step);
-      continue;
-    }
-    x.load(src + at);
-    if (pair) {
-      y.load(src + at + s.step);
-#pragma unroll
-      for (int k = 0; k < N; ++k) {
-        const float u = to_f32(x.e[k]), w = to_f32(y.e[k]);
-        x.e[k] = from_f32<T>(u * cs[2 * k] - w * cs[2 * k + 1]);
-        y.e[k] = from_f32<T>(w * cs[2 * k] + u * cs[2 * k + 1]);
+    for (int u = 0; u < kHeadsEach; ++u) {
+      const int h = h0 + u * s.per_token;
+      if (h >= heads) break;
+      if (h >= rotated) {  // a value head: chunks i and i + lanes
+        const T* src = static_cast<const T*>(a.v) + (long long)t * a.v_token + (h - rotated) * a.v_head;
+        if (i * N < D) x[u].load(src + i * N);
+        if ((i + s.lanes) * N < D) y[u].load(src + (i + s.lanes) * N);
+      } else {
+        const T* src = h < a.q_heads ? static_cast<const T*>(a.q) + (long long)t * a.q_token + h * a.q_head
+                                     : static_cast<const T*>(a.k) + (long long)t * a.k_token + (h - a.q_heads) * a.k_head;
+        x[u].load(src + at);
+        if (pair) y[u].load(src + at + s.step);
       }
-      x.store(dst + at);
-      y.store(dst + at + s.step);
-      continue;
     }
-    if constexpr (N > 1) {
-      if (inside) {
+  };
+  for (int t0 = blockIdx.x * tokens; t0 < a.T; t0 += gridDim.x * tokens) {
+    const int t = t0 + tl;
+    const bool working = group < s.groups && tl < tokens && t < a.T;
+    if (working) load(t, first_head);
+
+    // Which sequence a token belongs to: without a list by division, else by one
+    // warp's search, 32 starts at a time.
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    for (int k = warp; k < tokens; k += kAppendThreads / 32) {
+      const int tk = t0 + k;
+      if (tk >= a.T) break;
+      int b = -1, first = 0;
+      if (!a.q_start) {
+        b = tk / uniform;
+        first = b * uniform;
+      } else {
+        int lo = 0, n = a.B;  // the last start <= tk lies in [lo, lo + n), if any
+        while (n > 32) {
+          const int step = (n + 31) / 32;
+          const int pos = lo + lane * step;
+          const bool below = pos < lo + n && a.q_start[pos] <= tk;
+          const int c = __popc(__ballot_sync(0xFFFFFFFFu, below));
+          if (c == 0) break;
+          const int end = lo + n;
+          lo += (c - 1) * step;
+          n = min(step, end - lo);
+        }
+        const bool below = lane < n && lane < 32 && a.q_start[lo + lane] <= tk;
+        const int c = __popc(__ballot_sync(0xFFFFFFFFu, below));
+        if (c > 0) {
+          b = lo + c - 1;
+          first = a.q_start[b];
+          if (tk >= a.q_start[b + 1] || first < 0) b = -1;  // a token of no sequence
+        }
+      }
+      if (lane == 0) {
+        s_seq[k] = b;
+        s_pos[k] = b < 0 ? -1 : cached_tokens(a.cache_len, b) + (tk - first);
+      }
+    }
+    __syncthreads();
+    const int b = working ? s_seq[tl] : -1;
+    const int pos = working ? s_pos[tl] : -1;
+    __syncthreads();  // both are read before the next tokens' are written
+    if (b < 0) continue;
+    const bool placed = pos >= 0 && (!a.rope || pos < a.rope_positions);
+    const int page = placed ? page_of(a.cache, b, pos / a.cache.page_size) : -1;
+    const long long slot = page < 0 ? 0 : page * a.cache.page_stride + (pos % a.cache.page_size) * a.cache.slot_stride;
+    constexpr int kLoad = N > 1 ? 4 : 2;
+    float cs[2 * N];  // cosines and sines of this lane's pairs
+    if (placed && (pair || inside)) {
+      const float* r = a.rope + (long long)pos * a.rot + (inside ? at : i * 2 * N);
+      const int n = inside ? N : 2 * N;
 #pragma unroll
-        for (int k = 0; k < N; k += 2) {
-          const float u = to_f32(x.e[k]), w = to_f32(x.e[k + 1]);
-          x.e[k] = from_f32<T>(u * cs[k] - w * cs[k + 1]);
-          x.e[k + 1] = from_f32<T>(w * cs[k] + u * cs[k + 1]);
+      for (int k = 0; k < 2 * N; k += kLoad) {
+        if (k >= n) break;
+        if constexpr (kLoad == 4) {
+          *reinterpret_cast<float4*>(cs + k) = __ldg(reinterpret_cast<const float4*>(r + k));
+        } else {
+          cs[0] = r[0];
+          cs[1] = r[1];
         }
       }
     }
-    x.store(dst + at);
+
+    for (int h0 = first_head; h0 < heads; h0 += kHeadsEach * s.per_token) {
+      if (h0 != first_head) load(t, h0);
+#pragma unroll
+      for (int u = 0; u < kHeadsEach; ++u) {
+        const int h = h0 + u * s.per_token;
+        if (h >= heads) break;
+        if (h >= rotated) {
+          if (page < 0) continue;
+          T* dst = static_cast<T*>(a.cache.v) + slot + (h - rotated) * a.cache.head_stride;
+          if (i * N < D) x[u].store(dst + i * N);
+          if ((i + s.lanes) * N < D) y[u].store(dst + (i + s.lanes) * N);
+          continue;
+        }
+        const bool query = h < a.q_heads;
+        if (!query && page < 0) continue;
+        T* dst = query ? static_cast<T*>(a.q_out) + (long long)t * a.qo_token + h * a.qo_head
+                       : static_cast<T*>(a.cache.k) + slot + (h - a.q_heads) * a.cache.head_stride;
+        if (!placed) {  // a query without a place among the angles
+#pragma unroll
+          for (int k = 0; k < N; ++k) x[u].e[k] = y[u].e[k] = from_f32<T>(0.f);
+        } else if (pair) {
+#pragma unroll
+          for (int k = 0; k < N; ++k) {
+            const float v = to_f32(x[u].e[k]), w = to_f32(y[u].e[k]);
+            x[u].e[k] = from_f32<T>(v * cs[2 * k] - w * cs[2 * k + 1]);
+            y[u].e[k] = from_f32<T>(w * cs[2 * k] + v * cs[2 * k + 1]);
+          }
+        } else if (N > 1 && inside) {
+#pragma unroll
+          for (int k = 0; k + 1 < N; k += 2) {
+            const float v = to_f32(x[u].e[k]), w = to_f32(x[u].e[k + 1]);
+            x[u].e[k] = from_f32<T>(v * cs[k] - w * cs[k + 1]);
+            x[u].e[k + 1] = from_f32<T>(w * cs[k] + v * cs[k + 1]);
+          }
+        }
+        x[u].store(dst + at);
+        if (pair) y[u].store(dst + at + s.step);
+      }
+    }
   }
 }
 
@@ -188,10 +199,14 @@ cudaError_t launch(const AppendArgs& a, cudaStream_t stream) {
   s.lanes = s.pairs + s.inside + s.copies;
   const int heads = a.q_heads + 2 * a.cache.kv_heads;
   s.groups = kAppendThreads / s.lanes;
-  s.per_token = s.groups < heads ? s.groups : heads;
+  const int groups = (heads + kHeadsEach - 1) / kHeadsEach;
+  s.per_token = s.groups < groups ? s.groups : groups;
   const int tokens = s.groups / s.per_token;
-  kv_append_kernel<T, N><<<(a.T + tokens - 1) / tokens, kAppendThreads, 0, stream>>>(a, s);
-  return cudaGetLastError();
+  DeviceInfo dev;
+  const cudaError_t e = device_info(&dev);
+  if (e != cudaSuccess) return e;
+  const int all = (a.T + tokens - 1) / tokens, resident = dev.sm_count * kCtasPerSm;
+  return launch_dependent(kv_append_kernel<T, N>, dim3(all < resident ? all : resident), dim3(kAppendThreads), 0, stream, 1u, a, s);
 }
 
 template <typename T>
