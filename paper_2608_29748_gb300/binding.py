@@ -389,6 +389,8 @@ def run_round_sampled(x: dict, s: dict, ws: Workspace, out: RoundBuffers | None 
 
 # ---- around the round: paged cache, attention over it, sampling ---------------
 
+_append, _attend, _sample = lib.retrace_kv_append, lib.retrace_attend, lib.retrace_sample
+
 
 class _KvCacheStruct(ctypes.Structure):  # retrace_kv_cache (include/retrace.h)
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_stride", ctypes.c_int64),
@@ -415,49 +417,81 @@ class KvCache:
                                      k.shape[2], k.shape[3], _ptr(page_table), max(page_table.stride(0), page_table.shape[1]),
                                      page_table.shape[1], _dtype_code(k))
         self.ref = ctypes.addressof(self.struct)
+        self.scale = self.head_dim**-0.5
+        self.shape_B, self.shape_B1, self.shape_token = (self.B,), (self.B + 1,), (self.kv_heads, self.head_dim)
 
 
-def _packed(t, heads, T, cache, name):
-    if t.dim() != 3 or t.shape[0] != T or t.shape[2] != cache.head_dim or t.dtype != cache.dtype or \
-            (heads is not None and t.shape[1] != heads):
-        raise ValueError(f"{name} must be [{T}, {heads or 'heads'}, {cache.head_dim}] of the cache's dtype")
-    if t.stride(2) != 1:
-        raise ValueError(f"{name}: head_dim must be contiguous")
+# The checks below run on every call of a decoding loop whose kernels take a few
+# microseconds, so each is one comparison on the way that is taken, and what
+# exactly is wrong is worked out after one of them fails.
+def _refuse_packed(cache, T, tensors):
+    for name, t, heads in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("libretrace takes CUDA tensors")
+        if t.dim() != 3 or t.shape[0] != T or t.shape[2] != cache.head_dim or t.dtype != cache.dtype or \
+                (heads is not None and t.shape[1] != heads):
+            raise ValueError(f"{name} must be [{T}, {heads or 'heads'}, {cache.head_dim}] of the cache's dtype")
+        if t.stride(2) != 1:
+            raise ValueError(f"{name}: head_dim must be contiguous")
+
+
+def _refuse_lengths(cache, cache_len, q_start):
+    for name, t, n in (("cache_len", cache_len, cache.B), ("q_start", q_start, cache.B + 1)):
+        if t is None and name == "q_start":
+            continue
+        _int32(t, name)
+        if not t.is_cuda:
+            raise ValueError("libretrace takes CUDA tensors")
+        if t.shape != (n,) or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous [{n}]: the page table has {cache.B} rows")
 
 
 def _lengths(cache, cache_len, q_start):
-    _int32(cache_len, "cache_len")
-    if cache_len.shape != (cache.B,) or not cache_len.is_contiguous():
-        raise ValueError("cache_len must be a contiguous [B], B the rows of the page table")
-    if q_start is not None:
-        _int32(q_start, "q_start")
-        if q_start.shape != (cache.B + 1,) or not q_start.is_contiguous():
-            raise ValueError("q_start must be a contiguous [B + 1]")
+    """Device pointers of the lengths and of the list of starts."""
+    if cache_len.dtype != torch.int32 or cache_len.shape != cache.shape_B or not cache_len.is_cuda or not cache_len.is_contiguous():
+        _refuse_lengths(cache, cache_len, None)
+    if q_start is None:
+        return cache_len.data_ptr(), None
+    if q_start.dtype != torch.int32 or q_start.shape != cache.shape_B1 or not q_start.is_cuda or not q_start.is_contiguous():
+        _refuse_lengths(cache, cache_len, q_start)
+    return cache_len.data_ptr(), q_start.data_ptr()
 
 
 def retrace_kv_append(q, k, v, cache: KvCache, cache_len, rope, q_out=None, q_start=None, interleaved=False, stream=None):
     """Appends k and v [T, kv_heads, head_dim] to the cache, rotating k and q [T, q_heads, head_dim]
     (optional, into q_out) by rope [positions, rot/2, 2] (None: no rotation) on the way (see
     include/retrace.h)."""
-    T = k.shape[0]
-    _packed(k, cache.kv_heads, T, cache, "k")
-    _packed(v, cache.kv_heads, T, cache, "v")
-    _lengths(cache, cache_len, q_start)
-    q_heads, qs, os = 0, (0, 0), (0, 0)
+    shape = k.shape
+    T, dtype = shape[0], cache.dtype
+    k_token, k_head, k_last = k.stride()
+    v_token, v_head, v_last = v.stride()
+    if shape[1:] != cache.shape_token or v.shape != shape or k.dtype != dtype or v.dtype != dtype or k_last != 1 or v_last != 1 or \
+            not (k.is_cuda and v.is_cuda):
+        _refuse_packed(cache, T, (("k", k, cache.kv_heads), ("v", v, cache.kv_heads)))
+    q_ptr = out_ptr = None
+    q_heads = q_token = q_head = o_token = o_head = 0
     if q is not None:
-        q_heads = q.shape[1]
-        _packed(q, None, T, cache, "q")
-        _packed(q_out, q_heads, T, cache, "q_out")
-        qs, os = q.stride(), q_out.stride()
+        shape = q.shape
+        q_token, q_head, q_last = q.stride()
+        o_token, o_head, o_last = q_out.stride()
+        if shape[0] != T or shape[2] != cache.head_dim or q_out.shape != shape or q.dtype != dtype or q_out.dtype != dtype or \
+                q_last != 1 or o_last != 1 or not (q.is_cuda and q_out.is_cuda):
+            _refuse_packed(cache, T, (("q", q, None), ("q_out", q_out, q.shape[1])))
+        q_heads, q_ptr, out_ptr = shape[1], q.data_ptr(), q_out.data_ptr()
     positions = rot = 0
+    rope_ptr = None
     if rope is not None:
-        if rope.dtype != torch.float32 or rope.dim() != 3 or rope.shape[2] != 2 or not rope.is_contiguous():
-            raise ValueError("rope must be a contiguous float32 [positions, rot/2, 2]")
-        positions, rot = rope.shape[0], 2 * rope.shape[1]
-    ks, vs = k.stride(), v.stride()
-    _check(lib.retrace_kv_append(_ptr(q), qs[0], qs[1], q_heads, _ptr(k), ks[0], ks[1], _ptr(v), vs[0], vs[1], _ptr(q_start),
-                                 _ptr(cache_len), cache.B, T, _ptr(rope), positions, rot, int(interleaved), cache.ref,
-                                 _ptr(q_out) if q is not None else None, os[0], os[1], _stream(stream)))
+        if rope.dtype != torch.float32 or rope.dim() != 3 or rope.shape[2] != 2 or not rope.is_contiguous() or not rope.is_cuda:
+            raise ValueError("rope must be a contiguous float32 [positions, rot/2, 2] on the GPU")
+        positions, half, _ = rope.shape
+        rot, rope_ptr = 2 * half, rope.data_ptr()
+    len_ptr, start_ptr = _lengths(cache, cache_len, q_start)
+    status = _append(q_ptr, q_token, q_head, q_heads, k.data_ptr(), k_token, k_head, v.data_ptr(), v_token, v_head, start_ptr, len_ptr,
+                     cache.B, T, rope_ptr, positions, rot, interleaved, cache.ref, out_ptr, o_token, o_head, _stream(stream))
+    if status:
+        _check(status)
 
 
 class AttendWorkspace(Workspace):
@@ -472,34 +506,39 @@ def retrace_attend(q, cache: KvCache, cache_len, out, ws: AttendWorkspace, q_sta
                    causal=True, stream=None):
     """Attention of q [T, q_heads, head_dim] over the cache into out (see include/retrace.h);
     scale defaults to head_dim ** -0.5."""
-    T, q_heads, D = q.shape
-    _packed(q, None, T, cache, "q")
-    _packed(out, q_heads, T, cache, "out")
-    _lengths(cache, cache_len, q_start)
-    qs, os = q.stride(), out.stride()
-    _check(lib.retrace_attend(_ptr(q), qs[0], qs[1], q_heads, _ptr(q_start), _ptr(cache_len), cache.B, T,
-                              D ** -0.5 if scale is None else float(scale), int(window), int(sinks), int(causal), cache.ref,
-                              _ptr(out), os[0], os[1], ws.ptr, ws.nbytes, _stream(stream)))
+    shape = q.shape
+    q_token, q_head, q_last = q.stride()
+    o_token, o_head, o_last = out.stride()
+    if shape[2] != cache.head_dim or out.shape != shape or q.dtype != cache.dtype or out.dtype != cache.dtype or q_last != 1 or \
+            o_last != 1 or not (q.is_cuda and out.is_cuda):
+        _refuse_packed(cache, shape[0], (("q", q, None), ("out", out, shape[1])))
+    len_ptr, start_ptr = _lengths(cache, cache_len, q_start)
+    status = _attend(q.data_ptr(), q_token, q_head, shape[1], start_ptr, len_ptr, cache.B, shape[0],
+                     cache.scale if scale is None else scale, window, sinks, causal, cache.ref, out.data_ptr(), o_token, o_head,
+                     ws.ptr, ws.nbytes, _stream(stream))
+    if status:
+        _check(status)
 
 
-def _setting(t, B, dtype, name):
+def _setting(t, shape, dtype, name):
     if t is None:
         return None
-    if t.dtype != dtype or t.shape != (B,) or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous [B] {dtype}")
-    return _ptr(t)
+    if t.dtype != dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {list(shape)} {dtype} on the GPU")
+    return t.data_ptr()
 
 
 def retrace_sample(logits, uniforms, tokens, probs=None, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
     """Draws tokens [B, R] from logits [B, R, V] with the settings of each sequence ([B]) and the
     given uniforms [B, R] (see include/retrace.h)."""
     B, R, V = logits.shape
-    if logits.stride(2) != 1:
+    batch, step, last = logits.stride()
+    if last != 1:
         raise ValueError("logits: vocabulary dimension must be contiguous")
-    for t, dtype, name in ((uniforms, torch.float32, "uniforms"), (tokens, torch.int32, "tokens"), (probs, torch.float32, "probs")):
-        if t is not None and (t.dtype != dtype or t.shape != (B, R) or not t.is_contiguous()):
-            raise ValueError(f"{name} must be a contiguous [B, R] {dtype}")
-    _check(lib.retrace_sample(_ptr(logits), _dtype_code(logits), B, R, V, logits.stride(1), logits.stride(0), _ptr(uniforms),
-                              _setting(temperature, B, torch.float32, "temperature"), _setting(top_k, B, torch.int32, "top_k"),
-                              _setting(top_p, B, torch.float32, "top_p"), _setting(min_p, B, torch.float32, "min_p"),
-                              _ptr(tokens), _ptr(probs), _stream(stream)))
+    rows, each, f32, i32 = (B, R), (B,), torch.float32, torch.int32
+    status = _sample(_ptr(logits), _dtype_code(logits), B, R, V, step, batch, _setting(uniforms, rows, f32, "uniforms"),
+                     _setting(temperature, each, f32, "temperature"), _setting(top_k, each, i32, "top_k"),
+                     _setting(top_p, each, f32, "top_p"), _setting(min_p, each, f32, "min_p"),
+                     _setting(tokens, rows, i32, "tokens"), _setting(probs, rows, f32, "probs"), _stream(stream))
+    if status:
+        _check(status)

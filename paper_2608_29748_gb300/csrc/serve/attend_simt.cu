@@ -283,10 +283,11 @@ template <typename T, int DP, int R>
 cudaError_t launch(SimtParams& p, cudaStream_t stream) {
   constexpr size_t smem = sizeof(SimtShared<DP, R>);
   auto kernel = attend_simt_kernel<T, DP, R>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e != cudaSuccess) return e;
   DeviceInfo dev;
-  if ((e = device_info(&dev)) != cudaSuccess) return e;
+  cudaError_t e = device_info(&dev);
+  if (e != cudaSuccess) return e;
+  static std::atomic<uint64_t> allowed{0};
+  if ((e = allow_shared(kernel, smem, dev, allowed)) != cudaSuccess) return e;
   constexpr int kPerSm = smem <= 75 * 1024 ? 3 : smem <= 113 * 1024 ? 2 : 1;
   int grid = dev.sm_count * kPerSm;
   if (grid > kAttendMaxCtas) grid = kAttendMaxCtas;

@@ -779,10 +779,11 @@ cudaError_t launch(TcParams& p, cudaStream_t stream) {
   }
   constexpr size_t smem = Sh::kControl + sizeof(Control);
   static_assert(smem <= 227 * 1024, "shared memory of a CTA");
-  cudaError_t e = cudaFuncSetAttribute(attend_tc_kernel<DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e != cudaSuccess) return e;
   DeviceInfo dev;
-  if ((e = device_info(&dev)) != cudaSuccess) return e;
+  cudaError_t e = device_info(&dev);
+  if (e != cudaSuccess) return e;
+  static std::atomic<uint64_t> allowed{0};
+  if ((e = allow_shared(attend_tc_kernel<DP>, smem, dev, allowed)) != cudaSuccess) return e;
   const int grid = dev.sm_count < kAttendMaxTcCtas ? dev.sm_count : kAttendMaxTcCtas;
   e = launch_dependent(attend_tc_kernel<DP>, dim3(grid), dim3(kThreads), smem, stream, 1u, mq, mk, mv, p);
   if (e != cudaSuccess) return e;

@@ -1161,10 +1161,11 @@ __global__ void __launch_bounds__(kThreads, 4) sample_stream_kernel(SampleArgs a
   sample_by<T, Stream<T>>(a, 1, *reinterpret_cast<ClusterShared*>(raw));
 }
 
-template <typename K, typename... Args>
-cudaError_t launch_rows(K kernel, const SampleArgs& a, int C, cudaStream_t stream, Args... args) {
+template <auto kernel, typename... Args>
+cudaError_t launch_rows(const SampleArgs& a, const DeviceInfo& dev, int C, cudaStream_t stream, Args... args) {
   constexpr size_t smem = sizeof(ClusterShared);
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  static std::atomic<uint64_t> allowed{0};
+  const cudaError_t e = allow_shared(kernel, smem, dev, allowed);
   if (e != cudaSuccess) return e;
   return launch_dependent(kernel, dim3((unsigned)(a.B * a.R) * C), dim3(kThreads), smem, stream, (unsigned)C, a, args...);
 }
@@ -1182,11 +1183,11 @@ cudaError_t launch_typed(const SampleArgs& a, cudaStream_t stream) {
   int C = 1;
   while (C < kMaxCluster && need(C) > 1 && rows * C * 2 <= dev.sm_count) C *= 2;
   const int n = need(C);
-  if (rows * C > dev.sm_count || n > 10) return launch_rows(sample_stream_kernel<T>, a, 1, stream);
-  if (n <= 1) return launch_rows(sample_cluster_kernel<T, 1>, a, C, stream, C);
-  if (n <= 2) return launch_rows(sample_cluster_kernel<T, 2>, a, C, stream, C);
-  if (n <= 5) return launch_rows(sample_cluster_kernel<T, 5>, a, C, stream, C);
-  return launch_rows(sample_cluster_kernel<T, 10>, a, C, stream, C);
+  if (rows * C > dev.sm_count || n > 10) return launch_rows<sample_stream_kernel<T>>(a, dev, 1, stream);
+  if (n <= 1) return launch_rows<sample_cluster_kernel<T, 1>>(a, dev, C, stream, C);
+  if (n <= 2) return launch_rows<sample_cluster_kernel<T, 2>>(a, dev, C, stream, C);
+  if (n <= 5) return launch_rows<sample_cluster_kernel<T, 5>>(a, dev, C, stream, C);
+  return launch_rows<sample_cluster_kernel<T, 10>>(a, dev, C, stream, C);
 }
 
 }  // namespace

@@ -8,6 +8,17 @@ namespace retrace {
 
 constexpr int kMaxHeadDim = 256;
 
+// Lets a kernel have `bytes` of dynamic shared memory: asked of the runtime once per
+// device (`done`: a bit per device, the kernel's own), not on every call.
+template <typename K>
+cudaError_t allow_shared(K kernel, size_t bytes, const DeviceInfo& dev, std::atomic<uint64_t>& done) {
+  const uint64_t bit = 1ull << (dev.device & 63);
+  if (dev.device < 64 && (done.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
+
 struct AppendArgs {
   const void* q;  // NULL: keys and values only
   long long q_token, q_head;
