@@ -19,6 +19,7 @@ struct AttendShape {
   const int32_t* q_start;
   const int32_t* cache_len;
   int B, T, kv_heads;
+  int uniform;  // tokens of every sequence where there is no list
   int causal, window, sinks;
   int places;       // positions a sequence has places for: max_pages * page_size
   int unit_tokens;  // tokens of a unit
@@ -46,7 +47,12 @@ __device__ __forceinline__ UnitKeys unit_keys(const AttendShape& s, int c, int n
   return u;
 }
 
-__device__ __forceinline__ int units_of(const AttendShape& s, int n) { return (n + s.unit_tokens - 1) / s.unit_tokens; }
+__device__ __forceinline__ SeqTokens tokens_of(const AttendShape& s, int b) {
+  return s.q_start ? seq_tokens(s.q_start, s.B, s.T, b) : SeqTokens{b * s.uniform, s.uniform};
+}
+__device__ __forceinline__ int units_of(const AttendShape& s, int n) {
+  return n <= s.unit_tokens ? n > 0 : (n + s.unit_tokens - 1) / s.unit_tokens;
+}
 template <int kKeys>
 __device__ __forceinline__ int unit_cost(const AttendShape& s, int c, int n, int u) {
   return max(1, unit_keys<kKeys>(s, c, n, u * s.unit_tokens, min(n, (u + 1) * s.unit_tokens)).count);
@@ -61,7 +67,7 @@ __device__ __forceinline__ long long head_cost(const AttendShape& s, int b, bool
   int c = 0, units = 0;
   long long cost = 0;
   if (valid) {
-    q = seq_tokens(s.q_start, s.B, s.T, b);
+    q = tokens_of(s, b);
     c = cached_tokens(s.cache_len, b);
     units = units_of(s, q.n);
     if (units <= kAlone)
@@ -97,8 +103,8 @@ struct Piece {
   int row0, n, c;  // first packed row of the sequence, its tokens, its cached tokens
   int i0, i1;      // tokens of the unit
   UnitKeys keys;
-  int k0, k1;  // of keys.count (an empty unit: 0, 0)
-  int pieces;  // the CTAs that share the unit
+  int k0, k1;             // of keys.count (an empty unit: 0, 0)
+  int first_cta, pieces;  // the CTAs that share the unit
 };
 
 // x / y; a division of 64 bits takes many instructions, and costs rarely need them.
@@ -118,12 +124,13 @@ struct PieceWalk {
     head = p.head;
     unit = p.unit;
   }
-  // The piece at `at`, and on to the next one.  False at the end of the range.
-  template <int kKeys>
+  // The piece at `at`, and on to the next one.  False at the end of the range.  `pieces` is
+  // worked out only where it is asked for.
+  template <int kKeys, bool kPieces = false>
   __device__ __forceinline__ bool next(const AttendShape& s, const PlanStart& p, Piece* out) {
     if (at >= p.end) return false;
     for (;;) {
-      const SeqTokens q = seq_tokens(s.q_start, s.B, s.T, b);
+      const SeqTokens q = tokens_of(s, b);
       if (unit * (long long)s.unit_tokens < q.n) {
         out->b = b;
         out->head = head;
@@ -147,7 +154,11 @@ struct PieceWalk {
     const int cost = max(1, out->keys.count);
     const long long k0 = at - unit_begin, left = p.end - unit_begin;
     const int k1 = left < cost ? (int)left : cost;
-    out->pieces = (int)(quotient(unit_begin + cost - 1, p.share) - quotient(unit_begin, p.share)) + 1;
+    if (kPieces) {
+      const long long first = quotient(unit_begin, p.share);
+      out->first_cta = (int)first;
+      out->pieces = (int)(quotient(unit_begin + cost - 1, p.share) - first) + 1;
+    }
     out->k0 = out->keys.count ? (int)k0 : 0;
     out->k1 = out->keys.count ? k1 : 0;
     at = unit_begin + k1;
@@ -201,7 +212,7 @@ __device__ __forceinline__ void plan_start(const AttendShape& s, int grid, int l
     for (int i = 0; i < per; ++i) {
       const int b = tid * per + i;
       if (b >= s.B) break;
-      const SeqTokens q = seq_tokens(s.q_start, s.B, s.T, b);
+      const SeqTokens q = tokens_of(s, b);
       const int c = cached_tokens(s.cache_len, b), units = units_of(s, q.n);
       long long one = 0;
       for (int u = 0; u < units; ++u) one += unit_cost<kKeys>(s, c, q.n, u);

@@ -94,7 +94,7 @@ __global__ void __launch_bounds__(kThreads) attend_simt_kernel(const __grid_cons
 
   JoinUnit unit{};
   Piece pc;
-  while (walk.next<kKeys>(P.shape, plan, &pc)) {
+  while (walk.next<kKeys, true>(P.shape, plan, &pc)) {
     const int kv_head = pc.head / P.splits, part = pc.head % P.splits;
     const int G_all = a.q_heads / cache.kv_heads;
     const int G = min(P.group, G_all - part * P.group), h0 = kv_head * G_all + part * P.group;
@@ -328,6 +328,7 @@ cudaError_t launch_attend_simt(const AttendArgs& a, cudaStream_t stream) {
   p.shape.cache_len = a.cache_len;
   p.shape.B = a.B;
   p.shape.T = a.T;
+  p.shape.uniform = a.q_start ? 0 : a.T / a.B;
   p.shape.causal = a.causal;
   p.shape.window = a.window;
   p.shape.sinks = a.sinks;

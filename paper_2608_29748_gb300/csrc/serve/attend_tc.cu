@@ -33,6 +33,7 @@ constexpr int kThreads = 384;
 constexpr int kKeys = 128;  // keys of a tile
 constexpr int kRows = 128;  // rows of a tile
 constexpr unsigned long long kDrainNs = 20ull * 1000ull * 1000ull;
+constexpr int kJoinRows = 32;
 constexpr int kMasks = 16;  // ring of page masks: more than the tiles between loading and softmax
 
 struct TcParams {
@@ -41,9 +42,11 @@ struct TcParams {
   int group;          // query heads of a key/value head
   int tile_tokens;    // tokens of a row tile
   int q_box;          // tokens of a Q box
+  FastDivide page_size;
   int kv_box;         // slots of a K or V box: they lie within a page and divide a tile
   float scale2;       // |scale| log2(e)
   int negate;         // scale < 0
+  int join;           // parts are joined by the last CTA of a unit, else by a second kernel
 };
 
 template <int DP>
@@ -75,7 +78,7 @@ struct Control {
   PlanStart plan;
   long long sum[kThreads / 32];
   uint32_t tmem;
-  int abort;
+  int abort, last;
   PieceWalk walk[2];  // of the softmax streams
   Piece piece[2][2];  // this one and the next
   int more[2][2];
@@ -282,7 +285,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       // lane (half, box) loads one box of a tile
       const int boxes = kKeys / P.kv_box, half = lane / 16, box = lane % 16;
       const bool active = box < boxes && half < Sh::kHalves;
-      const int page_size = a.cache.page_size, box_rows = P.q_box * P.group;
+      const int box_rows = P.q_box * P.group;
       Control::Ring& ring = ct.ring[keys ? 0 : 1];
       const uint32_t slots = keys ? Sh::kRingK : Sh::kRingV, tiles_at = base + (keys ? 0 : Sh::kVOffset);
       uint32_t tiles = 0, slot = 0, phase = 0, used[2] = {0, 0};
@@ -298,9 +301,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         auto place_of = [&](int k) {  // of this lane's box of the piece's tile k
           Place x{a.cache.num_pages, 0};  // a box without a page lies outside the tensor: zeros
           if (active && k < nt) {
-            const int j = pc.keys.tile(pc.k0 + k) * kKeys + box * P.kv_box, i = j / page_size;
+            const int j = pc.keys.tile(pc.k0 + k) * kKeys + box * P.kv_box, i = P.page_size(j);
             const int page = page_of(a.cache, pc.b, i);
-            if (page >= 0) x = Place{page, j - i * page_size};
+            if (page >= 0) x = Place{page, j - i * P.page_size.by};
           }
           return x;
         };
@@ -497,16 +500,54 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) raise_abort(abort, a.status);
       }
     };
+    // The part of a unit of few rows is written: the last CTA of the unit to come here joins
+    // the parts, in the order of the CTAs' ranges.
+    auto join_parts = [&](const Piece& pc) {
+      __threadfence();
+      named_barrier<1, 256>();
+      if (tid == 128) ct.last = !*abort && atomicAdd(a.tickets + pc.first_cta, 1u) == (uint32_t)(pc.pieces - 1);
+      named_barrier<1, 256>();
+      if (ct.last) {
+        __threadfence();
+        if (tid == 128) a.tickets[pc.first_cta] = 0u;
+        constexpr int kLanes = DP / 4;  // threads of a row
+        const int col = (tid - 128) % kLanes * 4, rows = (pc.i1 - pc.i0) * G;
+        for (int r = (tid - 128) / kLanes; r < rows; r += 256 / kLanes) {
+          float top = -INFINITY, sum = 0.f;
+          float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+          for (int i = 0; i < pc.pieces; ++i) {
+            const float* from = a.partials + ((long long)(pc.first_cta + i) * 2 + (i == 0 ? 1 : 0)) * Sh::kPart;
+            const float2 st = __ldcg(reinterpret_cast<const float2*>(from + Sh::kPartRows * DP + r * 2));
+            const float4 y = __ldcg(reinterpret_cast<const float4*>(from + r * DP + col));
+            const bool any = st.x != -INFINITY;
+            const float up = fmaxf(top, st.x), f = any ? exp2_fast(top - up) : 1.f, g = any ? exp2_fast(st.x - up) : 0.f;
+            top = up;
+            sum = sum * f + st.y * g;
+            o.x = o.x * f + y.x * g;
+            o.y = o.y * f + y.y * g;
+            o.z = o.z * f + y.z * g;
+            o.w = o.w * f + y.w * g;
+          }
+          const float inv = sum == 0.f ? 0.f : 1.f / sum;
+          if (col < D)
+            *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + (long long)(pc.row0 + pc.i0 + r / G) * a.out_token +
+                                      (pc.head * G + r % G) * (long long)a.out_head + col) =
+                make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+        }
+      }
+      named_barrier<1, 256>();  // `last` has been read
+    };
     // One thread of the stream walks, a piece ahead; the pieces stay in shared memory.
     const bool walker = row == kRows - 32;
     if (walker) {
       ct.walk[s].start(plan);
-      ct.more[s][0] = ct.walk[s].next<kKeys>(P.shape, plan, &ct.piece[s][0]);
+      ct.more[s][0] = ct.walk[s].next<kKeys, true>(P.shape, plan, &ct.piece[s][0]);
     }
     for (int np = 0;; np ^= 1) {
       stream_barrier(s);
       if (!ct.more[s][np]) break;
-      if (walker) ct.more[s][np ^ 1] = ct.walk[s].next<kKeys>(P.shape, plan, &ct.piece[s][np ^ 1]);
+      if (walker) ct.more[s][np ^ 1] = ct.walk[s].next<kKeys, true>(P.shape, plan, &ct.piece[s][np ^ 1]);
       const Piece& pc = ct.piece[s][np];
       const int nt = pc.k1 - pc.k0, tokens = pc.i1 - pc.i0;
       const bool two = tokens > P.tile_tokens;
@@ -711,10 +752,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (whole) continue;
 
+      if (P.join) {
+        join_parts(pc);
+        continue;
+      }
       if (pc.k0 == 0)
         unit = JoinUnit{pc.pieces, tokens * G, min(tokens, P.tile_tokens) * G, pc.row0 + pc.i0, pc.head * G, G, {0, 0}};
     }
-    if (tid == 128) a.units[blockIdx.x] = unit;
+    if (!P.join && tid == 128) a.units[blockIdx.x] = unit;
   }
   tc_fence_before();
   __syncthreads();
@@ -761,7 +806,7 @@ bool encode(CUtensorMap* map, const void* base, int rank, const long long* dims,
 int gcd(int a, int b) { return b ? gcd(b, a % b) : a; }
 
 template <int DP>
-cudaError_t launch(TcParams& p, cudaStream_t stream) {
+cudaError_t launch(TcParams& p, const DeviceInfo& dev, cudaStream_t stream) {
   using Sh = TcShape<DP>;
   const AttendArgs& a = p.a;
   const retrace_kv_cache& c = a.cache;
@@ -779,15 +824,13 @@ cudaError_t launch(TcParams& p, cudaStream_t stream) {
   }
   constexpr size_t smem = Sh::kControl + sizeof(Control);
   static_assert(smem <= 227 * 1024, "shared memory of a CTA");
-  DeviceInfo dev;
-  cudaError_t e = device_info(&dev);
-  if (e != cudaSuccess) return e;
   static std::atomic<uint64_t> allowed{0};
-  if ((e = allow_shared(attend_tc_kernel<DP>, smem, dev, allowed)) != cudaSuccess) return e;
+  cudaError_t e = allow_shared(attend_tc_kernel<DP>, smem, dev, allowed);
+  if (e != cudaSuccess) return e;
   const int grid = dev.sm_count < kAttendMaxTcCtas ? dev.sm_count : kAttendMaxTcCtas;
   e = launch_dependent(attend_tc_kernel<DP>, dim3(grid), dim3(kThreads), smem, stream, 1u, mq, mk, mv, p);
   if (e != cudaSuccess) return e;
-  return launch_attend_join(a, PartShape{Sh::kPartRows, DP, 1}, grid, stream);
+  return p.join ? cudaSuccess : launch_attend_join(a, PartShape{Sh::kPartRows, DP, 1}, grid, stream);
 }
 
 }  // namespace
@@ -810,6 +853,9 @@ size_t attend_tc_partial_bytes(int head_dim) {
 }
 
 cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t stream) {
+  DeviceInfo dev;
+  const cudaError_t e = device_info(&dev);
+  if (e != cudaSuccess) return e;
   TcParams p{};
   p.a = a;
   const retrace_kv_cache& c = a.cache;
@@ -824,13 +870,20 @@ cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t stream) {
   p.shape.cache_len = a.cache_len;
   p.shape.B = a.B;
   p.shape.T = a.T;
+  p.shape.uniform = a.q_start ? 0 : a.T / a.B;
+  p.page_size = FastDivide::of(c.page_size);
   p.shape.kv_heads = c.kv_heads;
   p.shape.causal = a.causal;
   p.shape.window = a.window;
   p.shape.sinks = a.sinks;
   p.shape.places = c.max_pages * c.page_size;
   p.shape.unit_tokens = 2 * p.tile_tokens;
-  return c.head_dim <= 64 ? launch<64>(p, stream) : launch<128>(p, stream);
+  // Where units of few rows are shared by two or three CTAs, the last one joins the parts
+  // and spares a launch; more parts, or larger ones, are read by the whole device in a second
+  // kernel.  Tokens over a window of 1024 keys, 2048 units: 196 us here, 219 with it; 500
+  // keys, 512 units: 47 / 56; one token over 2048 keys, 8 units of nine parts: 21.1 / 18.2.
+  p.join = !a.q_start && (long long)p.shape.uniform * p.group <= kJoinRows && 2ll * a.B * c.kv_heads >= dev.sm_count;
+  return c.head_dim <= 64 ? launch<64>(p, dev, stream) : launch<128>(p, dev, stream);
 }
 
 }  // namespace retrace

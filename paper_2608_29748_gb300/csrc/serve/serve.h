@@ -38,11 +38,11 @@ struct AppendArgs {
 };
 cudaError_t launch_kv_append(const AppendArgs& a, cudaStream_t stream);
 
-// Workspace of retrace_attend: the status word (256 bytes), a JoinUnit per CTA, then
+// Workspace of retrace_attend: the status word (256 bytes), a JoinUnit per CTA, a ticket
+// per CTA (zero between calls: who takes a unit's last one clears it), then
 // two partial results per CTA (a CTA's range of work begins and ends inside a unit at
-// most): fp32 rows, and the maximum and sum of each.  Nothing in it outlives a call but
-// the status word, and its size does not depend on the batch, so one workspace serves
-// every call of its head size.
+// most): fp32 rows, and the maximum and sum of each.  Its size and layout do not depend on
+// the batch, so one workspace serves every call of its head size.
 constexpr int kAttendMaxCtas = 512;    // of the CUDA-core kernel
 constexpr int kAttendMaxTcCtas = 192;  // of the tensor-core kernel
 
@@ -55,7 +55,9 @@ struct JoinUnit {
   int unused[2];
 };
 constexpr size_t kAttendUnits = 256;
-constexpr size_t kAttendPartials = kAttendUnits + kAttendMaxCtas * sizeof(JoinUnit);
+constexpr size_t kAttendTickets = kAttendUnits + kAttendMaxCtas * sizeof(JoinUnit);
+constexpr size_t kAttendPartials = kAttendTickets + 256 * 4;
+static_assert(kAttendMaxTcCtas <= 256, "tickets");
 
 struct AttendArgs {
   const void* q;
@@ -71,6 +73,7 @@ struct AttendArgs {
   long long out_token, out_head;
   uint32_t* status;
   JoinUnit* units;
+  uint32_t* tickets;
   float* partials;
 };
 // A part: `rows` rows of `cols` floats, then their (maximum, sum).

@@ -145,6 +145,7 @@ retrace_status retrace_attend(const void* q, int64_t q_token_stride, int64_t q_h
   char* w = static_cast<char*>(ws);
   a.status = reinterpret_cast<uint32_t*>(w);
   a.units = reinterpret_cast<JoinUnit*>(w + kAttendUnits);
+  a.tickets = reinterpret_cast<uint32_t*>(w + kAttendTickets);
   a.partials = reinterpret_cast<float*>(w + kAttendPartials);
   const cudaError_t e = attend_tc_supported(a) ? launch_attend_tc(a, stream) : launch_attend_simt(a, stream);
   return e == cudaSuccess ? RETRACE_OK : cuda_fail(e, "attention kernel launch");

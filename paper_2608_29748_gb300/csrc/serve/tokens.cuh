@@ -8,6 +8,18 @@
 namespace retrace {
 namespace {
 
+// x / d for 0 <= x < 2^31 by a multiplication: q = (x + hi(x mul)) >> shift.
+struct FastDivide {
+  uint32_t mul;
+  int shift, by;
+  __host__ static FastDivide of(int d) {
+    int s = 0;
+    while ((1ll << s) < d) ++s;
+    return {(uint32_t)(((1ull << 32) * ((1ull << s) - (unsigned long long)d)) / (unsigned long long)d + 1), s, d};
+  }
+  __device__ __forceinline__ int operator()(int x) const { return (int)((__umulhi((uint32_t)x, mul) + (uint32_t)x) >> shift); }
+};
+
 // The tokens of sequence b: rows [first, first + n) of the packed tensors.  The
 // list is the caller's device data: whatever it holds, the rows stay in [0, T).
 struct SeqTokens {
