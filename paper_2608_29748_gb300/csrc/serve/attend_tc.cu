@@ -538,6 +538,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       named_barrier<1, 256>();  // `last` has been read
     };
+    // Where this thread's row goes, the tile's first token given.
+    auto row_out = [&](const Piece& pc, int t0) {
+      return static_cast<__nv_bfloat16*>(a.out) + (long long)(pc.row0 + pc.i0 + t0 + row / G) * a.out_token +
+             (pc.head * G + row % G) * (long long)a.out_head;
+    };
     // One thread of the stream walks, a piece ahead; the pieces stay in shared memory.
     const bool walker = row == kRows - 32;
     if (walker) {
@@ -556,11 +561,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool valid = row < rows, busy = (row & ~31) < rows;                          // this row, this warp
       const int p = pc.c + pc.i0 + t0 + row / G;
       const int hi = !valid ? -1 : a.causal ? p : pc.c + pc.n - 1, lo = a.window > 0 ? p - a.window + 1 : 0;
-      const long long at = (long long)(pc.row0 + pc.i0 + t0 + row / G) * a.out_token + (pc.head * G + row % G) * (long long)a.out_head;
-      __nv_bfloat16* out = static_cast<__nv_bfloat16*>(a.out) + at;
       if (nt == 0) {  // nothing is visible
-        if (valid && (two || s == 0) && ok)
+        if (valid && (two || s == 0) && ok) {
+          __nv_bfloat16* out = row_out(pc, t0);
           for (int c = 0; c < D; c += 8) *reinterpret_cast<uint4*>(out + c) = make_uint4(0u, 0u, 0u, 0u);
+        }
         continue;
       }
       float m = -INFINITY;                // of the raw scores
@@ -593,83 +598,100 @@ __global__ void __launch_bounds__(kThreads, 1)
                                       pages == boxes_mask(kKeys / P.kv_box));
         const bool masked = !__all_sync(0xFFFFFFFFu, whole);
         if (busy) {
-          float v[kKeys];
+          // Half of the row at a time, in a loop: less code, which a lone warp would wait for.
+#pragma unroll 1
+          for (int half = 0; half < 2; ++half) {
+            float v[64];
+            tmem_ld32(t_s + half * 64, v);
+            tmem_ld32(t_s + half * 64 + 32, v + 32);
+            tmem_wait_ld();
+            if (P.negate) {
 #pragma unroll
-          for (int c = 0; c < kKeys; c += 32) tmem_ld32(t_s + c, v + c);
-          tmem_wait_ld();
-          if (P.negate) {
-#pragma unroll
-            for (int c = 0; c < kKeys; ++c) v[c] = -v[c];
-          }
-          if (masked) {
-#pragma unroll
-            for (int w = 0; w < kKeys / 32; ++w) {
-              const int k0 = j0 + 32 * w;
-              const uint32_t see = seen_word(hi - k0, lo - k0, a.sinks - k0) & page_word(pages, P.kv_box, w);
-              if (__all_sync(0xFFFFFFFFu, !valid || see == ~0u)) continue;
-#pragma unroll
-              for (int c = 0; c < 32; ++c)
-                if (!(see >> c & 1u)) v[32 * w + c] = -INFINITY;
+              for (int c = 0; c < 64; ++c) v[c] = -v[c];
             }
-          }
-          auto top_of = [&]() {
-            float t[8];
+            if (masked) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) t[i] = max3(v[i], v[8 + i], v[16 + i]);
+              for (int w = 0; w < 2; ++w) {
+                const int k0 = j0 + 64 * half + 32 * w;
+                const uint32_t see = seen_word(hi - k0, lo - k0, a.sinks - k0) & page_word(pages, P.kv_box, 2 * half + w);
+                if (__all_sync(0xFFFFFFFFu, !valid || see == ~0u)) continue;
 #pragma unroll
-            for (int c = 24; c < 120; c += 16)
-#pragma unroll
-              for (int i = 0; i < 8; ++i) t[i] = max3(t[i], v[c + i], v[c + 8 + i]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) t[i] = fmaxf(t[i], v[120 + i]);
-            return max3(max3(t[0], t[1], t[2]), max3(t[3], t[4], t[5]), fmaxf(t[6], t[7]));
-          };
-          if (__any_sync(0xFFFFFFFFu, valid && m == -INFINITY)) {  // the first tile, or nothing seen so far
-            const float top = top_of();
-            if (m == -INFINITY) m = top;
-          }
-          // The weights refer to a maximum of before, without looking for this tile's.  Where their
-          // sum in a row shows that one may have grown past 2^14, and only there, the maximum is
-          // taken, O rescaled, and the tile done again.
-          float2 sum[2];
-          for (;;) {
-            const float ref = m == -INFINITY ? 0.f : -m * sl;
-            const float2 sl2 = make_float2(sl, sl), ref2 = make_float2(ref, ref);
-            sum[0] = sum[1] = make_float2(0.f, 0.f);
-#pragma unroll
-            for (int c = 0; c < kKeys; c += 32) {
-              uint32_t x[16];
-#pragma unroll
-              for (int i = 0; i < 16; ++i) {
-                float2 y = fma2(make_float2(v[c + 2 * i], v[c + 2 * i + 1]), sl2, ref2);
-                y.x = exp2_fast(y.x);
-                y.y = exp2_fast(y.y);
-                sum[i & 1] = add2(sum[i & 1], y);
-                x[i] = pack_bf16x2(y.x, y.y);
-              }
-              tmem_st16(t_s + c / 2, x);
-            }
-            const float2 both = add2(sum[0], sum[1]);
-            const bool raise = valid && both.x + both.y > 16384.f;
-            tmem_wait_st();
-            if (!__any_sync(0xFFFFFFFFu, raise)) break;
-            const float up = raise ? fmaxf(m, top_of()) : m, f = raise ? exp2_fast((m - up) * sl) : 1.f;
-            m = up;
-            l.x *= f;
-            l.y *= f;
-            if (done > 0) {
-#pragma unroll
-              for (int c = 0; c < DP; c += 8) {
-                float o[8];
-                tmem_ld8(t_o + c, o);
-                tmem_wait_ld();
-#pragma unroll
-                for (int i = 0; i < 8; ++i) o[i] *= f;
-                tmem_st8(t_o + c, o);
+                for (int c = 0; c < 32; ++c)
+                  if (!(see >> c & 1u)) v[32 * w + c] = -INFINITY;
               }
             }
+            auto top_of = [&]() {
+              float t[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) t[i] = max3(v[i], v[4 + i], v[8 + i]);
+#pragma unroll
+              for (int c = 12; c < 60; c += 8)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) t[i] = max3(t[i], v[c + i], v[c + 4 + i]);
+              return max3(max3(t[0], t[1], t[2]), max3(t[3], v[60], v[61]), fmaxf(v[62], v[63]));
+            };
+            if (__any_sync(0xFFFFFFFFu, valid && m == -INFINITY)) {  // nothing seen so far
+              const float top = top_of();
+              if (m == -INFINITY) m = top;
+            }
+            // The weights refer to a maximum of before, without looking for this one.  Where their
+            // sum in a row shows that one may have grown past 2^14, and only there, the maximum is
+            // taken, what was summed so far rescaled, and this half done again.
+            float2 sum[2];
+            for (;;) {
+              const float ref = m == -INFINITY ? 0.f : -m * sl;
+              const float2 sl2 = make_float2(sl, sl), ref2 = make_float2(ref, ref);
+              sum[0] = sum[1] = make_float2(0.f, 0.f);
+#pragma unroll
+              for (int c = 0; c < 64; c += 32) {
+                uint32_t x[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                  float2 y = fma2(make_float2(v[c + 2 * i], v[c + 2 * i + 1]), sl2, ref2);
+                  y.x = exp2_fast(y.x);
+                  y.y = exp2_fast(y.y);
+                  sum[i & 1] = add2(sum[i & 1], y);
+                  x[i] = pack_bf16x2(y.x, y.y);
+                }
+                tmem_st16(t_s + half * 32 + c / 2, x);
+              }
+              sum[0] = add2(sum[0], sum[1]);
+              const bool raise = valid && sum[0].x + sum[0].y > 16384.f;
+              if (!__any_sync(0xFFFFFFFFu, raise)) break;
+              tmem_wait_st();
+              const float up = raise ? fmaxf(m, top_of()) : m, f = raise ? exp2_fast((m - up) * sl) : 1.f;
+              m = up;
+              l.x *= f;
+              l.y *= f;
+              if (done > 0) {
+#pragma unroll
+                for (int c = 0; c < DP; c += 8) {
+                  float o[8];
+                  tmem_ld8(t_o + c, o);
+                  tmem_wait_ld();
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) o[i] *= f;
+                  tmem_st8(t_o + c, o);
+                }
+              }
+              if (half == 1) {  // the weights of the first half
+#pragma unroll
+                for (int c = 0; c < 32; c += 8) {
+                  float x[8];
+                  tmem_ld8(t_s + c, x);
+                  tmem_wait_ld();
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) {
+                    const uint32_t w = __float_as_uint(x[i]);
+                    x[i] = __uint_as_float(pack_bf16x2(bf16_lo(w) * f, bf16_hi(w) * f));
+                  }
+                  tmem_st8(t_s + c, x);
+                }
+              }
+            }
+            l = add2(l, sum[0]);
           }
-          l = add2(l, add2(sum[0], sum[1]));
+          tmem_wait_st();
         }
         ++done;
         tc_fence_before();
@@ -683,6 +705,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       tiles += nt;
 
       const float sum_l = l.x + l.y;
+      __nv_bfloat16* out = row_out(pc, two ? s * P.tile_tokens : 0);
       const bool whole = pc.pieces == 1;
       float* part = a.partials + ((long long)blockIdx.x * 2 + (pc.k0 == 0 ? 1 : 0)) * Sh::kPart;
       // Columns [c0, c1) of this thread's row: into the output, or into the part.
