@@ -437,10 +437,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (; j < nt; j += step) {
           const uint32_t k = (tiles + j) % Sh::kRingK, v = (tiles + j) % Sh::kRingV, before = (tiles + j - step) % Sh::kRingV;
           if (!wait_tile(0, k, two)) break;
-          if (j > first && ((!landed && !wait_tile(1, before, two)) || !wait(&ct.p_full[s], np++ & 1u))) break;
+          if (j > first && !landed && !wait_tile(1, before, two)) break;
           // With two row tiles the streams issue in turn: products that are issued together
           // share the tensor core and end together, and then it waits for both softmaxes.
           if (two && (s == 1 || batches > 0) && !wait(&ct.issued[s ^ 1], (s == 1 ? batches : batches - 1) & 1u)) break;
+          if (j > first && !wait(&ct.p_full[s], np++ & 1u)) break;
           if (j > first) values(before, j == first + step);
           // V of a tile at the edge of what the unit sees is there before its scores are: the
           // softmax clears rows of it
@@ -491,6 +492,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t t_s = tmem + lanes + s * 128, t_o = tmem + lanes + 256 + s * 128;
     const int G = P.group, D = a.cache.head_dim;
     const float sl = P.scale2;
+    const uint32_t all_boxes = boxes_mask(kKeys / P.kv_box);
     uint32_t ns = 0, tiles = 0;
     JoinUnit unit{};
     bool ok = true;
@@ -571,19 +573,26 @@ __global__ void __launch_bounds__(kThreads, 1)
       float m = -INFINITY;                // of the raw scores
       float2 l = make_float2(0.f, 0.f);  // the sum of 2^((score - m) sl), in two parts
       int done = 0;
+      const UnitKeys keys = pc.keys;
+      const int k0 = pc.k0;
       for (int j = two ? 0 : s; j < nt; j += two ? 1 : 2) {
-        const int tile = pc.keys.tile(pc.k0 + j), j0 = tile * kKeys;
+        // what is known of the tile before its scores are there
+        const int j0 = keys.tile(k0 + j) * kKeys;
+        const bool edge = j0 < keys.lo || j0 + kKeys - 1 > keys.hi;
+        // A row of the tile that holds no token is left as it is: nothing reads what it gives.
+        const bool in_sight = __all_sync(0xFFFFFFFFu, !valid || (j0 + kKeys - 1 <= hi && (j0 >= lo || j0 + kKeys <= a.sinks)));
         wait(&ct.s_full[s], ns++ & 1u);
         if (!ok) break;
         tc_fence_after();
         const uint32_t pages = ct.mask[(tiles + j) % kMasks];
+        const bool masked = !in_sight || pages != all_boxes;
         // A row of V that no row of the unit sees holds anything, and 0 times that need not
         // be 0: cleared before the product (V of such a tile landed before its scores were
         // issued).
-        if (j0 < pc.keys.lo || j0 + kKeys - 1 > pc.keys.hi) {
+        if (edge) {
           const uint32_t slot = (tiles + j) % Sh::kRingV;
           const int key = j0 + row;
-          if (key > pc.keys.hi || (key < pc.keys.lo && key >= a.sinks)) {
+          if (key > keys.hi || (key < keys.lo && key >= a.sinks)) {
 #pragma unroll
             for (int h = 0; h < Sh::kHalves; ++h)
 #pragma unroll
@@ -593,10 +602,6 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           fence_proxy_async_shared();
         }
-        // A row of the tile that holds no token is left as it is: nothing reads what it gives.
-        const bool whole = !valid || (j0 + kKeys - 1 <= hi && (j0 >= lo || j0 + kKeys <= a.sinks) &&
-                                      pages == boxes_mask(kKeys / P.kv_box));
-        const bool masked = !__all_sync(0xFFFFFFFFu, whole);
         if (busy) {
           // Half of the row at a time, in a loop: less code, which a lone warp would wait for.
 #pragma unroll 1
