@@ -24,6 +24,7 @@
 
 #include "../tc_pair.cuh"
 #include "attend_plan.cuh"
+#include "pairs.cuh"
 #include "serve.h"
 
 namespace retrace {
@@ -155,27 +156,6 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   float y;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
   return y;
-}
-// Two fp32 operations as one instruction.
-__device__ __forceinline__ uint64_t bits2(float2 v) {
-  uint64_t x;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(v.x), "f"(v.y));
-  return x;
-}
-__device__ __forceinline__ float2 floats2(uint64_t x) {
-  float2 v;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(x));
-  return v;
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
-  uint64_t y;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y) : "l"(bits2(a)), "l"(bits2(b)), "l"(bits2(c)));
-  return floats2(y);
-}
-__device__ __forceinline__ float2 add2(float2 a, float2 b) {
-  uint64_t y;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(bits2(a)), "l"(bits2(b)));
-  return floats2(y);
 }
 // Moves registers from the warpgroup of the copies and products to those of the softmax:
 // 128 x 88 + 256 x 208 are the 384 x 168 of the launch.
