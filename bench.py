@@ -68,7 +68,8 @@ TRAFFIC = {
 
 
 def kernel_sources_hash() -> str:
-    """Hash of every CUDA source of the library (kernels and their headers)."""
+    """Hash of every CUDA source of the round (kernels and their headers; the operators around
+    it, in csrc/serve, are not part of it)."""
     import hashlib
 
     h = hashlib.sha256()
