@@ -146,6 +146,8 @@ __global__ void __launch_bounds__(ManyShape<DP, E>::kThreads, ManyShape<DP, E>::
   typename Sh::Shared& sm = *reinterpret_cast<typename Sh::Shared*>(raw);
   const AttendArgs& a = P.a;
   const int tid = threadIdx.x, D = a.cache.head_dim, rg = tid / 16, lane = tid % 16;
+  pdl_launch_dependents();
+  pdl_wait();
   plan_start<kThreads, kKeys>(P.shape, gridDim.x, 1, &sm.plan, sm.sum);
   const PlanStart plan = sm.plan;
   PieceWalk walk;
@@ -186,11 +188,15 @@ __global__ void __launch_bounds__(ManyShape<DP, E>::kThreads, ManyShape<DP, E>::
     }
     __syncthreads();
     load(pc.k0, false);
+    load(pc.k0, true);
 
     for (int k = pc.k0; k < pc.k1; ++k) {
-      cp_async_wait<0>();  // K of this tile
-      __syncthreads();     // and V of the tile before is free
-      load(k, true);
+      if (k == pc.k0)
+        cp_async_wait<1>();  // K of this tile
+      else
+        cp_async_wait<0>();
+      __syncthreads();  // and V of the tile before is free
+      if (k > pc.k0) load(k, true);
       offsets(k + 1);
       float2 s[E][kKeysEach];
 #pragma unroll
@@ -327,6 +333,8 @@ __global__ void __launch_bounds__(FewShape<DP>::kThreads, FewShape<DP>::kPerSm) 
   const AttendArgs& a = P.a;
   const int tid = threadIdx.x, D = a.cache.head_dim, warp = tid / 32, lane = tid % 32;
   const int half = lane / 16, mine = lane % 16;  // of the scores: rows 4 half .. + 3, key `mine` of the warp
+  pdl_launch_dependents();
+  pdl_wait();
   plan_start<kThreads, kKeys>(P.shape, gridDim.x, 1, &sm.plan, sm.sum);
   const PlanStart plan = sm.plan;
   PieceWalk walk;
@@ -502,8 +510,7 @@ cudaError_t launch(K kernel, SimtParams& p, int DP, cudaStream_t stream, std::at
   p.group = (heads + p.splits - 1) / p.splits;
   p.shape.kv_heads = p.a.cache.kv_heads * p.splits;
   p.shape.unit_tokens = R / p.group;
-  kernel<<<grid, Sh::kThreads, smem, stream>>>(p);
-  if ((e = cudaGetLastError()) != cudaSuccess) return e;
+  if ((e = launch_dependent(kernel, dim3(grid), dim3(Sh::kThreads), smem, stream, 1u, p)) != cudaSuccess) return e;
   return launch_attend_join(p.a, PartShape{R, DP, 0}, grid, stream);
 }
 
