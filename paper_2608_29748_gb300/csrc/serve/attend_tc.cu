@@ -847,6 +847,9 @@ cudaError_t launch(TcParams& p, const DeviceInfo& dev, cudaStream_t stream) {
 
 }  // namespace
 
+// Every shape that fits, single tokens too, which fill few rows of a tile: 220 of them, 8 heads
+// of 128 over up to 1000 keys 169 us, on the CUDA cores 464; up to 79 keys 75 and 93.  (256
+// tokens, heads of 64 over up to 79 keys: 75 and 63, over up to 250 99 and 144.)
 bool attend_tc_supported(const AttendArgs& a) {
   const retrace_kv_cache& c = a.cache;
   const int G = a.q_heads / c.kv_heads;
