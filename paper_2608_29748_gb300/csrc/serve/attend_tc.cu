@@ -78,6 +78,11 @@ struct Control {
   uint64_t q_full[2], q_empty[2];
   uint64_t s_full[2];  // of a stream: S ready and the product with V before it done
   uint64_t p_full[2];  // P written, O rescaled
+  // O complete.  Not a phase of s_full: the next piece's first scores follow it with no p_full
+  // between them, so that one would complete twice while its waiter is still at the first.  The
+  // commits to s_full lie a p_full apart, and those to o_full a piece's p_full, which the softmax
+  // gives only after it has seen the phase before.
+  uint64_t o_full[2];
   uint64_t issued[2];  // two row tiles: a stream's products of a tile are on their way
   uint64_t done[2];    // after an expired wait: the issued products
   PlanStart plan;
@@ -236,6 +241,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(smem_u32(&ct.q_empty[s]), 2);  // both streams
       mbar_init(smem_u32(&ct.s_full[s]), 1);
       mbar_init(smem_u32(&ct.p_full[s]), 4);  // one arrival per warp of the stream
+      mbar_init(smem_u32(&ct.o_full[s]), 1);
       mbar_init(smem_u32(&ct.issued[s]), 1);
       mbar_init(smem_u32(&ct.done[s]), 1);
     }
@@ -448,7 +454,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const uint32_t before = (tiles + j - step) % Sh::kRingV;
           if ((!landed && !wait_tile(1, before, two)) || !wait(&ct.p_full[s], np++ & 1u)) break;
           values(before, j == first + step);
-          commit(&ct.s_full[s]);
+          commit(&ct.o_full[s]);
         } else {
           if (lane == 0) mbar_arrive(smem_u32(&ct.q_empty[q]));  // no tile for this stream
           next = next_work();
@@ -477,7 +483,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int G = P.group, D = a.cache.head_dim;
     const float sl = P.scale2;
     const uint32_t all_boxes = boxes_mask(kKeys / P.kv_box);
-    uint32_t ns = 0, tiles = 0;
+    uint32_t ns = 0, no = 0, tiles = 0;
     JoinUnit unit{};
     bool ok = true;
     auto wait = [&](uint64_t* bar, uint32_t parity) {
@@ -688,7 +694,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (lane == 0) mbar_arrive(smem_u32(&ct.p_full[s]));
       }
       if (done && ok) {  // O is complete
-        wait(&ct.s_full[s], ns++ & 1u);
+        wait(&ct.o_full[s], no++ & 1u);
         tc_fence_after();
       }
       tiles += nt;
