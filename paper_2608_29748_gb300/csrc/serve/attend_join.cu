@@ -17,10 +17,10 @@ namespace {
 constexpr int kThreads = 128;
 constexpr int kWarps = kThreads / 32;
 
-__device__ __forceinline__ float power(float x, int base2) {
-  if (!base2) return expf(x);
+__device__ __forceinline__ float power(float x, float scale2) {
+  if (scale2 == 0.f) return expf(x);
   float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x * scale2));
   return y;
 }
 
@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(kThreads) attend_join_kernel(const __grid_cons
           for (int i = 0; i < 8; ++i) {
             if (i0 + i >= unit.pieces) break;
             if (st[i].x == -INFINITY) continue;  // the part's keys are hidden from this row
-            const float up = fmaxf(top, st[i].x), f = power(top - up, part.base2), g = power(st[i].x - up, part.base2);
+            const float up = fmaxf(top, st[i].x), f = power(top - up, part.scale2), g = power(st[i].x - up, part.scale2);
             top = up;
             sum = sum * f + st[i].y * g;
             o[0] = o[0] * f + y[i].x * g;

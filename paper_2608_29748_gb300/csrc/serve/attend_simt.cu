@@ -511,7 +511,7 @@ cudaError_t launch(K kernel, SimtParams& p, int DP, cudaStream_t stream, std::at
   p.shape.kv_heads = p.a.cache.kv_heads * p.splits;
   p.shape.unit_tokens = R / p.group;
   if ((e = launch_dependent(kernel, dim3(grid), dim3(Sh::kThreads), smem, stream, 1u, p)) != cudaSuccess) return e;
-  return launch_attend_join(p.a, PartShape{R, DP, 0}, grid, stream);
+  return launch_attend_join(p.a, PartShape{R, DP, 0.f}, grid, stream);
 }
 
 template <typename T, int DP, int E>

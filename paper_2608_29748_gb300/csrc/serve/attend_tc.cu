@@ -39,6 +39,7 @@ constexpr int kKeys = 128;  // keys of a tile
 constexpr int kRows = 128;  // rows of a tile
 constexpr unsigned long long kDrainNs = 20ull * 1000ull * 1000ull;
 constexpr int kJoinRows = 32;  // most rows of a unit whose last CTA joins its parts (see `join`)
+constexpr float kFar = 8192.f;  // of a reference's exponent (see `far`)
 constexpr int kMasks = 16;  // ring of page masks: more than the tiles between loading and softmax
 
 struct TcParams {
@@ -513,7 +514,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             const float2 st = __ldcg(reinterpret_cast<const float2*>(from + Sh::kPartRows * DP + r * 2));
             const float4 y = __ldcg(reinterpret_cast<const float4*>(from + r * DP + col));
             const bool any = st.x != -INFINITY;
-            const float up = fmaxf(top, st.x), f = any ? exp2_fast(top - up) : 1.f, g = any ? exp2_fast(st.x - up) : 0.f;
+            const float up = fmaxf(top, st.x), f = any ? exp2_fast((top - up) * sl) : 1.f, g = any ? exp2_fast((st.x - up) * sl) : 0.f;
             top = up;
             sum = sum * f + st.y * g;
             o.x = o.x * f + y.x * g;
@@ -625,16 +626,61 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int i = 0; i < 4; ++i) t[i] = max3(t[i], v[c + i], v[c + 4 + i]);
               return max3(max3(t[0], t[1], t[2]), max3(t[3], v[60], v[61]), fmaxf(v[62], v[63]));
             };
-            if (__any_sync(0xFFFFFFFFu, valid && m == -INFINITY)) {  // nothing seen so far
-              const float top = top_of();
-              if (m == -INFINITY) m = top;
-            }
             // The weights refer to a maximum of before, without looking for this one.  Where their
             // sum in a row shows that one may have grown past 2^14, and only there, the maximum is
             // taken, what was summed so far rescaled, and this half done again.
+            // A row whose reference is `far` takes its maximum at once and subtracts it from the
+            // scores.  The rounding of m sl is at most 2^-12 of an exponent below that, less than what a
+            // weight loses in bf16; with scores of 2^30 it is some 2^5, and weights that are past 2^14 only
+            // through it stay so whatever maximum they refer to.
             float2 sum[2];
+            bool raise = false, any_raise = false, moved = false;
+            auto far = [&]() { return m != -INFINITY && !(fabsf(m) * sl < kFar); };
+            if (__any_sync(0xFFFFFFFFu, valid && !(fabsf(m) * sl < kFar))) {  // far, or nothing seen so far
+              const float top = top_of();
+              if (m == -INFINITY) m = top;
+              raise = valid && far();
+              any_raise = __any_sync(0xFFFFFFFFu, raise);
+            }
             for (;;) {
-              const float ref = m == -INFINITY ? 0.f : -m * sl;
+              if (any_raise) {
+                tmem_wait_st();
+                const float up = raise ? fmaxf(m, top_of()) : m, f = raise ? exp2_fast((m - up) * sl) : 1.f;
+                m = up;
+                l.x *= f;
+                l.y *= f;
+                if (done > 0) {
+#pragma unroll
+                  for (int c = 0; c < DP; c += 8) {
+                    float o[8];
+                    tmem_ld8(t_o + c, o);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) o[i] *= f;
+                    tmem_st8(t_o + c, o);
+                  }
+                }
+                if (half == 1) {  // the weights of the first half
+#pragma unroll
+                  for (int c = 0; c < 32; c += 8) {
+                    float x[8];
+                    tmem_ld8(t_s + c, x);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                      const uint32_t w = __float_as_uint(x[i]);
+                      x[i] = __uint_as_float(pack_bf16x2(bf16_lo(w) * f, bf16_hi(w) * f));
+                    }
+                    tmem_st8(t_s + c, x);
+                  }
+                }
+                if (valid && !moved && far()) {  // from here on no weight of this half is above 1
+                  moved = true;
+#pragma unroll
+                  for (int c = 0; c < 64; ++c) v[c] -= m;
+                }
+              }
+              const float ref = m == -INFINITY || moved ? 0.f : -m * sl;
               const float2 sl2 = make_float2(sl, sl), ref2 = make_float2(ref, ref);
               sum[0] = sum[1] = make_float2(0.f, 0.f);
 #pragma unroll
@@ -651,38 +697,9 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tmem_st16(t_s + half * 32 + c / 2, x);
               }
               sum[0] = add2(sum[0], sum[1]);
-              const bool raise = valid && sum[0].x + sum[0].y > 16384.f;
-              if (!__any_sync(0xFFFFFFFFu, raise)) break;
-              tmem_wait_st();
-              const float up = raise ? fmaxf(m, top_of()) : m, f = raise ? exp2_fast((m - up) * sl) : 1.f;
-              m = up;
-              l.x *= f;
-              l.y *= f;
-              if (done > 0) {
-#pragma unroll
-                for (int c = 0; c < DP; c += 8) {
-                  float o[8];
-                  tmem_ld8(t_o + c, o);
-                  tmem_wait_ld();
-#pragma unroll
-                  for (int i = 0; i < 8; ++i) o[i] *= f;
-                  tmem_st8(t_o + c, o);
-                }
-              }
-              if (half == 1) {  // the weights of the first half
-#pragma unroll
-                for (int c = 0; c < 32; c += 8) {
-                  float x[8];
-                  tmem_ld8(t_s + c, x);
-                  tmem_wait_ld();
-#pragma unroll
-                  for (int i = 0; i < 8; ++i) {
-                    const uint32_t w = __float_as_uint(x[i]);
-                    x[i] = __uint_as_float(pack_bf16x2(bf16_lo(w) * f, bf16_hi(w) * f));
-                  }
-                  tmem_st8(t_s + c, x);
-                }
-              }
+              raise = valid && sum[0].x + sum[0].y > 16384.f;
+              any_raise = __any_sync(0xFFFFFFFFu, raise);
+              if (!any_raise) break;
             }
             l = add2(l, sum[0]);
           }
@@ -725,7 +742,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       };
       auto put_stat = [&](float mm, float ll) {
         if (valid && !whole && ok)
-          *reinterpret_cast<float2*>(part + Sh::kPartRows * DP + ((two ? s * kRows : 0) + row) * 2) = make_float2(mm * sl, ll);
+          *reinterpret_cast<float2*>(part + Sh::kPartRows * DP + ((two ? s * kRows : 0) + row) * 2) = make_float2(mm, ll);
       };
       if (two) {
         const float inv = sum_l == 0.f ? 0.f : 1.f / sum_l;
@@ -848,7 +865,7 @@ cudaError_t launch(TcParams& p, const DeviceInfo& dev, cudaStream_t stream) {
   const int grid = dev.sm_count < kAttendMaxTcCtas ? dev.sm_count : kAttendMaxTcCtas;
   e = launch_dependent(attend_tc_kernel<DP>, dim3(grid), dim3(kThreads), smem, stream, 1u, mq, mk, mv, p);
   if (e != cudaSuccess) return e;
-  return p.join ? cudaSuccess : launch_attend_join(a, PartShape{Sh::kPartRows, DP, 1}, grid, stream);
+  return p.join ? cudaSuccess : launch_attend_join(a, PartShape{Sh::kPartRows, DP, p.scale2}, grid, stream);
 }
 
 }  // namespace
@@ -885,7 +902,7 @@ cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t stream) {
   p.tile_tokens = kRows / (p.group * p.q_box) * p.q_box;
   p.kv_box = gcd(c.page_size, kKeys);
   const float s = a.scale == 0.f ? 1e-30f : a.scale;  // 2^(1e-30 s) is 1, and -inf stays -inf
-  p.scale2 = fabsf(s) * 1.4426950408889634f;
+  p.scale2 = fminf(fabsf(s) * 1.4426950408889634f, 3.0e38f);
   p.negate = s < 0.f;
   p.shape.q_start = a.q_start;
   p.shape.cache_len = a.cache_len;

@@ -79,7 +79,7 @@ struct AttendArgs {
 // A part: `rows` rows of `cols` floats, then their (maximum, sum).
 struct PartShape {
   int rows, cols;
-  int base2;  // the maxima are binary exponents (else natural)
+  float scale2;  // weights are 2^(scale2 (x - maximum)); 0: e^(x - maximum)
 };
 cudaError_t launch_attend_join(const AttendArgs& a, PartShape part, int ctas, cudaStream_t stream);
 cudaError_t launch_attend_simt(const AttendArgs& a, cudaStream_t stream);
