@@ -39,7 +39,7 @@ constexpr int kKeys = 128;  // keys of a tile
 constexpr int kRows = 128;  // rows of a tile
 constexpr unsigned long long kDrainNs = 20ull * 1000ull * 1000ull;
 constexpr int kJoinRows = 32;  // most rows of a unit whose last CTA joins its parts (see `join`)
-constexpr float kFar = 8192.f;  // of a reference's exponent (see `far`)
+constexpr float kFar = 8192.f;  // of a reference's exponent (see the softmax)
 constexpr int kMasks = 16;  // ring of page masks: more than the tiles between loading and softmax
 
 struct TcParams {
@@ -626,60 +626,20 @@ __global__ void __launch_bounds__(kThreads, 1)
                 for (int i = 0; i < 4; ++i) t[i] = max3(t[i], v[c + i], v[c + 4 + i]);
               return max3(max3(t[0], t[1], t[2]), max3(t[3], v[60], v[61]), fmaxf(v[62], v[63]));
             };
+            if (__any_sync(0xFFFFFFFFu, valid && m == -INFINITY)) {  // nothing seen so far
+              const float top = top_of();
+              if (m == -INFINITY) m = top;
+            }
             // The weights refer to a maximum of before, without looking for this one.  Where their
             // sum in a row shows that one may have grown past 2^14, and only there, the maximum is
             // taken, what was summed so far rescaled, and this half done again.
-            // A row whose reference is `far` takes its maximum at once and subtracts it from the
+            // A row whose reference is far from zero takes its maximum at once and subtracts it from the
             // scores.  The rounding of m sl is at most 2^-12 of an exponent below that, less than what a
             // weight loses in bf16; with scores of 2^30 it is some 2^5, and weights that are past 2^14 only
             // through it stay so whatever maximum they refer to.
             float2 sum[2];
-            bool raise = false, any_raise = false, moved = false;
-            auto far = [&]() { return m != -INFINITY && !(fabsf(m) * sl < kFar); };
-            if (__any_sync(0xFFFFFFFFu, valid && !(fabsf(m) * sl < kFar))) {  // far, or nothing seen so far
-              const float top = top_of();
-              if (m == -INFINITY) m = top;
-              raise = valid && far();
-              any_raise = __any_sync(0xFFFFFFFFu, raise);
-            }
+            bool moved = false;
             for (;;) {
-              if (any_raise) {
-                tmem_wait_st();
-                const float up = raise ? fmaxf(m, top_of()) : m, f = raise ? exp2_fast((m - up) * sl) : 1.f;
-                m = up;
-                l.x *= f;
-                l.y *= f;
-                if (done > 0) {
-#pragma unroll
-                  for (int c = 0; c < DP; c += 8) {
-                    float o[8];
-                    tmem_ld8(t_o + c, o);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) o[i] *= f;
-                    tmem_st8(t_o + c, o);
-                  }
-                }
-                if (half == 1) {  // the weights of the first half
-#pragma unroll
-                  for (int c = 0; c < 32; c += 8) {
-                    float x[8];
-                    tmem_ld8(t_s + c, x);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                      const uint32_t w = __float_as_uint(x[i]);
-                      x[i] = __uint_as_float(pack_bf16x2(bf16_lo(w) * f, bf16_hi(w) * f));
-                    }
-                    tmem_st8(t_s + c, x);
-                  }
-                }
-                if (valid && !moved && far()) {  // from here on no weight of this half is above 1
-                  moved = true;
-#pragma unroll
-                  for (int c = 0; c < 64; ++c) v[c] -= m;
-                }
-              }
               const float ref = m == -INFINITY || moved ? 0.f : -m * sl;
               const float2 sl2 = make_float2(sl, sl), ref2 = make_float2(ref, ref);
               sum[0] = sum[1] = make_float2(0.f, 0.f);
@@ -697,9 +657,43 @@ __global__ void __launch_bounds__(kThreads, 1)
                 tmem_st16(t_s + half * 32 + c / 2, x);
               }
               sum[0] = add2(sum[0], sum[1]);
-              raise = valid && sum[0].x + sum[0].y > 16384.f;
-              any_raise = __any_sync(0xFFFFFFFFu, raise);
-              if (!any_raise) break;
+              const bool raise = valid && (sum[0].x + sum[0].y > 16384.f || fabsf(ref) >= kFar);
+              if (!__any_sync(0xFFFFFFFFu, raise)) break;
+              tmem_wait_st();
+              const float up = raise ? fmaxf(m, top_of()) : m, f = raise ? exp2_fast((m - up) * sl) : 1.f;
+              m = up;
+              l.x *= f;
+              l.y *= f;
+              if (done > 0) {
+#pragma unroll
+                for (int c = 0; c < DP; c += 8) {
+                  float o[8];
+                  tmem_ld8(t_o + c, o);
+                  tmem_wait_ld();
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) o[i] *= f;
+                  tmem_st8(t_o + c, o);
+                }
+              }
+              if (half == 1) {  // the weights of the first half
+#pragma unroll
+                for (int c = 0; c < 32; c += 8) {
+                  float x[8];
+                  tmem_ld8(t_s + c, x);
+                  tmem_wait_ld();
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) {
+                    const uint32_t w = __float_as_uint(x[i]);
+                    x[i] = __uint_as_float(pack_bf16x2(bf16_lo(w) * f, bf16_hi(w) * f));
+                  }
+                  tmem_st8(t_s + c, x);
+                }
+              }
+              if (valid && !moved && fabsf(m) * sl >= kFar) {  // no weight of this half is above 1 now
+                moved = true;
+#pragma unroll
+                for (int c = 0; c < 64; ++c) v[c] -= m;
+              }
             }
             l = add2(l, sum[0]);
           }
