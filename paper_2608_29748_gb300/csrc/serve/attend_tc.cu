@@ -660,8 +660,16 @@ __global__ void __launch_bounds__(kThreads, 1)
               const bool raise = valid && (sum[0].x + sum[0].y > 16384.f || fabsf(ref) >= kFar);
               if (!__any_sync(0xFFFFFFFFu, raise)) break;
               tmem_wait_st();
-              const float up = raise ? fmaxf(m, top_of()) : m, f = raise ? exp2_fast((m - up) * sl) : 1.f;
-              m = up;
+              // By a whole power of two where the maximum is near, so that weights that are in bf16
+              // already stay the same numbers.  (Far from zero it need not be one: there a score's own
+              // rounding is worth more than a weight's.)
+              float f = 1.f;
+              if (raise) {
+                const float top = fmaxf(m, top_of()), steps = ceilf((top - m) * sl);
+                const bool near = fabsf(top) * sl < kFar;
+                f = !near ? exp2_fast((m - top) * sl) : steps < 126.f ? __int_as_float((127 - (int)steps) << 23) : 0.f;
+                m = near ? m + __fdividef(steps, sl) : top;
+              }
               l.x *= f;
               l.y *= f;
               if (done > 0) {

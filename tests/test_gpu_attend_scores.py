@@ -24,12 +24,12 @@ def rt():
     return binding
 
 
-def check(x, rt, scale):
+def check(x, rt, scale, **mask):
     ws = rt.AttendWorkspace(x.Hq, x.Hkv, x.D, x.dtype)
-    rt.retrace_attend(x.q, x.cache(rt), x.cache_len, x.out, ws, q_start=x.q_start, scale=scale)
+    rt.retrace_attend(x.q, x.cache(rt), x.cache_len, x.out, ws, q_start=x.q_start, scale=scale, **mask)
     torch.cuda.synchronize()
     assert ws.check() == 0
-    want, spread = ref.attend(f64(x.q), f64(x.k), f64(x.v), x.table.cpu().numpy(), x.starts, x.cached, scale)
+    want, spread = ref.attend(f64(x.q), f64(x.k), f64(x.v), x.table.cpu().numpy(), x.starts, x.cached, scale, **mask)
     tol = 2.0**-8 * (spread + np.abs(want)) if x.dtype == BF16 else 1e-5 * spread
     err = np.abs(f64(x.out) - want)
     assert np.all(err <= tol + 1e-30), (float(err.max()), np.argwhere(err > tol)[:4])
@@ -98,3 +98,24 @@ def test_jumps_between_tiles(rt, dtype):
             values[n // 2 + 1] = 2 * far
             put(x, b, values)
         check(x, rt, 1.0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("low, high", [(3.5, 11.75), (3.5, 11.0), (3.484375, 10.3125), (3.59375, 9.75), (2.234375, 10.5), (5.15625, 10.625)])
+def test_weights_are_rounded_once(rt, dtype, low, high):
+    """A maximum that appears in the second half of a tile rescales the weights of the first
+    half, which are rounded already.  These scores lose most if that rounds them again."""
+    n, c = 140, 244
+    x = Batch([(n, c)], 1, 1, 64, 16, dtype)
+    x.q.zero_()
+    x.q[..., 0] = 1.0
+    x.k.zero_()
+    x.v.zero_()
+    values = np.full(n + c, -120.0)
+    values[:128], values[128:192], values[197] = 0.0, low, high
+    put(x, 0, values)
+    p = torch.arange(128, 192, device="cuda")
+    x.v[x.table[0, p // 16].long(), p % 16, 0] = (1 + torch.arange(64, device="cuda") / 64).to(dtype)
+    check(x, rt, 1.0, causal=False)
+    x.v[x.table[0, p // 16].long(), p % 16, 0] = (1 + 1 / 128 + torch.arange(64, device="cuda") / 64).to(dtype)
+    check(x, rt, 1.0, causal=False)
