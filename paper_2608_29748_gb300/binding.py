@@ -402,8 +402,9 @@ class _KvCacheStruct(ctypes.Structure):  # retrace_kv_cache (include/retrace.h)
 
 class KvCache:
     """A paged cache: k and v [num_pages, page_size, kv_heads, head_dim] (any strides,
-    the same for both, head_dim contiguous) and page_table [B, max_pages] int32.  Keeps the
-    tensors; their contents may change between calls."""
+    the same for both, head_dim contiguous) and page_table [B, max_pages] int32, whose rows are
+    apart in memory (sequences may have the same pages).  Keeps the tensors; their contents may
+    change between calls."""
 
     def __init__(self, k, v, page_table):
         if k.dim() != 4 or v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype or k.stride(3) != 1:
@@ -411,6 +412,9 @@ class KvCache:
         _int32(page_table, "page_table")
         if page_table.dim() != 2 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
             raise ValueError("page_table must be [B, max_pages], the pages of a sequence contiguous")
+        # a row of the table begins where the one before has ended (the stride of one row is not used)
+        if page_table.shape[0] > 1 and page_table.stride(0) < page_table.shape[1]:
+            raise ValueError("the rows of page_table must not share storage: an expanded table needs .contiguous()")
         self.k, self.v, self.page_table = k, v, page_table
         self.B, self.kv_heads, self.head_dim, self.dtype = page_table.shape[0], k.shape[2], k.shape[3], k.dtype
         self.struct = _KvCacheStruct(_ptr(k), _ptr(v), k.stride(0), k.stride(1), k.stride(2), k.shape[0], k.shape[1],

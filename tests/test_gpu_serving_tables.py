@@ -1,0 +1,51 @@
+"""Page tables of unusual layouts: refused, or read as they are.
+
+Tolerance, in fp32: a score of 64 products has an error of about 8 * 2^-24 of their
+absolute sum (20 to 40 here), so a weight one of 2e-5 of it.
+"""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import serving_oracle as ref
+from serving import Batch, f64
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def rt():
+    from paper_2608_29748_gb300 import binding
+
+    return binding
+
+
+def test_tables_with_equal_rows(rt):
+    """Three sequences over the same pages: refused as an expanded row, right as rows of their own."""
+    x = Batch([(2, 60)] * 3, 4, 2, 64, 16, torch.float32, seed=1)
+    shared = x.table[:1].expand(3, -1)
+    with pytest.raises(ValueError, match="page_table"):
+        rt.KvCache(x.k, x.v, shared)
+    x.table = shared.contiguous()
+    ws = rt.AttendWorkspace(4, 2, 64, x.dtype)
+    rt.retrace_attend(x.q, x.cache(rt), x.cache_len, x.out, ws, q_start=x.q_start)
+    want, spread = ref.attend(f64(x.q), f64(x.k), f64(x.v), x.table.cpu().numpy(), x.starts, x.cached, 0.125)
+    assert np.all(np.abs(f64(x.out) - want) <= 2e-5 * spread) and ws.check() == 0
+
+
+def test_tables_with_rows_apart(rt):
+    """A part of a wider table, and a single row of any stride."""
+    for lens in ([(2, 60), (1, 31), (5, 0)], [(3, 40)]):
+        x = Batch(lens, 4, 2, 64, 16, torch.float32, seed=2)
+        wide = torch.full((len(lens), x.table.shape[1] + 3), 10**6, dtype=torch.int32, device="cuda")
+        wide[:, 1:-2] = x.table
+        tables = [wide[:, 1:-2]]
+        if len(lens) == 1:
+            tables.append(x.table.as_strided(x.table.shape, (0, 1)))
+        for table in tables:
+            x.table = table
+            ws = rt.AttendWorkspace(4, 2, 64, x.dtype)
+            rt.retrace_attend(x.q, x.cache(rt), x.cache_len, x.out, ws, q_start=x.q_start)
+            want, spread = ref.attend(f64(x.q), f64(x.k), f64(x.v), x.table.cpu().numpy(), x.starts, x.cached, 0.125)
+            assert np.all(np.abs(f64(x.out) - want) <= 2e-5 * spread) and ws.check() == 0
