@@ -452,7 +452,7 @@ struct ClusterShared {
   u64 part[kWarps];
   float wtop[kWarps];
   int bin[2];
-  float before, upto;
+  u64 before, upto;
   int entries;  // of the list that are kept
   // written by this CTA, read by the others of the cluster
   float top;
@@ -712,51 +712,41 @@ __device__ __forceinline__ void sample_by(const SampleArgs& a, int C, ClusterSha
   };
   // Of a histogram over the cluster (sm.count): the first bin at which the running sum
   // reaches `lo` (positive), the first at which it reaches `hi` (the last bin where none
-  // does), and what is before the former; the histogram is cleared.  In fp32, which holds
-  // counts of at most 2^24 exactly (fp64 would take several times as long here).
+  // does), and what is before the former; the histogram is cleared.  In whole numbers: a bin
+  // has one thread that finds it, and every CTA of a cluster finds the same, as its barriers
+  // further on need.
   struct Bins {
     int x, y;
-    float before, inside;  // of bin x; of bins x to y
+    u64 before, inside;  // of bin x; of bins x to y
   };
-  auto find_bins = [&](int bins, float lo, float hi) {
+  auto find_bins = [&](int bins, u64 lo, u64 hi) {
     if (tid < 2) sm.bin[tid] = bins - 1;
-    if (tid == 0) sm.before = sm.upto = 0.f;
+    if (tid == 0) sm.before = sm.upto = 0;
     sync();
     // thread t sums bins 4t to 4t + 3 over the CTAs
-    float x[4] = {0.f, 0.f, 0.f, 0.f};
+    u64 x[4] = {0, 0, 0, 0};
     if (4 * tid < bins) {
 #pragma unroll
       for (int c = 0; c < kMaxCluster; ++c) {
         if (c >= C) break;
         const float4 y = many ? ld_cluster_f4(remote(&sm.count[4 * tid], c)) : *reinterpret_cast<const float4*>(&sm.count[4 * tid]);
-        x[0] += (float)__float_as_uint(y.x);
-        x[1] += (float)__float_as_uint(y.y);
-        x[2] += (float)__float_as_uint(y.z);
-        x[3] += (float)__float_as_uint(y.w);
+        x[0] += __float_as_uint(y.x);
+        x[1] += __float_as_uint(y.y);
+        x[2] += __float_as_uint(y.z);
+        x[3] += __float_as_uint(y.w);
       }
     }
-    const float mine = (x[0] + x[1]) + (x[2] + x[3]);
-    float upto = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const float y = __shfl_up_sync(0xFFFFFFFFu, upto, o);
-      if (lane >= o) upto += y;
-    }
-    if (lane == 31) sm.wtop[warp] = upto;
-    __syncthreads();
-    float before = upto - mine;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w)
-      if (w < warp) before += sm.wtop[w];
+    u64 all;
+    u64 before = block_scan((x[0] + x[1]) + (x[2] + x[3]), sm.part, &all);
     if (4 * tid < bins) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if (before < lo && before + x[i] >= lo) {
-          atomicMin(&sm.bin[0], 4 * tid + i);
+          sm.bin[0] = 4 * tid + i;
           sm.before = before;
         }
         if (before < hi && before + x[i] >= hi) {
-          atomicMin(&sm.bin[1], 4 * tid + i);
+          sm.bin[1] = 4 * tid + i;
           sm.upto = before + x[i];
         }
         before += x[i];
@@ -764,7 +754,7 @@ __device__ __forceinline__ void sample_by(const SampleArgs& a, int C, ClusterSha
     }
     sync();  // every CTA has read the histograms
     if (4 * tid < kFineBins) *reinterpret_cast<uint4*>(&sm.count[4 * tid]) = make_uint4(0u, 0u, 0u, 0u);
-    const Bins found{sm.bin[0], sm.bin[1], sm.before, sm.upto - sm.before};
+    const Bins found{sm.bin[0], sm.bin[1], sm.before, sm.upto > sm.before ? sm.upto - sm.before : 0};
     __syncthreads();
     return found;
   };
@@ -855,7 +845,7 @@ __device__ __forceinline__ void sample_by(const SampleArgs& a, int C, ClusterSha
       }
     });
     const float want = (float)(by_k ? f.top_k : kListTopP) * share;
-    const float reach = f.top_k == 1 ? 1.f : want + 4.f * sqrtf(want) + 4.f;
+    const u64 reach = f.top_k == 1 ? 1 : (u64)ceilf(want + 4.f * sqrtf(want) + 4.f);
     const int bin = find_bins(kBins, reach, reach).x;
     floor = fmaxf(kLowest, top - (bin < kBins - 1 ? (float)(bin + 1) : kBins + 1.f) / row.ys);
   } else {
@@ -956,27 +946,28 @@ __device__ __forceinline__ void sample_by(const SampleArgs& a, int C, ClusterSha
     // The histograms hold counts, or masses without their low bits, so that they fit 32:
     // what these lack is at most a bit per token, far below the slack.
     const int bits = 64 - __clzll((long long)whole), low = !counts && bits > 32 ? bits - 32 : 0;
-    const float unit = 1.f / (float)(1ull << low), goal = (float)target * unit, slack = counts ? 0.f : 1e-3f * goal + 1.f;
+    const u64 goal = (target + (1ull << low) - 1) >> low, slack = counts ? 0 : goal / 1024 + 1;
+    auto from_goal = [&](u64 goal) { return goal > slack ? goal - slack : 1; };
     constexpr float kSplit = (float)(kFineBins / kBins);
     each([&](float v, int i) {
       const float y = row.depth(v) * kSplit;
       const uint32_t w = counts ? 1u : row.mass(v) >> low;
       if (y < (float)kFineBins && in(v, i)) atomicAdd(&sm.count[(int)y], w);
     });
-    const Bins coarse = find_bins(kFineBins, fmaxf(goal - slack, 0.5f), goal + slack);
+    const Bins coarse = find_bins(kFineBins, from_goal(goal), goal + slack);
     float lo = (float)coarse.x / kSplit, hi = (float)(coarse.y + 1) / kSplit;
     // About how many tokens these bins hold, from their mass and the weight there: where that
     // is more than the list takes, a second histogram within them.
-    const float each_w = counts ? 1.f : fmaxf(1.f, kUnit * unit * expf(-hi / kBinsPerNat));
-    if (coarse.inside > each_w * (float)(kList / 2)) {
+    const float each_w = counts ? 1.f : fmaxf(1.f, kUnit / (float)(1ull << low) * expf(-hi / kBinsPerNat));
+    if ((float)coarse.inside > each_w * (float)(kList / 2)) {
       const float from_y = lo, per = (float)kFineBins / (hi - lo) * 0.999f;
       each([&](float v, int i) {
         const float y = row.depth(v);
         const uint32_t w = counts ? 1u : row.mass(v) >> low;
         if (y >= from_y && y < hi && in(v, i)) atomicAdd(&sm.count[(int)((y - from_y) * per)], w);
       });
-      const float left = goal - coarse.before;
-      const Bins fine = find_bins(kFineBins, fmaxf(left - slack, 0.5f), left + slack);
+      const u64 left = goal - min(goal, coarse.before);
+      const Bins fine = find_bins(kFineBins, from_goal(left), left + slack);
       // the bins' limits, moved apart by more than their rounding
       lo = from_y + ((float)fine.x / per) * 0.9999f - 1e-5f * from_y;
       hi = from_y + ((float)(fine.y + 1) / per) * 1.0001f + 1e-5f * from_y;
