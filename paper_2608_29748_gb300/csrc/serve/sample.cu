@@ -717,7 +717,7 @@ __device__ __forceinline__ void sample_by(const SampleArgs& a, int C, ClusterSha
   // further on need.
   struct Bins {
     int x, y;
-    u64 before, inside;  // of bin x; of bins x to y
+    u64 before, inside;  // of bin x; of bins x to y, also where y is the last one
   };
   auto find_bins = [&](int bins, u64 lo, u64 hi) {
     if (tid < 2) sm.bin[tid] = bins - 1;
@@ -754,7 +754,7 @@ __device__ __forceinline__ void sample_by(const SampleArgs& a, int C, ClusterSha
     }
     sync();  // every CTA has read the histograms
     if (4 * tid < kFineBins) *reinterpret_cast<uint4*>(&sm.count[4 * tid]) = make_uint4(0u, 0u, 0u, 0u);
-    const Bins found{sm.bin[0], sm.bin[1], sm.before, sm.upto > sm.before ? sm.upto - sm.before : 0};
+    const Bins found{sm.bin[0], sm.bin[1], sm.before, (sm.bin[1] == bins - 1 ? all : sm.upto) - sm.before};
     __syncthreads();
     return found;
   };
@@ -943,45 +943,58 @@ __device__ __forceinline__ void sample_by(const SampleArgs& a, int C, ClusterSha
     const int from_i = (int)key_index(from);
     auto in = [&](float v, int i) { return v > from_v || (v == from_v && (uint32_t)i <= (uint32_t)from_i); };
     auto metric = [&](float v) -> u64 { return counts ? 1u : row.mass(v); };
-    // The histograms hold counts, or masses without their low bits, so that they fit 32:
-    // what these lack is at most a bit per token, far below the slack.
+    // The histograms hold counts, or masses without their low bits, so that they fit 32: a running
+    // sum lacks less than a unit per token.
     const int bits = 64 - __clzll((long long)whole), low = !counts && bits > 32 ? bits - 32 : 0;
-    const u64 goal = (target + (1ull << low) - 1) >> low, slack = counts ? 0 : goal / 1024 + 1;
-    auto from_goal = [&](u64 goal) { return goal > slack ? goal - slack : 1; };
+    auto place = [&](u64 goal, int low) {
+      const u64 lack = low ? V : 0;
+      goal = (goal + (1ull << low) - 1) >> low;
+      return find_bins(kFineBins, goal > lack ? goal - lack : 1, goal);
+    };
     constexpr float kSplit = (float)(kFineBins / kBins);
     each([&](float v, int i) {
       const float y = row.depth(v) * kSplit;
       const uint32_t w = counts ? 1u : row.mass(v) >> low;
       if (y < (float)kFineBins && in(v, i)) atomicAdd(&sm.count[(int)y], w);
     });
-    const Bins coarse = find_bins(kFineBins, from_goal(goal), goal + slack);
+    const Bins coarse = place(target, low);
     float lo = (float)coarse.x / kSplit, hi = (float)(coarse.y + 1) / kSplit;
     // About how many tokens these bins hold, from their mass and the weight there: where that
-    // is more than the list takes, a second histogram within them.
+    // is more than the list takes, a second histogram within them, in the units that their mass
+    // allows, and the exact sum of what is before them.
+    u64 above = 0;
+    float from_y = 0.f;  // `above` has what is before it
     const float each_w = counts ? 1.f : fmaxf(1.f, kUnit / (float)(1ull << low) * expf(-hi / kBinsPerNat));
     if ((float)coarse.inside > each_w * (float)(kList / 2)) {
-      const float from_y = lo, per = (float)kFineBins / (hi - lo) * 0.999f;
+      const u64 most = coarse.inside + (low ? V : 0);
+      const int less = max(0, 64 - __clzll((long long)most) + low - 32);
+      const float per = (float)kFineBins / (hi - lo) * 0.999f;
+      from_y = lo;
       each([&](float v, int i) {
         const float y = row.depth(v);
-        const uint32_t w = counts ? 1u : row.mass(v) >> low;
-        if (y >= from_y && y < hi && in(v, i)) atomicAdd(&sm.count[(int)((y - from_y) * per)], w);
+        const uint32_t w = counts ? 1u : row.mass(v);
+        above += y < from_y ? w : 0u;
+        if (y >= from_y && y < hi && in(v, i)) atomicAdd(&sm.count[(int)((y - from_y) * per)], w >> less);
       });
-      const u64 left = goal - min(goal, coarse.before);
-      const Bins fine = find_bins(kFineBins, from_goal(left), left + slack);
+      above = cluster_sum(above);
+      const Bins fine = place(target - min(target, above), less);
       // the bins' limits, moved apart by more than their rounding
       lo = from_y + ((float)fine.x / per) * 0.9999f - 1e-5f * from_y;
       hi = from_y + ((float)(fine.y + 1) / per) * 1.0001f + 1e-5f * from_y;
     }
-    u64 above = 0;
+    u64 between = 0;
     if (tid == 0) sm.listed = 0;
     __syncthreads();
     each([&](float v, int i) {
       const float y = row.depth(v);
-      const uint32_t w = counts ? 1u : row.mass(v);
-      above += y < lo ? w : 0u;
-      if (y >= lo && y < hi && i < V && in(v, i)) append(v, i);
+      if (y >= from_y && y < hi) {
+        if (y < lo)
+          between += metric(v);
+        else if (i < V && in(v, i))
+          append(v, i);
+      }
     });
-    above = cluster_sum(above);
+    above += cluster_sum(between);
     const int n = gather_lists();
     if (rank == 0) {
       if (tid == 0) sm.key = 0;
