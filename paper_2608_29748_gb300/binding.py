@@ -389,6 +389,7 @@ def run_round_sampled(x: dict, s: dict, ws: Workspace, out: RoundBuffers | None 
 
 # ---- around the round: paged cache, attention over it, sampling ---------------
 
+_FAR = 2**31 - 1
 _append, _attend, _sample = lib.retrace_kv_append, lib.retrace_attend, lib.retrace_sample
 
 
@@ -517,6 +518,8 @@ def retrace_attend(q, cache: KvCache, cache_len, out, ws: AttendWorkspace, q_sta
             o_last != 1 or not (q.is_cuda and out.is_cuda):
         _refuse_packed(cache, shape[0], (("q", q, None), ("out", out, shape[1])))
     len_ptr, start_ptr = _lengths(cache, cache_len, q_start)
+    if not (0 <= window <= _FAR and 0 <= sinks <= _FAR):  # past 32 bits another number would arrive
+        window, sinks = max(-1, min(window, _FAR)), max(-1, min(sinks, _FAR))
     status = _attend(q.data_ptr(), q_token, q_head, shape[1], start_ptr, len_ptr, cache.B, shape[0],
                      cache.scale if scale is None else scale, window, sinks, causal, cache.ref, out.data_ptr(), o_token, o_head,
                      ws.ptr, ws.nbytes, _stream(stream))

@@ -49,3 +49,19 @@ def test_tables_with_rows_apart(rt):
             rt.retrace_attend(x.q, x.cache(rt), x.cache_len, x.out, ws, q_start=x.q_start)
             want, spread = ref.attend(f64(x.q), f64(x.k), f64(x.v), x.table.cpu().numpy(), x.starts, x.cached, 0.125)
             assert np.all(np.abs(f64(x.out) - want) <= 2e-5 * spread) and ws.check() == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_windows_and_sinks_past_32_bits(rt, dtype):
+    """More than any sequence is long: everything is seen, as with 2^31 - 1."""
+    x = Batch([(2, 300), (9, 40)], 4, 2, 64, 16, dtype, seed=3)
+    ws, cache = rt.AttendWorkspace(4, 2, 64, dtype), x.cache(rt)
+    call = lambda **mask: (rt.retrace_attend(x.q, cache, x.cache_len, x.out, ws, q_start=x.q_start, **mask), x.out.clone())[1]  # noqa: E731
+    want = call()
+    for far in (2**31 - 1, 2**31, 2**32, 2**32 + 7, 2**63 - 1):
+        assert torch.equal(call(window=far), want)
+        assert torch.equal(call(window=5, sinks=far), want)
+    with pytest.raises(rt.RetraceError):
+        call(window=-(2**33))
+    with pytest.raises(rt.RetraceError):
+        call(window=5, sinks=-1)
