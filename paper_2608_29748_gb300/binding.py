@@ -478,6 +478,8 @@ def retrace_kv_append(q, k, v, cache: KvCache, cache_len, rope, q_out=None, q_st
     q_ptr = out_ptr = None
     q_heads = q_token = q_head = o_token = o_head = 0
     if q is not None:
+        if q_out is None:
+            raise ValueError("q needs q_out, which may be q itself")
         shape = q.shape
         q_token, q_head, q_last = q.stride()
         o_token, o_head, o_last = q_out.stride()

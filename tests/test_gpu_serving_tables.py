@@ -65,3 +65,13 @@ def test_windows_and_sinks_past_32_bits(rt, dtype):
         call(window=-(2**33))
     with pytest.raises(rt.RetraceError):
         call(window=5, sinks=-1)
+
+
+def test_queries_without_a_place_to_go(rt):
+    """Refused by name, before anything is enqueued."""
+    x = Batch([(2, 20)], 4, 2, 64, 16, torch.float32, seed=4)
+    before = x.k.clone()
+    with pytest.raises(ValueError, match="q_out"):
+        rt.retrace_kv_append(x.q, x.nk, x.nv, x.cache(rt), x.cache_len, None)
+    torch.cuda.synchronize()
+    assert torch.equal(x.k, before)
