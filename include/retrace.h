@@ -442,7 +442,8 @@ retrace_status retrace_verify_noalloc(const void* logits, retrace_dtype dtype, i
  * memory).  Element (page, slot, head, i) of k and v lies at
  * page*page_stride + slot*slot_stride + head*head_stride + i; position p of
  * sequence b is slot p % page_size of page
- * page_table[b*table_stride + p / page_size].  A page outside [0, num_pages),
+ * page_table[b*table_stride + p / page_size] (rows of the table do not overlap;
+ * sequences may hold the same pages).  A page outside [0, num_pages),
  * or a position beyond max_pages*page_size, means that the position has no
  * place: it is neither written nor attended to. */
 typedef struct {
@@ -480,8 +481,9 @@ retrace_status retrace_kv_append(const void* q, int64_t q_token_stride, int64_t 
                                  int64_t q_out_token_stride, int64_t q_out_head_stride, cudaStream_t stream);
 
 /* Bytes of workspace that retrace_attend needs, whatever the batch (0 for invalid
- * arguments).  A workspace of its own, zeroed once with retrace_workspace_init;
- * retrace_workspace_check reads its status word. */
+ * arguments): room for the parts of every CTA, in bf16 26 MB for heads of up to 64, 51 up to
+ * 128 and 34 above, in fp32 13, 26 and 34.  A workspace of its own, zeroed once with
+ * retrace_workspace_init; retrace_workspace_check reads its status word. */
 size_t retrace_attend_workspace_bytes(int q_heads, int kv_heads, int head_dim, retrace_dtype dtype);
 
 /* Attention of T packed query tokens over the cache (their own keys and values
@@ -490,21 +492,24 @@ size_t retrace_attend_workspace_bytes(int q_heads, int kv_heads, int head_dim, r
  * position p sees position j >= 0 iff
  *     j <= p (causal != 0), or j <= cache_len[b] + n_b - 1 (causal == 0: the
  *     block's n_b tokens see each other both ways, as a drafter's block does), and
- *     window <= 0, or j > p - window, or j < sinks (a sliding window, and the
+ *     window == 0, or j > p - window, or j < sinks (a sliding window, and the
  *     first `sinks` tokens that stay visible), and
  *     j has a place in the cache.
  *   out[t, h] = sum_j softmax_j(scale q.k_j) v_j over the visible j; zero where
  *   nothing is visible.
  * What lies at positions that no token of a sequence sees does not matter (slots
- * never written, pages given away), whatever its bits.
+ * never written, pages given away), whatever its bits.  A position that only some
+ * tokens of a sequence see weighs 0 for the others, and 0 times an infinity or NaN in v is
+ * NaN there: such a value may reach tokens of the same call that do not see it.
+ * Scores may have any size that fp32 holds.
  *   q, out      [T, q_heads, head_dim], strides in elements, head_dim contiguous.
  * bf16: products on tensor cores with fp32 accumulation, the softmax in fp32 with
  * the weights rounded to bf16 before the product with v, out rounded once.  fp32:
  * FFMA throughout.  Tensor cores need head_dim <= 128 a multiple of 8, 16-byte
  * aligned bases and strides, page_size a multiple of 8 and at most 128 query heads
  * per key/value head in whole groups of 8 rows (lcm(8, group) <= 128); other shapes
- * run on FFMA.  head_dim <= 256.  One stream, no host synchronisation; the same
- * inputs on the same device give the same bits. */
+ * run on FFMA, in bf16 with the weights kept in fp32.  head_dim <= 256.  One stream, no
+ * host synchronisation; the same inputs on the same device give the same bits. */
 retrace_status retrace_attend(const void* q, int64_t q_token_stride, int64_t q_head_stride, int q_heads,
                               const int32_t* q_start, const int32_t* cache_len, int B, int T, float scale,
                               int window, int sinks, int causal, const retrace_kv_cache* cache, void* out,
@@ -528,11 +533,20 @@ retrace_status retrace_attend(const void* q, int64_t q_token_stride, int64_t q_h
  *                running sum of the kept probabilities exceeds uniform times their
  *                sum.  -1 if every logit of the row is -inf.
  *   probs        [B, R] fp32 out, optional: the token's probability among the kept
- *                ones (the drafter's q of speculative sampling), 0 with token -1.
+ *                ones, 0 with token -1.
  * A NaN logit counts as -inf; among +inf logits each has the same probability and
  * the others none.  A token's weight is exp((logit - max) / temperature) in
  * fp32, taken to 31 binary places, and the sums are whole numbers, so they do not
- * depend on their order: the same inputs give the same token whatever the batch. */
+ * depend on their order: the same inputs give the same token whatever the batch.
+ * Drafts for retrace_verify_sampled and retrace_round_sampled: those take the drafter's
+ * logits and one setting for all sequences, from which they compute the drafter's
+ * distribution again.  So a draft is drawn as they assume where every sequence has that
+ * temperature (> 0), top_k (1 to 64) and top_p, and min_p is off.  With other settings, or
+ * settings that differ, the drafts come from another distribution than the one they are
+ * verified against, and the committed tokens do not follow the target's.
+ * A row where more than 4096 tokens have the logit at which a filter cuts takes a slow
+ * way (151936 equal logits: 25 ms for top_k or top_p, 50 for both; about twice that for a
+ * thousand rows). */
 retrace_status retrace_sample(const void* logits, retrace_dtype dtype, int B, int R, int V, int64_t row_stride,
                               int64_t batch_stride, const float* uniforms, const float* temperature,
                               const int32_t* top_k, const float* top_p, const float* min_p, int32_t* tokens,

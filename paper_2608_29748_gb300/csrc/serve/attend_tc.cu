@@ -20,7 +20,7 @@
 // tensor core that does 8192 flop a cycle: 1024 of the 2790 cycles that the bytes take
 // at D = 128, so tokens and blocks are bound by HBM, and a row tile that is not full costs
 // nothing: 64 blocks of 17 tokens over up to 8192, 8 heads of 128, 5.5 TB/s (221 us).  Prompts are
-// bound by the chain of products and softmax: four of up to 4096 tokens, 32 heads, 772 TFLOP/s (369 us),
+// bound by the chain of products and softmax: four of up to 4096 tokens, 32 heads, 794 TFLOP/s (359 us),
 // the tensor core busy for about half of the time (a softmax of 128 x 128 is some 2000
 // cycles of its warpgroup, each product 512).  One token over 2048 keys is latency: 18 us with
 // the joining kernel.
@@ -873,8 +873,8 @@ cudaError_t launch(TcParams& p, const DeviceInfo& dev, cudaStream_t stream) {
 }  // namespace
 
 // Every shape that fits, single tokens too, which fill few rows of a tile: 220 of them, 8 heads
-// of 128 over up to 1000 keys 169 us, on the CUDA cores 464; up to 79 keys 75 and 93.  (256
-// tokens, heads of 64 over up to 79 keys: 75 and 63, over up to 250 99 and 144.)
+// of 128 over up to 1000 keys 163 us, on the CUDA cores 464; up to 79 keys 74 and 93.  (256
+// tokens, heads of 64 over up to 79 keys: 71 and 66, over up to 250 95 and 146.)
 bool attend_tc_supported(const AttendArgs& a) {
   const retrace_kv_cache& c = a.cache;
   const int G = a.q_heads / c.kv_heads;
@@ -920,8 +920,8 @@ cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t stream) {
   p.shape.unit_tokens = 2 * p.tile_tokens;
   // Where units of few rows are shared by two or three CTAs, the last one joins the parts
   // and spares a launch; more parts, or larger ones, are read by the whole device in a second
-  // kernel.  Tokens over a window of 1024 keys, 2048 units: 196 us here, 219 with it; 500
-  // keys, 512 units: 47 / 56; one token over 2048 keys, 8 units of nine parts: 21.1 / 18.2.
+  // kernel.  Tokens over a window of 1024 keys, 2048 units: 186 us here, 201 with it; 500
+  // keys, 512 units: 43 / 51; one token over 2048 keys, 8 units of nine parts: 21.0 / 18.2.
   p.join = !a.q_start && (long long)p.shape.uniform * p.group <= kJoinRows && 2ll * a.B * c.kv_heads >= dev.sm_count;
   return c.head_dim <= 64 ? launch<64>(p, dev, stream) : launch<128>(p, dev, stream);
 }

@@ -17,13 +17,18 @@
 // and an exact sum.  Whatever does not fit (thousands of tokens with one logit) goes to
 // sample_row: radix selection over the 32-bit keys of the logits.
 //
-// With many rows a CTA takes one and streams it (Stream), four of them to an SM,
-// and later passes over the row, where needed, find it in L2: 4096 rows are 46 MB at a
-// time.  With few rows a cluster of up to eight CTAs holds one in registers (Held), so
-// that every later pass is arithmetic.
-// 4096 rows of 151936 in bf16 with filters of their own: 287 us, 4.3 TB/s; 16 of them, top-k 20 and
-// top-p: 14 us, all latency.  528 flat rows of 32003 in fp32, top-p 0.98: 146 us, seven
+// With many rows a CTA takes one and streams it (Stream), four of them to an SM.  Where a
+// list suffices the row is read once.  Later passes read it again: 608 rows of 151936 in bf16 are
+// 185 MB at a time, more than L2 holds, and 1024 of them under top-p 0.9 read 1.40 GB for 311 MB
+// of rows, at a sixth of the memory's rate.  With few rows a cluster of up to eight CTAs holds
+// one in registers (Held), so that later passes are arithmetic; of ten bf16 vectors to a thread, as
+// 16 rows of 151936 have, some spill.
+// 4096 rows of 151936 in bf16 with filters of their own: 288 us, 4.3 TB/s; 16 of them, top-k 20 and
+// top-p: 14 us, all latency.  528 flat rows of 32003 in fp32, top-p 0.98: 136 us, seven
 // passes of about 25 instructions and an exponential a logit.
+// More than 4096 tokens with the deciding logit (sample_row): an atomic a token and digit, nearly all on
+// one address; 151936 equal logits take 25 ms for top-k or top-p and 50 for both, a thousand such
+// rows 53 and 103.
 #include <math.h>
 
 #include <type_traits>
@@ -64,7 +69,7 @@ __device__ __forceinline__ float weight(float x, float top, float inv_t) {
 }
 __device__ __forceinline__ uint32_t whole_weight(float e) { return __float2uint_rn(e * kUnit); }
 
-// x n for a float x in [0, 1] and n < 2^53, rounded to 53 bits as their product in fp64
+// x n for a float x in [0, 1] and n <= 2^55 (2^24 weights of 2^31), rounded to 53 bits as their product in fp64
 // is, in whole numbers (fp64 arithmetic is slow here): its floor, or its ceiling.
 __device__ __forceinline__ u64 scaled(float x, u64 n, bool up) {
   const uint32_t bits = __float_as_uint(x);
@@ -76,7 +81,7 @@ __device__ __forceinline__ u64 scaled(float x, u64 n, bool up) {
   // to 53 bits, nearest, ties to even
   const int length = hi ? 128 - __clzll((long long)hi) : 64 - __clzll((long long)lo);
   if (length > 53) {
-    const int cut = length - 53;  // at most 24
+    const int cut = length - 53;  // at most 27
     const u64 rest = lo & ((1ull << cut) - 1), half = 1ull << (cut - 1);
     lo = lo >> cut | hi << (64 - cut);
     lo += rest > half || (rest == half && (lo & 1));
@@ -97,7 +102,8 @@ __device__ __forceinline__ u64 top_p_target(float p, u64 total) {
   const u64 want = p > 0.f ? scaled(p, total, true) : 0;
   return want < 1 ? 1 : want;
 }
-// e of a weight among the sum of whole weights.
+// e of a weight among the sum of whole weights; the sum rounded to fp32, which moves the result by
+// no more than its own rounding.
 __device__ __forceinline__ float probability(float e, u64 sum) { return __fdiv_rn(e * kUnit, (float)sum); }
 
 template <typename T>
@@ -1199,7 +1205,8 @@ cudaError_t launch_typed(const SampleArgs& a, cudaStream_t stream) {
   // Two of its CTAs fit an SM: with one, 15 clusters of eight find room, and 16 rows of
   // 151936 took 24.0 us, as two rounds of 12.9, where they take 14.1; streamed 18.7.
   // One row: 12.9, streamed 18.2; 64 rows of 20000: 10.9 in clusters of two, streamed 12.2;
-  // 144: 9.5 and 12.5.
+  // 144: 9.5 and 12.5.  From 20 rows of 151936 on, clusters of four would need more than ten vectors to a
+  // thread, and rows are streamed: 19 rows 15.2, 20 19.1, 64 19.3, 128 24.6, 256 30.6.
   int C = 1;
   while (C < kMaxCluster && need(C) > 1 && rows * C * 2 <= dev.sm_count) C *= 2;
   const int n = need(C);
