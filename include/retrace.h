@@ -97,7 +97,11 @@ typedef enum {
   RETRACE_ERR_DEVICE = 5       /* a kernel reported a bounded-wait expiry        */
 } retrace_status;
 
-typedef enum { RETRACE_F32 = 0, RETRACE_BF16 = 1 } retrace_dtype;
+typedef enum {
+  RETRACE_F32 = 0,
+  RETRACE_BF16 = 1,
+  RETRACE_E4M3 = 2 /* 8-bit floating point, of a cache alone (retrace_kv_cache_fp8) */
+} retrace_dtype;
 
 /* Thread-local, NUL-terminated description of the last non-OK status returned
  * on this thread ("" if none).  Owned by the library; valid until the next call
@@ -551,6 +555,93 @@ retrace_status retrace_sample(const void* logits, retrace_dtype dtype, int B, in
                               int64_t batch_stride, const float* uniforms, const float* temperature,
                               const int32_t* top_k, const float* top_p, const float* min_p, int32_t* tokens,
                               float* probs, cudaStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * The cache in 8 bits, and its pages.
+ * ------------------------------------------------------------------------- */
+
+/* A paged cache of 8-bit floating-point numbers with a power of two for each page
+ * and head: element (page, slot, head, i) of k stands for
+ *     e4m3(k element) * 2^k_exp[page*exp_page_stride + head*exp_head_stride],
+ * and v likewise.  (e4m3: 4 bits of exponent, 3 of mantissa, largest value 448, no
+ * infinity.)  Exponents outside [-40, 40] are taken as the nearest end.
+ * pages.dtype is RETRACE_E4M3, its strides count elements, that is bytes.  A page is the block that
+ * shares a scale; scales are powers of two because e4m3 is a floating format: a finer
+ * scale would win less than one bit of range, and rescaling what a page holds is exact
+ * down to 2^-9 of its unit. */
+typedef struct {
+  retrace_kv_cache pages;
+  int8_t* k_exp; /* [num_pages, kv_heads] */
+  int8_t* v_exp;
+  int64_t exp_page_stride, exp_head_stride; /* elements, the same for k and v */
+} retrace_kv_cache_fp8;
+
+/* retrace_kv_append into a cache in 8 bits.  q, k, v, q_out are `dtype` (BF16 or F32); the
+ * rotation is that of retrace_kv_append, in fp32, each product rounded before the sum,
+ * and q_out is rounded once.  For each page that the call writes, each head, and k and v
+ * apart:
+ *     a  = the largest magnitude among the call's rotated tokens in that page (NaN does
+ *          not count), e = the least exponent in [-40, 40] with a <= 448 * 2^e;
+ *     if the first slot that the call writes is slot 0, the page's exponent becomes e;
+ *     else it becomes max(e, the one before), and if that raised it, the slots before the
+ *     first written one are rounded to the new unit (to the nearest, ties to even: exact
+ *     for what is at least 2^-6 of it then);
+ *     the tokens are rounded once from fp32, to the nearest, ties to even; magnitudes
+ *     beyond 448 * 2^e (infinities, or e = 40) become the largest one, NaN stays NaN.
+ * Slots behind the last token are left as they are; whatever they held is in another
+ * unit after the exponent changed.  So a rejected token with large values costs its page at most
+ * low bits of small values, until the page's slot 0 is written again.  Each page that the call writes
+ * belongs to one sequence, once: what two places of the table that write the same page
+ * leave there is not specified.  Tokens without a place, or beyond the angles, are treated as in
+ * retrace_kv_append and count nowhere.  One launch. */
+retrace_status retrace_kv_append_fp8(const void* q, int64_t q_token_stride, int64_t q_head_stride, int q_heads,
+                                     const void* k, int64_t k_token_stride, int64_t k_head_stride, const void* v,
+                                     int64_t v_token_stride, int64_t v_head_stride, retrace_dtype dtype,
+                                     const int32_t* q_start, const int32_t* cache_len, int B, int T, const float* rope,
+                                     int rope_positions, int rot, int interleaved, const retrace_kv_cache_fp8* cache,
+                                     void* q_out, int64_t q_out_token_stride, int64_t q_out_head_stride,
+                                     cudaStream_t stream);
+
+/* retrace_attend over a cache in 8 bits: the same definition, with k and v the values
+ * that the cache stands for; q and out are `dtype` (BF16 or F32).  The workspace is that of
+ * retrace_attend_workspace_bytes(q_heads, kv_heads, head_dim, RETRACE_E4M3), whatever
+ * `dtype`.  FFMA throughout, with the weights kept in fp32.  A NaN in v at a position that only some tokens of
+ * a call see may reach the others, as in retrace_attend. */
+retrace_status retrace_attend_fp8(const void* q, int64_t q_token_stride, int64_t q_head_stride, int q_heads,
+                                  retrace_dtype dtype, const int32_t* q_start, const int32_t* cache_len, int B, int T,
+                                  float scale, int window, int sinks, int causal, const retrace_kv_cache_fp8* cache,
+                                  void* out, int64_t out_token_stride, int64_t out_head_stride, void* ws,
+                                  size_t ws_bytes, cudaStream_t stream);
+
+/* Gives each sequence of a batch the pages that its tokens need, takes back those that
+ * it no longer needs, and lists where the new tokens go: what a decoding loop does
+ * before a block (new_len: the block's tokens) and after its round (cache_len: the
+ * committed tokens, new_len 0), or for a finished sequence (both 0), without the host.
+ *   cache_len, new_len  [B] int32: tokens in the cache, and to come (a negative new_len counts
+ *                as 0).  Sequence b needs ceil(min(cache_len + new_len, max_pages *
+ *                page_size) / page_size) pages, none if that is negative.
+ *   page_table   [B, max_pages] in and out, held [B] in and out: the first held[b] entries of
+ *                row b are its pages, which no other row holds.  New pages go behind them; the
+ *                entries of pages given back become -1; others are left as they are.
+ *   free_pages   [num_pages] in and out, a stack: entries 0 .. counts[0]-1 are the free
+ *                pages.  In the order of the sequences, and of the places in a row, pages are
+ *                taken from the top downwards; then the pages given back are put on top so
+ *                that the first of them lies uppermost (what is given back can be
+ *                taken in the same order from the next call on).
+ *   counts       [2] in and out: free pages; out: pages that this call lacked.  Where the
+ *                stack is empty, the entries that lack a page become -1, held counts
+ *                those that the row got, and a later call tries again.
+ *   q_start      [B+1] out: where each sequence's new tokens start among all (at most T),
+ *                as the other calls take it.  May be NULL if slots is.
+ *   slots        [T] int64 out, optional: page * page_size + slot of each new token's
+ *                position, -1 where it has no place, and behind the last sequence's
+ *                tokens.
+ * page_table, held and free_pages hold what a call leaves there; other values give
+ * unspecified ones, within the arrays.  T is not read without slots and q_start. */
+retrace_status retrace_kv_reserve(const int32_t* cache_len, const int32_t* new_len, int B, int page_size,
+                                  int32_t* page_table, int64_t table_stride, int max_pages, int32_t* held,
+                                  int32_t* free_pages, int num_pages, int32_t* counts, int32_t* q_start, int64_t* slots,
+                                  int T, cudaStream_t stream);
 
 #ifdef __cplusplus
 }

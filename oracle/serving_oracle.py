@@ -1,5 +1,6 @@
 """Float64 CPU statement of the operators around a round: appending to a paged
-cache with the position rotation, attention over that cache, and sampling.
+cache with the position rotation, attention over that cache, and sampling; the cache in 8 bits
+and the pages of a batch.
 
 Written from their definitions, token by token; it shares no code with the CUDA
 path.  Caches are [pages, page_size, kv_heads, head_dim], a position p of
@@ -111,3 +112,84 @@ def sample(x, u, temperature, top_k, top_p, min_p):
     run = np.cumsum(probs[by_index])
     at = min(int(np.searchsorted(run, u, side="right")), tokens.size - 1)
     return int(tokens[by_index[at]]), float(probs[by_index[at]])
+
+
+def e4m3(x):
+    """The e4m3 number nearest to each x, of two equally near ones the even one; beyond 448 the largest."""
+    x = np.array(x, np.float64)
+    _, e = np.frexp(np.where(np.isfinite(x), x, 0.0))
+    step = np.exp2(np.maximum(e - 1, -6) - 3.0)
+    return np.clip(np.rint(x / step) * step, -448.0, 448.0)
+
+
+def page_exponent(x):
+    """The least e in [-40, 40] with max |x| <= 448 * 2 ** e (NaN does not count)."""
+    a = np.abs(np.asarray(x, np.float64))
+    a = float(np.max(np.where(np.isnan(a), 0.0, a), initial=0.0))
+    e = -40
+    while e < 40 and a > 448.0 * 2.0**e:
+        e += 1
+    return e
+
+
+def append_fp8(q, k, v, k_codes, v_codes, k_exp, v_exp, table, starts, cache_len, rope, interleaved,
+               rounded=True):
+    """(q_out, k_codes, v_codes, k_exp, v_exp) after the append.  Codes are e4m3 numbers as float64; not `rounded`:
+    those of the new tokens as they are before their rounding."""
+    codes = [np.array(x, np.float64) for x in (k_codes, v_codes)]
+    exps = [np.array(x, np.int64) for x in (k_exp, v_exp)]
+    qo = np.zeros(q.shape)
+    pages, size = codes[0].shape[:2]
+    for b in range(len(cache_len)):
+        written = {}  # page: [(slot, token)]
+        rows = {}
+        for t in range(starts[b], starts[b + 1]):
+            p = int(cache_len[b]) + t - starts[b]
+            if p < 0 or (rope is not None and p >= rope.shape[0]):
+                continue
+            cs = np.zeros((0, 2)) if rope is None else rope[p]
+            qo[t] = [rotate(x, cs, interleaved) for x in q[t]]
+            rows[t] = (np.array([rotate(x, cs, interleaved) for x in k[t]]), np.array(v[t], np.float64))
+            at = place(table, pages, size, b, p)
+            if at is not None:
+                written.setdefault(at[0], []).append((at[1], t))
+        for page, tokens in written.items():
+            first = min(slot for slot, _ in tokens)
+            for i in range(2):
+                for h in range(k.shape[1]):
+                    e = page_exponent([rows[t][i][h] for _, t in tokens])
+                    if first > 0:
+                        old = min(max(int(exps[i][page, h]), -40), 40)
+                        e = max(e, old)
+                        if e > old:
+                            codes[i][page, :first, h] = e4m3(codes[i][page, :first, h] * 2.0 ** (old - e))
+                    for slot, t in tokens:
+                        x = rows[t][i][h] * 2.0**-e
+                        codes[i][page, slot, h] = e4m3(x) if rounded else x
+                    exps[i][page, h] = e
+    return qo, *codes, *exps
+
+
+def reserve(cache_len, new_len, page_size, table, held, free, tokens):
+    """(table, held, free, missing, starts, slots) after a call; `free` is a list whose end is the top, `tokens` the
+    length of slots."""
+    table, held, free = np.array(table), list(held), list(free)
+    missing, given, starts, slots = 0, [], [0], []
+    for b, (c, n) in enumerate(zip(cache_len, new_len)):
+        n = max(int(n), 0)
+        need = -(-min(max(int(c) + n, 0), table.shape[1] * page_size) // page_size)
+        given += table[b, need:held[b]].tolist()
+        table[b, need:held[b]] = -1
+        held[b] = min(held[b], need)
+        for i in range(held[b], need):
+            if free:
+                table[b, i] = free.pop()
+                held[b] = i + 1
+            else:
+                table[b, i] = -1
+                missing += 1
+        for i in range(n):
+            at = place(table, 1 << 31, page_size, b, int(c) + i)
+            slots.append(-1 if at is None else at[0] * page_size + at[1])
+        starts.append(min(starts[-1] + n, tokens))
+    return table, held, free + given[::-1], missing, starts, (slots + [-1] * tokens)[:tokens]

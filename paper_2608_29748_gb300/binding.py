@@ -17,6 +17,7 @@ from . import build as _build
 
 RETRACE_F32 = 0
 RETRACE_BF16 = 1
+RETRACE_E4M3 = 2
 
 _STATUS = {
     0: "RETRACE_OK",
@@ -67,7 +68,11 @@ def _load() -> ctypes.CDLL:
     lib.retrace_attend_workspace_bytes.restype = SZ
     lib.retrace_attend.argtypes = [P, I64, I64, I, P, P, I, I, F, I, I, I, P, P, I64, I64, P, SZ, P]
     lib.retrace_sample.argtypes = [P, I, I, I, I, I64, I64, P, P, P, P, P, P, P, P]
+    lib.retrace_kv_append_fp8.argtypes = [P, I64, I64, I, P, I64, I64, P, I64, I64, I, P, P, I, I, P, I, I, I, P, P, I64, I64, P]
+    lib.retrace_attend_fp8.argtypes = [P, I64, I64, I, I, P, P, I, I, F, I, I, I, P, P, I64, I64, P, SZ, P]
+    lib.retrace_kv_reserve.argtypes = [P, P, I, I, P, I64, I, P, P, I, P, P, P, I, P]
     for name in ("retrace_kv_append", "retrace_attend", "retrace_sample",
+                 "retrace_kv_append_fp8", "retrace_attend_fp8", "retrace_kv_reserve",
                  "retrace_workspace_init", "retrace_workspace_check", "retrace_verify",
                  "retrace_align_refine", "retrace_gate_fuse", "retrace_round", "retrace_round_lowrank",
                  "retrace_verify_sampled", "retrace_round_sampled", "retrace_wait_selftest",
@@ -390,7 +395,9 @@ def run_round_sampled(x: dict, s: dict, ws: Workspace, out: RoundBuffers | None 
 # ---- around the round: paged cache, attention over it, sampling ---------------
 
 _FAR = 2**31 - 1
+_E4M3 = torch.float8_e4m3fn
 _append, _attend, _sample = lib.retrace_kv_append, lib.retrace_attend, lib.retrace_sample
+_append_fp8, _attend_fp8, _reserve = lib.retrace_kv_append_fp8, lib.retrace_attend_fp8, lib.retrace_kv_reserve
 
 
 class _KvCacheStruct(ctypes.Structure):  # retrace_kv_cache (include/retrace.h)
@@ -399,6 +406,16 @@ class _KvCacheStruct(ctypes.Structure):  # retrace_kv_cache (include/retrace.h)
                 ("page_size", ctypes.c_int), ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
                 ("page_table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("max_pages", ctypes.c_int),
                 ("dtype", ctypes.c_int)]
+
+
+def _page_rows(page_table):
+    _int32(page_table, "page_table")
+    if page_table.dim() != 2 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+        raise ValueError("page_table must be [B, max_pages], the pages of a sequence contiguous")
+    # a row of the table begins where the one before has ended (the stride of one row is not used)
+    if page_table.shape[0] > 1 and page_table.stride(0) < page_table.shape[1]:
+        raise ValueError("the rows of page_table must not share storage: an expanded table needs .contiguous()")
+    return max(page_table.stride(0), page_table.shape[1])
 
 
 class KvCache:
@@ -410,34 +427,62 @@ class KvCache:
     def __init__(self, k, v, page_table):
         if k.dim() != 4 or v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype or k.stride(3) != 1:
             raise ValueError("k and v must be [pages, page_size, kv_heads, head_dim] of one dtype and layout, head_dim contiguous")
-        _int32(page_table, "page_table")
-        if page_table.dim() != 2 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
-            raise ValueError("page_table must be [B, max_pages], the pages of a sequence contiguous")
-        # a row of the table begins where the one before has ended (the stride of one row is not used)
-        if page_table.shape[0] > 1 and page_table.stride(0) < page_table.shape[1]:
-            raise ValueError("the rows of page_table must not share storage: an expanded table needs .contiguous()")
+        table_stride = _page_rows(page_table)
         self.k, self.v, self.page_table = k, v, page_table
         self.B, self.kv_heads, self.head_dim, self.dtype = page_table.shape[0], k.shape[2], k.shape[3], k.dtype
         self.struct = _KvCacheStruct(_ptr(k), _ptr(v), k.stride(0), k.stride(1), k.stride(2), k.shape[0], k.shape[1],
-                                     k.shape[2], k.shape[3], _ptr(page_table), max(page_table.stride(0), page_table.shape[1]),
-                                     page_table.shape[1], _dtype_code(k))
+                                     k.shape[2], k.shape[3], _ptr(page_table), table_stride, page_table.shape[1], self._code(k))
         self.ref = ctypes.addressof(self.struct)
         self.scale = self.head_dim**-0.5
         self.shape_B, self.shape_B1, self.shape_token = (self.B,), (self.B + 1,), (self.kv_heads, self.head_dim)
+
+    @staticmethod
+    def _code(k):
+        return _dtype_code(k)
+
+
+class _KvCacheFp8Struct(ctypes.Structure):  # retrace_kv_cache_fp8 (include/retrace.h)
+    _fields_ = [("pages", _KvCacheStruct), ("k_exp", ctypes.c_void_p), ("v_exp", ctypes.c_void_p),
+                ("exp_page_stride", ctypes.c_int64), ("exp_head_stride", ctypes.c_int64)]
+
+
+class KvCacheFp8(KvCache):
+    """A paged cache in 8 bits: k and v as KvCache takes them, of torch.float8_e4m3fn, and k_exp and
+    v_exp [num_pages, kv_heads] int8 (any strides, the same for both): an element stands for its value
+    times 2 ** exp of its page and head (see include/retrace.h)."""
+
+    def __init__(self, k, v, page_table, k_exp, v_exp):
+        super().__init__(k, v, page_table)
+        if k_exp.dtype != torch.int8 or v_exp.dtype != torch.int8 or k_exp.shape != (k.shape[0], k.shape[2]) or \
+                v_exp.shape != k_exp.shape or v_exp.stride() != k_exp.stride() or \
+                any(n > 1 and x == 0 for n, x in zip(k_exp.shape, k_exp.stride())):
+            raise ValueError(f"k_exp and v_exp must be int8 [{k.shape[0]}, {k.shape[2]}] of one layout, not expanded: a power of two for each "
+                             "page and head")
+        self.k_exp, self.v_exp = k_exp, v_exp
+        self.struct = _KvCacheFp8Struct(self.struct, _ptr(k_exp), _ptr(v_exp), k_exp.stride(0), k_exp.stride(1))
+        self.ref = ctypes.addressof(self.struct)
+
+    @staticmethod
+    def _code(k):
+        if k.dtype != _E4M3:
+            raise TypeError(f"a cache in 8 bits is torch.float8_e4m3fn, not {k.dtype}")
+        return RETRACE_E4M3
 
 
 # The checks below run on every call of a decoding loop whose kernels take a few
 # microseconds, so each is one comparison on the way that is taken, and what
 # exactly is wrong is worked out after one of them fails.
-def _refuse_packed(cache, T, tensors):
+def _refuse_packed(cache, T, tensors, dtype=None):
+    whose = "the cache's dtype" if dtype is None else f"{dtype}"
+    dtype = cache.dtype if dtype is None else dtype
     for name, t, heads in tensors:
         if t is None:
             continue
         if not t.is_cuda:
             raise ValueError("libretrace takes CUDA tensors")
-        if t.dim() != 3 or t.shape[0] != T or t.shape[2] != cache.head_dim or t.dtype != cache.dtype or \
+        if t.dim() != 3 or t.shape[0] != T or t.shape[2] != cache.head_dim or t.dtype != dtype or \
                 (heads is not None and t.shape[1] != heads):
-            raise ValueError(f"{name} must be [{T}, {heads or 'heads'}, {cache.head_dim}] of the cache's dtype")
+            raise ValueError(f"{name} must be [{T}, {heads or 'heads'}, {cache.head_dim}] of {whose}")
         if t.stride(2) != 1:
             raise ValueError(f"{name}: head_dim must be contiguous")
 
@@ -502,10 +547,11 @@ def retrace_kv_append(q, k, v, cache: KvCache, cache_len, rope, q_out=None, q_st
 
 
 class AttendWorkspace(Workspace):
-    """Workspace of retrace_attend: one serves every call of these head counts and size."""
+    """Workspace of retrace_attend and retrace_attend_fp8: one serves every call of these head counts and size.
+    dtype: the cache's (torch.float8_e4m3fn for a cache in 8 bits, whatever the queries are)."""
 
     def __init__(self, q_heads, kv_heads, head_dim, dtype, device=None, stream=None):
-        code = RETRACE_BF16 if dtype == torch.bfloat16 else RETRACE_F32
+        code = RETRACE_BF16 if dtype == torch.bfloat16 else RETRACE_E4M3 if dtype == _E4M3 else RETRACE_F32
         self._allocate(int(lib.retrace_attend_workspace_bytes(q_heads, kv_heads, head_dim, code)), device, stream)
 
 
@@ -549,5 +595,119 @@ def retrace_sample(logits, uniforms, tokens, probs=None, temperature=None, top_k
                      _setting(temperature, each, f32, "temperature"), _setting(top_k, each, i32, "top_k"),
                      _setting(top_p, each, f32, "top_p"), _setting(min_p, each, f32, "min_p"),
                      _setting(tokens, rows, i32, "tokens"), _setting(probs, rows, f32, "probs"), _stream(stream))
+    if status:
+        _check(status)
+
+
+# ---- the cache in 8 bits, and its pages -----------------------------------------
+
+def retrace_kv_append_fp8(q, k, v, cache: KvCacheFp8, cache_len, rope, q_out=None, q_start=None, interleaved=False, stream=None):
+    """retrace_kv_append into a cache in 8 bits; q, k, v and q_out are all bf16 or all fp32 (see
+    include/retrace.h)."""
+    if cache.dtype != _E4M3:
+        raise TypeError("retrace_kv_append_fp8 takes a KvCacheFp8")
+    shape, dtype = k.shape, k.dtype
+    T = shape[0]
+    k_token, k_head, k_last = k.stride()
+    v_token, v_head, v_last = v.stride()
+    if shape[1:] != cache.shape_token or v.shape != shape or k.dtype != dtype or v.dtype != dtype or k_last != 1 or v_last != 1 or \
+            not (k.is_cuda and v.is_cuda):
+        _refuse_packed(cache, T, (("k", k, cache.kv_heads), ("v", v, cache.kv_heads)), dtype)
+    q_ptr = out_ptr = None
+    q_heads = q_token = q_head = o_token = o_head = 0
+    if q is not None:
+        if q_out is None:
+            raise ValueError("q needs q_out, which may be q itself")
+        shape = q.shape
+        q_token, q_head, q_last = q.stride()
+        o_token, o_head, o_last = q_out.stride()
+        if shape[0] != T or shape[2] != cache.head_dim or q_out.shape != shape or q.dtype != dtype or q_out.dtype != dtype or \
+                q_last != 1 or o_last != 1 or not (q.is_cuda and q_out.is_cuda):
+            _refuse_packed(cache, T, (("q", q, None), ("q_out", q_out, q.shape[1])), dtype)
+        q_heads, q_ptr, out_ptr = shape[1], q.data_ptr(), q_out.data_ptr()
+    positions = rot = 0
+    rope_ptr = None
+    if rope is not None:
+        if rope.dtype != torch.float32 or rope.dim() != 3 or rope.shape[2] != 2 or not rope.is_contiguous() or not rope.is_cuda:
+            raise ValueError("rope must be a contiguous float32 [positions, rot/2, 2] on the GPU")
+        positions, half, _ = rope.shape
+        rot, rope_ptr = 2 * half, rope.data_ptr()
+    len_ptr, start_ptr = _lengths(cache, cache_len, q_start)
+    status = _append_fp8(q_ptr, q_token, q_head, q_heads, k.data_ptr(), k_token, k_head, v.data_ptr(), v_token, v_head, _dtype_code(k),
+                         start_ptr, len_ptr, cache.B, T, rope_ptr, positions, rot, interleaved, cache.ref, out_ptr, o_token, o_head,
+                         _stream(stream))
+    if status:
+        _check(status)
+
+
+def retrace_attend_fp8(q, cache: KvCacheFp8, cache_len, out, ws: AttendWorkspace, q_start=None, scale=None, window=0, sinks=0,
+                       causal=True, stream=None):
+    """retrace_attend over a cache in 8 bits; q and out are both bf16 or both fp32, the workspace is one for
+    torch.float8_e4m3fn (see include/retrace.h)."""
+    if cache.dtype != _E4M3:
+        raise TypeError("retrace_attend_fp8 takes a KvCacheFp8")
+    shape, dtype = q.shape, q.dtype
+    q_token, q_head, q_last = q.stride()
+    o_token, o_head, o_last = out.stride()
+    if shape[2] != cache.head_dim or out.shape != shape or out.dtype != dtype or q_last != 1 or \
+            o_last != 1 or not (q.is_cuda and out.is_cuda):
+        _refuse_packed(cache, shape[0], (("q", q, None), ("out", out, shape[1])), dtype)
+    len_ptr, start_ptr = _lengths(cache, cache_len, q_start)
+    if not (0 <= window <= _FAR and 0 <= sinks <= _FAR):  # past 32 bits another number would arrive
+        window, sinks = max(-1, min(window, _FAR)), max(-1, min(sinks, _FAR))
+    status = _attend_fp8(q.data_ptr(), q_token, q_head, shape[1], _dtype_code(q), start_ptr, len_ptr, cache.B, shape[0],
+                         cache.scale if scale is None else scale, window, sinks, causal, cache.ref, out.data_ptr(), o_token, o_head,
+                         ws.ptr, ws.nbytes, _stream(stream))
+    if status:
+        _check(status)
+
+
+class PagePool:
+    """The page tables of a batch and the free pages of its cache, for retrace_kv_reserve: page_table
+    [B, max_pages] (the one that the cache has), free_pages [num_pages], counts [2] and held [B], all int32
+    (see include/retrace.h).  Keeps the tensors, which calls change in place."""
+
+    def __init__(self, page_table, page_size, free_pages, counts, held):
+        table_stride = _page_rows(page_table)
+        B, max_pages = page_table.shape
+        for name, t, n in (("free_pages", free_pages, None), ("counts", counts, 2), ("held", held, B)):
+            _int32(t, name)
+            if t.dim() != 1 or (n is not None and t.shape[0] != n) or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous [{'num_pages' if n is None else n}]")
+        self.page_table, self.page_size, self.free_pages, self.counts, self.held = page_table, int(page_size), free_pages, counts, held
+        self.shape_B, self.shape_B1 = (B,), (B + 1,)
+        self.args = (B, self.page_size, _ptr(page_table), table_stride, max_pages, _ptr(held), _ptr(free_pages), free_pages.shape[0],
+                     _ptr(counts))
+
+    @classmethod
+    def of(cls, num_pages, page_size, B, max_pages, device="cuda"):
+        """Tables without pages, and all pages free (page 0 on top)."""
+        new = lambda n, x: torch.full((n,), x, dtype=torch.int32, device=device)  # noqa: E731
+        counts = new(2, 0)
+        counts[0] = num_pages
+        return cls(new(B * max_pages, -1).view(B, max_pages), page_size,
+                   torch.arange(num_pages - 1, -1, -1, dtype=torch.int32, device=device), counts, new(B, 0))
+
+
+def retrace_kv_reserve(cache_len, new_len, pool: PagePool, q_start=None, slots=None, stream=None):
+    """Gives each sequence the pages that cache_len [B] + new_len [B] tokens need and takes back the others; into
+    q_start [B+1] and slots [T] (int64; needs q_start) where the new tokens start and go (see
+    include/retrace.h)."""
+    for name, t, shape in (("cache_len", cache_len, pool.shape_B), ("new_len", new_len, pool.shape_B), ("q_start", q_start, pool.shape_B1)):
+        if t is not None or name != "q_start":
+            if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous() or not t.is_cuda:
+                _int32(t, name)
+                raise ValueError(f"{name} must be a contiguous {list(shape)} on the GPU: the page table has {shape[0]} rows" if name != "q_start"
+                                 else f"q_start must be a contiguous {list(shape)} on the GPU")
+    # without a list of slots q_start is cut off nowhere
+    T, slots_ptr = 1 << 30, None
+    if slots is not None:
+        if slots.dtype != torch.int64 or slots.dim() != 1 or not slots.is_contiguous() or not slots.is_cuda:
+            raise ValueError("slots must be a contiguous int64 [T] on the GPU")
+        if q_start is None:
+            raise ValueError("slots needs q_start")
+        T, slots_ptr = slots.shape[0], slots.data_ptr()
+    status = _reserve(cache_len.data_ptr(), new_len.data_ptr(), *pool.args, None if q_start is None else q_start.data_ptr(), slots_ptr, T,
+                      _stream(stream))
     if status:
         _check(status)

@@ -107,7 +107,7 @@ cudaError_t launch_attend_join(const AttendArgs& a, PartShape part, int ctas, cu
   const cudaError_t e = device_info(&dev);
   if (e != cudaSuccess) return e;
   const dim3 grid(dev.sm_count * 2), block(kThreads);
-  if (a.cache.dtype == RETRACE_BF16)
+  if (a.dtype == RETRACE_BF16)
     return launch_dependent(attend_join_kernel<__nv_bfloat16>, grid, block, 0, stream, 1u, a, part, ctas);
   return launch_dependent(attend_join_kernel<float>, grid, block, 0, stream, 1u, a, part, ctas);
 }

@@ -93,30 +93,8 @@ __global__ void __launch_bounds__(kAppendThreads, kCtasPerSm) kv_append_kernel(c
     for (int k = warp; k < tokens; k += kAppendThreads / 32) {
       const int tk = t0 + k;
       if (tk >= a.T) break;
-      int b = -1, first = 0;
-      if (!a.q_start) {
-        b = tk / uniform;
-        first = b * uniform;
-      } else {
-        int lo = 0, n = a.B;  // the last start <= tk lies in [lo, lo + n), if any
-        while (n > 32) {
-          const int step = (n + 31) / 32;
-          const int pos = lo + lane * step;
-          const bool below = pos < lo + n && a.q_start[pos] <= tk;
-          const int c = __popc(__ballot_sync(0xFFFFFFFFu, below));
-          if (c == 0) break;
-          const int end = lo + n;
-          lo += (c - 1) * step;
-          n = min(step, end - lo);
-        }
-        const bool below = lane < n && lane < 32 && a.q_start[lo + lane] <= tk;
-        const int c = __popc(__ballot_sync(0xFFFFFFFFu, below));
-        if (c > 0) {
-          b = lo + c - 1;
-          first = a.q_start[b];
-          if (tk >= a.q_start[b + 1] || first < 0) b = -1;  // a token of no sequence
-        }
-      }
+      int first;
+      const int b = sequence_of(a.q_start, a.B, uniform, tk, lane, &first);
       if (lane == 0) {
         s_seq[k] = b;
         s_pos[k] = b < 0 ? -1 : cached_tokens(a.cache_len, b) + (tk - first);

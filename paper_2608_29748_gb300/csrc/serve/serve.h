@@ -35,8 +35,13 @@ struct AppendArgs {
   retrace_kv_cache cache;
   void* q_out;
   long long qo_token, qo_head;
+  // a cache in 8 bits alone
+  retrace_dtype dtype;  // of q, k, v and q_out
+  int8_t *k_exp, *v_exp;
+  long long exp_page, exp_head;
 };
 cudaError_t launch_kv_append(const AppendArgs& a, cudaStream_t stream);
+cudaError_t launch_kv_append_fp8(const AppendArgs& a, cudaStream_t stream);
 
 // Workspace of retrace_attend: the status word (256 bytes), a JoinUnit per CTA, a ticket
 // per CTA (zero between calls: who takes a unit's last one clears it), then
@@ -75,6 +80,10 @@ struct AttendArgs {
   JoinUnit* units;
   uint32_t* tickets;
   float* partials;
+  retrace_dtype dtype;  // of q and out
+  // a cache in 8 bits alone
+  const int8_t *k_exp, *v_exp;
+  long long exp_page, exp_head;
 };
 // A part: `rows` rows of `cols` floats, then their (maximum, sum).
 struct PartShape {
@@ -83,6 +92,7 @@ struct PartShape {
 };
 cudaError_t launch_attend_join(const AttendArgs& a, PartShape part, int ctas, cudaStream_t stream);
 cudaError_t launch_attend_simt(const AttendArgs& a, cudaStream_t stream);
+cudaError_t launch_attend_simt_fp8(const AttendArgs& a, cudaStream_t stream);
 size_t attend_simt_partial_bytes(int head_dim);
 cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t stream);
 size_t attend_tc_partial_bytes(int head_dim);
@@ -101,5 +111,22 @@ struct SampleArgs {
   float* probs;
 };
 cudaError_t launch_sample(const SampleArgs& a, retrace_dtype dtype, cudaStream_t stream);
+
+struct ReserveArgs {
+  const int32_t* cache_len;
+  const int32_t* new_len;
+  int B, page_size;
+  int32_t* page_table;
+  long long table_stride;
+  int max_pages;
+  int32_t* held;
+  int32_t* free_pages;
+  int num_pages;
+  int32_t* counts;
+  int32_t* q_start;
+  long long* slots;
+  int T;
+};
+cudaError_t launch_kv_reserve(const ReserveArgs& a, cudaStream_t stream);
 
 }  // namespace retrace

@@ -34,6 +34,34 @@ __device__ __forceinline__ SeqTokens seq_tokens(const int32_t* q_start, int B, i
   return {lo, max(hi - lo, 0)};
 }
 
+// The sequence of token t and its first token; -1: of none.  Called by a whole warp: without a list
+// (`uniform` tokens each) by division, else by a search of 32 starts at a time.
+__device__ __forceinline__ int sequence_of(const int32_t* q_start, int B, int uniform, int t, int lane, int* first) {
+  if (!q_start) {
+    const int b = t / uniform;
+    *first = b * uniform;
+    return b;
+  }
+  *first = 0;
+  int lo = 0, n = B;  // the last start <= t lies in [lo, lo + n), if any
+  while (n > 32) {
+    const int step = (n + 31) / 32;
+    const int pos = lo + lane * step;
+    const bool below = pos < lo + n && q_start[pos] <= t;
+    const int c = __popc(__ballot_sync(0xFFFFFFFFu, below));
+    if (c == 0) break;
+    const int end = lo + n;
+    lo += (c - 1) * step;
+    n = min(step, end - lo);
+  }
+  const bool below = lane < n && lane < 32 && q_start[lo + lane] <= t;
+  const int c = __popc(__ballot_sync(0xFFFFFFFFu, below));
+  if (c == 0) return -1;
+  const int b = lo + c - 1;
+  *first = q_start[b];
+  return t >= q_start[b + 1] || *first < 0 ? -1 : b;  // a token of no sequence
+}
+
 // Lengths outside (-2^30, 2^30) are taken as the nearest end, so that positions
 // stay in 32 bits (a sequence has at most 2^30 places).
 __device__ __forceinline__ int cached_tokens(const int32_t* cache_len, int b) {
