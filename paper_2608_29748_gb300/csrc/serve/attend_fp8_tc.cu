@@ -1,0 +1,816 @@
+// Attention over a cache in 8 bits on the tensor cores (bf16 queries).
+//
+// The keys are on the M side: per tile of 128 keys and up to 72 rows (query tokens times the
+// heads of a group) a CTA computes, all products in 8 bits with fp32 accumulation,
+//     S^T = K Q^T      [keys, rows]: K as it lies in the cache; a query is the sum of two e4m3 numbers
+//                      (its leading 4 bits and the other 4, times 2^-4), in columns of their own;
+//     t = scale S 2^ke, p = 2^(t + ve - m), l += p 2^-ve       a key's exponents ke and ve are its
+//                      thread's: one thread per key and half of the rows;
+//     O^T += V^T P^T   [head dim, rows]: V as it lies; a weight is the sum of three e5m2 numbers of 3
+//                      bits each, in columns of their own.
+// e5m2 is the upper byte of an fp16 number, so the first two parts of a weight are bytes of it and of
+// what is left, and the last is rounded: 9 bits in all where a bf16 weight has 8, down to 2^-9,
+// and multiples of 2^-16 below.  m is chosen so that the largest weight of a row's first tile is 2^9, and
+// raised (O and l rescaled) when one passes 2^15; so a weight is off by at most 2^-9 of it or 2^-26 of
+// the row's largest.
+// Nothing is converted but the queries, once, and the weights: keys and values go from HBM to shared
+// memory to the tensor core, 256 D bytes a tile, 1400 cycles of an SM's share of HBM at D = 128.  The
+// products are 4 (2 rows + 3 rows) cycles at D = 128, shared memory moves some 1100 cycles' worth at
+// 72 rows, and the softmax does 128 rows exponentials: with few rows on the N side all of
+// it scales with the rows that there are.
+//
+// Warps 0 and 1 copy K, 2 and 3 V (TMA boxes of the slots of a page, dealt out by turns); warp 4 issues
+// the products; warps 5-7 take the queries apart, a piece ahead; warps 8-15 are the softmax,
+// warps 8-11 of the first half of the rows and 12-15 of the second.  S and P have two buffers: the
+// scores of a tile are computed during the softmax of the one before.
+#include <math.h>
+
+#include "attend_plan.cuh"
+#include "fp8.cuh"
+#include "pairs.cuh"
+#include "tc_ops.cuh"
+
+namespace retrace {
+namespace {
+
+constexpr int kThreads = 512;
+constexpr int kKeys = 128;  // keys of a tile
+constexpr unsigned long long kDrainNs = 20ull * 1000ull * 1000ull;
+constexpr int kInfoTiles = 16;  // ring of tiles' units: more than the tiles between loading and softmax
+constexpr int kMostBoxes = 16;  // of a tile: pages of 8 slots
+constexpr float kFirstTop = 9.f, kMostTop = 15.f;
+constexpr float kNone = 1e30f;  // minus the reference of a row that has seen nothing
+
+struct TcParams {
+  AttendArgs a;
+  AttendShape shape;  // unit_tokens: of a row tile
+  int group;          // query heads of a key/value head
+  FastDivide by_group, page_size;
+  int kv_box;   // slots of a box: they lie within a page and divide a tile
+  float scale2;  // scale log2(e)
+};
+
+// kHalf rows to each of the two softmax warpgroups, in chunks of 16 (the last of 4: 36 = 16 + 16 + 4).
+template <int DP, int kHalf>
+struct TcShape {
+  static constexpr int kRows = 2 * kHalf;
+  static constexpr int kChunks = (kHalf + 15) / 16;
+  __host__ __device__ static constexpr int rows_of(int chunk) { return kHalf - 16 * chunk < 16 ? kHalf - 16 * chunk : 16; }
+  // Columns of a half: of S 2 a row (the two parts of a chunk's queries side by side), of O 3 a row,
+  // a chunk's rounded up to 16.
+  static constexpr int kS = 2 * kHalf;
+  static constexpr int kO = 48 * (kChunks - 1) + (3 * rows_of(kChunks - 1) + 15) / 16 * 16;
+  static constexpr int kSColumns = 2 * kS, kOColumns = 2 * kO;
+  static_assert(kSColumns % 16 == 0 && kOColumns % 16 == 0 && kOColumns <= 256, "columns of a product");
+  static constexpr int kOAt = 2 * kSColumns;
+  static_assert(kOAt + kOColumns <= 512, "columns of TMEM");
+
+  static constexpr int kTileBytes = kKeys * DP;
+  static constexpr int kPAtoms = (kOColumns + 127) / 128;      // 128-byte columns of P
+  static constexpr int kPBytes = kPAtoms * kKeys * 128;
+  static constexpr int kQBytes = (kSColumns * DP + 1023) / 1024 * 1024;
+  static constexpr int kControlBytes = 12 * 1024;
+  static constexpr int kRoom = (227 * 1024 - kControlBytes - 2 * kPBytes - 2 * kQBytes) / kTileBytes;
+  static constexpr int kRingV = (kRoom + 1) / 2 < 8 ? (kRoom + 1) / 2 : 8, kRingK = kRoom / 2 < 8 ? kRoom / 2 : 8;
+  static_assert(kRingK >= 3 && kRingV >= 4, "tiles in flight");
+  static constexpr int kVAt = kRingK * kTileBytes, kPAt = kVAt + kRingV * kTileBytes, kQAt = kPAt + 2 * kPBytes;
+  static constexpr int kControl = kQAt + 2 * kQBytes;
+  static constexpr int kPart = kRows * (DP + 2);  // floats of a part
+};
+
+// A box's keys: scores are multiplied by k and k / 16, weights are 2^(.. + v), sums take them times inv.
+struct BoxUnits {
+  float k, v, inv;
+  int there;  // has a page
+};
+
+template <int kHalf>
+struct Control {
+  uint64_t full[2][8], empty[2][8];  // rings of K and V
+  uint64_t q_full[2], q_empty[2];
+  uint64_t s_full[2];   // scores ready
+  uint64_t p_full[2];   // weights written, the scores' buffer read
+  uint64_t pv_done[2];  // the product with V done, the weights' buffer free
+  uint64_t done;        // after an expired wait: the issued products
+  PlanStart plan;
+  long long sum[kThreads / 32];
+  uint32_t tmem;
+  int abort;
+  PieceWalk walk[2];  // of the softmax warpgroups
+  Piece piece[2][2];  // this one and the next
+  int more[2][2];
+  BoxUnits units[kInfoTiles][kMostBoxes];
+  alignas(16) float factor[2][2 * kHalf];  // of a row: scale log2(e) times its queries' unit
+  long long out[2][2 * kHalf];             // where a row goes, elements
+  alignas(16) float minus[2 * kHalf];      // minus a row's reference
+  alignas(16) float scale[2 * kHalf];      // of a raised row's sums; at the end 1 / sum
+  float part[2][4][kHalf];                 // per warp: a row's maximum, or sum
+};
+
+// ---- instructions -------------------------------------------------------------
+// D[tmem] (+)= A[smem] * B[smem], 8-bit inputs, fp32 accumulation.
+__device__ __forceinline__ void tc_mma_8bit(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// kind::f8f6f4: fp32 accumulator (bits 4-5 = 1); formats of A (7-9) and B (10-12): e4m3 0, e5m2 1; A and B
+// MN-major (15, 16); N >> 3 (17-22), M >> 4 (24-28).
+__host__ __device__ constexpr uint32_t idesc_8bit(int N, bool values) {
+  return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((128u >> 4) << 24) | (values ? 1u << 10 | 1u << 15 | 1u << 16 : 0u);
+}
+// Rows of DP bytes with the swizzle of their width, 8 rows a group; `lead`: from one column of DP (of P: 128)
+// bytes to the next, for an MN-major operand.
+template <int kWidth>
+__device__ __forceinline__ uint64_t rows_desc(uint32_t saddr, uint32_t lead) {
+  constexpr uint64_t mode = kWidth == 128 ? 2 : 4;
+  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)((kWidth * 8) >> 4) << 32 | (uint64_t)1 << 46 | mode << 61;
+}
+
+template <int N>
+__device__ __forceinline__ void tmem_load(uint32_t at, float* v) {
+  uint32_t* r = reinterpret_cast<uint32_t*>(v);
+  if constexpr (N == 32) {
+    tmem_ld32(at, v);
+  } else if constexpr (N == 16) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+                   "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(at)
+                 : "memory");
+  } else if constexpr (N == 8) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(at)
+                 : "memory");
+  } else {
+    static_assert(N == 4, "4, 8, 16 or 32 columns");
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+  }
+}
+__device__ __forceinline__ void tmem_store4(uint32_t at, const float* v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]) : "memory");
+}
+// 128 threads' agreement on whether any of them says so.
+__device__ __forceinline__ bool any_of_half(int half, bool mine) {
+  uint32_t p = mine;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %0, 0;\n\t"
+      "barrier.cta.red.or.pred q, %1, 128, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "+r"(p)
+      : "r"(2 + half)
+      : "memory");
+  return p != 0;
+}
+__device__ __forceinline__ void half_barrier(int half) { asm volatile("bar.sync %0, 128;" ::"r"(2 + half) : "memory"); }
+
+// Registers from the copies, products and queries to the softmax: 256 x 64 + 256 x 192 are the launch's 512 x 128.
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 64;"); }
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 192;"); }
+
+__device__ __forceinline__ uint32_t halves(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t minus_halves(uint32_t a, uint32_t b) {
+  const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t to_e5m2x2(uint32_t h) {
+  __half2_raw r;
+  r.x = (unsigned short)(h & 0xFFFFu);
+  r.y = (unsigned short)(h >> 16);
+  return __nv_cvt_halfraw2_to_fp8x2(r, __NV_SATFINITE, __NV_E5M2);
+}
+// The three parts of four weights, none negative, a byte each.
+__device__ __forceinline__ void take_apart(const float (&w)[4], uint32_t& first, uint32_t& second, uint32_t& third) {
+  const uint32_t a = halves(w[0], w[1]), b = halves(w[2], w[3]);
+  const uint32_t a1 = minus_halves(a, a & 0xFF00FF00u), b1 = minus_halves(b, b & 0xFF00FF00u);
+  const uint32_t a2 = minus_halves(a1, a1 & 0xFF00FF00u), b2 = minus_halves(b1, b1 & 0xFF00FF00u);
+  first = __byte_perm(a, b, 0x7531);
+  second = __byte_perm(a1, b1, 0x7531);
+  third = to_e5m2x2(a2) | to_e5m2x2(b2) << 16;
+}
+
+template <int I>
+struct Index {
+  static constexpr int value = I;
+};
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void each_chunk(F&& f) {
+  if constexpr (I < N) {
+    f(Index<I>{});
+    each_chunk<N, I + 1>(f);
+  }
+}
+
+template <int DP, int kHalf>
+__global__ void __launch_bounds__(kThreads, 1)
+    attend_fp8_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                         const __grid_constant__ TcParams P) {
+  using Sh = TcShape<DP, kHalf>;
+  static_assert(sizeof(Control<kHalf>) <= Sh::kControlBytes, "room of the control block");
+  extern __shared__ __align__(1024) uint8_t smem[];
+  Control<kHalf>& ct = *reinterpret_cast<Control<kHalf>*>(smem + Sh::kControl);
+  volatile int* abort = &ct.abort;
+  const uint32_t base = smem_u32(smem);
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+  const AttendArgs& a = P.a;
+
+  if (tid == 0) {
+    ct.abort = 0;
+    for (int r = 0; r < 2; ++r)
+      for (int s = 0; s < 8; ++s) {
+        mbar_init(smem_u32(&ct.full[r][s]), 2);  // two copying warps
+        mbar_init(smem_u32(&ct.empty[r][s]), 1);
+      }
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(smem_u32(&ct.q_full[s]), 3);
+      mbar_init(smem_u32(&ct.q_empty[s]), 9);  // the products, and the softmax warps
+      mbar_init(smem_u32(&ct.s_full[s]), 1);
+      mbar_init(smem_u32(&ct.p_full[s]), 8);
+      mbar_init(smem_u32(&ct.pv_done[s]), 1);
+    }
+    mbar_init(smem_u32(&ct.done), 1);
+    fence_mbar_init();
+    tma_prefetch_desc(&tm_k);
+    tma_prefetch_desc(&tm_v);
+  }
+  if (warp == 4) {
+    tmem_alloc(smem_u32(&ct.tmem), 512);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = ct.tmem;
+  pdl_launch_dependents();
+  pdl_wait();
+  plan_start<kThreads, kKeys>(P.shape, gridDim.x, 2, &ct.plan, ct.sum);
+  const PlanStart& plan = ct.plan;
+  if (warp < 8) {
+    fewer_registers();
+    PieceWalk walk;
+    walk.start(plan);
+    Piece pc;
+    bool ok = true, drain = false;
+    if (warp < 4) {
+      // ---- copies of K (warps 0, 1) and V (2, 3): every other box each ----
+      const int ring = warp / 2, turn = warp % 2;
+      const bool keys = ring == 0;
+      const CUtensorMap* map = keys ? &tm_k : &tm_v;
+      const int boxes = kKeys / P.kv_box, box = lane * 2 + turn, mine = (boxes + 1 - turn) / 2;
+      const bool active = box < boxes;
+      const uint32_t slots = keys ? Sh::kRingK : Sh::kRingV, tiles_at = base + (keys ? 0 : Sh::kVAt);
+      uint32_t tiles = 0, slot = 0, phase = 0;
+      while (ok && walk.next<kKeys>(P.shape, plan, &pc)) {
+        const int nt = pc.k1 - pc.k0;
+        if (nt == 0) continue;
+        struct Place {
+          int page, slot;
+        };
+        auto place_of = [&](int k) {  // of this lane's box of the piece's tile k
+          Place x{a.cache.num_pages, 0};  // a box without a page lies outside the tensor: zeros
+          if (active && k < nt) {
+            const int j = pc.keys.tile(pc.k0 + k) * kKeys + box * P.kv_box, i = P.page_size(j);
+            const int page = page_of(a.cache, pc.b, i);
+            if (page >= 0) x = Place{page, j - i * P.page_size.by};
+          }
+          return x;
+        };
+        auto units_of_box = [&](const Place& x) {
+          BoxUnits u{1.f, 0.f, 1.f, 0};
+          if (keys && x.page < a.cache.num_pages) {
+            const int ve = page_exponent(a, a.v_exp, x.page, pc.head);
+            u = BoxUnits{power_of_two(page_exponent(a, a.k_exp, x.page, pc.head)), (float)ve, power_of_two(-ve), 1};
+          }
+          return u;
+        };
+        // pages are looked up two tiles ahead of their copies, their exponents one
+        Place now = place_of(0), next = place_of(1);
+        BoxUnits units = units_of_box(now);
+        for (int k = 0; k < nt && ok; ++k) {
+          const Place after = place_of(k + 2);
+          const BoxUnits units_next = units_of_box(next);
+          ok = warp_wait_all(&ct.empty[ring][slot], phase ^ 1u, abort);
+          if (!ok) break;
+          const uint32_t bar = smem_u32(&ct.full[ring][slot]);
+          if (keys && active) ct.units[tiles % kInfoTiles][box] = units;
+          __syncwarp();
+          if (lane == 0) mbar_arrive_expect_tx(bar, mine * P.kv_box * DP);
+          __syncwarp();
+          if (active)
+            tma_load_4d(tiles_at + slot * Sh::kTileBytes + box * P.kv_box * DP, map, 0, pc.head, now.slot, now.page, bar);
+          if (++slot == slots) {
+            slot = 0;
+            phase ^= 1u;
+          }
+          ++tiles;
+          now = next;
+          next = after;
+          units = units_next;
+        }
+      }
+      drain = !ok;
+    } else if (warp == 4) {
+      // ---- products ----
+      constexpr uint32_t kScores = idesc_8bit(Sh::kSColumns, false), kValues = idesc_8bit(Sh::kOColumns, true);
+      uint32_t tiles = 0, pieces = 0, v_seen = 0;
+      auto wait = [&](uint64_t* bar, uint32_t parity) {
+        ok = ok && warp_wait_all(bar, parity, abort);
+        return ok;
+      };
+      auto commit = [&](uint64_t* bar) {
+        if (elect_one()) tc_commit(smem_u32(bar));
+        __syncwarp();
+      };
+      // V of all tiles up to this one has landed
+      auto wait_values = [&](uint32_t tile) {
+        for (; ok && v_seen <= tile; ++v_seen) wait(&ct.full[1][v_seen % Sh::kRingV], v_seen / Sh::kRingV & 1u);
+        return ok;
+      };
+      auto scores = [&](int i, uint32_t q) {
+        const uint32_t g = tiles + i, slot = g % Sh::kRingK;
+        if (!wait(&ct.full[0][slot], g / Sh::kRingK & 1u)) return;
+        // V of a tile at the edge of what the unit sees is there before its scores are: the softmax
+        // clears rows of it
+        const int j0 = pc.keys.tile(pc.k0 + i) * kKeys;
+        if ((j0 < pc.keys.lo || j0 + kKeys - 1 > pc.keys.hi) && !wait_values(g)) return;
+        tc_fence_after();
+        if (elect_one()) {
+          const uint64_t kd = rows_desc<DP>(base + slot * Sh::kTileBytes, 16), qd = rows_desc<DP>(base + Sh::kQAt + q * Sh::kQBytes, 16);
+#pragma unroll
+          for (int k = 0; k < DP / 32; ++k) tc_mma_8bit(tmem + (g & 1u) * Sh::kSColumns, kd + 2 * k, qd + 2 * k, kScores, k > 0);
+        }
+        __syncwarp();
+        commit(&ct.s_full[g & 1u]);
+        commit(&ct.empty[0][slot]);
+      };
+      while (ok && walk.next<kKeys>(P.shape, plan, &pc)) {
+        const int nt = pc.k1 - pc.k0;
+        if (nt == 0) continue;
+        const uint32_t q = pieces & 1u;
+        if (!wait(&ct.q_full[q], pieces >> 1 & 1u)) break;
+        ++pieces;
+        scores(0, q);
+        if (ok && nt > 1) scores(1, q);
+        for (int i = 0; i < nt && ok; ++i) {
+          const uint32_t g = tiles + i, slot = g % Sh::kRingV;
+          if (!wait_values(g) || !wait(&ct.p_full[g & 1u], g >> 1 & 1u)) break;
+          tc_fence_after();
+          if (elect_one()) {
+            // 64 columns of the head dimension fill half of M: the other half is the same again
+            const uint64_t vd = rows_desc<DP>(base + Sh::kVAt + slot * Sh::kTileBytes, 0);
+            const uint64_t pd = rows_desc<128>(base + Sh::kPAt + (g & 1u) * Sh::kPBytes, kKeys * 128);
+#pragma unroll
+            for (int k = 0; k < kKeys / 32; ++k)
+              tc_mma_8bit(tmem + Sh::kOAt, vd + k * (32 * DP >> 4), pd + k * (32 * 128 >> 4), kValues, i + k > 0);
+          }
+          __syncwarp();
+          commit(&ct.pv_done[g & 1u]);
+          commit(&ct.empty[1][slot]);
+          if (i + 2 < nt) scores(i + 2, q);
+        }
+        if (!ok) break;
+        commit(&ct.q_empty[q]);
+        tiles += nt;
+      }
+      if (!ok) {
+        volatile int never = 0;
+        commit(&ct.done);
+        mbar_wait_bounded(smem_u32(&ct.done), 0, &never);
+      }
+    } else {
+      // ---- queries: rows of 128 or 64 bytes, each a sum of two e4m3 numbers times its row's unit ----
+      constexpr int kEach = DP / 32;  // elements of a lane
+      const int D = a.cache.head_dim;
+      uint32_t pieces = 0;
+      while (ok && walk.next<kKeys>(P.shape, plan, &pc)) {
+        if (pc.k1 == pc.k0) continue;
+        const uint32_t buffer = pieces & 1u;
+        ok = warp_wait_all(&ct.q_empty[buffer], (pieces >> 1 & 1u) ^ 1u, abort);
+        if (!ok) break;
+        ++pieces;
+        const int rows = (pc.i1 - pc.i0) * P.group;
+        uint8_t* to = smem + Sh::kQAt + buffer * Sh::kQBytes;
+        for (int r0 = warp - 5; r0 < Sh::kRows; r0 += 3 * 4) {
+          // four rows' loads at a time
+          uint32_t raw[4][kEach / 2];
+          int token[4], head[4];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int r = r0 + 3 * u;
+            token[u] = P.by_group(r);
+            head[u] = r - token[u] * P.group;
+            token[u] += pc.row0 + pc.i0;
+            head[u] += pc.head * P.group;
+#pragma unroll
+            for (int e = 0; e < kEach / 2; ++e) raw[u][e] = 0u;
+            if (r < rows && lane * kEach < D) {
+              const __nv_bfloat16* from = static_cast<const __nv_bfloat16*>(a.q) + token[u] * a.q_token + head[u] * a.q_head + lane * kEach;
+              if constexpr (kEach == 4)
+                *reinterpret_cast<uint2*>(raw[u]) = *reinterpret_cast<const uint2*>(from);
+              else
+                raw[u][0] = *reinterpret_cast<const uint32_t*>(from);
+            }
+          }
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int r = r0 + 3 * u;
+            if (r >= Sh::kRows) break;
+            // magnitudes as whole numbers: infinities and NaN are the largest
+            uint32_t most = 0u;
+#pragma unroll
+            for (int e = 0; e < kEach / 2; ++e) most = max(most, max(raw[u][e] & 0x7FFFu, raw[u][e] >> 16 & 0x7FFFu));
+            const uint32_t top = __reduce_max_sync(0xFFFFFFFFu, most) << 16;
+            // the least exponent with top <= 448 times its power of two; a row with an infinity or a
+            // NaN is NaN throughout, as its scores are
+            const int e = min(max((int)(top >> 23) - 127 - 8 + ((top & 0x7FFFFFu) > 0x600000u), -120), 120);
+            const float down = power_of_two(-e);
+            const bool nan = top >= 0x7F800000u;
+            uint32_t lead = 0u, rest = 0u;
+#pragma unroll
+            for (int i = 0; i < kEach / 2; ++i) {
+              const float x = bf16_lo(raw[u][i]) * down, y = bf16_hi(raw[u][i]) * down;
+              const uint32_t c = to_e4m3x2(x, y);
+              const float2 f = e4m3_floats(c);
+              lead |= c << (16 * i);
+              rest |= to_e4m3x2((x - f.x) * 16.f, (y - f.y) * 16.f) << (16 * i);
+            }
+            if (nan) lead = 0x7F7F7F7Fu;
+            // the columns of the row's two parts
+            const int half = r / kHalf, in = r % kHalf, chunk = in / 16, c = in % 16, size = min(16, kHalf - 16 * chunk);
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+              const int n = half * Sh::kS + 32 * chunk + part * size + c, at = lane * kEach;
+              const int chunk16 = DP == 128 ? (at / 16) ^ (n & 7) : (at / 16) ^ (n >> 1 & 3);
+              uint8_t* dst = to + n * DP + chunk16 * 16 + at % 16;
+              if constexpr (kEach == 4)
+                *reinterpret_cast<uint32_t*>(dst) = part ? rest : lead;
+              else
+                *reinterpret_cast<uint16_t*>(dst) = (uint16_t)(part ? rest : lead);
+            }
+            if (lane == 0) {
+              ct.factor[buffer][r] = r < rows ? P.scale2 * power_of_two(e) : 0.f;
+              ct.out[buffer][r] = token[u] * a.out_token + head[u] * a.out_head;
+            }
+          }
+        }
+        fence_proxy_async_shared();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&ct.q_full[buffer]));
+      }
+    }
+    if (!ok && lane == 0) raise_abort(abort, a.status);
+    // After an expired wait: time for this CTA's copies in flight to land.
+    if (drain) {
+      const unsigned long long t0 = global_ns();
+      while (global_ns() - t0 < kDrainNs) __nanosleep(1000);
+    }
+    __syncwarp();
+  } else {
+    more_registers();
+    // ---- softmax: half h of the rows, one thread per key ----
+    const int h = warp >= 12, key = tid & 127, quarter = warp & 3, r0 = h * kHalf;
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    const uint32_t t_o = tmem + lanes + Sh::kOAt + h * Sh::kO;
+    const int D = a.cache.head_dim, G = P.group;
+    const float* minus = ct.minus + r0;
+    uint32_t tiles = 0, pieces = 0;
+    JoinUnit unit{};
+    bool ok = true;
+    // After an expired wait a warp goes on without waiting, and writes nothing: the warps of a half meet
+    // at the same barriers all the same.
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      if (ok && !warp_wait_all(bar, parity, abort)) {
+        ok = false;
+        if (lane == 0) raise_abort(abort, a.status);
+      }
+    };
+    // One thread of the half walks, a piece ahead; the pieces stay in shared memory.
+    const bool walker = key == 96;
+    if (walker) {
+      ct.walk[h].start(plan);
+      ct.more[h][0] = ct.walk[h].template next<kKeys, true>(P.shape, plan, &ct.piece[h][0]);
+    }
+    for (int np = 0;; np ^= 1) {
+      half_barrier(h);
+      if (!ct.more[h][np]) break;
+      if (walker) ct.more[h][np ^ 1] = ct.walk[h].template next<kKeys, true>(P.shape, plan, &ct.piece[h][np ^ 1]);
+      const Piece& pc = ct.piece[h][np];
+      const int nt = pc.k1 - pc.k0, rows = (pc.i1 - pc.i0) * G;
+      if (nt == 0) {  // nothing is visible
+        for (int i = key; i < kHalf * D; i += 128) {
+          const int r = r0 + i / D, token = P.by_group(r);
+          if (r < rows)
+            static_cast<__nv_bfloat16*>(a.out)[(long long)(pc.row0 + pc.i0 + token) * a.out_token +
+                                               (pc.head * G + r - token * G) * (long long)a.out_head + i % D] = __float2bfloat16_rn(0.f);
+        }
+        continue;
+      }
+      const uint32_t buffer = pieces & 1u;
+      wait(&ct.q_full[buffer], pieces >> 1 & 1u);
+      ++pieces;
+      const float* factor = ct.factor[buffer] + r0;
+      // A row of the tile that holds no token refers to a number that no weight comes near.
+      if (key < kHalf) ct.minus[r0 + key] = r0 + key < rows ? kNone : -kNone;
+      half_barrier(h);
+      float2 l[kHalf / 2];  // sums of this thread's keys
+#pragma unroll
+      for (int i = 0; i < kHalf / 2; ++i) l[i] = make_float2(0.f, 0.f);
+      const UnitKeys keys = pc.keys;
+      const int first = pc.c + pc.i0, k0 = pc.k0;  // position of the unit's first token
+
+      for (int j = 0; j < nt; ++j) {
+        // what is known of the tile before its scores are there
+        const uint32_t g = tiles + j, b = g & 1u;
+        const int j0 = keys.tile(k0 + j) * kKeys, at = j0 + key;
+        const bool edge = j0 < keys.lo || j0 + kKeys - 1 > keys.hi;
+        // The key is seen by the rows [from, to).
+        int from = 0, to = rows;
+        if (a.causal && at > first) from = (at - first) * G;
+        if (a.window > 0 && at >= a.sinks && at - first + a.window < P.shape.unit_tokens)
+          to = max(at - first + a.window, 0) * G;
+        if (at > keys.hi) to = 0;
+        from -= r0;
+        to -= r0;
+        wait(&ct.s_full[b], g >> 1 & 1u);
+        tc_fence_after();
+        const BoxUnits u = ct.units[g % kInfoTiles][key / P.kv_box];
+        if (!u.there) to = from = -1000;
+        const bool masked = !__all_sync(0xFFFFFFFFu, from <= 0 && to >= min(rows - r0, kHalf));
+        // A row of V that no row of the unit sees holds anything, and 0 times that need not be 0:
+        // cleared before the product (V of such a tile landed before its scores were issued).
+        if (edge && (at > keys.hi || (at < keys.lo && at >= a.sinks))) {
+          uint8_t* v = smem + Sh::kVAt + (g % Sh::kRingV) * Sh::kTileBytes + key * DP;
+#pragma unroll
+          for (int c = h; c < DP / 16; c += 2)  // half of the row each; the lanes begin at different banks
+            *reinterpret_cast<uint4*>(v + ((c + 2 * key) % (DP / 16)) * 16) = make_uint4(0u, 0u, 0u, 0u);
+        }
+
+        const uint32_t t_s = tmem + lanes + b * Sh::kSColumns + h * Sh::kS;
+        float y[kHalf];  // exponents of the weights
+        auto exponents = [&](bool referred) {
+          float s[2 * kHalf];
+          each_chunk<Sh::kChunks>([&](auto chunk) {
+            constexpr int c = decltype(chunk)::value;
+            tmem_load<2 * Sh::rows_of(c)>(t_s + 32 * c, s + 32 * c);
+          });
+          tmem_wait_ld();
+          const float2 sixteenth = make_float2(0.0625f, 0.0625f), unit2 = make_float2(u.k, u.k), v2 = make_float2(u.v, u.v);
+          each_chunk<Sh::kChunks>([&](auto chunk) {
+            constexpr int c = decltype(chunk)::value, n = Sh::rows_of(c);
+#pragma unroll
+            for (int i = 0; i < n; i += 2) {
+              const int r = 16 * c + i;
+              // The product with the factor is rounded before the reference is taken off, so that the
+              // largest weight is what it was chosen to be, however far from zero the scores are.
+              float2 x = fma2(make_float2(s[32 * c + n + i], s[32 * c + n + i + 1]), sixteenth, make_float2(s[32 * c + i], s[32 * c + i + 1]));
+              x = mul2(mul2(x, unit2), *reinterpret_cast<const float2*>(factor + r));
+              if (referred) x = add2(x, *reinterpret_cast<const float2*>(minus + r));
+              x = add2(x, v2);
+              y[r] = x.x;
+              y[r + 1] = x.y;
+            }
+          });
+          if (masked) {
+#pragma unroll
+            for (int r = 0; r < kHalf; ++r)
+              if (r < from || r >= to) y[r] = -INFINITY;
+          }
+        };
+        exponents(true);
+        float top = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < kHalf; r += 2) top = max3(top, y[r], y[r + 1]);
+        if (any_of_half(h, top > kMostTop)) {
+          // A weight has outgrown its reference, or a row sees its first keys: the rows' maxima over
+          // the tile, new references, and what was summed so far in the new unit.
+          exponents(false);
+#pragma unroll
+          for (int r = 0; r < kHalf; ++r) {
+            const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, ordered_bits(y[r]));
+            if (lane == 0) ct.part[h][quarter][r] = __uint_as_float(most & 0x80000000u ? most & 0x7FFFFFFFu : ~most);
+          }
+          half_barrier(h);
+          if (key < kHalf) {
+            const float old = ct.minus[r0 + key];
+            const float most = fmaxf(fmaxf(ct.part[h][0][key], ct.part[h][1][key]), fmaxf(ct.part[h][2][key], ct.part[h][3][key]));
+            float f = 1.f;
+            if (most + old > kMostTop) {
+              const float now = kFirstTop - most;
+              f = old == kNone ? 0.f : exp2_fast(now - old);
+              ct.minus[r0 + key] = now;
+            }
+            ct.scale[r0 + key] = f;
+          }
+          half_barrier(h);
+#pragma unroll
+          for (int r = 0; r < kHalf; r += 2) l[r / 2] = mul2(l[r / 2], *reinterpret_cast<const float2*>(ct.scale + r0 + r));
+          if (j > 0) {
+            const uint32_t before = g - 1;
+            wait(&ct.pv_done[before & 1u], before >> 1 & 1u);
+            tc_fence_after();
+            each_chunk<Sh::kChunks>([&](auto chunk) {
+              constexpr int c = decltype(chunk)::value, n = Sh::rows_of(c);
+#pragma unroll
+              for (int part = 0; part < 3; ++part)
+#pragma unroll
+                for (int i = 0; i < n; i += 4) {
+                  float o[4];
+                  const uint32_t column = t_o + 48 * c + part * n + i;
+                  tmem_load<4>(column, o);
+                  tmem_wait_ld();
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) o[e] *= ct.scale[r0 + 16 * c + i + e];
+                  tmem_store4(column, o);
+                }
+            });
+            tmem_wait_st();
+          }
+          exponents(true);
+        }
+
+        // The weights' buffer is free when the product of two tiles ago is done.
+        if (g >= 2) wait(&ct.pv_done[b], (g >> 1 & 1u) ^ 1u);
+        uint8_t* weights = smem + Sh::kPAt + b * Sh::kPBytes + key * 128;
+        const float2 inv2 = make_float2(u.inv, u.inv);
+        each_chunk<Sh::kChunks>([&](auto chunk) {
+          constexpr int c = decltype(chunk)::value, n = Sh::rows_of(c);
+          uint32_t w[(3 * n + 15) / 16 * 4];
+#pragma unroll
+          for (int i = 3 * n / 4; i < (3 * n + 15) / 16 * 4; ++i) w[i] = 0u;
+#pragma unroll
+          for (int i = 0; i < n; i += 4) {
+            float e[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) e[k] = exp2_fast(y[16 * c + i + k]);
+            l[(16 * c + i) / 2] = fma2(make_float2(e[0], e[1]), inv2, l[(16 * c + i) / 2]);
+            l[(16 * c + i) / 2 + 1] = fma2(make_float2(e[2], e[3]), inv2, l[(16 * c + i) / 2 + 1]);
+            take_apart(e, w[i / 4], w[n / 4 + i / 4], w[2 * (n / 4) + i / 4]);
+          }
+#pragma unroll
+          for (int i = 0; i < (3 * n + 15) / 16; ++i) {
+            const int column = h * Sh::kO + 48 * c + 16 * i;
+            *reinterpret_cast<uint4*>(weights + column / 128 * (kKeys * 128) + ((column % 128 / 16) ^ (key & 7)) * 16) =
+                make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+          }
+        });
+        fence_proxy_async_shared();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&ct.p_full[b]));
+      }
+      tiles += nt;
+
+      // The rows' sums over the half's 128 threads: each step of a warp's sum halves the rows that a lane has.
+      each_chunk<Sh::kChunks>([&](auto chunk) {
+        constexpr int c = decltype(chunk)::value, n = Sh::rows_of(c);
+        float v[n];
+#pragma unroll
+        for (int i = 0; i < n; ++i) v[i] = i % 2 ? l[8 * c + i / 2].y : l[8 * c + i / 2].x;
+#pragma unroll
+        for (int o = n / 2; o > 0; o >>= 1)
+#pragma unroll
+          for (int i = 0; i < o; ++i) {
+            const bool upper = lane & o;
+            const float other = __shfl_xor_sync(0xFFFFFFFFu, upper ? v[i] : v[i + o], o);
+            v[i] = (upper ? v[i + o] : v[i]) + other;
+          }
+#pragma unroll
+        for (int o = n; o < 32; o <<= 1) v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], o);
+        if (lane < n) ct.part[h][quarter][16 * c + lane] = v[0];
+      });
+      half_barrier(h);
+      const bool whole = pc.pieces == 1;
+      float* part = a.partials + ((long long)blockIdx.x * 2 + (pc.k0 == 0 ? 1 : 0)) * Sh::kPart;
+      if (key < kHalf) {
+        const float sum = (ct.part[h][0][key] + ct.part[h][1][key]) + (ct.part[h][2][key] + ct.part[h][3][key]);
+        ct.scale[r0 + key] = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
+        const float m = -ct.minus[r0 + key];
+        if (!whole && ok && r0 + key < rows)
+          *reinterpret_cast<float2*>(part + Sh::kRows * DP + (r0 + key) * 2) = make_float2(sum == 0.f ? -INFINITY : m, sum);
+      }
+      half_barrier(h);
+      // O is complete
+      if (ok) {
+        const uint32_t last = tiles - 1;
+        wait(&ct.pv_done[last & 1u], last >> 1 & 1u);
+        tc_fence_after();
+      }
+      if (ok) {
+        each_chunk<Sh::kChunks>([&](auto chunk) {
+          constexpr int c = decltype(chunk)::value, n = Sh::rows_of(c);
+          if (r0 + 16 * c >= rows) return;
+          float o[3 * n];
+#pragma unroll
+          for (int p = 0; p < 3; ++p) tmem_load<n>(t_o + 48 * c + p * n, o + p * n);
+          tmem_wait_ld();
+#pragma unroll
+          for (int i = 0; i < n; ++i) {
+            const int r = r0 + 16 * c + i;
+            if (r >= rows || key >= DP) break;  // `key` is the lane: the element of the head
+            const float x = (o[i] + (o[n + i] + o[2 * n + i])) * ct.scale[r];
+            if (!whole)
+              part[r * DP + key] = x;
+            else if (key < D)
+              static_cast<__nv_bfloat16*>(a.out)[ct.out[buffer][r] + key] = __float2bfloat16_rn(x);
+          }
+        });
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&ct.q_empty[buffer]));
+      if (!whole && h == 0 && pc.k0 == 0) unit = JoinUnit{pc.pieces, rows, rows, pc.row0 + pc.i0, pc.head * G, G, {0, 0}};
+    }
+    if (tid == 256) a.units[blockIdx.x] = unit;
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 4) tmem_dealloc(tmem, 512);
+}
+
+template <int DP, int kHalf>
+cudaError_t launch(TcParams& p, const DeviceInfo& dev, cudaStream_t stream) {
+  using Sh = TcShape<DP, kHalf>;
+  const AttendArgs& a = p.a;
+  const retrace_kv_cache& c = a.cache;
+  p.shape.unit_tokens = Sh::kRows / p.group;
+  CUtensorMap mk, mv;
+  const long long dims[4] = {c.head_dim, c.kv_heads, c.page_size, c.num_pages};
+  const long long strides[4] = {1, c.head_stride, c.slot_stride, c.page_stride};
+  const int box[4] = {DP, 1, p.kv_box, 1};
+  const CUtensorMapSwizzle swizzle = DP == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
+  if (!encode(&mk, c.k, 4, dims, strides, box, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, swizzle) ||
+      !encode(&mv, c.v, 4, dims, strides, box, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, swizzle))
+    return cudaErrorInvalidValue;
+  constexpr size_t smem = Sh::kControl + sizeof(Control<kHalf>);
+  static_assert(smem <= 227 * 1024, "shared memory of a CTA");
+  static std::atomic<uint64_t> allowed{0};
+  cudaError_t e = allow_shared(attend_fp8_tc_kernel<DP, kHalf>, smem, dev, allowed);
+  if (e != cudaSuccess) return e;
+  const int grid = dev.sm_count < kAttendMaxTcCtas ? dev.sm_count : kAttendMaxTcCtas;
+  e = launch_dependent(attend_fp8_tc_kernel<DP, kHalf>, dim3(grid), dim3(kThreads), smem, stream, 1u, mk, mv, p);
+  if (e != cudaSuccess) return e;
+  return launch_attend_join(a, PartShape{Sh::kRows, DP, 1.f}, grid, stream);
+}
+
+template <int DP>
+cudaError_t launch_rows(TcParams& p, const DeviceInfo& dev, cudaStream_t stream) {
+  // By the rows that a sequence has on average; a group of query heads is never divided.
+  const long long rows = (long long)p.a.T * p.group, B = p.a.B;
+  if (p.group <= 8 && rows <= 8 * B) return launch<DP, 4>(p, dev, stream);
+  if (p.group <= 16 && rows <= 16 * B) return launch<DP, 8>(p, dev, stream);
+  if (p.group <= 32 && rows <= 32 * B) return launch<DP, 16>(p, dev, stream);
+  return launch<DP, 36>(p, dev, stream);
+}
+
+}  // namespace
+
+bool attend_fp8_tc_supported(const AttendArgs& a) {
+  const retrace_kv_cache& c = a.cache;
+  auto whole = [](long long x, int n) { return x % n == 0; };
+  auto stride = [&](long long x, int extent) { return extent <= 1 || (x > 0 && whole(x, 16)); };
+  return a.dtype == RETRACE_BF16 && c.head_dim <= 128 && whole(c.head_dim, 4) && whole(c.page_size, 8) && c.num_pages > 0 &&
+         a.q_heads / c.kv_heads <= 72 && stride(c.page_stride, c.num_pages) && stride(c.slot_stride, c.page_size) &&
+         stride(c.head_stride, c.kv_heads) && whole(a.q_token, 4) && whole(a.q_head, 4) && ((uintptr_t)a.q & 7u) == 0 &&
+         (((uintptr_t)c.k | (uintptr_t)c.v) & 15u) == 0;
+}
+
+size_t attend_fp8_tc_partial_bytes(int head_dim) {
+  if (head_dim > 128) return 0;
+  return (size_t)kAttendMaxTcCtas * 2 * (head_dim <= 64 ? TcShape<64, 36>::kPart : TcShape<128, 36>::kPart) * 4;
+}
+
+cudaError_t launch_attend_fp8_tc(const AttendArgs& a, cudaStream_t stream) {
+  DeviceInfo dev;
+  const cudaError_t e = device_info(&dev);
+  if (e != cudaSuccess) return e;
+  TcParams p{};
+  p.a = a;
+  const retrace_kv_cache& c = a.cache;
+  p.group = a.q_heads / c.kv_heads;
+  p.by_group = FastDivide::of(p.group);
+  p.page_size = FastDivide::of(c.page_size);
+  p.kv_box = gcd(c.page_size, kKeys);
+  p.scale2 = a.scale * 1.4426950408889634f;
+  p.shape.q_start = a.q_start;
+  p.shape.cache_len = a.cache_len;
+  p.shape.B = a.B;
+  p.shape.T = a.T;
+  p.shape.uniform = a.q_start ? 0 : a.T / a.B;
+  p.shape.kv_heads = c.kv_heads;
+  p.shape.causal = a.causal;
+  p.shape.window = a.window;
+  p.shape.sinks = a.sinks;
+  p.shape.places = c.max_pages * c.page_size;
+  return c.head_dim <= 64 ? launch_rows<64>(p, dev, stream) : launch_rows<128>(p, dev, stream);
+}
+
+}  // namespace retrace

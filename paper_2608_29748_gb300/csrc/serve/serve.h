@@ -97,6 +97,9 @@ size_t attend_simt_partial_bytes(int head_dim);
 cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t stream);
 size_t attend_tc_partial_bytes(int head_dim);
 bool attend_tc_supported(const AttendArgs& a);
+cudaError_t launch_attend_fp8_tc(const AttendArgs& a, cudaStream_t stream);
+size_t attend_fp8_tc_partial_bytes(int head_dim);
+bool attend_fp8_tc_supported(const AttendArgs& a);
 
 struct SampleArgs {
   const void* logits;

@@ -174,7 +174,9 @@ size_t retrace_attend_workspace_bytes(int q_heads, int kv_heads, int head_dim, r
   if (kv_heads < 1 || q_heads < 1 || q_heads % kv_heads || head_dim < 1 || head_dim > kMaxHeadDim ||
       (!dtype_ok(dtype) && dtype != RETRACE_E4M3))
     return 0;
-  const size_t tc = dtype == RETRACE_BF16 ? attend_tc_partial_bytes(head_dim) : 0;
+  const size_t tc = dtype == RETRACE_BF16   ? attend_tc_partial_bytes(head_dim)
+                    : dtype == RETRACE_E4M3 ? attend_fp8_tc_partial_bytes(head_dim)
+                                            : 0;
   return kAttendPartials + std::max(attend_simt_partial_bytes(head_dim), tc);
 }
 
@@ -254,7 +256,7 @@ retrace_status retrace_attend_fp8(const void* q, int64_t q_token_stride, int64_t
   a.exp_page = cache->exp_page_stride;
   a.exp_head = cache->exp_head_stride;
   if ((st = use_workspace(&a, ws, ws_bytes)) != RETRACE_OK) return st;
-  const cudaError_t e = launch_attend_simt_fp8(a, stream);
+  const cudaError_t e = attend_fp8_tc_supported(a) ? launch_attend_fp8_tc(a, stream) : launch_attend_simt_fp8(a, stream);
   return e == cudaSuccess ? RETRACE_OK : cuda_fail(e, "attention kernel launch");
 }
 
