@@ -9,10 +9,9 @@
 //     O^T += V^T P^T   [head dim, rows]: V as it lies; a weight is the sum of three e5m2 numbers of 3
 //                      bits each, in columns of their own.
 // e5m2 is the upper byte of an fp16 number, so the first two parts of a weight are bytes of it and of
-// what is left, and the last is rounded: 9 bits in all where a bf16 weight has 8, down to 2^-9,
-// and multiples of 2^-16 below.  m is chosen so that the largest weight of a row's first tile is 2^9, and
-// raised (O and l rescaled) when one passes 2^15; so a weight is off by at most 2^-9 of it or 2^-26 of
-// the row's largest.
+// what is left, and the last, times 2^5, is rounded: 9 bits in all, where a bf16 weight has 8, or multiples
+// of 2^-21.  m is chosen so that the largest weight of a row's first tile is 2^4, and raised (O and l
+// rescaled) when one passes 2^15; so a weight is off by at most 2^-9 of it or 2^-26 of the row's largest.
 // Nothing is converted but the queries, once, and the weights: keys and values go from HBM to shared
 // memory to the tensor core, 256 D bytes a tile, 1400 cycles of an SM's share of HBM at D = 128.  The
 // products are 4 (2 rows + 3 rows) cycles at D = 128, shared memory moves some 1100 cycles' worth at
@@ -38,7 +37,7 @@ constexpr int kKeys = 128;  // keys of a tile
 constexpr unsigned long long kDrainNs = 20ull * 1000ull * 1000ull;
 constexpr int kInfoTiles = 16;  // ring of tiles' units: more than the tiles between loading and softmax
 constexpr int kMostBoxes = 16;  // of a tile: pages of 8 slots
-constexpr float kFirstTop = 9.f, kMostTop = 15.f;
+constexpr float kFirstTop = 4.f, kMostTop = 15.f;
 constexpr float kNone = 1e30f;  // minus the reference of a row that has seen nothing
 
 struct TcParams {
@@ -90,7 +89,7 @@ struct Control {
   uint64_t q_full[2], q_empty[2];
   uint64_t s_full[2];   // scores ready
   uint64_t p_full[2];   // weights written, the scores' buffer read
-  uint64_t pv_done[2];  // the product with V done, the weights' buffer free
+  uint64_t pv_done[2];  // the product with V done
   uint64_t done;        // after an expired wait: the issued products
   PlanStart plan;
   long long sum[kThreads / 32];
@@ -154,6 +153,11 @@ __device__ __forceinline__ void tmem_load(uint32_t at, float* v) {
 __device__ __forceinline__ void tmem_store4(uint32_t at, const float* v) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]) : "memory");
 }
+__device__ __forceinline__ float warp_max(float x) {
+  float y;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
+}
 // 128 threads' agreement on whether any of them says so.
 __device__ __forceinline__ bool any_of_half(int half, bool mine) {
   uint32_t p = mine;
@@ -181,20 +185,24 @@ __device__ __forceinline__ uint32_t minus_halves(uint32_t a, uint32_t b) {
   const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
   return *reinterpret_cast<const uint32_t*>(&h);
 }
+__device__ __forceinline__ uint32_t times_32(uint32_t a) {
+  const __half2 h = __hmul2(*reinterpret_cast<const __half2*>(&a), __float2half2_rn(32.f));
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
 __device__ __forceinline__ uint32_t to_e5m2x2(uint32_t h) {
   __half2_raw r;
   r.x = (unsigned short)(h & 0xFFFFu);
   r.y = (unsigned short)(h >> 16);
   return __nv_cvt_halfraw2_to_fp8x2(r, __NV_SATFINITE, __NV_E5M2);
 }
-// The three parts of four weights, none negative, a byte each.
+// The three parts of four weights, none negative, a byte each; the third times 2^5.
 __device__ __forceinline__ void take_apart(const float (&w)[4], uint32_t& first, uint32_t& second, uint32_t& third) {
   const uint32_t a = halves(w[0], w[1]), b = halves(w[2], w[3]);
   const uint32_t a1 = minus_halves(a, a & 0xFF00FF00u), b1 = minus_halves(b, b & 0xFF00FF00u);
   const uint32_t a2 = minus_halves(a1, a1 & 0xFF00FF00u), b2 = minus_halves(b1, b1 & 0xFF00FF00u);
   first = __byte_perm(a, b, 0x7531);
   second = __byte_perm(a1, b1, 0x7531);
-  third = to_e5m2x2(a2) | to_e5m2x2(b2) << 16;
+  third = to_e5m2x2(times_32(a2)) | to_e5m2x2(times_32(b2)) << 16;
 }
 
 template <int I>
@@ -261,59 +269,69 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok = true, drain = false;
     if (warp < 4) {
       // ---- copies of K (warps 0, 1) and V (2, 3): every other box each ----
+      // Lane (tile, box) looks up and copies a box of each of a batch of tiles.  What it reads for
+      // the next batch is not used before the present one has been copied: the warp would wait for it.
       const int ring = warp / 2, turn = warp % 2;
       const bool keys = ring == 0;
       const CUtensorMap* map = keys ? &tm_k : &tm_v;
-      const int boxes = kKeys / P.kv_box, box = lane * 2 + turn, mine = (boxes + 1 - turn) / 2;
-      const bool active = box < boxes;
+      const int boxes = kKeys / P.kv_box, mine = (boxes + 1 - turn) / 2;
+      const int batch = min(32 / max(mine, 1), 8), my_tile = mine > 0 ? lane / mine : 32, box = mine > 0 ? lane % mine * 2 + turn : 0;
       const uint32_t slots = keys ? Sh::kRingK : Sh::kRingV, tiles_at = base + (keys ? 0 : Sh::kVAt);
       uint32_t tiles = 0, slot = 0, phase = 0;
+      struct Lookup {
+        int slot;          // within the page
+        bool listed;       // the table has an entry for it
+        const int32_t* at;
+      };
+      auto lookup = [&](int k) {  // of this lane's box of tile k + my_tile of the piece
+        Lookup x{0, false, a.cache.page_table};
+        k += my_tile;
+        if (my_tile < batch && k < pc.k1 - pc.k0) {
+          const int j = pc.keys.tile(pc.k0 + k) * kKeys + box * P.kv_box, i = P.page_size(j);
+          x.slot = j - i * P.page_size.by;
+          x.listed = i < a.cache.max_pages;
+          if (x.listed) x.at += pc.b * a.cache.table_stride + i;
+        }
+        return x;
+      };
       while (ok && walk.next<kKeys>(P.shape, plan, &pc)) {
         const int nt = pc.k1 - pc.k0;
         if (nt == 0) continue;
-        struct Place {
-          int page, slot;
-        };
-        auto place_of = [&](int k) {  // of this lane's box of the piece's tile k
-          Place x{a.cache.num_pages, 0};  // a box without a page lies outside the tensor: zeros
-          if (active && k < nt) {
-            const int j = pc.keys.tile(pc.k0 + k) * kKeys + box * P.kv_box, i = P.page_size(j);
-            const int page = page_of(a.cache, pc.b, i);
-            if (page >= 0) x = Place{page, j - i * P.page_size.by};
+        Lookup now = lookup(0);
+        int page = now.listed ? *now.at : -1;
+        for (int k = 0; k < nt && ok; k += batch) {
+          // a box without a page lies outside the tensor: zeros
+          if (page < 0 || page >= a.cache.num_pages) page = a.cache.num_pages;
+          const bool there = page < a.cache.num_pages;
+          int ke = 0, ve = 0;
+          if (keys && there) {
+            const long long at = page * a.exp_page + pc.head * a.exp_head;
+            ke = a.k_exp[at];
+            ve = a.v_exp[at];
           }
-          return x;
-        };
-        auto units_of_box = [&](const Place& x) {
-          BoxUnits u{1.f, 0.f, 1.f, 0};
-          if (keys && x.page < a.cache.num_pages) {
-            const int ve = page_exponent(a, a.v_exp, x.page, pc.head);
-            u = BoxUnits{power_of_two(page_exponent(a, a.k_exp, x.page, pc.head)), (float)ve, power_of_two(-ve), 1};
+          const Lookup next = lookup(k + batch);
+          const int next_page = next.listed ? *next.at : -1;
+          for (int t = 0; t < min(batch, nt - k); ++t) {
+            ok = warp_wait_all(&ct.empty[ring][slot], phase ^ 1u, abort);
+            if (!ok) break;
+            const uint32_t bar = smem_u32(&ct.full[ring][slot]);
+            const bool active = my_tile == t;
+            if (keys && active)
+              ct.units[tiles % kInfoTiles][box] = there ? BoxUnits{power_of_two(clamp_exponent(ke)), (float)clamp_exponent(ve), power_of_two(-clamp_exponent(ve)), 1}
+                                                        : BoxUnits{1.f, 0.f, 1.f, 0};
+            __syncwarp();
+            if (lane == 0) mbar_arrive_expect_tx(bar, mine * P.kv_box * DP);
+            __syncwarp();
+            if (active)
+              tma_load_4d(tiles_at + slot * Sh::kTileBytes + box * P.kv_box * DP, map, 0, pc.head, now.slot, page, bar);
+            if (++slot == slots) {
+              slot = 0;
+              phase ^= 1u;
+            }
+            ++tiles;
           }
-          return u;
-        };
-        // pages are looked up two tiles ahead of their copies, their exponents one
-        Place now = place_of(0), next = place_of(1);
-        BoxUnits units = units_of_box(now);
-        for (int k = 0; k < nt && ok; ++k) {
-          const Place after = place_of(k + 2);
-          const BoxUnits units_next = units_of_box(next);
-          ok = warp_wait_all(&ct.empty[ring][slot], phase ^ 1u, abort);
-          if (!ok) break;
-          const uint32_t bar = smem_u32(&ct.full[ring][slot]);
-          if (keys && active) ct.units[tiles % kInfoTiles][box] = units;
-          __syncwarp();
-          if (lane == 0) mbar_arrive_expect_tx(bar, mine * P.kv_box * DP);
-          __syncwarp();
-          if (active)
-            tma_load_4d(tiles_at + slot * Sh::kTileBytes + box * P.kv_box * DP, map, 0, pc.head, now.slot, now.page, bar);
-          if (++slot == slots) {
-            slot = 0;
-            phase ^= 1u;
-          }
-          ++tiles;
           now = next;
-          next = after;
-          units = units_next;
+          page = next_page;
         }
       }
       drain = !ok;
@@ -584,18 +602,23 @@ __global__ void __launch_bounds__(kThreads, 1)
               if (r < from || r >= to) y[r] = -INFINITY;
           }
         };
-        exponents(true);
-        float top = -INFINITY;
+        // The first tile sets the references.  After it a weight may outgrow its own, or a row may see its
+        // first keys: then, too, the rows' maxima over the tile, new references, and what was summed so far
+        // in the new unit.
+        bool raise = j == 0;
+        if (j > 0) {
+          exponents(true);
+          float top = -INFINITY;
 #pragma unroll
-        for (int r = 0; r < kHalf; r += 2) top = max3(top, y[r], y[r + 1]);
-        if (any_of_half(h, top > kMostTop)) {
-          // A weight has outgrown its reference, or a row sees its first keys: the rows' maxima over
-          // the tile, new references, and what was summed so far in the new unit.
+          for (int r = 0; r < kHalf; r += 2) top = max3(top, y[r], y[r + 1]);
+          raise = any_of_half(h, top > kMostTop);
+        }
+        if (raise) {
           exponents(false);
 #pragma unroll
           for (int r = 0; r < kHalf; ++r) {
-            const uint32_t most = __reduce_max_sync(0xFFFFFFFFu, ordered_bits(y[r]));
-            if (lane == 0) ct.part[h][quarter][r] = __uint_as_float(most & 0x80000000u ? most & 0x7FFFFFFFu : ~most);
+            const float most = warp_max(y[r]);
+            if (lane == 0) ct.part[h][quarter][r] = most;
           }
           half_barrier(h);
           if (key < kHalf) {
@@ -610,34 +633,37 @@ __global__ void __launch_bounds__(kThreads, 1)
             ct.scale[r0 + key] = f;
           }
           half_barrier(h);
-#pragma unroll
-          for (int r = 0; r < kHalf; r += 2) l[r / 2] = mul2(l[r / 2], *reinterpret_cast<const float2*>(ct.scale + r0 + r));
           if (j > 0) {
+#pragma unroll
+            for (int r = 0; r < kHalf; r += 2) l[r / 2] = mul2(l[r / 2], *reinterpret_cast<const float2*>(ct.scale + r0 + r));
             const uint32_t before = g - 1;
             wait(&ct.pv_done[before & 1u], before >> 1 & 1u);
             tc_fence_after();
             each_chunk<Sh::kChunks>([&](auto chunk) {
               constexpr int c = decltype(chunk)::value, n = Sh::rows_of(c);
 #pragma unroll
-              for (int part = 0; part < 3; ++part)
+              for (int part = 0; part < 3; ++part) {
+                float o[n];
+                tmem_load<n>(t_o + 48 * c + part * n, o);
+                tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < n; i += 4) {
-                  float o[4];
-                  const uint32_t column = t_o + 48 * c + part * n + i;
-                  tmem_load<4>(column, o);
-                  tmem_wait_ld();
+                for (int i = 0; i < n; ++i) o[i] *= ct.scale[r0 + 16 * c + i];
 #pragma unroll
-                  for (int e = 0; e < 4; ++e) o[e] *= ct.scale[r0 + 16 * c + i + e];
-                  tmem_store4(column, o);
-                }
+                for (int i = 0; i < n; i += 4) tmem_store4(t_o + 48 * c + part * n + i, o + i);
+              }
             });
             tmem_wait_st();
           }
-          exponents(true);
+#pragma unroll
+          for (int r = 0; r < kHalf; r += 2) {
+            const float2 x = add2(make_float2(y[r], y[r + 1]), *reinterpret_cast<const float2*>(minus + r));
+            y[r] = x.x;
+            y[r + 1] = x.y;
+          }
         }
 
-        // The weights' buffer is free when the product of two tiles ago is done.
-        if (g >= 2) wait(&ct.pv_done[b], (g >> 1 & 1u) ^ 1u);
+        // The weights' buffer is free: its product was issued before the scores of this tile, and a commit
+        // waits for all that was issued before it.
         uint8_t* weights = smem + Sh::kPAt + b * Sh::kPBytes + key * 128;
         const float2 inv2 = make_float2(u.inv, u.inv);
         each_chunk<Sh::kChunks>([&](auto chunk) {
@@ -715,7 +741,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int i = 0; i < n; ++i) {
             const int r = r0 + 16 * c + i;
             if (r >= rows || key >= DP) break;  // `key` is the lane: the element of the head
-            const float x = (o[i] + (o[n + i] + o[2 * n + i])) * ct.scale[r];
+            const float x = (o[i] + (o[n + i] + o[2 * n + i] * 0.03125f)) * ct.scale[r];
             if (!whole)
               part[r * DP + key] = x;
             else if (key < D)
@@ -747,8 +773,10 @@ cudaError_t launch(TcParams& p, const DeviceInfo& dev, cudaStream_t stream) {
   const long long strides[4] = {1, c.head_stride, c.slot_stride, c.page_stride};
   const int box[4] = {DP, 1, p.kv_box, 1};
   const CUtensorMapSwizzle swizzle = DP == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
-  if (!encode(&mk, c.k, 4, dims, strides, box, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, swizzle) ||
-      !encode(&mv, c.v, 4, dims, strides, box, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, swizzle))
+  // A row of a head is all that lies together: what L2 would fetch beyond it is another head's.
+  const CUtensorMapL2promotion promotion = DP == 128 ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_64B;
+  if (!encode(&mk, c.k, 4, dims, strides, box, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, swizzle, promotion) ||
+      !encode(&mv, c.v, 4, dims, strides, box, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, swizzle, promotion))
     return cudaErrorInvalidValue;
   constexpr size_t smem = Sh::kControl + sizeof(Control<kHalf>);
   static_assert(smem <= 227 * 1024, "shared memory of a CTA");

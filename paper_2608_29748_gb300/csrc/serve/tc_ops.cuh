@@ -100,7 +100,8 @@ EncodeFn encode_fn() {
 // first; bf16 with the 128-byte swizzle if nothing else is said.
 bool encode(CUtensorMap* map, const void* base, int rank, const long long* dims, const long long* strides, const int* box,
             CUtensorMapDataType type = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, int size = 2,
-            CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
+            CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B,
+            CUtensorMapL2promotion promotion = CU_TENSOR_MAP_L2_PROMOTION_L2_256B) {
   EncodeFn fn = encode_fn();
   if (!fn) return false;
   cuuint64_t d[4], st[3];
@@ -112,7 +113,7 @@ bool encode(CUtensorMap* map, const void* base, int rank, const long long* dims,
     if (i > 0) st[i - 1] = dims[i] > 1 ? (cuuint64_t)strides[i] * size : 16;  // the stride of a single one is not used
   }
   return fn(map, type, (cuuint32_t)rank, const_cast<void*>(base), d, st, b, one,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, promotion,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
