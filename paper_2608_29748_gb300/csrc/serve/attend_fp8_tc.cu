@@ -19,9 +19,10 @@
 // it scales with the rows that there are.
 //
 // Warps 0 and 1 copy K, 2 and 3 V (TMA boxes of the slots of a page, dealt out by turns); warp 4 issues
-// the products; warps 5-7 take the queries apart, a piece ahead; warps 8-15 are the softmax,
-// warps 8-11 of the first half of the rows and 12-15 of the second.  S and P have two buffers: the
-// scores of a tile are computed during the softmax of the one before.
+// the scores' products, warp 5 those with V; warps 6 and 7 take the queries apart, a piece ahead.  The softmax has groups of four
+// warps, a thread to a key.  Up to 32 rows, two groups take the even and the odd tiles, each
+// with references, sums and an O of its own, joined at the end: a tile's way through a group is
+// latency, twice what its bytes take.  For 72 rows three groups have 24 rows each of every tile.
 #include <math.h>
 
 #include "attend_plan.cuh"
@@ -32,13 +33,14 @@
 namespace retrace {
 namespace {
 
-constexpr int kThreads = 512;
 constexpr int kKeys = 128;  // keys of a tile
 constexpr unsigned long long kDrainNs = 20ull * 1000ull * 1000ull;
 constexpr int kInfoTiles = 16;  // ring of tiles' units: more than the tiles between loading and softmax
 constexpr int kMostBoxes = 16;  // of a tile: pages of 8 slots
+constexpr int kBase = 256;      // threads before the softmax's
 constexpr float kFirstTop = 4.f, kMostTop = 15.f;
-constexpr float kNone = 1e30f;  // minus the reference of a row that has seen nothing
+constexpr float kNone = 1e30f;     // in place of the reference of a row that has seen nothing
+constexpr float kFar = 4194304.f;  // 2^22: references up to it are whole numbers, and sums of two are exact
 
 struct TcParams {
   AttendArgs a;
@@ -49,30 +51,40 @@ struct TcParams {
   float scale2;  // scale log2(e)
 };
 
-// kHalf rows to each of the two softmax warpgroups, in chunks of 16 (the last of 4: 36 = 16 + 16 + 4).
-template <int DP, int kHalf>
+// R rows to a thread of the softmax, in chunks of 16 (the last may be of 8).  Two streams (`kStreams`
+// 2): a group has every other tile and all rows; one: the groups share the rows of every tile.
+template <int DP, int R>
 struct TcShape {
-  static constexpr int kRows = 2 * kHalf;
-  static constexpr int kChunks = (kHalf + 15) / 16;
-  __host__ __device__ static constexpr int rows_of(int chunk) { return kHalf - 16 * chunk < 16 ? kHalf - 16 * chunk : 16; }
-  // Columns of a half: of S 2 a row (the two parts of a chunk's queries side by side), of O 3 a row,
-  // a chunk's rounded up to 16.
-  static constexpr int kS = 2 * kHalf;
-  static constexpr int kO = 48 * (kChunks - 1) + (3 * rows_of(kChunks - 1) + 15) / 16 * 16;
-  static constexpr int kSColumns = 2 * kS, kOColumns = 2 * kO;
-  static_assert(kSColumns % 16 == 0 && kOColumns % 16 == 0 && kOColumns <= 256, "columns of a product");
-  static constexpr int kOAt = 2 * kSColumns;
-  static_assert(kOAt + kOColumns <= 512, "columns of TMEM");
+  static constexpr int kStreams = R == 24 ? 1 : 2, kGroups = R == 24 ? 3 : 2;
+  static constexpr int kThreads = kBase + 128 * kGroups;
+  static constexpr int kRows = kStreams == 2 ? R : R * kGroups;
+  static constexpr int kBuffers = 2 * kStreams;  // of S and P
+  static constexpr int kChunks = (R + 15) / 16;
+  __host__ __device__ static constexpr int rows_of(int chunk) { return R - 16 * chunk < 16 ? R - 16 * chunk : 16; }
+  // Columns of S: 2 a row, the two parts of a chunk's queries side by side, group after group.
+  static constexpr int kSGroup = 2 * R, kSColumns = kStreams == 2 ? kSGroup : kSGroup * kGroups;
+  // Columns of O (and of P): 3 a row; all groups' first chunks, then all second ones.
+  static constexpr int kShare = kStreams == 2 ? 1 : kGroups;
+  __host__ __device__ static constexpr int o_column(int group, int chunk) {
+    return 48 * kShare * chunk + 3 * rows_of(chunk) * (kStreams == 2 ? 0 : group);
+  }
+  static constexpr int kOColumns = (3 * R * kShare + 15) / 16 * 16;
+  static_assert(kSColumns % 16 == 0 && kOColumns <= 256, "columns of a product");
+  static constexpr int kOAt = kBuffers * kSColumns;
+  static_assert(kOAt + kStreams * kOColumns <= 512, "columns of TMEM");
+  // Registers of a thread: the launch's, and what the softmax takes of the others'.
+  static constexpr int kFewer = kGroups == 3 ? 56 : 64, kMore = kGroups == 3 ? 120 : 192;
+  static_assert(kBase * kFewer + 128 * kGroups * kMore <= kThreads * (65536 / kThreads / 8 * 8), "registers of a CTA");
 
   static constexpr int kTileBytes = kKeys * DP;
-  static constexpr int kPAtoms = (kOColumns + 127) / 128;      // 128-byte columns of P
+  static constexpr int kPAtoms = (kOColumns + 127) / 128;  // 128-byte columns of P
   static constexpr int kPBytes = kPAtoms * kKeys * 128;
   static constexpr int kQBytes = (kSColumns * DP + 1023) / 1024 * 1024;
   static constexpr int kControlBytes = 12 * 1024;
-  static constexpr int kRoom = (227 * 1024 - kControlBytes - 2 * kPBytes - 2 * kQBytes) / kTileBytes;
+  static constexpr int kRoom = (227 * 1024 - kControlBytes - kBuffers * kPBytes - 2 * kQBytes) / kTileBytes;
   static constexpr int kRingV = (kRoom + 1) / 2 < 8 ? (kRoom + 1) / 2 : 8, kRingK = kRoom / 2 < 8 ? kRoom / 2 : 8;
-  static_assert(kRingK >= 3 && kRingV >= 4, "tiles in flight");
-  static constexpr int kVAt = kRingK * kTileBytes, kPAt = kVAt + kRingV * kTileBytes, kQAt = kPAt + 2 * kPBytes;
+  static_assert(kRingK >= 3 && kRingV >= kBuffers, "tiles in flight");
+  static constexpr int kVAt = kRingK * kTileBytes, kPAt = kVAt + kRingV * kTileBytes, kQAt = kPAt + kBuffers * kPBytes;
   static constexpr int kControl = kQAt + 2 * kQBytes;
   static constexpr int kPart = kRows * (DP + 2);  // floats of a part
 };
@@ -83,27 +95,29 @@ struct BoxUnits {
   int there;  // has a page
 };
 
-template <int kHalf>
+template <int R>
 struct Control {
   uint64_t full[2][8], empty[2][8];  // rings of K and V
   uint64_t q_full[2], q_empty[2];
-  uint64_t s_full[2];   // scores ready
-  uint64_t p_full[2];   // weights written, the scores' buffer read
-  uint64_t pv_done[2];  // the product with V done
-  uint64_t done;        // after an expired wait: the issued products
+  uint64_t s_full[4];   // scores ready
+  uint64_t p_full[4];   // weights written, the scores' buffer read
+  uint64_t pv_done[4];  // the product with V done
+  uint64_t done[2];     // after an expired wait: the issued products
   PlanStart plan;
-  long long sum[kThreads / 32];
+  long long sum[(kBase + 384) / 32];
   uint32_t tmem;
   int abort;
-  PieceWalk walk[2];  // of the softmax warpgroups
-  Piece piece[2][2];  // this one and the next
-  int more[2][2];
+  PieceWalk walk[3];  // of the softmax groups
+  Piece piece[3][2];  // this one and the next
+  int more[3][2];
   BoxUnits units[kInfoTiles][kMostBoxes];
-  alignas(16) float factor[2][2 * kHalf];  // of a row: scale log2(e) times its queries' unit
-  long long out[2][2 * kHalf];             // where a row goes, elements
-  alignas(16) float minus[2 * kHalf];      // minus a row's reference
-  alignas(16) float scale[2 * kHalf];      // of a raised row's sums; at the end 1 / sum
-  float part[2][4][kHalf];                 // per warp: a row's maximum, or sum
+  alignas(16) float factor[2][72];  // of a row: scale log2(e) times its queries' unit
+  long long out[2][72];             // where a row goes, elements
+  // Of a group's rows: what is added to exponents (minus the reference), and, where that is far from
+  // zero, added to the difference; how the reference moves; at the end the factors of the streams' O.
+  alignas(16) float minus[3][R], rest[3][R], move[3][R];
+  alignas(16) float scale[3][R];
+  float part[3][4][R];  // per warp: a row's maximum, or sum
 };
 
 // ---- instructions -------------------------------------------------------------
@@ -153,13 +167,23 @@ __device__ __forceinline__ void tmem_load(uint32_t at, float* v) {
 __device__ __forceinline__ void tmem_store4(uint32_t at, const float* v) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]) : "memory");
 }
-__device__ __forceinline__ float warp_max(float x) {
-  float y;
-  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
-  return y;
+// Rows (N of them) over the lanes of a warp by `join`: each step halves the rows that a lane has.  Lane i
+// ends with row i % N, in v[0].
+template <int N, typename Join>
+__device__ __forceinline__ void join_lanes(float* v, int lane, Join&& join) {
+#pragma unroll
+  for (int o = N / 2; o > 0; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < o; ++i) {
+      const bool upper = lane & o;
+      const float other = __shfl_xor_sync(0xFFFFFFFFu, upper ? v[i] : v[i + o], o);
+      v[i] = join(upper ? v[i + o] : v[i], other);
+    }
+#pragma unroll
+  for (int o = N; o < 32; o <<= 1) v[0] = join(v[0], __shfl_xor_sync(0xFFFFFFFFu, v[0], o));
 }
-// 128 threads' agreement on whether any of them says so.
-__device__ __forceinline__ bool any_of_half(int half, bool mine) {
+// A group's agreement on whether any of its threads says so.
+__device__ __forceinline__ bool any_of_group(int group, bool mine) {
   uint32_t p = mine;
   asm volatile(
       "{\n\t.reg .pred p, q;\n\t"
@@ -167,15 +191,21 @@ __device__ __forceinline__ bool any_of_half(int half, bool mine) {
       "barrier.cta.red.or.pred q, %1, 128, p;\n\t"
       "selp.u32 %0, 1, 0, q;\n\t}"
       : "+r"(p)
-      : "r"(2 + half)
+      : "r"(2 + group)
       : "memory");
   return p != 0;
 }
-__device__ __forceinline__ void half_barrier(int half) { asm volatile("bar.sync %0, 128;" ::"r"(2 + half) : "memory"); }
+__device__ __forceinline__ void group_barrier(int group) { asm volatile("bar.sync %0, 128;" ::"r"(2 + group) : "memory"); }
 
-// Registers from the copies, products and queries to the softmax: 256 x 64 + 256 x 192 are the launch's 512 x 128.
-__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 64;"); }
-__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 192;"); }
+// Registers from the copies, products and queries to the softmax.
+template <int kCount>
+__device__ __forceinline__ void fewer_registers() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kCount));
+}
+template <int kCount>
+__device__ __forceinline__ void more_registers() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kCount));
+}
 
 __device__ __forceinline__ uint32_t halves(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
@@ -217,14 +247,15 @@ __device__ __forceinline__ void each_chunk(F&& f) {
   }
 }
 
-template <int DP, int kHalf>
-__global__ void __launch_bounds__(kThreads, 1)
+template <int DP, int R>
+__global__ void __launch_bounds__(TcShape<DP, R>::kThreads, 1)
     attend_fp8_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                          const __grid_constant__ TcParams P) {
-  using Sh = TcShape<DP, kHalf>;
-  static_assert(sizeof(Control<kHalf>) <= Sh::kControlBytes, "room of the control block");
+  using Sh = TcShape<DP, R>;
+  constexpr int kThreads = Sh::kThreads, kBuffers = Sh::kBuffers;
+  static_assert(sizeof(Control<R>) <= Sh::kControlBytes, "room of the control block");
   extern __shared__ __align__(1024) uint8_t smem[];
-  Control<kHalf>& ct = *reinterpret_cast<Control<kHalf>*>(smem + Sh::kControl);
+  Control<R>& ct = *reinterpret_cast<Control<R>*>(smem + Sh::kControl);
   volatile int* abort = &ct.abort;
   const uint32_t base = smem_u32(smem);
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
@@ -238,13 +269,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         mbar_init(smem_u32(&ct.empty[r][s]), 1);
       }
     for (int s = 0; s < 2; ++s) {
-      mbar_init(smem_u32(&ct.q_full[s]), 3);
-      mbar_init(smem_u32(&ct.q_empty[s]), 9);  // the products, and the softmax warps
+      mbar_init(smem_u32(&ct.done[s]), 1);
+      mbar_init(smem_u32(&ct.q_full[s]), 2);
+      mbar_init(smem_u32(&ct.q_empty[s]), 1 + 4 * Sh::kGroups);  // the products, and the softmax warps
+    }
+    for (int s = 0; s < 4; ++s) {
       mbar_init(smem_u32(&ct.s_full[s]), 1);
-      mbar_init(smem_u32(&ct.p_full[s]), 8);
+      mbar_init(smem_u32(&ct.p_full[s]), 4 * Sh::kGroups / Sh::kStreams);  // the warps that have the tile
       mbar_init(smem_u32(&ct.pv_done[s]), 1);
     }
-    mbar_init(smem_u32(&ct.done), 1);
     fence_mbar_init();
     tma_prefetch_desc(&tm_k);
     tma_prefetch_desc(&tm_v);
@@ -262,7 +295,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   plan_start<kThreads, kKeys>(P.shape, gridDim.x, 2, &ct.plan, ct.sum);
   const PlanStart& plan = ct.plan;
   if (warp < 8) {
-    fewer_registers();
+    fewer_registers<Sh::kFewer>();
     PieceWalk walk;
     walk.start(plan);
     Piece pc;
@@ -312,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const Lookup next = lookup(k + batch);
           const int next_page = next.listed ? *next.at : -1;
           for (int t = 0; t < min(batch, nt - k); ++t) {
-            ok = warp_wait_all(&ct.empty[ring][slot], phase ^ 1u, abort);
+            ok = warp_wait_quick(&ct.empty[ring][slot], phase ^ 1u, abort);
             if (!ok) break;
             const uint32_t bar = smem_u32(&ct.full[ring][slot]);
             const bool active = my_tile == t;
@@ -335,73 +368,69 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       drain = !ok;
-    } else if (warp == 4) {
-      // ---- products ----
-      constexpr uint32_t kScores = idesc_8bit(Sh::kSColumns, false), kValues = idesc_8bit(Sh::kOColumns, true);
-      uint32_t tiles = 0, pieces = 0, v_seen = 0;
+    } else if (warp == 4 || warp == 5) {
+      // ---- products: scores (warp 4) and O (warp 5) ----
+      // Issuing a tile's products and commits takes some 500 cycles of a warp; one warp for both had
+      // 1100 a tile, and was the bound with few rows.
+      const bool values = warp == 5;
+      uint32_t tiles = 0, pieces = 0;
       auto wait = [&](uint64_t* bar, uint32_t parity) {
-        ok = ok && warp_wait_all(bar, parity, abort);
+        ok = ok && warp_wait_quick(bar, parity, abort);
         return ok;
-      };
-      auto commit = [&](uint64_t* bar) {
-        if (elect_one()) tc_commit(smem_u32(bar));
-        __syncwarp();
-      };
-      // V of all tiles up to this one has landed
-      auto wait_values = [&](uint32_t tile) {
-        for (; ok && v_seen <= tile; ++v_seen) wait(&ct.full[1][v_seen % Sh::kRingV], v_seen / Sh::kRingV & 1u);
-        return ok;
-      };
-      auto scores = [&](int i, uint32_t q) {
-        const uint32_t g = tiles + i, slot = g % Sh::kRingK;
-        if (!wait(&ct.full[0][slot], g / Sh::kRingK & 1u)) return;
-        // V of a tile at the edge of what the unit sees is there before its scores are: the softmax
-        // clears rows of it
-        const int j0 = pc.keys.tile(pc.k0 + i) * kKeys;
-        if ((j0 < pc.keys.lo || j0 + kKeys - 1 > pc.keys.hi) && !wait_values(g)) return;
-        tc_fence_after();
-        if (elect_one()) {
-          const uint64_t kd = rows_desc<DP>(base + slot * Sh::kTileBytes, 16), qd = rows_desc<DP>(base + Sh::kQAt + q * Sh::kQBytes, 16);
-#pragma unroll
-          for (int k = 0; k < DP / 32; ++k) tc_mma_8bit(tmem + (g & 1u) * Sh::kSColumns, kd + 2 * k, qd + 2 * k, kScores, k > 0);
-        }
-        __syncwarp();
-        commit(&ct.s_full[g & 1u]);
-        commit(&ct.empty[0][slot]);
       };
       while (ok && walk.next<kKeys>(P.shape, plan, &pc)) {
         const int nt = pc.k1 - pc.k0;
         if (nt == 0) continue;
         const uint32_t q = pieces & 1u;
-        if (!wait(&ct.q_full[q], pieces >> 1 & 1u)) break;
-        ++pieces;
-        scores(0, q);
-        if (ok && nt > 1) scores(1, q);
-        for (int i = 0; i < nt && ok; ++i) {
-          const uint32_t g = tiles + i, slot = g % Sh::kRingV;
-          if (!wait_values(g) || !wait(&ct.p_full[g & 1u], g >> 1 & 1u)) break;
-          tc_fence_after();
-          if (elect_one()) {
-            // 64 columns of the head dimension fill half of M: the other half is the same again
-            const uint64_t vd = rows_desc<DP>(base + Sh::kVAt + slot * Sh::kTileBytes, 0);
-            const uint64_t pd = rows_desc<128>(base + Sh::kPAt + (g & 1u) * Sh::kPBytes, kKeys * 128);
+        if (!values) {
+          constexpr uint32_t kDesc = idesc_8bit(Sh::kSColumns, false);
+          if (!wait(&ct.q_full[q], pieces >> 1 & 1u)) break;
+          for (int i = 0; i < nt; ++i) {
+            const uint32_t g = tiles + i, b = g % kBuffers, slot = g % Sh::kRingK;
+            if (!wait(&ct.full[0][slot], g / Sh::kRingK & 1u)) break;
+            if (g >= kBuffers && !wait(&ct.p_full[b], (g / kBuffers & 1u) ^ 1u)) break;  // S has been read
+            tc_fence_after();
+            if (elect_one()) {
+              const uint64_t kd = rows_desc<DP>(base + slot * Sh::kTileBytes, 16), qd = rows_desc<DP>(base + Sh::kQAt + q * Sh::kQBytes, 16);
 #pragma unroll
-            for (int k = 0; k < kKeys / 32; ++k)
-              tc_mma_8bit(tmem + Sh::kOAt, vd + k * (32 * DP >> 4), pd + k * (32 * 128 >> 4), kValues, i + k > 0);
+              for (int k = 0; k < DP / 32; ++k) tc_mma_8bit(tmem + b * Sh::kSColumns, kd + 2 * k, qd + 2 * k, kDesc, k > 0);
+              tc_commit(smem_u32(&ct.s_full[b]));
+              tc_commit(smem_u32(&ct.empty[0][slot]));
+            }
+            __syncwarp();
           }
+          if (!ok) break;
+          if (elect_one()) tc_commit(smem_u32(&ct.q_empty[q]));
           __syncwarp();
-          commit(&ct.pv_done[g & 1u]);
-          commit(&ct.empty[1][slot]);
-          if (i + 2 < nt) scores(i + 2, q);
+        } else {
+          constexpr uint32_t kDesc = idesc_8bit(Sh::kOColumns, true);
+          for (int i = 0; i < nt; ++i) {
+            const uint32_t g = tiles + i, b = g % kBuffers, slot = g % Sh::kRingV;
+            if (!wait(&ct.full[1][slot], g / Sh::kRingV & 1u) || !wait(&ct.p_full[b], g / kBuffers & 1u)) break;
+            tc_fence_after();
+            if (elect_one()) {
+              // 64 columns of the head dimension fill half of M: the other half is the same again
+              const uint64_t vd = rows_desc<DP>(base + Sh::kVAt + slot * Sh::kTileBytes, 0);
+              const uint64_t pd = rows_desc<128>(base + Sh::kPAt + b * Sh::kPBytes, kKeys * 128);
+              const uint32_t t_o = tmem + Sh::kOAt + i % Sh::kStreams * Sh::kOColumns;
+#pragma unroll
+              for (int k = 0; k < kKeys / 32; ++k)
+                tc_mma_8bit(t_o, vd + k * (32 * DP >> 4), pd + k * (32 * 128 >> 4), kDesc, i >= Sh::kStreams || k > 0);
+              tc_commit(smem_u32(&ct.pv_done[b]));
+              tc_commit(smem_u32(&ct.empty[1][slot]));
+            }
+            __syncwarp();
+          }
+          if (!ok) break;
         }
-        if (!ok) break;
-        commit(&ct.q_empty[q]);
+        ++pieces;
         tiles += nt;
       }
       if (!ok) {
         volatile int never = 0;
-        commit(&ct.done);
-        mbar_wait_bounded(smem_u32(&ct.done), 0, &never);
+        if (elect_one()) tc_commit(smem_u32(&ct.done[values]));
+        __syncwarp();
+        mbar_wait_bounded(smem_u32(&ct.done[values]), 0, &never);
       }
     } else {
       // ---- queries: rows of 128 or 64 bytes, each a sum of two e4m3 numbers times its row's unit ----
@@ -411,18 +440,18 @@ __global__ void __launch_bounds__(kThreads, 1)
       while (ok && walk.next<kKeys>(P.shape, plan, &pc)) {
         if (pc.k1 == pc.k0) continue;
         const uint32_t buffer = pieces & 1u;
-        ok = warp_wait_all(&ct.q_empty[buffer], (pieces >> 1 & 1u) ^ 1u, abort);
+        ok = warp_wait_quick(&ct.q_empty[buffer], (pieces >> 1 & 1u) ^ 1u, abort);
         if (!ok) break;
         ++pieces;
         const int rows = (pc.i1 - pc.i0) * P.group;
         uint8_t* to = smem + Sh::kQAt + buffer * Sh::kQBytes;
-        for (int r0 = warp - 5; r0 < Sh::kRows; r0 += 3 * 4) {
+        for (int r0 = warp - 6; r0 < Sh::kRows; r0 += 2 * 4) {
           // four rows' loads at a time
           uint32_t raw[4][kEach / 2];
           int token[4], head[4];
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
-            const int r = r0 + 3 * u;
+            const int r = r0 + 2 * u;
             token[u] = P.by_group(r);
             head[u] = r - token[u] * P.group;
             token[u] += pc.row0 + pc.i0;
@@ -439,7 +468,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
-            const int r = r0 + 3 * u;
+            const int r = r0 + 2 * u;
             if (r >= Sh::kRows) break;
             // magnitudes as whole numbers: infinities and NaN are the largest
             uint32_t most = 0u;
@@ -462,10 +491,10 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             if (nan) lead = 0x7F7F7F7Fu;
             // the columns of the row's two parts
-            const int half = r / kHalf, in = r % kHalf, chunk = in / 16, c = in % 16, size = min(16, kHalf - 16 * chunk);
+            const int group = r / R, in = r % R, chunk = in / 16, c = in % 16, size = min(16, R - 16 * chunk);
 #pragma unroll
             for (int part = 0; part < 2; ++part) {
-              const int n = half * Sh::kS + 32 * chunk + part * size + c, at = lane * kEach;
+              const int n = group * Sh::kSGroup + 32 * chunk + part * size + c, at = lane * kEach;
               const int chunk16 = DP == 128 ? (at / 16) ^ (n & 7) : (at / 16) ^ (n >> 1 & 3);
               uint8_t* dst = to + n * DP + chunk16 * 16 + at % 16;
               if constexpr (kEach == 4)
@@ -492,39 +521,39 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     __syncwarp();
   } else {
-    more_registers();
-    // ---- softmax: half h of the rows, one thread per key ----
-    const int h = warp >= 12, key = tid & 127, quarter = warp & 3, r0 = h * kHalf;
+    more_registers<Sh::kMore>();
+    // ---- softmax: group h, one thread per key ----
+    constexpr bool kTwo = Sh::kStreams == 2;
+    const int h = (warp - kBase / 32) / 4, key = tid & 127, quarter = warp & 3, r0 = kTwo ? 0 : h * R;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    const uint32_t t_o = tmem + lanes + Sh::kOAt + h * Sh::kO;
+    const uint32_t t_o = tmem + lanes + Sh::kOAt + (kTwo ? h * Sh::kOColumns : 0);
     const int D = a.cache.head_dim, G = P.group;
-    const float* minus = ct.minus + r0;
     uint32_t tiles = 0, pieces = 0;
     JoinUnit unit{};
     bool ok = true;
-    // After an expired wait a warp goes on without waiting, and writes nothing: the warps of a half meet
+    // After an expired wait a warp goes on without waiting, and writes nothing: the warps of a group meet
     // at the same barriers all the same.
     auto wait = [&](uint64_t* bar, uint32_t parity) {
-      if (ok && !warp_wait_all(bar, parity, abort)) {
+      if (ok && !warp_wait_quick(bar, parity, abort)) {
         ok = false;
         if (lane == 0) raise_abort(abort, a.status);
       }
     };
-    // One thread of the half walks, a piece ahead; the pieces stay in shared memory.
+    // One thread of the group walks, a piece ahead; the pieces stay in shared memory.
     const bool walker = key == 96;
     if (walker) {
       ct.walk[h].start(plan);
       ct.more[h][0] = ct.walk[h].template next<kKeys, true>(P.shape, plan, &ct.piece[h][0]);
     }
     for (int np = 0;; np ^= 1) {
-      half_barrier(h);
+      group_barrier(h);
       if (!ct.more[h][np]) break;
       if (walker) ct.more[h][np ^ 1] = ct.walk[h].template next<kKeys, true>(P.shape, plan, &ct.piece[h][np ^ 1]);
       const Piece& pc = ct.piece[h][np];
       const int nt = pc.k1 - pc.k0, rows = (pc.i1 - pc.i0) * G;
       if (nt == 0) {  // nothing is visible
-        for (int i = key; i < kHalf * D; i += 128) {
-          const int r = r0 + i / D, token = P.by_group(r);
+        for (int i = h * 128 + key; i < Sh::kRows * D; i += 128 * Sh::kGroups) {
+          const int r = i / D, token = P.by_group(r);
           if (r < rows)
             static_cast<__nv_bfloat16*>(a.out)[(long long)(pc.row0 + pc.i0 + token) * a.out_token +
                                                (pc.head * G + r - token * G) * (long long)a.out_head + i % D] = __float2bfloat16_rn(0.f);
@@ -536,17 +565,22 @@ __global__ void __launch_bounds__(kThreads, 1)
       ++pieces;
       const float* factor = ct.factor[buffer] + r0;
       // A row of the tile that holds no token refers to a number that no weight comes near.
-      if (key < kHalf) ct.minus[r0 + key] = r0 + key < rows ? kNone : -kNone;
-      half_barrier(h);
-      float2 l[kHalf / 2];  // sums of this thread's keys
+      if (key < R) {
+        ct.minus[h][key] = r0 + key < rows ? kNone : -kNone;
+        ct.rest[h][key] = 0.f;
+      }
+      group_barrier(h);
+      float2 l[R / 2];  // sums of this thread's keys
 #pragma unroll
-      for (int i = 0; i < kHalf / 2; ++i) l[i] = make_float2(0.f, 0.f);
+      for (int i = 0; i < R / 2; ++i) l[i] = make_float2(0.f, 0.f);
+      bool far = false;  // some row's reference is far from zero
       const UnitKeys keys = pc.keys;
       const int first = pc.c + pc.i0, k0 = pc.k0;  // position of the unit's first token
+      const bool idle = r0 >= rows;
 
-      for (int j = 0; j < nt; ++j) {
+      for (int j = kTwo ? h : 0; j < nt; j += Sh::kStreams) {
         // what is known of the tile before its scores are there
-        const uint32_t g = tiles + j, b = g & 1u;
+        const uint32_t g = tiles + j, b = g % kBuffers;
         const int j0 = keys.tile(k0 + j) * kKeys, at = j0 + key;
         const bool edge = j0 < keys.lo || j0 + kKeys - 1 > keys.hi;
         // The key is seen by the rows [from, to).
@@ -557,136 +591,193 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (at > keys.hi) to = 0;
         from -= r0;
         to -= r0;
-        wait(&ct.s_full[b], g >> 1 & 1u);
+        wait(&ct.s_full[b], g / kBuffers & 1u);
+        if (g >= kBuffers) wait(&ct.pv_done[b], (g / kBuffers & 1u) ^ 1u);  // the weights' buffer is free
         tc_fence_after();
         const BoxUnits u = ct.units[g % kInfoTiles][key / P.kv_box];
         if (!u.there) to = from = -1000;
-        const bool masked = !__all_sync(0xFFFFFFFFu, from <= 0 && to >= min(rows - r0, kHalf));
         // A row of V that no row of the unit sees holds anything, and 0 times that need not be 0:
-        // cleared before the product (V of such a tile landed before its scores were issued).
-        if (edge && (at > keys.hi || (at < keys.lo && at >= a.sinks))) {
-          uint8_t* v = smem + Sh::kVAt + (g % Sh::kRingV) * Sh::kTileBytes + key * DP;
+        // cleared before the product.
+        if (edge && (kTwo || h == 0)) {
+          // (the slot's phase before is over: its product was issued before the one waited for above)
+          wait(&ct.full[1][g % Sh::kRingV], g / Sh::kRingV & 1u);
+          if (at > keys.hi || (at < keys.lo && at >= a.sinks)) {
+            uint8_t* v = smem + Sh::kVAt + (g % Sh::kRingV) * Sh::kTileBytes + key * DP;
 #pragma unroll
-          for (int c = h; c < DP / 16; c += 2)  // half of the row each; the lanes begin at different banks
-            *reinterpret_cast<uint4*>(v + ((c + 2 * key) % (DP / 16)) * 16) = make_uint4(0u, 0u, 0u, 0u);
+            for (int c = 0; c < DP / 16; ++c)  // the lanes begin at different banks
+              *reinterpret_cast<uint4*>(v + ((c + 2 * key) % (DP / 16)) * 16) = make_uint4(0u, 0u, 0u, 0u);
+          }
         }
-
-        const uint32_t t_s = tmem + lanes + b * Sh::kSColumns + h * Sh::kS;
-        float y[kHalf];  // exponents of the weights
-        auto exponents = [&](bool referred) {
-          float s[2 * kHalf];
-          each_chunk<Sh::kChunks>([&](auto chunk) {
-            constexpr int c = decltype(chunk)::value;
-            tmem_load<2 * Sh::rows_of(c)>(t_s + 32 * c, s + 32 * c);
-          });
-          tmem_wait_ld();
+        if (!idle) {
+          const bool masked = !__all_sync(0xFFFFFFFFu, from <= 0 && to >= min(rows - r0, R));
+          const uint32_t t_s = tmem + lanes + b * Sh::kSColumns + (kTwo ? 0 : h * Sh::kSGroup);
           const float2 sixteenth = make_float2(0.0625f, 0.0625f), unit2 = make_float2(u.k, u.k), v2 = make_float2(u.v, u.v);
-          each_chunk<Sh::kChunks>([&](auto chunk) {
-            constexpr int c = decltype(chunk)::value, n = Sh::rows_of(c);
+          float y[R];  // exponents of the weights
+          auto hide = [&]() {
+            if (!masked) return;
 #pragma unroll
-            for (int i = 0; i < n; i += 2) {
-              const int r = 16 * c + i;
-              // The product with the factor is rounded before the reference is taken off, so that the
-              // largest weight is what it was chosen to be, however far from zero the scores are.
-              float2 x = fma2(make_float2(s[32 * c + n + i], s[32 * c + n + i + 1]), sixteenth, make_float2(s[32 * c + i], s[32 * c + i + 1]));
-              x = mul2(mul2(x, unit2), *reinterpret_cast<const float2*>(factor + r));
-              if (referred) x = add2(x, *reinterpret_cast<const float2*>(minus + r));
-              x = add2(x, v2);
-              y[r] = x.x;
-              y[r + 1] = x.y;
-            }
-          });
-          if (masked) {
-#pragma unroll
-            for (int r = 0; r < kHalf; ++r)
+            for (int r = 0; r < R; ++r)
               if (r < from || r >= to) y[r] = -INFINITY;
-          }
-        };
-        // The first tile sets the references.  After it a weight may outgrow its own, or a row may see its
-        // first keys: then, too, the rows' maxima over the tile, new references, and what was summed so far
-        // in the new unit.
-        bool raise = j == 0;
-        if (j > 0) {
-          exponents(true);
-          float top = -INFINITY;
-#pragma unroll
-          for (int r = 0; r < kHalf; r += 2) top = max3(top, y[r], y[r + 1]);
-          raise = any_of_half(h, top > kMostTop);
-        }
-        if (raise) {
-          exponents(false);
-#pragma unroll
-          for (int r = 0; r < kHalf; ++r) {
-            const float most = warp_max(y[r]);
-            if (lane == 0) ct.part[h][quarter][r] = most;
-          }
-          half_barrier(h);
-          if (key < kHalf) {
-            const float old = ct.minus[r0 + key];
-            const float most = fmaxf(fmaxf(ct.part[h][0][key], ct.part[h][1][key]), fmaxf(ct.part[h][2][key], ct.part[h][3][key]));
-            float f = 1.f;
-            if (most + old > kMostTop) {
-              const float now = kFirstTop - most;
-              f = old == kNone ? 0.f : exp2_fast(now - old);
-              ct.minus[r0 + key] = now;
-            }
-            ct.scale[r0 + key] = f;
-          }
-          half_barrier(h);
-          if (j > 0) {
-#pragma unroll
-            for (int r = 0; r < kHalf; r += 2) l[r / 2] = mul2(l[r / 2], *reinterpret_cast<const float2*>(ct.scale + r0 + r));
-            const uint32_t before = g - 1;
-            wait(&ct.pv_done[before & 1u], before >> 1 & 1u);
-            tc_fence_after();
+          };
+          // Scores in the keys' units, two rows at a time: f(row, scores).
+          auto scores = [&](auto&& f) {
+            float s[2 * R];
+            each_chunk<Sh::kChunks>([&](auto chunk) {
+              constexpr int c = decltype(chunk)::value;
+              tmem_load<2 * Sh::rows_of(c)>(t_s + 32 * c, s + 32 * c);
+            });
+            tmem_wait_ld();
             each_chunk<Sh::kChunks>([&](auto chunk) {
               constexpr int c = decltype(chunk)::value, n = Sh::rows_of(c);
 #pragma unroll
-              for (int part = 0; part < 3; ++part) {
-                float o[n];
-                tmem_load<n>(t_o + 48 * c + part * n, o);
-                tmem_wait_ld();
-#pragma unroll
-                for (int i = 0; i < n; ++i) o[i] *= ct.scale[r0 + 16 * c + i];
-#pragma unroll
-                for (int i = 0; i < n; i += 4) tmem_store4(t_o + 48 * c + part * n + i, o + i);
+              for (int i = 0; i < n; i += 2) {
+                const float2 x = fma2(make_float2(s[32 * c + n + i], s[32 * c + n + i + 1]), sixteenth, make_float2(s[32 * c + i], s[32 * c + i + 1]));
+                f(16 * c + i, mul2(x, unit2));
               }
             });
-            tmem_wait_st();
-          }
-#pragma unroll
-          for (int r = 0; r < kHalf; r += 2) {
-            const float2 x = add2(make_float2(y[r], y[r + 1]), *reinterpret_cast<const float2*>(minus + r));
+            hide();
+          };
+          auto put = [&](int r, const float2& x) {
             y[r] = x.x;
             y[r + 1] = x.y;
-          }
-        }
+          };
+          auto two = [](const float* p) { return *reinterpret_cast<const float2*>(p); };
+          // The product with the factor rounded before the reference is taken off, for references far from
+          // zero; `fresh`: rows that have none keep their exponents.
+          auto exact = [&](bool fresh) {
+            scores([&](int r, const float2& x) {
+              float2 ref = two(ct.minus[h] + r);
+              if (fresh && ref.x == kNone) ref.x = 0.f;
+              if (fresh && ref.y == kNone) ref.y = 0.f;
+              put(r, add2(add2(add2(mul2(x, two(factor + r)), ref), v2), two(ct.rest[h] + r)));
+            });
+          };
+          auto exponents = [&]() {
+            if (far)
+              exact(false);
+            else
+              scores([&](int r, const float2& x) { put(r, add2(fma2(x, two(factor + r), two(ct.minus[h] + r)), v2)); });
+          };
+          // The rows' maxima, to ct.part.
+          auto maxima = [&]() {
+            each_chunk<Sh::kChunks>([&](auto chunk) {
+              constexpr int c = decltype(chunk)::value, n = Sh::rows_of(c);
+              float v[n];
+#pragma unroll
+              for (int i = 0; i < n; ++i) v[i] = y[16 * c + i];
+              join_lanes<n>(v, lane, [](float p, float q) { return fmaxf(p, q); });
+              if (lane < n) ct.part[h][quarter][16 * c + lane] = v[0];
+            });
+            group_barrier(h);
+          };
+          auto most_of = [&](int r) { return fmaxf(fmaxf(ct.part[h][0][r], ct.part[h][1][r]), fmaxf(ct.part[h][2][r], ct.part[h][3][r])); };
 
-        // The weights' buffer is free: its product was issued before the scores of this tile, and a commit
-        // waits for all that was issued before it.
-        uint8_t* weights = smem + Sh::kPAt + b * Sh::kPBytes + key * 128;
-        const float2 inv2 = make_float2(u.inv, u.inv);
-        each_chunk<Sh::kChunks>([&](auto chunk) {
-          constexpr int c = decltype(chunk)::value, n = Sh::rows_of(c);
-          uint32_t w[(3 * n + 15) / 16 * 4];
+          // The first tile sets the references.  After it a weight may outgrow its own, or a row may see
+          // its first keys: then, too, the rows' maxima over the tile, new references (whole numbers,
+          // so that they are the same however often they move), and what was summed so far in the new unit.
+          const bool fresh = j < Sh::kStreams;
+          bool raise = fresh;
+          if (!fresh) {
+            exponents();
+            float top = -INFINITY;
 #pragma unroll
-          for (int i = 3 * n / 4; i < (3 * n + 15) / 16 * 4; ++i) w[i] = 0u;
-#pragma unroll
-          for (int i = 0; i < n; i += 4) {
-            float e[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) e[k] = exp2_fast(y[16 * c + i + k]);
-            l[(16 * c + i) / 2] = fma2(make_float2(e[0], e[1]), inv2, l[(16 * c + i) / 2]);
-            l[(16 * c + i) / 2 + 1] = fma2(make_float2(e[2], e[3]), inv2, l[(16 * c + i) / 2 + 1]);
-            take_apart(e, w[i / 4], w[n / 4 + i / 4], w[2 * (n / 4) + i / 4]);
+            for (int r = 0; r < R; r += 2) top = max3(top, y[r], y[r + 1]);
+            raise = any_of_group(h, top > kMostTop);
           }
+          if (raise) {
+            exact(true);
+            maxima();
+            float old = 0.f, old_rest = 0.f, now = 0.f, now_rest = 0.f, move = 0.f;
+            bool pending = false;
+            if (key < R) {
+              old = now = ct.minus[h][key];
+              old_rest = now_rest = ct.rest[h][key];
+              const float most = most_of(key), by = floorf(kFirstTop - most);
+              if (old == kNone ? most > -INFINITY : most > kMostTop) {
+                const float from_zero = old == kNone ? 0.f : old;
+                if (fabsf(from_zero) >= kFar) {
+                  now_rest = old_rest + by;
+                  move = by;
+                } else if (fabsf(from_zero + by) < kFar) {
+                  now = from_zero + by;
+                  move = by;
+                } else {  // the maximum itself, and what is left of it over the tile
+                  now = from_zero - most;
+                  pending = true;
+                }
+                ct.minus[h][key] = now;
+                ct.rest[h][key] = now_rest;
+              }
+              ct.move[h][key] = move;
+            }
+            const bool again = any_of_group(h, pending);
+            if (again) {
+              exact(false);
+              maxima();
+              if (pending) {
+                now_rest = floorf(kFirstTop - most_of(key));
+                ct.rest[h][key] = now_rest;
+              }
+              far = true;
+            }
+            if (key < R) ct.scale[h][key] = old == kNone ? 0.f : exp2_fast((now - old) + (now_rest - old_rest));
+            group_barrier(h);
+            if (!fresh) {
 #pragma unroll
-          for (int i = 0; i < (3 * n + 15) / 16; ++i) {
-            const int column = h * Sh::kO + 48 * c + 16 * i;
-            *reinterpret_cast<uint4*>(weights + column / 128 * (kKeys * 128) + ((column % 128 / 16) ^ (key & 7)) * 16) =
-                make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+              for (int r = 0; r < R; r += 2) l[r / 2] = mul2(l[r / 2], two(ct.scale[h] + r));
+              const uint32_t before = g - Sh::kStreams;
+              wait(&ct.pv_done[before % kBuffers], before / kBuffers & 1u);
+              tc_fence_after();
+              each_chunk<Sh::kChunks>([&](auto chunk) {
+                constexpr int c = decltype(chunk)::value, n = Sh::rows_of(c);
+#pragma unroll
+                for (int part = 0; part < 3; ++part) {
+                  float o[n];
+                  const uint32_t column = t_o + Sh::o_column(h, c) + part * n;
+                  tmem_load<n>(column, o);
+                  tmem_wait_ld();
+#pragma unroll
+                  for (int i = 0; i < n; ++i) o[i] *= ct.scale[h][16 * c + i];
+#pragma unroll
+                  for (int i = 0; i < n; i += 4) tmem_store4(column + i, o + i);
+                }
+              });
+              tmem_wait_st();
+            }
+            if (again) {
+              exact(false);
+            } else {
+#pragma unroll
+              for (int r = 0; r < R; r += 2) put(r, add2(make_float2(y[r], y[r + 1]), two(ct.move[h] + r)));
+            }
           }
-        });
+
+          uint8_t* weights = smem + Sh::kPAt + b * Sh::kPBytes + key * 128;
+          const float2 inv2 = make_float2(u.inv, u.inv);
+          each_chunk<Sh::kChunks>([&](auto chunk) {
+            constexpr int c = decltype(chunk)::value, n = Sh::rows_of(c);
+            uint32_t w[3 * n / 4];
+#pragma unroll
+            for (int i = 0; i < n; i += 4) {
+              float e[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) e[k] = exp2_fast(y[16 * c + i + k]);
+              l[(16 * c + i) / 2] = fma2(make_float2(e[0], e[1]), inv2, l[(16 * c + i) / 2]);
+              l[(16 * c + i) / 2 + 1] = fma2(make_float2(e[2], e[3]), inv2, l[(16 * c + i) / 2 + 1]);
+              take_apart(e, w[i / 4], w[n / 4 + i / 4], w[2 * (n / 4) + i / 4]);
+            }
+            const int column = Sh::o_column(h, c);
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+              const int x = column + i * n;
+              uint8_t* to_w = weights + x / 128 * (kKeys * 128) + ((x % 128 / 16) ^ (key & 7)) * 16 + x % 16;
+              if constexpr (n == 16)
+                *reinterpret_cast<uint4*>(to_w) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+              else
+                *reinterpret_cast<uint2*>(to_w) = make_uint2(w[2 * i], w[2 * i + 1]);
+            }
+          });
+        }
         fence_proxy_async_shared();
         tc_fence_before();
         __syncwarp();
@@ -694,59 +785,98 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       tiles += nt;
 
-      // The rows' sums over the half's 128 threads: each step of a warp's sum halves the rows that a lane has.
+      // The rows' sums over the group's threads.
       each_chunk<Sh::kChunks>([&](auto chunk) {
         constexpr int c = decltype(chunk)::value, n = Sh::rows_of(c);
         float v[n];
 #pragma unroll
         for (int i = 0; i < n; ++i) v[i] = i % 2 ? l[8 * c + i / 2].y : l[8 * c + i / 2].x;
-#pragma unroll
-        for (int o = n / 2; o > 0; o >>= 1)
-#pragma unroll
-          for (int i = 0; i < o; ++i) {
-            const bool upper = lane & o;
-            const float other = __shfl_xor_sync(0xFFFFFFFFu, upper ? v[i] : v[i + o], o);
-            v[i] = (upper ? v[i + o] : v[i]) + other;
-          }
-#pragma unroll
-        for (int o = n; o < 32; o <<= 1) v[0] += __shfl_xor_sync(0xFFFFFFFFu, v[0], o);
+        join_lanes<n>(v, lane, [](float p, float q) { return p + q; });
         if (lane < n) ct.part[h][quarter][16 * c + lane] = v[0];
       });
-      half_barrier(h);
+      if constexpr (kTwo)
+        named_barrier<1, 256>();
+      else
+        group_barrier(h);
       const bool whole = pc.pieces == 1;
       float* part = a.partials + ((long long)blockIdx.x * 2 + (pc.k0 == 0 ? 1 : 0)) * Sh::kPart;
-      if (key < kHalf) {
-        const float sum = (ct.part[h][0][key] + ct.part[h][1][key]) + (ct.part[h][2][key] + ct.part[h][3][key]);
-        ct.scale[r0 + key] = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
-        const float m = -ct.minus[r0 + key];
-        if (!whole && ok && r0 + key < rows)
-          *reinterpret_cast<float2*>(part + Sh::kRows * DP + (r0 + key) * 2) = make_float2(sum == 0.f ? -INFINITY : m, sum);
+      auto sum_of = [&](int s, int r) { return (ct.part[s][0][r] + ct.part[s][1][r]) + (ct.part[s][2][r] + ct.part[s][3][r]); };
+      if (key < R) {
+        // What O is multiplied by, so that it refers to `top`: to a number, where minus and rest are two.
+        const float m = -(ct.minus[h][key] + ct.rest[h][key]);
+        float sum = sum_of(h, key), top = m, f;
+        if constexpr (kTwo) {  // the larger reference for both streams
+          const float other = -(ct.minus[h ^ 1][key] + ct.rest[h ^ 1][key]), other_sum = sum_of(h ^ 1, key);
+          const bool mine = ct.minus[h][key] != kNone, theirs = ct.minus[h ^ 1][key] != kNone;
+          top = !theirs ? m : !mine ? other : fmaxf(m, other);
+          f = mine ? exp2_fast(-((ct.minus[h][key] + top) + ct.rest[h][key])) : 0.f;
+          sum = sum * f + other_sum * (theirs ? exp2_fast(-((ct.minus[h ^ 1][key] + top) + ct.rest[h ^ 1][key])) : 0.f);
+        } else {
+          f = exp2_fast(-((ct.minus[h][key] + top) + ct.rest[h][key]));
+          sum *= f;
+        }
+        ct.scale[h][key] = whole ? (sum == 0.f ? 0.f : f / sum) : f;
+        if (!whole && ok && r0 + key < rows && (!kTwo || h == 0))
+          *reinterpret_cast<float2*>(part + Sh::kRows * DP + (r0 + key) * 2) = make_float2(sum == 0.f ? -INFINITY : top, sum);
       }
-      half_barrier(h);
+      if constexpr (kTwo)
+        named_barrier<1, 256>();
+      else
+        group_barrier(h);
       // O is complete
       if (ok) {
         const uint32_t last = tiles - 1;
-        wait(&ct.pv_done[last & 1u], last >> 1 & 1u);
+        wait(&ct.pv_done[last % kBuffers], last / kBuffers & 1u);
         tc_fence_after();
       }
-      if (ok) {
+      // `key` is the lane, the element of the head; row r of x[i] goes out.
+      auto put_rows = [&](int from, const float* x, int n) {
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+          const int r = from + i;
+          if (r >= rows || key >= DP) break;
+          if (!whole)
+            part[r * DP + key] = x[i];
+          else if (key < D)
+            static_cast<__nv_bfloat16*>(a.out)[ct.out[buffer][r] + key] = __float2bfloat16_rn(x[i]);
+        }
+      };
+      if constexpr (kTwo) {
+        // half of the rows to each group, from both streams' O (the second has none where there was one tile)
+        constexpr int n = R / 2, c = R == 32 ? 16 : R;  // rows of a chunk
+        const int from = h * n;
+        if (ok && from < rows) {
+          float x[n];
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            if (s == 1 && nt == 1) break;
+            float o[3 * n];
+            const uint32_t column = tmem + lanes + Sh::kOAt + s * Sh::kOColumns + (R == 32 ? 48 * h : from);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) tmem_load<n>(column + p * c, o + p * n);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < n; ++i) {
+              const float f = ct.scale[s][from + i], y = o[i] + (o[n + i] + o[2 * n + i] * 0.03125f);
+              x[i] = s == 0 ? (f == 0.f ? 0.f : y * f) : (f == 0.f ? x[i] : fmaf(y, f, x[i]));
+            }
+          }
+          put_rows(from, x, n);
+        }
+        tc_fence_before();
+        named_barrier<1, 256>();  // both are through with O
+        tc_fence_after();
+      } else if (ok) {
         each_chunk<Sh::kChunks>([&](auto chunk) {
           constexpr int c = decltype(chunk)::value, n = Sh::rows_of(c);
           if (r0 + 16 * c >= rows) return;
           float o[3 * n];
 #pragma unroll
-          for (int p = 0; p < 3; ++p) tmem_load<n>(t_o + 48 * c + p * n, o + p * n);
+          for (int p = 0; p < 3; ++p) tmem_load<n>(t_o + Sh::o_column(h, c) + p * n, o + p * n);
           tmem_wait_ld();
 #pragma unroll
-          for (int i = 0; i < n; ++i) {
-            const int r = r0 + 16 * c + i;
-            if (r >= rows || key >= DP) break;  // `key` is the lane: the element of the head
-            const float x = (o[i] + (o[n + i] + o[2 * n + i] * 0.03125f)) * ct.scale[r];
-            if (!whole)
-              part[r * DP + key] = x;
-            else if (key < D)
-              static_cast<__nv_bfloat16*>(a.out)[ct.out[buffer][r] + key] = __float2bfloat16_rn(x);
-          }
+          for (int i = 0; i < n; ++i) o[i] = (o[i] + (o[n + i] + o[2 * n + i] * 0.03125f)) * ct.scale[h][16 * c + i];
+          put_rows(r0 + 16 * c, o, n);
         });
       }
       tc_fence_before();
@@ -754,7 +884,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (lane == 0) mbar_arrive(smem_u32(&ct.q_empty[buffer]));
       if (!whole && h == 0 && pc.k0 == 0) unit = JoinUnit{pc.pieces, rows, rows, pc.row0 + pc.i0, pc.head * G, G, {0, 0}};
     }
-    if (tid == 256) a.units[blockIdx.x] = unit;
+    if (tid == kBase) a.units[blockIdx.x] = unit;
   }
   tc_fence_before();
   __syncthreads();
@@ -762,9 +892,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == 4) tmem_dealloc(tmem, 512);
 }
 
-template <int DP, int kHalf>
+template <int DP, int R>
 cudaError_t launch(TcParams& p, const DeviceInfo& dev, cudaStream_t stream) {
-  using Sh = TcShape<DP, kHalf>;
+  using Sh = TcShape<DP, R>;
   const AttendArgs& a = p.a;
   const retrace_kv_cache& c = a.cache;
   p.shape.unit_tokens = Sh::kRows / p.group;
@@ -778,13 +908,13 @@ cudaError_t launch(TcParams& p, const DeviceInfo& dev, cudaStream_t stream) {
   if (!encode(&mk, c.k, 4, dims, strides, box, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, swizzle, promotion) ||
       !encode(&mv, c.v, 4, dims, strides, box, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, swizzle, promotion))
     return cudaErrorInvalidValue;
-  constexpr size_t smem = Sh::kControl + sizeof(Control<kHalf>);
+  constexpr size_t smem = Sh::kControl + sizeof(Control<R>);
   static_assert(smem <= 227 * 1024, "shared memory of a CTA");
   static std::atomic<uint64_t> allowed{0};
-  cudaError_t e = allow_shared(attend_fp8_tc_kernel<DP, kHalf>, smem, dev, allowed);
+  cudaError_t e = allow_shared(attend_fp8_tc_kernel<DP, R>, smem, dev, allowed);
   if (e != cudaSuccess) return e;
   const int grid = dev.sm_count < kAttendMaxTcCtas ? dev.sm_count : kAttendMaxTcCtas;
-  e = launch_dependent(attend_fp8_tc_kernel<DP, kHalf>, dim3(grid), dim3(kThreads), smem, stream, 1u, mk, mv, p);
+  e = launch_dependent(attend_fp8_tc_kernel<DP, R>, dim3(grid), dim3(Sh::kThreads), smem, stream, 1u, mk, mv, p);
   if (e != cudaSuccess) return e;
   return launch_attend_join(a, PartShape{Sh::kRows, DP, 1.f}, grid, stream);
 }
@@ -793,10 +923,10 @@ template <int DP>
 cudaError_t launch_rows(TcParams& p, const DeviceInfo& dev, cudaStream_t stream) {
   // By the rows that a sequence has on average; a group of query heads is never divided.
   const long long rows = (long long)p.a.T * p.group, B = p.a.B;
-  if (p.group <= 8 && rows <= 8 * B) return launch<DP, 4>(p, dev, stream);
-  if (p.group <= 16 && rows <= 16 * B) return launch<DP, 8>(p, dev, stream);
-  if (p.group <= 32 && rows <= 32 * B) return launch<DP, 16>(p, dev, stream);
-  return launch<DP, 36>(p, dev, stream);
+  if (p.group <= 8 && rows <= 8 * B) return launch<DP, 8>(p, dev, stream);
+  if (p.group <= 16 && rows <= 16 * B) return launch<DP, 16>(p, dev, stream);
+  if (p.group <= 32 && rows <= 32 * B) return launch<DP, 32>(p, dev, stream);
+  return launch<DP, 24>(p, dev, stream);
 }
 
 }  // namespace
@@ -813,7 +943,7 @@ bool attend_fp8_tc_supported(const AttendArgs& a) {
 
 size_t attend_fp8_tc_partial_bytes(int head_dim) {
   if (head_dim > 128) return 0;
-  return (size_t)kAttendMaxTcCtas * 2 * (head_dim <= 64 ? TcShape<64, 36>::kPart : TcShape<128, 36>::kPart) * 4;
+  return (size_t)kAttendMaxTcCtas * 2 * (head_dim <= 64 ? TcShape<64, 24>::kPart : TcShape<128, 24>::kPart) * 4;
 }
 
 cudaError_t launch_attend_fp8_tc(const AttendArgs& a, cudaStream_t stream) {

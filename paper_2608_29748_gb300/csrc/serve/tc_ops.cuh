@@ -73,6 +73,11 @@ __device__ __forceinline__ bool warp_wait_all(uint64_t* bar, uint32_t parity, vo
   const bool ok = mbar_wait_bounded(smem_u32(bar), parity, abort);
   return __all_sync(0xFFFFFFFFu, ok);
 }
+// The same, for waits that are often over when they begin: 15 cycles then, the loop's first turn 170.
+__device__ __forceinline__ bool warp_wait_quick(uint64_t* bar, uint32_t parity, volatile int* abort) {
+  if (__all_sync(0xFFFFFFFFu, mbar_try_wait(smem_u32(bar), parity))) return true;
+  return warp_wait_all(bar, parity, abort);
+}
 template <int id, int threads>
 __device__ __forceinline__ void named_barrier() {
   asm volatile("bar.sync %0, %1;" ::"n"(id), "n"(threads) : "memory");
