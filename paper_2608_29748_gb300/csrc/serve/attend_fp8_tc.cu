@@ -18,11 +18,14 @@
 // 72 rows, and the softmax does 128 rows exponentials: with few rows on the N side all of
 // it scales with the rows that there are.
 //
-// Warps 0 and 1 copy K, 2 and 3 V (TMA boxes of the slots of a page, dealt out by turns); warp 4 issues
-// the scores' products, warp 5 those with V; warps 6 and 7 take the queries apart, a piece ahead.  The softmax has groups of four
-// warps, a thread to a key.  Up to 32 rows, two groups take the even and the odd tiles, each
-// with references, sums and an O of its own, joined at the end: a tile's way through a group is
-// latency, twice what its bytes take.  For 72 rows three groups have 24 rows each of every tile.
+// Warps of a CTA: copies of K and of V (TMA boxes of the slots of a page), the products, the queries
+// (taken apart a piece ahead), and the softmax in groups of four warps, a thread to a key.  Up to 16
+// rows a CTA has one group, and an SM two CTAs: a tile's way through the softmax, and the beginning
+// and end of a piece, are latencies, and the other CTA works meanwhile.  Up to 72 rows three groups
+// have 24 rows each, an SM one CTA, and there are two warps for each other job.
+//
+// CTAs take the heads one after another, all sequences under each: then a sequence's heads, whose rows
+// of 128 bytes lie side by side, are read by several CTAs at about the same time, and not by one in turn.
 #include <math.h>
 
 #include "attend_plan.cuh"
@@ -37,7 +40,6 @@ constexpr int kKeys = 128;  // keys of a tile
 constexpr unsigned long long kDrainNs = 20ull * 1000ull * 1000ull;
 constexpr int kInfoTiles = 16;  // ring of tiles' units: more than the tiles between loading and softmax
 constexpr int kMostBoxes = 16;  // of a tile: pages of 8 slots
-constexpr int kBase = 256;      // threads before the softmax's
 constexpr float kFirstTop = 4.f, kMostTop = 15.f;
 constexpr float kNone = 1e30f;     // in place of the reference of a row that has seen nothing
 constexpr float kFar = 4194304.f;  // 2^22: references up to it are whole numbers, and sums of two are exact
@@ -51,40 +53,39 @@ struct TcParams {
   float scale2;  // scale log2(e)
 };
 
-// R rows to a thread of the softmax, in chunks of 16 (the last may be of 8).  Two streams (`kStreams`
-// 2): a group has every other tile and all rows; one: the groups share the rows of every tile.
+// R rows to a thread of the softmax, in chunks of 16 (the last may be of 8).
 template <int DP, int R>
 struct TcShape {
-  static constexpr int kStreams = R == 24 ? 1 : 2, kGroups = R == 24 ? 3 : 2;
+  static constexpr int kGroups = R == 24 ? 3 : 1;
+  static constexpr bool kFew = kGroups == 1;
+  static constexpr int kPerSm = kFew ? 2 : 1;
+  static constexpr int kJobs = kFew ? 1 : 2;  // warps of each job but the softmax
+  static constexpr int kBase = 128 * kJobs;   // threads before the softmax's
   static constexpr int kThreads = kBase + 128 * kGroups;
-  static constexpr int kRows = kStreams == 2 ? R : R * kGroups;
-  static constexpr int kBuffers = 2 * kStreams;  // of S and P
+  static constexpr int kRows = R * kGroups;
   static constexpr int kChunks = (R + 15) / 16;
   __host__ __device__ static constexpr int rows_of(int chunk) { return R - 16 * chunk < 16 ? R - 16 * chunk : 16; }
   // Columns of S: 2 a row, the two parts of a chunk's queries side by side, group after group.
-  static constexpr int kSGroup = 2 * R, kSColumns = kStreams == 2 ? kSGroup : kSGroup * kGroups;
+  static constexpr int kSGroup = 2 * R, kSColumns = kSGroup * kGroups;
   // Columns of O (and of P): 3 a row; all groups' first chunks, then all second ones.
-  static constexpr int kShare = kStreams == 2 ? 1 : kGroups;
-  __host__ __device__ static constexpr int o_column(int group, int chunk) {
-    return 48 * kShare * chunk + 3 * rows_of(chunk) * (kStreams == 2 ? 0 : group);
-  }
-  static constexpr int kOColumns = (3 * R * kShare + 15) / 16 * 16;
+  __host__ __device__ static constexpr int o_column(int group, int chunk) { return 48 * kGroups * chunk + 3 * rows_of(chunk) * group; }
+  static constexpr int kOColumns = (3 * kRows + 15) / 16 * 16;
   static_assert(kSColumns % 16 == 0 && kOColumns <= 256, "columns of a product");
-  static constexpr int kOAt = kBuffers * kSColumns;
-  static_assert(kOAt + kStreams * kOColumns <= 512, "columns of TMEM");
-  // Registers of a thread: the launch's, and what the softmax takes of the others'.
-  static constexpr int kFewer = kGroups == 3 ? 56 : 64, kMore = kGroups == 3 ? 120 : 192;
-  static_assert(kBase * kFewer + 128 * kGroups * kMore <= kThreads * (65536 / kThreads / 8 * 8), "registers of a CTA");
+  static constexpr int kOAt = 2 * kSColumns, kTmem = 512 / kPerSm;
+  static_assert(kOAt + kOColumns <= kTmem, "columns of TMEM");
+  // Registers of a thread: what the softmax takes of the others' of the launch.
+  static constexpr int kFewer = kFew ? 64 : 56, kMore = kFew ? 192 : 120;
+  static_assert(kBase * kFewer + 128 * kGroups * kMore <= kThreads * (65536 / (kThreads * kPerSm) / 8 * 8), "registers of a CTA");
 
   static constexpr int kTileBytes = kKeys * DP;
-  static constexpr int kPAtoms = (kOColumns + 127) / 128;  // 128-byte columns of P
-  static constexpr int kPBytes = kPAtoms * kKeys * 128;
+  static constexpr int kPWidth = kOColumns > 64 ? 128 : kOColumns > 32 ? 64 : 32;  // bytes of a key's columns of P side by side
+  static constexpr int kPBytes = (kOColumns + kPWidth - 1) / kPWidth * kKeys * kPWidth;
   static constexpr int kQBytes = (kSColumns * DP + 1023) / 1024 * 1024;
-  static constexpr int kControlBytes = 12 * 1024;
-  static constexpr int kRoom = (227 * 1024 - kControlBytes - kBuffers * kPBytes - 2 * kQBytes) / kTileBytes;
+  static constexpr int kControlBytes = kFew ? 7 * 1024 : 12 * 1024;
+  static constexpr int kRoom = ((kFew ? 113 : 227) * 1024 - kControlBytes - 2 * kPBytes - 2 * kQBytes) / kTileBytes;
   static constexpr int kRingV = (kRoom + 1) / 2 < 8 ? (kRoom + 1) / 2 : 8, kRingK = kRoom / 2 < 8 ? kRoom / 2 : 8;
-  static_assert(kRingK >= 3 && kRingV >= kBuffers, "tiles in flight");
-  static constexpr int kVAt = kRingK * kTileBytes, kPAt = kVAt + kRingV * kTileBytes, kQAt = kPAt + kBuffers * kPBytes;
+  static_assert(kRingK >= 2 && kRingV >= 2, "tiles in flight");
+  static constexpr int kVAt = kRingK * kTileBytes, kPAt = kVAt + kRingV * kTileBytes, kQAt = kPAt + 2 * kPBytes;
   static constexpr int kControl = kQAt + 2 * kQBytes;
   static constexpr int kPart = kRows * (DP + 2);  // floats of a part
 };
@@ -95,29 +96,31 @@ struct BoxUnits {
   int there;  // has a page
 };
 
-template <int R>
+template <int R, int kGroups>
 struct Control {
   uint64_t full[2][8], empty[2][8];  // rings of K and V
   uint64_t q_full[2], q_empty[2];
-  uint64_t s_full[4];   // scores ready
-  uint64_t p_full[4];   // weights written, the scores' buffer read
-  uint64_t pv_done[4];  // the product with V done
+  uint64_t s_full[2];   // scores ready
+  uint64_t p_full[2];   // weights written, the scores' buffer read
+  uint64_t pv_done[2];  // the product with V done, the weights' buffer free
   uint64_t done[2];     // after an expired wait: the issued products
   PlanStart plan;
-  long long sum[(kBase + 384) / 32];
+  long long sum[20];
   uint32_t tmem;
   int abort;
-  PieceWalk walk[3];  // of the softmax groups
-  Piece piece[3][2];  // this one and the next
-  int more[3][2];
+  PieceWalk walk[kGroups];  // of the softmax groups
+  Piece piece[kGroups][2];  // this one and the next
+  int more[kGroups][2];
   BoxUnits units[kInfoTiles][kMostBoxes];
-  alignas(16) float factor[2][72];  // of a row: scale log2(e) times its queries' unit
-  long long out[2][72];             // where a row goes, elements
+  int2 q_range[2][2];  // largest and smallest exponent of the rows of a warp
+  int even[2];         // the rows have one unit
+  float one_factor[2];                        // scale log2(e) times it
+  alignas(16) float factor[2][R * kGroups];   // and times a row's own
+  long long out[2][R * kGroups];              // where a row goes, elements
   // Of a group's rows: what is added to exponents (minus the reference), and, where that is far from
-  // zero, added to the difference; how the reference moves; at the end the factors of the streams' O.
-  alignas(16) float minus[3][R], rest[3][R], move[3][R];
-  alignas(16) float scale[3][R];
-  float part[3][4][R];  // per warp: a row's maximum, or sum
+  // zero, added to the difference; how the reference moves; what sums, and at the end O, are multiplied by.
+  alignas(16) float minus[kGroups][R], rest[kGroups][R], move[kGroups][R], scale[kGroups][R];
+  float part[kGroups][4][R];  // per warp: a row's maximum, or sum
 };
 
 // ---- instructions -------------------------------------------------------------
@@ -135,11 +138,11 @@ __device__ __forceinline__ void tc_mma_8bit(uint32_t d_tmem, uint64_t a_desc, ui
 __host__ __device__ constexpr uint32_t idesc_8bit(int N, bool values) {
   return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((128u >> 4) << 24) | (values ? 1u << 10 | 1u << 15 | 1u << 16 : 0u);
 }
-// Rows of DP bytes with the swizzle of their width, 8 rows a group; `lead`: from one column of DP (of P: 128)
+// Rows of kWidth bytes with the swizzle of their width, 8 rows a group; `lead`: from one column of kWidth
 // bytes to the next, for an MN-major operand.
 template <int kWidth>
 __device__ __forceinline__ uint64_t rows_desc(uint32_t saddr, uint32_t lead) {
-  constexpr uint64_t mode = kWidth == 128 ? 2 : 4;
+  constexpr uint64_t mode = kWidth == 128 ? 2 : kWidth == 64 ? 4 : 6;
   return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)((kWidth * 8) >> 4) << 32 | (uint64_t)1 << 46 | mode << 61;
 }
 
@@ -219,11 +222,16 @@ __device__ __forceinline__ uint32_t times_32(uint32_t a) {
   const __half2 h = __hmul2(*reinterpret_cast<const __half2*>(&a), __float2half2_rn(32.f));
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-__device__ __forceinline__ uint32_t to_e5m2x2(uint32_t h) {
-  __half2_raw r;
-  r.x = (unsigned short)(h & 0xFFFFu);
-  r.y = (unsigned short)(h >> 16);
-  return __nv_cvt_halfraw2_to_fp8x2(r, __NV_SATFINITE, __NV_E5M2);
+// Four fp16 numbers to e5m2, to the nearest, a byte each.
+__device__ __forceinline__ uint32_t to_e5m2x4(uint32_t a, uint32_t b) {
+  uint32_t y;
+  asm("{\n\t.reg .b16 lo, hi;\n\t"
+      "cvt.rn.satfinite.e5m2x2.f16x2 lo, %1;\n\t"
+      "cvt.rn.satfinite.e5m2x2.f16x2 hi, %2;\n\t"
+      "mov.b32 %0, {lo, hi};\n\t}"
+      : "=r"(y)
+      : "r"(a), "r"(b));
+  return y;
 }
 // The three parts of four weights, none negative, a byte each; the third times 2^5.
 __device__ __forceinline__ void take_apart(const float (&w)[4], uint32_t& first, uint32_t& second, uint32_t& third) {
@@ -232,7 +240,7 @@ __device__ __forceinline__ void take_apart(const float (&w)[4], uint32_t& first,
   const uint32_t a2 = minus_halves(a1, a1 & 0xFF00FF00u), b2 = minus_halves(b1, b1 & 0xFF00FF00u);
   first = __byte_perm(a, b, 0x7531);
   second = __byte_perm(a1, b1, 0x7531);
-  third = to_e5m2x2(times_32(a2)) | to_e5m2x2(times_32(b2)) << 16;
+  third = to_e5m2x4(times_32(a2), times_32(b2));
 }
 
 template <int I>
@@ -248,14 +256,15 @@ __device__ __forceinline__ void each_chunk(F&& f) {
 }
 
 template <int DP, int R>
-__global__ void __launch_bounds__(TcShape<DP, R>::kThreads, 1)
+__global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPerSm)
     attend_fp8_tc_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                          const __grid_constant__ TcParams P) {
   using Sh = TcShape<DP, R>;
-  constexpr int kThreads = Sh::kThreads, kBuffers = Sh::kBuffers;
-  static_assert(sizeof(Control<R>) <= Sh::kControlBytes, "room of the control block");
+  using Ct = Control<R, Sh::kGroups>;
+  constexpr int kThreads = Sh::kThreads, kBase = Sh::kBase, kJobs = Sh::kJobs;
+  static_assert(sizeof(Ct) <= Sh::kControlBytes, "room of the control block");
   extern __shared__ __align__(1024) uint8_t smem[];
-  Control<R>& ct = *reinterpret_cast<Control<R>*>(smem + Sh::kControl);
+  Ct& ct = *reinterpret_cast<Ct*>(smem + Sh::kControl);
   volatile int* abort = &ct.abort;
   const uint32_t base = smem_u32(smem);
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
@@ -265,25 +274,23 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, 1)
     ct.abort = 0;
     for (int r = 0; r < 2; ++r)
       for (int s = 0; s < 8; ++s) {
-        mbar_init(smem_u32(&ct.full[r][s]), 2);  // two copying warps
+        mbar_init(smem_u32(&ct.full[r][s]), kJobs);  // copying warps
         mbar_init(smem_u32(&ct.empty[r][s]), 1);
       }
     for (int s = 0; s < 2; ++s) {
       mbar_init(smem_u32(&ct.done[s]), 1);
-      mbar_init(smem_u32(&ct.q_full[s]), 2);
+      mbar_init(smem_u32(&ct.q_full[s]), kJobs);
       mbar_init(smem_u32(&ct.q_empty[s]), 1 + 4 * Sh::kGroups);  // the products, and the softmax warps
-    }
-    for (int s = 0; s < 4; ++s) {
       mbar_init(smem_u32(&ct.s_full[s]), 1);
-      mbar_init(smem_u32(&ct.p_full[s]), 4 * Sh::kGroups / Sh::kStreams);  // the warps that have the tile
+      mbar_init(smem_u32(&ct.p_full[s]), 4 * Sh::kGroups);
       mbar_init(smem_u32(&ct.pv_done[s]), 1);
     }
     fence_mbar_init();
     tma_prefetch_desc(&tm_k);
     tma_prefetch_desc(&tm_v);
   }
-  if (warp == 4) {
-    tmem_alloc(smem_u32(&ct.tmem), 512);
+  if (warp == 3 * kJobs) {
+    tmem_alloc(smem_u32(&ct.tmem), Sh::kTmem);
     tmem_relinquish();
   }
   tc_fence_before();
@@ -292,23 +299,23 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, 1)
   const uint32_t tmem = ct.tmem;
   pdl_launch_dependents();
   pdl_wait();
-  plan_start<kThreads, kKeys>(P.shape, gridDim.x, 2, &ct.plan, ct.sum);
+  plan_start<kThreads, kKeys, true>(P.shape, gridDim.x, 2, &ct.plan, ct.sum);
   const PlanStart& plan = ct.plan;
-  if (warp < 8) {
+  if (warp < 4 * kJobs) {
     fewer_registers<Sh::kFewer>();
     PieceWalk walk;
     walk.start(plan);
     Piece pc;
     bool ok = true, drain = false;
-    if (warp < 4) {
-      // ---- copies of K (warps 0, 1) and V (2, 3): every other box each ----
+    if (warp < 2 * kJobs) {
+      // ---- copies of K, and of V: every other box each where there are two warps ----
       // Lane (tile, box) looks up and copies a box of each of a batch of tiles.  What it reads for
       // the next batch is not used before the present one has been copied: the warp would wait for it.
-      const int ring = warp / 2, turn = warp % 2;
+      const int ring = warp / kJobs, turn = warp % kJobs;
       const bool keys = ring == 0;
       const CUtensorMap* map = keys ? &tm_k : &tm_v;
-      const int boxes = kKeys / P.kv_box, mine = (boxes + 1 - turn) / 2;
-      const int batch = min(32 / max(mine, 1), 8), my_tile = mine > 0 ? lane / mine : 32, box = mine > 0 ? lane % mine * 2 + turn : 0;
+      const int boxes = kKeys / P.kv_box, mine = (boxes + kJobs - 1 - turn) / kJobs;
+      const int batch = min(32 / max(mine, 1), 8), my_tile = mine > 0 ? lane / mine : 32, box = mine > 0 ? lane % mine * kJobs + turn : 0;
       const uint32_t slots = keys ? Sh::kRingK : Sh::kRingV, tiles_at = base + (keys ? 0 : Sh::kVAt);
       uint32_t tiles = 0, slot = 0, phase = 0;
       struct Lookup {
@@ -327,7 +334,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, 1)
         }
         return x;
       };
-      while (ok && walk.next<kKeys>(P.shape, plan, &pc)) {
+      while (ok && walk.next<kKeys, false, true>(P.shape, plan, &pc)) {
         const int nt = pc.k1 - pc.k0;
         if (nt == 0) continue;
         Lookup now = lookup(0);
@@ -368,76 +375,85 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, 1)
         }
       }
       drain = !ok;
-    } else if (warp == 4 || warp == 5) {
-      // ---- products: scores (warp 4) and O (warp 5) ----
-      // Issuing a tile's products and commits takes some 500 cycles of a warp; one warp for both had
-      // 1100 a tile, and was the bound with few rows.
-      const bool values = warp == 5;
+    } else if (warp < 3 * kJobs) {
+      // ---- products: scores (the first warp) and O (the second), or both (of one) ----
+      // Issuing a tile's products and commits takes a warp some 1100 cycles for both.
+      const bool does_scores = warp == 2 * kJobs, does_values = warp == 3 * kJobs - 1;
       uint32_t tiles = 0, pieces = 0;
       auto wait = [&](uint64_t* bar, uint32_t parity) {
         ok = ok && warp_wait_quick(bar, parity, abort);
         return ok;
       };
-      while (ok && walk.next<kKeys>(P.shape, plan, &pc)) {
+      auto scores = [&](int i) {
+        constexpr uint32_t kDesc = idesc_8bit(Sh::kSColumns, false);
+        const uint32_t g = tiles + i, b = g & 1u, slot = g % Sh::kRingK;
+        if (!wait(&ct.full[0][slot], g / Sh::kRingK & 1u)) return;
+        if (kJobs == 2 && g >= 2 && !wait(&ct.p_full[b], (g >> 1 & 1u) ^ 1u)) return;  // S has been read
+        tc_fence_after();
+        if (elect_one()) {
+          const uint64_t kd = rows_desc<DP>(base + slot * Sh::kTileBytes, 16), qd = rows_desc<DP>(base + Sh::kQAt + (pieces & 1u) * Sh::kQBytes, 16);
+#pragma unroll
+          for (int k = 0; k < DP / 32; ++k) tc_mma_8bit(tmem + b * Sh::kSColumns, kd + 2 * k, qd + 2 * k, kDesc, k > 0);
+          tc_commit(smem_u32(&ct.s_full[b]));
+          tc_commit(smem_u32(&ct.empty[0][slot]));
+        }
+        __syncwarp();
+      };
+      auto values = [&](int i) {
+        constexpr uint32_t kDesc = idesc_8bit(Sh::kOColumns, true);
+        const uint32_t g = tiles + i, b = g & 1u, slot = g % Sh::kRingV;
+        if (!wait(&ct.full[1][slot], g / Sh::kRingV & 1u) || !wait(&ct.p_full[b], g >> 1 & 1u)) return;
+        tc_fence_after();
+        if (elect_one()) {
+          // 64 columns of the head dimension fill half of M: the other half is the same again
+          const uint64_t vd = rows_desc<DP>(base + Sh::kVAt + slot * Sh::kTileBytes, 0);
+          const uint64_t pd = rows_desc<Sh::kPWidth>(base + Sh::kPAt + b * Sh::kPBytes, kKeys * Sh::kPWidth);
+#pragma unroll
+          for (int k = 0; k < kKeys / 32; ++k)
+            tc_mma_8bit(tmem + Sh::kOAt, vd + k * (32 * DP >> 4), pd + k * (32 * Sh::kPWidth >> 4), kDesc, i + k > 0);
+          tc_commit(smem_u32(&ct.pv_done[b]));
+          tc_commit(smem_u32(&ct.empty[1][slot]));
+        }
+        __syncwarp();
+      };
+      while (ok && walk.next<kKeys, false, true>(P.shape, plan, &pc)) {
         const int nt = pc.k1 - pc.k0;
         if (nt == 0) continue;
-        const uint32_t q = pieces & 1u;
-        if (!values) {
-          constexpr uint32_t kDesc = idesc_8bit(Sh::kSColumns, false);
-          if (!wait(&ct.q_full[q], pieces >> 1 & 1u)) break;
-          for (int i = 0; i < nt; ++i) {
-            const uint32_t g = tiles + i, b = g % kBuffers, slot = g % Sh::kRingK;
-            if (!wait(&ct.full[0][slot], g / Sh::kRingK & 1u)) break;
-            if (g >= kBuffers && !wait(&ct.p_full[b], (g / kBuffers & 1u) ^ 1u)) break;  // S has been read
-            tc_fence_after();
-            if (elect_one()) {
-              const uint64_t kd = rows_desc<DP>(base + slot * Sh::kTileBytes, 16), qd = rows_desc<DP>(base + Sh::kQAt + q * Sh::kQBytes, 16);
-#pragma unroll
-              for (int k = 0; k < DP / 32; ++k) tc_mma_8bit(tmem + b * Sh::kSColumns, kd + 2 * k, qd + 2 * k, kDesc, k > 0);
-              tc_commit(smem_u32(&ct.s_full[b]));
-              tc_commit(smem_u32(&ct.empty[0][slot]));
-            }
-            __syncwarp();
+        if (does_scores && !wait(&ct.q_full[pieces & 1u], pieces >> 1 & 1u)) break;
+        if constexpr (kJobs == 1) {
+          scores(0);
+          if (nt > 1) scores(1);
+          for (int i = 0; i < nt && ok; ++i) {
+            values(i);
+            if (ok && i + 2 < nt) scores(i + 2);
           }
-          if (!ok) break;
-          if (elect_one()) tc_commit(smem_u32(&ct.q_empty[q]));
-          __syncwarp();
         } else {
-          constexpr uint32_t kDesc = idesc_8bit(Sh::kOColumns, true);
-          for (int i = 0; i < nt; ++i) {
-            const uint32_t g = tiles + i, b = g % kBuffers, slot = g % Sh::kRingV;
-            if (!wait(&ct.full[1][slot], g / Sh::kRingV & 1u) || !wait(&ct.p_full[b], g / kBuffers & 1u)) break;
-            tc_fence_after();
-            if (elect_one()) {
-              // 64 columns of the head dimension fill half of M: the other half is the same again
-              const uint64_t vd = rows_desc<DP>(base + Sh::kVAt + slot * Sh::kTileBytes, 0);
-              const uint64_t pd = rows_desc<128>(base + Sh::kPAt + b * Sh::kPBytes, kKeys * 128);
-              const uint32_t t_o = tmem + Sh::kOAt + i % Sh::kStreams * Sh::kOColumns;
-#pragma unroll
-              for (int k = 0; k < kKeys / 32; ++k)
-                tc_mma_8bit(t_o, vd + k * (32 * DP >> 4), pd + k * (32 * 128 >> 4), kDesc, i >= Sh::kStreams || k > 0);
-              tc_commit(smem_u32(&ct.pv_done[b]));
-              tc_commit(smem_u32(&ct.empty[1][slot]));
-            }
-            __syncwarp();
-          }
-          if (!ok) break;
+          for (int i = 0; i < nt && ok; ++i)
+            if (does_scores)
+              scores(i);
+            else
+              values(i);
+        }
+        if (!ok) break;
+        if (does_scores) {
+          if (elect_one()) tc_commit(smem_u32(&ct.q_empty[pieces & 1u]));
+          __syncwarp();
         }
         ++pieces;
         tiles += nt;
       }
       if (!ok) {
         volatile int never = 0;
-        if (elect_one()) tc_commit(smem_u32(&ct.done[values]));
+        if (elect_one()) tc_commit(smem_u32(&ct.done[does_values]));
         __syncwarp();
-        mbar_wait_bounded(smem_u32(&ct.done[values]), 0, &never);
+        mbar_wait_bounded(smem_u32(&ct.done[does_values]), 0, &never);
       }
     } else {
       // ---- queries: rows of 128 or 64 bytes, each a sum of two e4m3 numbers times its row's unit ----
       constexpr int kEach = DP / 32;  // elements of a lane
       const int D = a.cache.head_dim;
       uint32_t pieces = 0;
-      while (ok && walk.next<kKeys>(P.shape, plan, &pc)) {
+      while (ok && walk.next<kKeys, false, true>(P.shape, plan, &pc)) {
         if (pc.k1 == pc.k0) continue;
         const uint32_t buffer = pieces & 1u;
         ok = warp_wait_quick(&ct.q_empty[buffer], (pieces >> 1 & 1u) ^ 1u, abort);
@@ -445,41 +461,69 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, 1)
         ++pieces;
         const int rows = (pc.i1 - pc.i0) * P.group;
         uint8_t* to = smem + Sh::kQAt + buffer * Sh::kQBytes;
-        for (int r0 = warp - 6; r0 < Sh::kRows; r0 += 2 * 4) {
-          // four rows' loads at a time
-          uint32_t raw[4][kEach / 2];
-          int token[4], head[4];
+        // Eight rows' elements at a time.
+        constexpr int kAtOnce = 8;
+        const int which = warp - 3 * kJobs;
+        uint32_t raw[kAtOnce][kEach / 2];
+        auto load = [&](int r0) {
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const int r = r0 + 2 * u;
-            token[u] = P.by_group(r);
-            head[u] = r - token[u] * P.group;
-            token[u] += pc.row0 + pc.i0;
-            head[u] += pc.head * P.group;
+          for (int u = 0; u < kAtOnce; ++u) {
+            const int r = r0 + kJobs * u, token = P.by_group(r), head = r - token * P.group;
 #pragma unroll
             for (int e = 0; e < kEach / 2; ++e) raw[u][e] = 0u;
             if (r < rows && lane * kEach < D) {
-              const __nv_bfloat16* from = static_cast<const __nv_bfloat16*>(a.q) + token[u] * a.q_token + head[u] * a.q_head + lane * kEach;
+              const __nv_bfloat16* from = static_cast<const __nv_bfloat16*>(a.q) + (long long)(pc.row0 + pc.i0 + token) * a.q_token +
+                                          (pc.head * P.group + head) * a.q_head + lane * kEach;
               if constexpr (kEach == 4)
                 *reinterpret_cast<uint2*>(raw[u]) = *reinterpret_cast<const uint2*>(from);
               else
                 raw[u][0] = *reinterpret_cast<const uint32_t*>(from);
             }
           }
+        };
+        // Magnitudes as whole numbers: infinities and NaN are the largest.
+        auto most_of = [&](int u) {
+          uint32_t most = 0u;
 #pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const int r = r0 + 2 * u;
+          for (int e = 0; e < kEach / 2; ++e) most = max(most, max(raw[u][e] & 0x7FFFu, raw[u][e] >> 16 & 0x7FFFu));
+          return __reduce_max_sync(0xFFFFFFFFu, most) << 16;
+        };
+        // The least exponent with a magnitude <= 448 times its power of two.
+        auto exponent_of = [](uint32_t top) { return min(max((int)(top >> 23) - 127 - 8 + ((top & 0x7FFFFFu) > 0x600000u), -120), 120); };
+        // The rows have the largest row's unit, and then the softmax one factor for all; where a row is much
+        // smaller (2^-6, of some 2^-17 that its elements may be off in that unit), each has its own.
+        int high = -120, low = 120;
+        for (int r0 = which; r0 < rows; r0 += kJobs * kAtOnce) {
+          load(r0);
+#pragma unroll
+          for (int u = 0; u < kAtOnce; ++u) {
+            const uint32_t top = most_of(u);
+            if (top != 0u && top < 0x7F800000u) {
+              high = max(high, exponent_of(top));
+              low = min(low, exponent_of(top));
+            }
+          }
+        }
+        if constexpr (kJobs == 2) {
+          if (lane == 0) ct.q_range[buffer][which] = make_int2(high, low);
+          named_barrier<5, 64>();
+          high = max(high, ct.q_range[buffer][which ^ 1].x);
+          low = min(low, ct.q_range[buffer][which ^ 1].y);
+        }
+        const bool even = high - low <= 6;
+        if (lane == 0 && which == 0) {
+          ct.even[buffer] = even;
+          ct.one_factor[buffer] = P.scale2 * power_of_two(high);
+        }
+        for (int r0 = which; r0 < Sh::kRows; r0 += kJobs * kAtOnce) {
+          if (Sh::kRows > kAtOnce) load(r0);  // else they are there
+#pragma unroll
+          for (int u = 0; u < kAtOnce; ++u) {
+            const int r = r0 + kJobs * u;
             if (r >= Sh::kRows) break;
-            // magnitudes as whole numbers: infinities and NaN are the largest
-            uint32_t most = 0u;
-#pragma unroll
-            for (int e = 0; e < kEach / 2; ++e) most = max(most, max(raw[u][e] & 0x7FFFu, raw[u][e] >> 16 & 0x7FFFu));
-            const uint32_t top = __reduce_max_sync(0xFFFFFFFFu, most) << 16;
-            // the least exponent with top <= 448 times its power of two; a row with an infinity or a
-            // NaN is NaN throughout, as its scores are
-            const int e = min(max((int)(top >> 23) - 127 - 8 + ((top & 0x7FFFFFu) > 0x600000u), -120), 120);
+            const uint32_t top = most_of(u);
+            const int e = even ? high : exponent_of(top);
             const float down = power_of_two(-e);
-            const bool nan = top >= 0x7F800000u;
             uint32_t lead = 0u, rest = 0u;
 #pragma unroll
             for (int i = 0; i < kEach / 2; ++i) {
@@ -489,7 +533,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, 1)
               lead |= c << (16 * i);
               rest |= to_e4m3x2((x - f.x) * 16.f, (y - f.y) * 16.f) << (16 * i);
             }
-            if (nan) lead = 0x7F7F7F7Fu;
+            if (top >= 0x7F800000u) lead = 0x7F7F7F7Fu;  // an infinity or a NaN: NaN throughout, as its scores are
             // the columns of the row's two parts
             const int group = r / R, in = r % R, chunk = in / 16, c = in % 16, size = min(16, R - 16 * chunk);
 #pragma unroll
@@ -503,8 +547,9 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, 1)
                 *reinterpret_cast<uint16_t*>(dst) = (uint16_t)(part ? rest : lead);
             }
             if (lane == 0) {
-              ct.factor[buffer][r] = r < rows ? P.scale2 * power_of_two(e) : 0.f;
-              ct.out[buffer][r] = token[u] * a.out_token + head[u] * a.out_head;
+              const int token = P.by_group(r);
+              ct.factor[buffer][r] = P.scale2 * power_of_two(e);
+              ct.out[buffer][r] = (pc.row0 + pc.i0 + token) * a.out_token + (pc.head * P.group + r - token * P.group) * a.out_head;
             }
           }
         }
@@ -523,10 +568,9 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, 1)
   } else {
     more_registers<Sh::kMore>();
     // ---- softmax: group h, one thread per key ----
-    constexpr bool kTwo = Sh::kStreams == 2;
-    const int h = (warp - kBase / 32) / 4, key = tid & 127, quarter = warp & 3, r0 = kTwo ? 0 : h * R;
+    const int h = (warp - kBase / 32) / 4, key = tid & 127, quarter = warp & 3, r0 = h * R;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    const uint32_t t_o = tmem + lanes + Sh::kOAt + (kTwo ? h * Sh::kOColumns : 0);
+    const uint32_t t_o = tmem + lanes + Sh::kOAt;
     const int D = a.cache.head_dim, G = P.group;
     uint32_t tiles = 0, pieces = 0;
     JoinUnit unit{};
@@ -543,12 +587,12 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, 1)
     const bool walker = key == 96;
     if (walker) {
       ct.walk[h].start(plan);
-      ct.more[h][0] = ct.walk[h].template next<kKeys, true>(P.shape, plan, &ct.piece[h][0]);
+      ct.more[h][0] = ct.walk[h].template next<kKeys, true, true>(P.shape, plan, &ct.piece[h][0]);
     }
     for (int np = 0;; np ^= 1) {
       group_barrier(h);
       if (!ct.more[h][np]) break;
-      if (walker) ct.more[h][np ^ 1] = ct.walk[h].template next<kKeys, true>(P.shape, plan, &ct.piece[h][np ^ 1]);
+      if (walker) ct.more[h][np ^ 1] = ct.walk[h].template next<kKeys, true, true>(P.shape, plan, &ct.piece[h][np ^ 1]);
       const Piece& pc = ct.piece[h][np];
       const int nt = pc.k1 - pc.k0, rows = (pc.i1 - pc.i0) * G;
       if (nt == 0) {  // nothing is visible
@@ -573,14 +617,15 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, 1)
       float2 l[R / 2];  // sums of this thread's keys
 #pragma unroll
       for (int i = 0; i < R / 2; ++i) l[i] = make_float2(0.f, 0.f);
-      bool far = false;  // some row's reference is far from zero
+      bool far = !ct.even[buffer];  // factors differ, or some row's reference is far from zero
+      const float one_factor = ct.one_factor[buffer];
       const UnitKeys keys = pc.keys;
       const int first = pc.c + pc.i0, k0 = pc.k0;  // position of the unit's first token
       const bool idle = r0 >= rows;
 
-      for (int j = kTwo ? h : 0; j < nt; j += Sh::kStreams) {
+      for (int j = 0; j < nt; ++j) {
         // what is known of the tile before its scores are there
-        const uint32_t g = tiles + j, b = g % kBuffers;
+        const uint32_t g = tiles + j, b = g & 1u;
         const int j0 = keys.tile(k0 + j) * kKeys, at = j0 + key;
         const bool edge = j0 < keys.lo || j0 + kKeys - 1 > keys.hi;
         // The key is seen by the rows [from, to).
@@ -591,14 +636,14 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, 1)
         if (at > keys.hi) to = 0;
         from -= r0;
         to -= r0;
-        wait(&ct.s_full[b], g / kBuffers & 1u);
-        if (g >= kBuffers) wait(&ct.pv_done[b], (g / kBuffers & 1u) ^ 1u);  // the weights' buffer is free
+        wait(&ct.s_full[b], g >> 1 & 1u);
+        if (g >= 2) wait(&ct.pv_done[b], (g >> 1 & 1u) ^ 1u);  // the weights' buffer is free
         tc_fence_after();
         const BoxUnits u = ct.units[g % kInfoTiles][key / P.kv_box];
         if (!u.there) to = from = -1000;
         // A row of V that no row of the unit sees holds anything, and 0 times that need not be 0:
         // cleared before the product.
-        if (edge && (kTwo || h == 0)) {
+        if (edge && h == 0) {
           // (the slot's phase before is over: its product was issued before the one waited for above)
           wait(&ct.full[1][g % Sh::kRingV], g / Sh::kRingV & 1u);
           if (at > keys.hi || (at < keys.lo && at >= a.sinks)) {
@@ -610,16 +655,17 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, 1)
         }
         if (!idle) {
           const bool masked = !__all_sync(0xFFFFFFFFu, from <= 0 && to >= min(rows - r0, R));
-          const uint32_t t_s = tmem + lanes + b * Sh::kSColumns + (kTwo ? 0 : h * Sh::kSGroup);
+          const uint32_t t_s = tmem + lanes + b * Sh::kSColumns + h * Sh::kSGroup;
           const float2 sixteenth = make_float2(0.0625f, 0.0625f), unit2 = make_float2(u.k, u.k), v2 = make_float2(u.v, u.v);
-          float y[R];  // exponents of the weights
+          const float2 factor2 = make_float2(u.k * one_factor, u.k * one_factor);
+          float y[R];  // exponents of the weights, then the weights
           auto hide = [&]() {
             if (!masked) return;
 #pragma unroll
             for (int r = 0; r < R; ++r)
               if (r < from || r >= to) y[r] = -INFINITY;
           };
-          // Scores in the keys' units, two rows at a time: f(row, scores).
+          // Scores, four rows at a time: f(row, two of them, two of them).
           auto scores = [&](auto&& f) {
             float s[2 * R];
             each_chunk<Sh::kChunks>([&](auto chunk) {
@@ -630,33 +676,55 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, 1)
             each_chunk<Sh::kChunks>([&](auto chunk) {
               constexpr int c = decltype(chunk)::value, n = Sh::rows_of(c);
 #pragma unroll
-              for (int i = 0; i < n; i += 2) {
-                const float2 x = fma2(make_float2(s[32 * c + n + i], s[32 * c + n + i + 1]), sixteenth, make_float2(s[32 * c + i], s[32 * c + i + 1]));
-                f(16 * c + i, mul2(x, unit2));
+              for (int i = 0; i < n; i += 4) {
+                float2 x[2];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                  const int at = 32 * c + i + 2 * k;
+                  x[k] = fma2(make_float2(s[at + n], s[at + n + 1]), sixteenth, make_float2(s[at], s[at + 1]));
+                }
+                f(16 * c + i, x[0], x[1]);
               }
             });
             hide();
           };
-          auto put = [&](int r, const float2& x) {
-            y[r] = x.x;
-            y[r + 1] = x.y;
+          auto put = [&](int r, const float2& p, const float2& q) {
+            y[r] = p.x;
+            y[r + 1] = p.y;
+            y[r + 2] = q.x;
+            y[r + 3] = q.y;
           };
-          auto two = [](const float* p) { return *reinterpret_cast<const float2*>(p); };
+          struct Four {
+            float2 p, q;
+          };
+          auto four = [](const float* from) {
+            const float4 x = *reinterpret_cast<const float4*>(from);
+            return Four{make_float2(x.x, x.y), make_float2(x.z, x.w)};
+          };
           // The product with the factor rounded before the reference is taken off, for references far from
           // zero; `fresh`: rows that have none keep their exponents.
           auto exact = [&](bool fresh) {
-            scores([&](int r, const float2& x) {
-              float2 ref = two(ct.minus[h] + r);
-              if (fresh && ref.x == kNone) ref.x = 0.f;
-              if (fresh && ref.y == kNone) ref.y = 0.f;
-              put(r, add2(add2(add2(mul2(x, two(factor + r)), ref), v2), two(ct.rest[h] + r)));
+            scores([&](int r, const float2& x0, const float2& x1) {
+              const Four factors = four(factor + r), rest = four(ct.rest[h] + r);
+              Four ref = four(ct.minus[h] + r);
+              if (fresh) {
+                if (ref.p.x == kNone) ref.p.x = 0.f;
+                if (ref.p.y == kNone) ref.p.y = 0.f;
+                if (ref.q.x == kNone) ref.q.x = 0.f;
+                if (ref.q.y == kNone) ref.q.y = 0.f;
+              }
+              put(r, add2(add2(add2(mul2(mul2(x0, unit2), factors.p), ref.p), v2), rest.p),
+                  add2(add2(add2(mul2(mul2(x1, unit2), factors.q), ref.q), v2), rest.q));
             });
           };
           auto exponents = [&]() {
             if (far)
               exact(false);
             else
-              scores([&](int r, const float2& x) { put(r, add2(fma2(x, two(factor + r), two(ct.minus[h] + r)), v2)); });
+              scores([&](int r, const float2& x0, const float2& x1) {
+                const Four ref = four(ct.minus[h] + r);
+                put(r, add2(fma2(x0, factor2, ref.p), v2), add2(fma2(x1, factor2, ref.q), v2));
+              });
           };
           // The rows' maxima, to ct.part.
           auto maxima = [&]() {
@@ -675,16 +743,19 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, 1)
           // The first tile sets the references.  After it a weight may outgrow its own, or a row may see
           // its first keys: then, too, the rows' maxima over the tile, new references (whole numbers,
           // so that they are the same however often they move), and what was summed so far in the new unit.
-          const bool fresh = j < Sh::kStreams;
+          const bool fresh = j == 0;
           bool raise = fresh;
           if (!fresh) {
             exponents();
             float top = -INFINITY;
 #pragma unroll
             for (int r = 0; r < R; r += 2) top = max3(top, y[r], y[r + 1]);
+            // (the weights do not wait for the answer: exponents are worked out again where they move)
+#pragma unroll
+            for (int r = 0; r < R; ++r) y[r] = exp2_fast(y[r]);
             raise = any_of_group(h, top > kMostTop);
           }
-          if (raise) {
+          if (__builtin_expect(raise, false)) {
             exact(true);
             maxima();
             float old = 0.f, old_rest = 0.f, now = 0.f, now_rest = 0.f, move = 0.f;
@@ -724,9 +795,9 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, 1)
             group_barrier(h);
             if (!fresh) {
 #pragma unroll
-              for (int r = 0; r < R; r += 2) l[r / 2] = mul2(l[r / 2], two(ct.scale[h] + r));
-              const uint32_t before = g - Sh::kStreams;
-              wait(&ct.pv_done[before % kBuffers], before / kBuffers & 1u);
+              for (int r = 0; r < R; r += 2) l[r / 2] = mul2(l[r / 2], *reinterpret_cast<const float2*>(ct.scale[h] + r));
+              const uint32_t before = g - 1;
+              wait(&ct.pv_done[before & 1u], before >> 1 & 1u);
               tc_fence_after();
               each_chunk<Sh::kChunks>([&](auto chunk) {
                 constexpr int c = decltype(chunk)::value, n = Sh::rows_of(c);
@@ -748,20 +819,24 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, 1)
               exact(false);
             } else {
 #pragma unroll
-              for (int r = 0; r < R; r += 2) put(r, add2(make_float2(y[r], y[r + 1]), two(ct.move[h] + r)));
+              for (int r = 0; r < R; r += 4) {
+                const Four move = four(ct.move[h] + r);
+                put(r, add2(make_float2(y[r], y[r + 1]), move.p), add2(make_float2(y[r + 2], y[r + 3]), move.q));
+              }
             }
+#pragma unroll
+            for (int r = 0; r < R; ++r) y[r] = exp2_fast(y[r]);
           }
 
-          uint8_t* weights = smem + Sh::kPAt + b * Sh::kPBytes + key * 128;
+          uint8_t* weights = smem + Sh::kPAt + b * Sh::kPBytes + key * Sh::kPWidth;
+          const int turn = Sh::kPWidth == 128 ? key & 7 : Sh::kPWidth == 64 ? key >> 1 & 3 : key >> 2 & 1;  // the swizzle
           const float2 inv2 = make_float2(u.inv, u.inv);
           each_chunk<Sh::kChunks>([&](auto chunk) {
             constexpr int c = decltype(chunk)::value, n = Sh::rows_of(c);
             uint32_t w[3 * n / 4];
 #pragma unroll
             for (int i = 0; i < n; i += 4) {
-              float e[4];
-#pragma unroll
-              for (int k = 0; k < 4; ++k) e[k] = exp2_fast(y[16 * c + i + k]);
+              const float e[4] = {y[16 * c + i], y[16 * c + i + 1], y[16 * c + i + 2], y[16 * c + i + 3]};
               l[(16 * c + i) / 2] = fma2(make_float2(e[0], e[1]), inv2, l[(16 * c + i) / 2]);
               l[(16 * c + i) / 2 + 1] = fma2(make_float2(e[2], e[3]), inv2, l[(16 * c + i) / 2 + 1]);
               take_apart(e, w[i / 4], w[n / 4 + i / 4], w[2 * (n / 4) + i / 4]);
@@ -770,7 +845,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, 1)
 #pragma unroll
             for (int i = 0; i < 3; ++i) {
               const int x = column + i * n;
-              uint8_t* to_w = weights + x / 128 * (kKeys * 128) + ((x % 128 / 16) ^ (key & 7)) * 16 + x % 16;
+              uint8_t* to_w = weights + x / Sh::kPWidth * (kKeys * Sh::kPWidth) + ((x % Sh::kPWidth / 16) ^ turn) * 16 + x % 16;
               if constexpr (n == 16)
                 *reinterpret_cast<uint4*>(to_w) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
               else
@@ -794,39 +869,23 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, 1)
         join_lanes<n>(v, lane, [](float p, float q) { return p + q; });
         if (lane < n) ct.part[h][quarter][16 * c + lane] = v[0];
       });
-      if constexpr (kTwo)
-        named_barrier<1, 256>();
-      else
-        group_barrier(h);
+      group_barrier(h);
       const bool whole = pc.pieces == 1;
       float* part = a.partials + ((long long)blockIdx.x * 2 + (pc.k0 == 0 ? 1 : 0)) * Sh::kPart;
       auto sum_of = [&](int s, int r) { return (ct.part[s][0][r] + ct.part[s][1][r]) + (ct.part[s][2][r] + ct.part[s][3][r]); };
       if (key < R) {
-        // What O is multiplied by, so that it refers to `top`: to a number, where minus and rest are two.
+        // What O is multiplied by, so that it refers to m: to a number, where minus and rest are two.
         const float m = -(ct.minus[h][key] + ct.rest[h][key]);
-        float sum = sum_of(h, key), top = m, f;
-        if constexpr (kTwo) {  // the larger reference for both streams
-          const float other = -(ct.minus[h ^ 1][key] + ct.rest[h ^ 1][key]), other_sum = sum_of(h ^ 1, key);
-          const bool mine = ct.minus[h][key] != kNone, theirs = ct.minus[h ^ 1][key] != kNone;
-          top = !theirs ? m : !mine ? other : fmaxf(m, other);
-          f = mine ? exp2_fast(-((ct.minus[h][key] + top) + ct.rest[h][key])) : 0.f;
-          sum = sum * f + other_sum * (theirs ? exp2_fast(-((ct.minus[h ^ 1][key] + top) + ct.rest[h ^ 1][key])) : 0.f);
-        } else {
-          f = exp2_fast(-((ct.minus[h][key] + top) + ct.rest[h][key]));
-          sum *= f;
-        }
+        const float f = exp2_fast(-((ct.minus[h][key] + m) + ct.rest[h][key])), sum = sum_of(h, key) * f;
         ct.scale[h][key] = whole ? (sum == 0.f ? 0.f : f / sum) : f;
-        if (!whole && ok && r0 + key < rows && (!kTwo || h == 0))
-          *reinterpret_cast<float2*>(part + Sh::kRows * DP + (r0 + key) * 2) = make_float2(sum == 0.f ? -INFINITY : top, sum);
+        if (!whole && ok && r0 + key < rows)
+          *reinterpret_cast<float2*>(part + Sh::kRows * DP + (r0 + key) * 2) = make_float2(sum == 0.f ? -INFINITY : m, sum);
       }
-      if constexpr (kTwo)
-        named_barrier<1, 256>();
-      else
-        group_barrier(h);
+      group_barrier(h);
       // O is complete
       if (ok) {
         const uint32_t last = tiles - 1;
-        wait(&ct.pv_done[last % kBuffers], last / kBuffers & 1u);
+        wait(&ct.pv_done[last & 1u], last >> 1 & 1u);
         tc_fence_after();
       }
       // `key` is the lane, the element of the head; row r of x[i] goes out.
@@ -841,32 +900,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, 1)
             static_cast<__nv_bfloat16*>(a.out)[ct.out[buffer][r] + key] = __float2bfloat16_rn(x[i]);
         }
       };
-      if constexpr (kTwo) {
-        // half of the rows to each group, from both streams' O (the second has none where there was one tile)
-        constexpr int n = R / 2, c = R == 32 ? 16 : R;  // rows of a chunk
-        const int from = h * n;
-        if (ok && from < rows) {
-          float x[n];
-#pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            if (s == 1 && nt == 1) break;
-            float o[3 * n];
-            const uint32_t column = tmem + lanes + Sh::kOAt + s * Sh::kOColumns + (R == 32 ? 48 * h : from);
-#pragma unroll
-            for (int p = 0; p < 3; ++p) tmem_load<n>(column + p * c, o + p * n);
-            tmem_wait_ld();
-#pragma unroll
-            for (int i = 0; i < n; ++i) {
-              const float f = ct.scale[s][from + i], y = o[i] + (o[n + i] + o[2 * n + i] * 0.03125f);
-              x[i] = s == 0 ? (f == 0.f ? 0.f : y * f) : (f == 0.f ? x[i] : fmaf(y, f, x[i]));
-            }
-          }
-          put_rows(from, x, n);
-        }
-        tc_fence_before();
-        named_barrier<1, 256>();  // both are through with O
-        tc_fence_after();
-      } else if (ok) {
+      if (ok) {
         each_chunk<Sh::kChunks>([&](auto chunk) {
           constexpr int c = decltype(chunk)::value, n = Sh::rows_of(c);
           if (r0 + 16 * c >= rows) return;
@@ -889,7 +923,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, 1)
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 4) tmem_dealloc(tmem, 512);
+  if (warp == 3 * kJobs) tmem_dealloc(tmem, Sh::kTmem);
 }
 
 template <int DP, int R>
@@ -908,12 +942,13 @@ cudaError_t launch(TcParams& p, const DeviceInfo& dev, cudaStream_t stream) {
   if (!encode(&mk, c.k, 4, dims, strides, box, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, swizzle, promotion) ||
       !encode(&mv, c.v, 4, dims, strides, box, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, swizzle, promotion))
     return cudaErrorInvalidValue;
-  constexpr size_t smem = Sh::kControl + sizeof(Control<R>);
-  static_assert(smem <= 227 * 1024, "shared memory of a CTA");
+  constexpr size_t smem = Sh::kControl + sizeof(Control<R, Sh::kGroups>);
+  static_assert(smem <= (Sh::kFew ? 113 : 227) * 1024, "shared memory of a CTA");
   static std::atomic<uint64_t> allowed{0};
   cudaError_t e = allow_shared(attend_fp8_tc_kernel<DP, R>, smem, dev, allowed);
   if (e != cudaSuccess) return e;
-  const int grid = dev.sm_count < kAttendMaxTcCtas ? dev.sm_count : kAttendMaxTcCtas;
+  const int grid = Sh::kPerSm * (dev.sm_count < kAttendMaxTcCtas ? dev.sm_count : kAttendMaxTcCtas);
+  static_assert(2 * kAttendMaxTcCtas <= kAttendMaxCtas, "entries of the CTAs");
   e = launch_dependent(attend_fp8_tc_kernel<DP, R>, dim3(grid), dim3(Sh::kThreads), smem, stream, 1u, mk, mv, p);
   if (e != cudaSuccess) return e;
   return launch_attend_join(a, PartShape{Sh::kRows, DP, 1.f}, grid, stream);
@@ -925,7 +960,6 @@ cudaError_t launch_rows(TcParams& p, const DeviceInfo& dev, cudaStream_t stream)
   const long long rows = (long long)p.a.T * p.group, B = p.a.B;
   if (p.group <= 8 && rows <= 8 * B) return launch<DP, 8>(p, dev, stream);
   if (p.group <= 16 && rows <= 16 * B) return launch<DP, 16>(p, dev, stream);
-  if (p.group <= 32 && rows <= 32 * B) return launch<DP, 32>(p, dev, stream);
   return launch<DP, 24>(p, dev, stream);
 }
 

@@ -3,7 +3,7 @@
 // A unit is the rows of `unit_tokens` consecutive tokens of a sequence under one
 // key/value head (G query heads each), its cost the number of key tiles that any
 // of its rows sees, at least one (an empty unit writes zeros).  The units follow
-// one another by sequence, head, token; CTA i takes the costs [i share, (i+1) share) of
+// one another by sequence, head, token (or by head, sequence, token); CTA i takes the costs [i share, (i+1) share) of
 // that row, so the CTAs have the same number of key tiles whatever the lengths are, and
 // a long context is split over as many CTAs as it fills.  The lengths are device data,
 // so every CTA finds its own range: one scan over the sequences.  A unit that several
@@ -125,8 +125,8 @@ struct PieceWalk {
     unit = p.unit;
   }
   // The piece at `at`, and on to the next one.  False at the end of the range.  `pieces` is
-  // worked out only where it is asked for.
-  template <int kKeys, bool kPieces = false>
+  // worked out only where it is asked for.  kHeads: all sequences under a head follow one another.
+  template <int kKeys, bool kPieces = false, bool kHeads = false>
   __device__ __forceinline__ bool next(const AttendShape& s, const PlanStart& p, Piece* out) {
     if (at >= p.end) return false;
     for (;;) {
@@ -144,7 +144,12 @@ struct PieceWalk {
       }
       // past the sequence's last unit: the next head, or the next sequence
       unit = 0;
-      if (q.n > 0 && head + 1 < s.kv_heads) {
+      if constexpr (kHeads) {
+        if (++b >= s.B) {
+          b = 0;
+          if (++head >= s.kv_heads) return false;
+        }
+      } else if (q.n > 0 && head + 1 < s.kv_heads) {
         ++head;
       } else {
         head = 0;
@@ -171,8 +176,8 @@ struct PieceWalk {
 };
 
 // Finds this CTA's share; all kThreads threads of the CTA call it.  `s_sum` has
-// one entry per warp.  At least `least` key tiles to a CTA.
-template <int kThreads, int kKeys>
+// one entry per warp.  At least `least` key tiles to a CTA.  kHeads: as in PieceWalk.
+template <int kThreads, int kKeys, bool kHeads = false>
 __device__ __forceinline__ void plan_start(const AttendShape& s, int grid, int least, PlanStart* s_plan, long long* s_sum) {
   static_assert(kThreads % 32 == 0, "whole warps");
   const int tid = threadIdx.x;
@@ -181,7 +186,7 @@ __device__ __forceinline__ void plan_start(const AttendShape& s, int grid, int l
   long long mine = 0;
   for (int i = 0; i < per; ++i) {
     const int b = tid * per + i;
-    mine += head_cost<kKeys>(s, b, b < s.B) * s.kv_heads;
+    mine += head_cost<kKeys>(s, b, b < s.B) * (kHeads ? 1 : s.kv_heads);
   }
   // Inclusive scan over the threads: warps, then their sums.
   long long x = mine;
@@ -197,7 +202,8 @@ __device__ __forceinline__ void plan_start(const AttendShape& s, int grid, int l
     if (w < tid / 32) before += s_sum[w];
     total += s_sum[w];
   }
-  const long long upto = before + x, from = upto - mine;
+  const long long upto = before + x, from = upto - mine, one_head = total;
+  if (kHeads) total *= s.kv_heads;
   if (total == 0) {
     if (tid == 0) *s_plan = PlanStart{0, 0, 0, 0, 0, 0, 0, 0};
     __syncthreads();
@@ -205,9 +211,12 @@ __device__ __forceinline__ void plan_start(const AttendShape& s, int grid, int l
   }
   const long long even = quotient(total + grid - 1, grid), share = even > least ? even : least;
   const long long begin = share * blockIdx.x, end = begin + share < total ? begin + share : total;
+  // Where the range begins among the costs that the threads have summed.
+  const int first_head = kHeads && begin < total ? (int)quotient(begin, one_head) : 0;
+  const long long start = kHeads ? begin - first_head * one_head : begin;
   if (begin >= total) {
     if (tid == 0) *s_plan = PlanStart{total, 0, 0, 0, share, 0, 0, 0};
-  } else if (from <= begin && begin < upto) {  // one thread: its sequences hold the start
+  } else if (from <= start && start < upto) {  // one thread: its sequences hold the start
     long long at = from;
     for (int i = 0; i < per; ++i) {
       const int b = tid * per + i;
@@ -216,19 +225,20 @@ __device__ __forceinline__ void plan_start(const AttendShape& s, int grid, int l
       const int c = cached_tokens(s.cache_len, b), units = units_of(s, q.n);
       long long one = 0;
       for (int u = 0; u < units; ++u) one += unit_cost<kKeys>(s, c, q.n, u);
-      if (begin < at + one * s.kv_heads) {
-        const int head = (int)quotient(begin - at, one);
-        at += head * one;
+      const long long all = kHeads ? one : one * s.kv_heads;
+      if (start < at + all) {
+        const int head = kHeads ? first_head : (int)quotient(start - at, one);
+        if (!kHeads) at += head * one;
         int u = 0;
         for (;; ++u) {
           const int cost = unit_cost<kKeys>(s, c, q.n, u);
-          if (begin < at + cost) break;
+          if (start < at + cost) break;
           at += cost;
         }
-        *s_plan = PlanStart{total, begin, end, at, share, b, head, u};
+        *s_plan = PlanStart{total, begin, end, at + (begin - start), share, b, head, u};
         break;
       }
-      at += one * s.kv_heads;
+      at += all;
     }
   }
   __syncthreads();
