@@ -8,10 +8,11 @@
 //                      thread's: one thread per key and half of the rows;
 //     O^T += V^T P^T   [head dim, rows]: V as it lies; a weight is the sum of three e5m2 numbers of 3
 //                      bits each, in columns of their own.
-// e5m2 is the upper byte of an fp16 number, so the first two parts of a weight are bytes of it and of
-// what is left, and the last, times 2^5, is rounded: 9 bits in all, where a bf16 weight has 8, or multiples
-// of 2^-21.  m is chosen so that the largest weight of a row's first tile is 2^4, and raised (O and l
-// rescaled) when one passes 2^15; so a weight is off by at most 2^-9 of it or 2^-26 of the row's largest.
+// e5m2 is the upper byte of an fp16 number, so the first part of a weight is a byte of it and the second
+// a byte of what is left, times 4; the last, times 32, is rounded: 9 bits in all, where a bf16 weight has 8,
+// down to 2^-13, and within 2^-22 below.  m puts the largest weight of a row's first tile at 2^4 (lower if
+// the tile shows few keys) and is raised, O and l rescaled, when a weight passes 2^15.  So a weight is off by
+// at most 2^-9 of it, or by 2^-26 of the row's largest (2^-19 from few keys).
 // Nothing is converted but the queries, once, and the weights: keys and values go from HBM to shared
 // memory to the tensor core, 256 D bytes a tile, 1400 cycles of an SM's share of HBM at D = 128.  The
 // products are 4 (2 rows + 3 rows) cycles at D = 128, shared memory moves some 1100 cycles' worth at
@@ -22,7 +23,7 @@
 // (taken apart a piece ahead), and the softmax in groups of four warps, a thread to a key.  Up to 16
 // rows a CTA has one group, and an SM two CTAs: a tile's way through the softmax, and the beginning
 // and end of a piece, are latencies, and the other CTA works meanwhile.  Up to 72 rows three groups
-// have 24 rows each, an SM one CTA, and there are two warps for each other job.
+// have 24 rows each, an SM one CTA, and the products two warps, the queries four.
 //
 // CTAs take the heads one after another, all sequences under each: then a sequence's heads, whose rows
 // of 128 bytes lie side by side, are read by several CTAs at about the same time, and not by one in turn.
@@ -59,8 +60,8 @@ struct TcShape {
   static constexpr int kGroups = R == 24 ? 3 : 1;
   static constexpr bool kFew = kGroups == 1;
   static constexpr int kPerSm = kFew ? 2 : 1;
-  static constexpr int kJobs = kFew ? 1 : 2;  // warps of each job but the softmax
-  static constexpr int kBase = 128 * kJobs;   // threads before the softmax's
+  static constexpr int kProducts = kFew ? 1 : 2, kQueries = kFew ? 1 : 4;   // warps
+  static constexpr int kBase = kFew ? 128 : 256;                            // threads before the softmax's
   static constexpr int kThreads = kBase + 128 * kGroups;
   static constexpr int kRows = R * kGroups;
   static constexpr int kChunks = (R + 15) / 16;
@@ -112,7 +113,7 @@ struct Control {
   Piece piece[kGroups][2];  // this one and the next
   int more[kGroups][2];
   BoxUnits units[kInfoTiles][kMostBoxes];
-  int2 q_range[2][2];  // largest and smallest exponent of the rows of a warp
+  int2 q_range[2][4];  // largest and smallest exponent of the rows of a warp
   int even[2];         // the rows have one unit
   float one_factor[2];                        // scale log2(e) times it
   alignas(16) float factor[2][R * kGroups];   // and times a row's own
@@ -218,8 +219,9 @@ __device__ __forceinline__ uint32_t minus_halves(uint32_t a, uint32_t b) {
   const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-__device__ __forceinline__ uint32_t times_32(uint32_t a) {
-  const __half2 h = __hmul2(*reinterpret_cast<const __half2*>(&a), __float2half2_rn(32.f));
+template <int kBy>
+__device__ __forceinline__ uint32_t times(uint32_t a) {
+  const __half2 h = __hmul2(*reinterpret_cast<const __half2*>(&a), __float2half2_rn((float)kBy));
   return *reinterpret_cast<const uint32_t*>(&h);
 }
 // Four fp16 numbers to e5m2, to the nearest, a byte each.
@@ -233,14 +235,14 @@ __device__ __forceinline__ uint32_t to_e5m2x4(uint32_t a, uint32_t b) {
       : "r"(a), "r"(b));
   return y;
 }
-// The three parts of four weights, none negative, a byte each; the third times 2^5.
+// The three parts of four weights, none negative, a byte each; the second times 4, the third times 32.
 __device__ __forceinline__ void take_apart(const float (&w)[4], uint32_t& first, uint32_t& second, uint32_t& third) {
   const uint32_t a = halves(w[0], w[1]), b = halves(w[2], w[3]);
-  const uint32_t a1 = minus_halves(a, a & 0xFF00FF00u), b1 = minus_halves(b, b & 0xFF00FF00u);
+  const uint32_t a1 = times<4>(minus_halves(a, a & 0xFF00FF00u)), b1 = times<4>(minus_halves(b, b & 0xFF00FF00u));
   const uint32_t a2 = minus_halves(a1, a1 & 0xFF00FF00u), b2 = minus_halves(b1, b1 & 0xFF00FF00u);
   first = __byte_perm(a, b, 0x7531);
   second = __byte_perm(a1, b1, 0x7531);
-  third = to_e5m2x4(times_32(a2), times_32(b2));
+  third = to_e5m2x4(times<8>(a2), times<8>(b2));
 }
 
 template <int I>
@@ -261,7 +263,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
                          const __grid_constant__ TcParams P) {
   using Sh = TcShape<DP, R>;
   using Ct = Control<R, Sh::kGroups>;
-  constexpr int kThreads = Sh::kThreads, kBase = Sh::kBase, kJobs = Sh::kJobs;
+  constexpr int kThreads = Sh::kThreads, kBase = Sh::kBase, kProducts = Sh::kProducts, kQueries = Sh::kQueries;
   static_assert(sizeof(Ct) <= Sh::kControlBytes, "room of the control block");
   extern __shared__ __align__(1024) uint8_t smem[];
   Ct& ct = *reinterpret_cast<Ct*>(smem + Sh::kControl);
@@ -274,12 +276,12 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
     ct.abort = 0;
     for (int r = 0; r < 2; ++r)
       for (int s = 0; s < 8; ++s) {
-        mbar_init(smem_u32(&ct.full[r][s]), kJobs);  // copying warps
+        mbar_init(smem_u32(&ct.full[r][s]), 1);
         mbar_init(smem_u32(&ct.empty[r][s]), 1);
       }
     for (int s = 0; s < 2; ++s) {
       mbar_init(smem_u32(&ct.done[s]), 1);
-      mbar_init(smem_u32(&ct.q_full[s]), kJobs);
+      mbar_init(smem_u32(&ct.q_full[s]), kQueries);
       mbar_init(smem_u32(&ct.q_empty[s]), 1 + 4 * Sh::kGroups);  // the products, and the softmax warps
       mbar_init(smem_u32(&ct.s_full[s]), 1);
       mbar_init(smem_u32(&ct.p_full[s]), 4 * Sh::kGroups);
@@ -289,7 +291,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
     tma_prefetch_desc(&tm_k);
     tma_prefetch_desc(&tm_v);
   }
-  if (warp == 3 * kJobs) {
+  if (warp == 3) {
     tmem_alloc(smem_u32(&ct.tmem), Sh::kTmem);
     tmem_relinquish();
   }
@@ -301,84 +303,90 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
   pdl_wait();
   plan_start<kThreads, kKeys, true>(P.shape, gridDim.x, 2, &ct.plan, ct.sum);
   const PlanStart& plan = ct.plan;
-  if (warp < 4 * kJobs) {
+  if (warp < kBase / 32) {
     fewer_registers<Sh::kFewer>();
     PieceWalk walk;
     walk.start(plan);
     Piece pc;
     bool ok = true, drain = false;
-    if (warp < 2 * kJobs) {
-      // ---- copies of K, and of V: every other box each where there are two warps ----
-      // Lane (tile, box) looks up and copies a box of each of a batch of tiles.  What it reads for
-      // the next batch is not used before the present one has been copied: the warp would wait for it.
-      const int ring = warp / kJobs, turn = warp % kJobs;
-      const bool keys = ring == 0;
+    if (warp < 2) {
+      // ---- copies of K (warp 0) and V (1) ----
+      // Lane (tile, box) looks up and copies a box of each of a batch of tiles.  A batch's pages are read
+      // two batches ahead of its copies, their exponents one, whether it is of the same piece or not:
+      // the warp never waits for what it has just asked for.
+      const bool keys = warp == 0;
       const CUtensorMap* map = keys ? &tm_k : &tm_v;
-      const int boxes = kKeys / P.kv_box, mine = (boxes + kJobs - 1 - turn) / kJobs;
-      const int batch = min(32 / max(mine, 1), 8), my_tile = mine > 0 ? lane / mine : 32, box = mine > 0 ? lane % mine * kJobs + turn : 0;
+      const int boxes = kKeys / P.kv_box, batch = min(32 / boxes, 8), my_tile = lane / boxes, box = lane % boxes;
       const uint32_t slots = keys ? Sh::kRingK : Sh::kRingV, tiles_at = base + (keys ? 0 : Sh::kVAt);
       uint32_t tiles = 0, slot = 0, phase = 0;
-      struct Lookup {
-        int slot;          // within the page
-        bool listed;       // the table has an entry for it
-        const int32_t* at;
+      struct Batch {
+        int count;       // tiles; 0: no more
+        int head, slot;  // slot: within the page
+        int page;
+        int ke, ve;
       };
-      auto lookup = [&](int k) {  // of this lane's box of tile k + my_tile of the piece
-        Lookup x{0, false, a.cache.page_table};
-        k += my_tile;
-        if (my_tile < batch && k < pc.k1 - pc.k0) {
-          const int j = pc.keys.tile(pc.k0 + k) * kKeys + box * P.kv_box, i = P.page_size(j);
-          x.slot = j - i * P.page_size.by;
-          x.listed = i < a.cache.max_pages;
-          if (x.listed) x.at += pc.b * a.cache.table_stride + i;
+      int nt = 0, k = 0;
+      auto pages = [&]() {  // of the next batch
+        Batch x{0, 0, 0, -1, 0, 0};
+        while (k >= nt) {
+          if (!walk.next<kKeys, false, true>(P.shape, plan, &pc)) return x;
+          nt = pc.k1 - pc.k0;
+          k = 0;
         }
+        x.count = min(batch, nt - k);
+        x.head = pc.head;
+        if (my_tile < x.count) {
+          const int j = pc.keys.tile(pc.k0 + k + my_tile) * kKeys + box * P.kv_box, i = P.page_size(j);
+          x.slot = j - i * P.page_size.by;
+          if (i < a.cache.max_pages) x.page = a.cache.page_table[pc.b * a.cache.table_stride + i];
+        }
+        k += batch;
         return x;
       };
-      while (ok && walk.next<kKeys, false, true>(P.shape, plan, &pc)) {
-        const int nt = pc.k1 - pc.k0;
-        if (nt == 0) continue;
-        Lookup now = lookup(0);
-        int page = now.listed ? *now.at : -1;
-        for (int k = 0; k < nt && ok; k += batch) {
-          // a box without a page lies outside the tensor: zeros
-          if (page < 0 || page >= a.cache.num_pages) page = a.cache.num_pages;
-          const bool there = page < a.cache.num_pages;
-          int ke = 0, ve = 0;
-          if (keys && there) {
-            const long long at = page * a.exp_page + pc.head * a.exp_head;
-            ke = a.k_exp[at];
-            ve = a.v_exp[at];
-          }
-          const Lookup next = lookup(k + batch);
-          const int next_page = next.listed ? *next.at : -1;
-          for (int t = 0; t < min(batch, nt - k); ++t) {
-            ok = warp_wait_quick(&ct.empty[ring][slot], phase ^ 1u, abort);
-            if (!ok) break;
-            const uint32_t bar = smem_u32(&ct.full[ring][slot]);
-            const bool active = my_tile == t;
-            if (keys && active)
-              ct.units[tiles % kInfoTiles][box] = there ? BoxUnits{power_of_two(clamp_exponent(ke)), (float)clamp_exponent(ve), power_of_two(-clamp_exponent(ve)), 1}
-                                                        : BoxUnits{1.f, 0.f, 1.f, 0};
-            __syncwarp();
-            if (lane == 0) mbar_arrive_expect_tx(bar, mine * P.kv_box * DP);
-            __syncwarp();
-            if (active)
-              tma_load_4d(tiles_at + slot * Sh::kTileBytes + box * P.kv_box * DP, map, 0, pc.head, now.slot, page, bar);
-            if (++slot == slots) {
-              slot = 0;
-              phase ^= 1u;
-            }
-            ++tiles;
-          }
-          now = next;
-          page = next_page;
+      auto exponents = [&](Batch& x) {
+        // a box without a page lies outside the tensor: zeros
+        if (x.page < 0 || x.page >= a.cache.num_pages) x.page = a.cache.num_pages;
+        if (keys && x.page < a.cache.num_pages) {
+          const long long at = x.page * a.exp_page + x.head * a.exp_head;
+          x.ke = a.k_exp[at];
+          x.ve = a.v_exp[at];
         }
+      };
+      Batch now = pages();
+      exponents(now);
+      Batch next = pages();
+      while (ok && now.count > 0) {
+        exponents(next);
+        const Batch after = pages();
+        for (int t = 0; t < now.count; ++t) {
+          ok = warp_wait_quick(&ct.empty[!keys][slot], phase ^ 1u, abort);
+          if (!ok) break;
+          const uint32_t bar = smem_u32(&ct.full[!keys][slot]);
+          const bool active = my_tile == t;
+          if (keys && active) {
+            const int ve = clamp_exponent(now.ve);
+            ct.units[tiles % kInfoTiles][box] = now.page < a.cache.num_pages ? BoxUnits{power_of_two(clamp_exponent(now.ke)), (float)ve, power_of_two(-ve), 1}
+                                                                             : BoxUnits{1.f, 0.f, 1.f, 0};
+          }
+          __syncwarp();
+          if (lane == 0) mbar_arrive_expect_tx(bar, Sh::kTileBytes);
+          __syncwarp();
+          if (active)
+            tma_load_4d(tiles_at + slot * Sh::kTileBytes + box * P.kv_box * DP, map, 0, now.head, now.slot, now.page, bar);
+          if (++slot == slots) {
+            slot = 0;
+            phase ^= 1u;
+          }
+          ++tiles;
+        }
+        now = next;
+        next = after;
       }
       drain = !ok;
-    } else if (warp < 3 * kJobs) {
+    } else if (warp < 2 + kProducts) {
       // ---- products: scores (the first warp) and O (the second), or both (of one) ----
       // Issuing a tile's products and commits takes a warp some 1100 cycles for both.
-      const bool does_scores = warp == 2 * kJobs, does_values = warp == 3 * kJobs - 1;
+      const bool does_scores = warp == 2, does_values = warp == 1 + kProducts;
       uint32_t tiles = 0, pieces = 0;
       auto wait = [&](uint64_t* bar, uint32_t parity) {
         ok = ok && warp_wait_quick(bar, parity, abort);
@@ -388,7 +396,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
         constexpr uint32_t kDesc = idesc_8bit(Sh::kSColumns, false);
         const uint32_t g = tiles + i, b = g & 1u, slot = g % Sh::kRingK;
         if (!wait(&ct.full[0][slot], g / Sh::kRingK & 1u)) return;
-        if (kJobs == 2 && g >= 2 && !wait(&ct.p_full[b], (g >> 1 & 1u) ^ 1u)) return;  // S has been read
+        if (kProducts == 2 && g >= 2 && !wait(&ct.p_full[b], (g >> 1 & 1u) ^ 1u)) return;  // S has been read
         tc_fence_after();
         if (elect_one()) {
           const uint64_t kd = rows_desc<DP>(base + slot * Sh::kTileBytes, 16), qd = rows_desc<DP>(base + Sh::kQAt + (pieces & 1u) * Sh::kQBytes, 16);
@@ -420,7 +428,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
         const int nt = pc.k1 - pc.k0;
         if (nt == 0) continue;
         if (does_scores && !wait(&ct.q_full[pieces & 1u], pieces >> 1 & 1u)) break;
-        if constexpr (kJobs == 1) {
+        if constexpr (kProducts == 1) {
           scores(0);
           if (nt > 1) scores(1);
           for (int i = 0; i < nt && ok; ++i) {
@@ -449,9 +457,10 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
         mbar_wait_bounded(smem_u32(&ct.done[does_values]), 0, &never);
       }
     } else {
-      // ---- queries: rows of 128 or 64 bytes, each a sum of two e4m3 numbers times its row's unit ----
-      constexpr int kEach = DP / 32;  // elements of a lane
-      const int D = a.cache.head_dim;
+      // ---- queries: rows of 128 or 64 bytes, each a sum of two e4m3 numbers times a unit ----
+      // A lane has 16 elements of a row.
+      constexpr int kLanes = DP / 16, kAtOnce = 32 / kLanes;
+      const int which = warp - 2 - kProducts, D = a.cache.head_dim, col = lane % kLanes * 16;
       uint32_t pieces = 0;
       while (ok && walk.next<kKeys, false, true>(P.shape, plan, &pc)) {
         if (pc.k1 == pc.k0) continue;
@@ -461,92 +470,77 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
         ++pieces;
         const int rows = (pc.i1 - pc.i0) * P.group;
         uint8_t* to = smem + Sh::kQAt + buffer * Sh::kQBytes;
-        // Eight rows' elements at a time.
-        constexpr int kAtOnce = 8;
-        const int which = warp - 3 * kJobs;
-        uint32_t raw[kAtOnce][kEach / 2];
-        auto load = [&](int r0) {
-#pragma unroll
-          for (int u = 0; u < kAtOnce; ++u) {
-            const int r = r0 + kJobs * u, token = P.by_group(r), head = r - token * P.group;
-#pragma unroll
-            for (int e = 0; e < kEach / 2; ++e) raw[u][e] = 0u;
-            if (r < rows && lane * kEach < D) {
-              const __nv_bfloat16* from = static_cast<const __nv_bfloat16*>(a.q) + (long long)(pc.row0 + pc.i0 + token) * a.q_token +
-                                          (pc.head * P.group + head) * a.q_head + lane * kEach;
-              if constexpr (kEach == 4)
-                *reinterpret_cast<uint2*>(raw[u]) = *reinterpret_cast<const uint2*>(from);
-              else
-                raw[u][0] = *reinterpret_cast<const uint32_t*>(from);
-            }
-          }
-        };
-        // Magnitudes as whole numbers: infinities and NaN are the largest.
-        auto most_of = [&](int u) {
+        uint4 raw[2];
+        uint32_t top;  // the row's largest magnitude, as bits: infinities and NaN are the largest
+        auto load = [&](int r) {
+          const int token = P.by_group(r);
+          const __nv_bfloat16* from = static_cast<const __nv_bfloat16*>(a.q) + (long long)(pc.row0 + pc.i0 + token) * a.q_token +
+                                      (pc.head * P.group + r - token * P.group) * a.q_head + col;
+          raw[0] = raw[1] = make_uint4(0u, 0u, 0u, 0u);
+          if (r < rows && col < D) raw[0] = *reinterpret_cast<const uint4*>(from);
+          if (r < rows && col + 8 < D) raw[1] = *reinterpret_cast<const uint4*>(from + 8);
+          constexpr uint32_t kMagnitude = 0x7FFF7FFFu;
           uint32_t most = 0u;
 #pragma unroll
-          for (int e = 0; e < kEach / 2; ++e) most = max(most, max(raw[u][e] & 0x7FFFu, raw[u][e] >> 16 & 0x7FFFu));
-          return __reduce_max_sync(0xFFFFFFFFu, most) << 16;
+          for (int i = 0; i < 2; ++i)
+            most = __vmaxu2(__vmaxu2(most, __vmaxu2(raw[i].x & kMagnitude, raw[i].y & kMagnitude)), __vmaxu2(raw[i].z & kMagnitude, raw[i].w & kMagnitude));
+#pragma unroll
+          for (int o = 1; o < kLanes; o <<= 1) most = __vmaxu2(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+          top = max(most & 0xFFFFu, most >> 16) << 16;
         };
         // The least exponent with a magnitude <= 448 times its power of two.
-        auto exponent_of = [](uint32_t top) { return min(max((int)(top >> 23) - 127 - 8 + ((top & 0x7FFFFFu) > 0x600000u), -120), 120); };
+        auto exponent_of = [](uint32_t t) { return min(max((int)(t >> 23) - 127 - 8 + ((t & 0x7FFFFFu) > 0x600000u), -120), 120); };
         // The rows have the largest row's unit, and then the softmax one factor for all; where a row is much
         // smaller (2^-6, of some 2^-17 that its elements may be off in that unit), each has its own.
         int high = -120, low = 120;
-        for (int r0 = which; r0 < rows; r0 += kJobs * kAtOnce) {
-          load(r0);
-#pragma unroll
-          for (int u = 0; u < kAtOnce; ++u) {
-            const uint32_t top = most_of(u);
-            if (top != 0u && top < 0x7F800000u) {
-              high = max(high, exponent_of(top));
-              low = min(low, exponent_of(top));
-            }
-          }
+        for (int r0 = which * kAtOnce; r0 < rows; r0 += kQueries * kAtOnce) {
+          load(r0 + lane / kLanes);
+          const bool counts = top != 0u && top < 0x7F800000u;
+          high = max(high, __reduce_max_sync(0xFFFFFFFFu, counts ? exponent_of(top) : -120));
+          low = min(low, __reduce_min_sync(0xFFFFFFFFu, counts ? exponent_of(top) : 120));
         }
-        if constexpr (kJobs == 2) {
+        if constexpr (kQueries > 1) {
           if (lane == 0) ct.q_range[buffer][which] = make_int2(high, low);
-          named_barrier<5, 64>();
-          high = max(high, ct.q_range[buffer][which ^ 1].x);
-          low = min(low, ct.q_range[buffer][which ^ 1].y);
+          named_barrier<5, 32 * kQueries>();
+#pragma unroll
+          for (int i = 0; i < kQueries; ++i) {
+            high = max(high, ct.q_range[buffer][i].x);
+            low = min(low, ct.q_range[buffer][i].y);
+          }
         }
         const bool even = high - low <= 6;
         if (lane == 0 && which == 0) {
           ct.even[buffer] = even;
           ct.one_factor[buffer] = P.scale2 * power_of_two(high);
         }
-        for (int r0 = which; r0 < Sh::kRows; r0 += kJobs * kAtOnce) {
-          if (Sh::kRows > kAtOnce) load(r0);  // else they are there
+        for (int r0 = which * kAtOnce; r0 < Sh::kRows; r0 += kQueries * kAtOnce) {
+          const int r = r0 + lane / kLanes;
+          load(r);
+          const int e = even ? high : exponent_of(top);
+          const float down = power_of_two(-e);
+          uint32_t lead[4], rest[4];
 #pragma unroll
-          for (int u = 0; u < kAtOnce; ++u) {
-            const int r = r0 + kJobs * u;
-            if (r >= Sh::kRows) break;
-            const uint32_t top = most_of(u);
-            const int e = even ? high : exponent_of(top);
-            const float down = power_of_two(-e);
-            uint32_t lead = 0u, rest = 0u;
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t w[2] = {i == 0 ? raw[0].x : i == 1 ? raw[0].z : i == 2 ? raw[1].x : raw[1].z,
+                                   i == 0 ? raw[0].y : i == 1 ? raw[0].w : i == 2 ? raw[1].y : raw[1].w};
+            lead[i] = rest[i] = 0u;
 #pragma unroll
-            for (int i = 0; i < kEach / 2; ++i) {
-              const float x = bf16_lo(raw[u][i]) * down, y = bf16_hi(raw[u][i]) * down;
+            for (int k = 0; k < 2; ++k) {
+              const float x = bf16_lo(w[k]) * down, y = bf16_hi(w[k]) * down;
               const uint32_t c = to_e4m3x2(x, y);
               const float2 f = e4m3_floats(c);
-              lead |= c << (16 * i);
-              rest |= to_e4m3x2((x - f.x) * 16.f, (y - f.y) * 16.f) << (16 * i);
+              lead[i] |= c << (16 * k);
+              rest[i] |= to_e4m3x2((x - f.x) * 16.f, (y - f.y) * 16.f) << (16 * k);
             }
-            if (top >= 0x7F800000u) lead = 0x7F7F7F7Fu;  // an infinity or a NaN: NaN throughout, as its scores are
+            if (top >= 0x7F800000u) lead[i] = 0x7F7F7F7Fu;  // an infinity or a NaN: NaN throughout, as its scores are
+          }
+          if (r < Sh::kRows) {
             // the columns of the row's two parts
-            const int group = r / R, in = r % R, chunk = in / 16, c = in % 16, size = min(16, R - 16 * chunk);
-#pragma unroll
-            for (int part = 0; part < 2; ++part) {
-              const int n = group * Sh::kSGroup + 32 * chunk + part * size + c, at = lane * kEach;
-              const int chunk16 = DP == 128 ? (at / 16) ^ (n & 7) : (at / 16) ^ (n >> 1 & 3);
-              uint8_t* dst = to + n * DP + chunk16 * 16 + at % 16;
-              if constexpr (kEach == 4)
-                *reinterpret_cast<uint32_t*>(dst) = part ? rest : lead;
-              else
-                *reinterpret_cast<uint16_t*>(dst) = (uint16_t)(part ? rest : lead);
-            }
-            if (lane == 0) {
+            const int group = r / R, in = r % R, chunk = in / 16, size = min(16, R - 16 * chunk), n = group * Sh::kSGroup + 32 * chunk + in % 16;
+            auto at = [&](int n) { return to + n * DP + ((col / 16) ^ (DP == 128 ? n & 7 : n >> 1 & 3)) * 16; };
+            *reinterpret_cast<uint4*>(at(n)) = make_uint4(lead[0], lead[1], lead[2], lead[3]);
+            *reinterpret_cast<uint4*>(at(n + size)) = make_uint4(rest[0], rest[1], rest[2], rest[3]);
+            if (col == 0) {
               const int token = P.by_group(r);
               ct.factor[buffer][r] = P.scale2 * power_of_two(e);
               ct.out[buffer][r] = (pc.row0 + pc.i0 + token) * a.out_token + (pc.head * P.group + r - token * P.group) * a.out_head;
@@ -622,6 +616,13 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
       const UnitKeys keys = pc.keys;
       const int first = pc.c + pc.i0, k0 = pc.k0;  // position of the unit's first token
       const bool idle = r0 >= rows;
+      // Where the largest weight of a row's first tile goes: lower if the unit sees few of its keys (sinks,
+      // a window's edge) and others follow, which are likely to have larger scores.
+      float first_top = kFirstTop;
+      if (nt > 1) {
+        const int a0 = keys.tile(k0) * kKeys, seen = min(a0 + kKeys, keys.hi + 1) - max(a0, keys.lo), sinks = min(a.sinks, a0 + kKeys) - a0;
+        first_top -= (float)min(max(__clz(max(max(seen, sinks), 1)) - 24, 0), 7);
+      }
 
       for (int j = 0; j < nt; ++j) {
         // what is known of the tile before its scores are there
@@ -763,7 +764,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
             if (key < R) {
               old = now = ct.minus[h][key];
               old_rest = now_rest = ct.rest[h][key];
-              const float most = most_of(key), by = floorf(kFirstTop - most);
+              const float most = most_of(key), by = floorf((fresh ? first_top : kFirstTop) - most);
               if (old == kNone ? most > -INFINITY : most > kMostTop) {
                 const float from_zero = old == kNone ? 0.f : old;
                 if (fabsf(from_zero) >= kFar) {
@@ -786,7 +787,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
               exact(false);
               maxima();
               if (pending) {
-                now_rest = floorf(kFirstTop - most_of(key));
+                now_rest = floorf((fresh ? first_top : kFirstTop) - most_of(key));
                 ct.rest[h][key] = now_rest;
               }
               far = true;
@@ -909,7 +910,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
           for (int p = 0; p < 3; ++p) tmem_load<n>(t_o + Sh::o_column(h, c) + p * n, o + p * n);
           tmem_wait_ld();
 #pragma unroll
-          for (int i = 0; i < n; ++i) o[i] = (o[i] + (o[n + i] + o[2 * n + i] * 0.03125f)) * ct.scale[h][16 * c + i];
+          for (int i = 0; i < n; ++i) o[i] = (o[i] + (o[n + i] * 0.25f + o[2 * n + i] * 0.03125f)) * ct.scale[h][16 * c + i];
           put_rows(r0 + 16 * c, o, n);
         });
       }
@@ -923,7 +924,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 3 * kJobs) tmem_dealloc(tmem, Sh::kTmem);
+  if (warp == 3) tmem_dealloc(tmem, Sh::kTmem);
 }
 
 template <int DP, int R>
@@ -969,10 +970,10 @@ bool attend_fp8_tc_supported(const AttendArgs& a) {
   const retrace_kv_cache& c = a.cache;
   auto whole = [](long long x, int n) { return x % n == 0; };
   auto stride = [&](long long x, int extent) { return extent <= 1 || (x > 0 && whole(x, 16)); };
-  return a.dtype == RETRACE_BF16 && c.head_dim <= 128 && whole(c.head_dim, 4) && whole(c.page_size, 8) && c.num_pages > 0 &&
+  return a.dtype == RETRACE_BF16 && c.head_dim <= 128 && whole(c.head_dim, 8) && whole(c.page_size, 8) && c.num_pages > 0 &&
          a.q_heads / c.kv_heads <= 72 && stride(c.page_stride, c.num_pages) && stride(c.slot_stride, c.page_size) &&
-         stride(c.head_stride, c.kv_heads) && whole(a.q_token, 4) && whole(a.q_head, 4) && ((uintptr_t)a.q & 7u) == 0 &&
-         (((uintptr_t)c.k | (uintptr_t)c.v) & 15u) == 0;
+         stride(c.head_stride, c.kv_heads) && whole(a.q_token, 8) && whole(a.q_head, 8) &&
+         (((uintptr_t)a.q | (uintptr_t)c.k | (uintptr_t)c.v) & 15u) == 0;
 }
 
 size_t attend_fp8_tc_partial_bytes(int head_dim) {

@@ -2,8 +2,8 @@
 
 Tolerance.  The keys and values are what the cache stands for, exactly.  With bf16 queries the
 result is rounded once (at most 2^-8 of it) and the weights lose at most 2^-8 of sum p |v|: half of
-that by a rounding to 9 bits (2^-9 of each weight), the rest by weights below 2^-18 of the row's largest,
-each off by at most 2^-26 of that one, of which there would have to be 2^17.  The scores' errors add
+that by a rounding to 9 bits (2^-9 of each weight), the rest by weights below 2^-17 of the row's largest,
+each off by at most 2^-26 of that one (2^-19 where the first keys are few).  The scores' errors add
 far less.  In fp32 a score of up to 256 products has an error of about sqrt(256) * 2^-24 of
 their absolute sum (20 to 40 here), which is the relative error of a weight: 2e-5 of sum p |v|.
 """
