@@ -20,7 +20,7 @@
 // it scales with the rows that there are.
 //
 // Warps of a CTA: copies of K and of V (TMA boxes of the slots of a page), the products, the queries
-// (taken apart a piece ahead), and the softmax in groups of four warps, a thread to a key.  Up to 16
+// (taken apart a piece ahead), and the softmax in groups of four warps, a thread to a key.  Up to 32
 // rows a CTA has one group, and an SM two CTAs: a tile's way through the softmax, and the beginning
 // and end of a piece, are latencies, and the other CTA works meanwhile.  Up to 72 rows three groups
 // have 24 rows each, an SM one CTA, and the products two warps, the queries four.
@@ -79,7 +79,7 @@ struct TcShape {
   static_assert(kBase * kFewer + 128 * kGroups * kMore <= kThreads * (65536 / (kThreads * kPerSm) / 8 * 8), "registers of a CTA");
 
   static constexpr int kTileBytes = kKeys * DP;
-  static constexpr int kPWidth = kOColumns > 64 ? 128 : kOColumns > 32 ? 64 : 32;  // bytes of a key's columns of P side by side
+  static constexpr int kPWidth = kOColumns == 96 ? 32 : kOColumns > 64 ? 128 : kOColumns > 32 ? 64 : 32;  // bytes of a key's columns of P side by side
   static constexpr int kPBytes = (kOColumns + kPWidth - 1) / kPWidth * kKeys * kPWidth;
   static constexpr int kQBytes = (kSColumns * DP + 1023) / 1024 * 1024;
   static constexpr int kControlBytes = kFew ? 7 * 1024 : 12 * 1024;
@@ -91,10 +91,10 @@ struct TcShape {
   static constexpr int kPart = kRows * (DP + 2);  // floats of a part
 };
 
-// A box's keys: scores are multiplied by k and k / 16, weights are 2^(.. + v), sums take them times inv.
+// A box's keys: scores are multiplied by k, weights are 2^(.. + v), sums take them times inv.  Without a
+// page v is minus infinity.
 struct BoxUnits {
-  float k, v, inv;
-  int there;  // has a page
+  float k, v, inv, unused;
 };
 
 template <int R, int kGroups>
@@ -245,6 +245,13 @@ __device__ __forceinline__ void take_apart(const float (&w)[4], uint32_t& first,
   third = to_e5m2x4(times<8>(a2), times<8>(b2));
 }
 
+__device__ __forceinline__ void st_shared(uint32_t at, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ void st_shared(uint32_t at, uint32_t x, uint32_t y) {
+  asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(x), "r"(y) : "memory");
+}
+
 template <int I>
 struct Index {
   static constexpr int value = I;
@@ -365,8 +372,8 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
           const bool active = my_tile == t;
           if (keys && active) {
             const int ve = clamp_exponent(now.ve);
-            ct.units[tiles % kInfoTiles][box] = now.page < a.cache.num_pages ? BoxUnits{power_of_two(clamp_exponent(now.ke)), (float)ve, power_of_two(-ve), 1}
-                                                                             : BoxUnits{1.f, 0.f, 1.f, 0};
+            ct.units[tiles % kInfoTiles][box] = now.page < a.cache.num_pages ? BoxUnits{power_of_two(clamp_exponent(now.ke)), (float)ve, power_of_two(-ve), 0.f}
+                                                                             : BoxUnits{1.f, -INFINITY, 1.f, 0.f};
           }
           __syncwarp();
           if (lane == 0) mbar_arrive_expect_tx(bar, Sh::kTileBytes);
@@ -396,7 +403,9 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
         constexpr uint32_t kDesc = idesc_8bit(Sh::kSColumns, false);
         const uint32_t g = tiles + i, b = g & 1u, slot = g % Sh::kRingK;
         if (!wait(&ct.full[0][slot], g / Sh::kRingK & 1u)) return;
-        if (kProducts == 2 && g >= 2 && !wait(&ct.p_full[b], (g >> 1 & 1u) ^ 1u)) return;  // S has been read
+        // The product of two tiles ago is done: S has been read and the weights' buffer is free.  (A warp that
+        // issues both has issued it before, and a commit waits for all that was issued before it.)
+        if (kProducts == 2 && g >= 2 && !wait(&ct.pv_done[b], (g >> 1 & 1u) ^ 1u)) return;
         tc_fence_after();
         if (elect_one()) {
           const uint64_t kd = rows_desc<DP>(base + slot * Sh::kTileBytes, 16), qd = rows_desc<DP>(base + Sh::kQAt + (pieces & 1u) * Sh::kQBytes, 16);
@@ -565,6 +574,9 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
     const int h = (warp - kBase / 32) / 4, key = tid & 127, quarter = warp & 3, r0 = h * R;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
     const uint32_t t_o = tmem + lanes + Sh::kOAt;
+    // This key's weights, with the swizzle of its row: a column of 16 bytes is one exclusive or away.
+    const uint32_t my_weights = (base + Sh::kPAt + key * Sh::kPWidth) ^
+                                (Sh::kPWidth == 128 ? key & 7 : Sh::kPWidth == 64 ? key >> 1 & 3 : key >> 2 & 1) * 16;
     const int D = a.cache.head_dim, G = P.group;
     uint32_t tiles = 0, pieces = 0;
     JoinUnit unit{};
@@ -616,6 +628,11 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
       const UnitKeys keys = pc.keys;
       const int first = pc.c + pc.i0, k0 = pc.k0;  // position of the unit's first token
       const bool idle = r0 >= rows;
+      const int my_box = key / P.kv_box;
+      // The tiles that begin in this range: not after the first token's last key less a tile, not before
+      // the last token's first key.
+      const int inner_hi = min(keys.hi, a.causal ? first : pc.c + pc.n - 1) - (kKeys - 1);
+      const int inner_lo = a.window > 0 ? pc.c + pc.i1 - a.window : 0;
       // Where the largest weight of a row's first tile goes: lower if the unit sees few of its keys (sinks,
       // a window's edge) and others follow, which are likely to have larger scores.
       float first_top = kFirstTop;
@@ -625,28 +642,30 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
       }
 
       for (int j = 0; j < nt; ++j) {
-        // what is known of the tile before its scores are there
         const uint32_t g = tiles + j, b = g & 1u;
-        const int j0 = keys.tile(k0 + j) * kKeys, at = j0 + key;
-        const bool edge = j0 < keys.lo || j0 + kKeys - 1 > keys.hi;
-        // The key is seen by the rows [from, to).
-        int from = 0, to = rows;
-        if (a.causal && at > first) from = (at - first) * G;
-        if (a.window > 0 && at >= a.sinks && at - first + a.window < P.shape.unit_tokens)
-          to = max(at - first + a.window, 0) * G;
-        if (at > keys.hi) to = 0;
-        from -= r0;
-        to -= r0;
+        const int j0 = keys.tile(k0 + j) * kKeys;
+        const bool inner = j0 >= inner_lo && j0 <= inner_hi;  // every row sees every key that has a page
+        // Else the key is seen by the rows [from, to).
+        int from = 0, to = R;
+        if (!inner) {
+          const int at = j0 + key;
+          to = rows;
+          if (a.causal && at > first) from = (at - first) * G;
+          if (a.window > 0 && at >= a.sinks && at - first + a.window < P.shape.unit_tokens)
+            to = max(at - first + a.window, 0) * G;
+          if (at > keys.hi) to = 0;
+          from -= r0;
+          to -= r0;
+        }
         wait(&ct.s_full[b], g >> 1 & 1u);
-        if (g >= 2) wait(&ct.pv_done[b], (g >> 1 & 1u) ^ 1u);  // the weights' buffer is free
         tc_fence_after();
-        const BoxUnits u = ct.units[g % kInfoTiles][key / P.kv_box];
-        if (!u.there) to = from = -1000;
+        const BoxUnits u = ct.units[g % kInfoTiles][my_box];
         // A row of V that no row of the unit sees holds anything, and 0 times that need not be 0:
         // cleared before the product.
-        if (edge && h == 0) {
-          // (the slot's phase before is over: its product was issued before the one waited for above)
+        if (!inner && h == 0 && (j0 < keys.lo || j0 + kKeys - 1 > keys.hi)) {
+          // (the slot's phase before is over: the scores of this tile waited for a later product)
           wait(&ct.full[1][g % Sh::kRingV], g / Sh::kRingV & 1u);
+          const int at = j0 + key;
           if (at > keys.hi || (at < keys.lo && at >= a.sinks)) {
             uint8_t* v = smem + Sh::kVAt + (g % Sh::kRingV) * Sh::kTileBytes + key * DP;
 #pragma unroll
@@ -655,13 +674,12 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
           }
         }
         if (!idle) {
-          const bool masked = !__all_sync(0xFFFFFFFFu, from <= 0 && to >= min(rows - r0, R));
           const uint32_t t_s = tmem + lanes + b * Sh::kSColumns + h * Sh::kSGroup;
           const float2 sixteenth = make_float2(0.0625f, 0.0625f), unit2 = make_float2(u.k, u.k), v2 = make_float2(u.v, u.v);
           const float2 factor2 = make_float2(u.k * one_factor, u.k * one_factor);
           float y[R];  // exponents of the weights, then the weights
           auto hide = [&]() {
-            if (!masked) return;
+            if (inner) return;
 #pragma unroll
             for (int r = 0; r < R; ++r)
               if (r < from || r >= to) y[r] = -INFINITY;
@@ -829,8 +847,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
             for (int r = 0; r < R; ++r) y[r] = exp2_fast(y[r]);
           }
 
-          uint8_t* weights = smem + Sh::kPAt + b * Sh::kPBytes + key * Sh::kPWidth;
-          const int turn = Sh::kPWidth == 128 ? key & 7 : Sh::kPWidth == 64 ? key >> 1 & 3 : key >> 2 & 1;  // the swizzle
+          const uint32_t weights = my_weights + b * Sh::kPBytes;
           const float2 inv2 = make_float2(u.inv, u.inv);
           each_chunk<Sh::kChunks>([&](auto chunk) {
             constexpr int c = decltype(chunk)::value, n = Sh::rows_of(c);
@@ -846,11 +863,11 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
 #pragma unroll
             for (int i = 0; i < 3; ++i) {
               const int x = column + i * n;
-              uint8_t* to_w = weights + x / Sh::kPWidth * (kKeys * Sh::kPWidth) + ((x % Sh::kPWidth / 16) ^ turn) * 16 + x % 16;
+              const uint32_t at_w = (weights ^ (uint32_t)(x % Sh::kPWidth / 16 * 16)) + x / Sh::kPWidth * (kKeys * Sh::kPWidth) + x % 16;
               if constexpr (n == 16)
-                *reinterpret_cast<uint4*>(to_w) = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+                st_shared(at_w, w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
               else
-                *reinterpret_cast<uint2*>(to_w) = make_uint2(w[2 * i], w[2 * i + 1]);
+                st_shared(at_w, w[2 * i], w[2 * i + 1]);
             }
           });
         }
@@ -961,6 +978,7 @@ cudaError_t launch_rows(TcParams& p, const DeviceInfo& dev, cudaStream_t stream)
   const long long rows = (long long)p.a.T * p.group, B = p.a.B;
   if (p.group <= 8 && rows <= 8 * B) return launch<DP, 8>(p, dev, stream);
   if (p.group <= 16 && rows <= 16 * B) return launch<DP, 16>(p, dev, stream);
+  if (p.group <= 32 && rows <= 32 * B) return launch<DP, 32>(p, dev, stream);
   return launch<DP, 24>(p, dev, stream);
 }
 
