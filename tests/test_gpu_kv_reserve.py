@@ -37,8 +37,7 @@ class Pages:
         out = torch.full((T,), -9, dtype=torch.int64, device="cuda") if slots else None
         (run or self.rt.retrace_kv_reserve)(i32(cached), i32(new), self.pool, q_start=q_start, slots=out)
         torch.cuda.synchronize()
-        self.table, self.held, self.free, missing, starts, want = ref.reserve(cached, new, self.page, self.table, self.held, self.free,
-                                                                              T if slots else 1 << 30)
+        self.table, self.held, self.free, missing, starts, want = ref.reserve(cached, new, self.page, self.table, self.held, self.free, T)
         p = self.pool
         assert p.counts.tolist() == [len(self.free), missing]
         assert p.held.tolist() == self.held and np.array_equal(p.page_table.cpu().numpy(), self.table)
