@@ -13,10 +13,14 @@ One round of the loop, for a batch of sequences on one stream:
   lengths   grow by the committed tokens; what was rejected is overwritten by the next
             append.
 
+With --cache fp8 the caches hold 8 bits an element (retrace_kv_append_fp8, retrace_attend_fp8) in
+pages from a pool: retrace_kv_reserve gives each sequence those of its next block, and takes back
+what the committed tokens do not need.
+
 Nothing is read back until the end.  With top_k = 1 the tokens are those that the target
 alone gives, one after another.
 
-    python examples/decode_loop.py [--tokens 64] [--batch 4] [--dtype bf16|f32] [--top-k 1]
+    python examples/decode_loop.py [--tokens 64] [--batch 4] [--dtype bf16|f32] [--top-k 1] [--cache same|fp8]
 """
 
 from __future__ import annotations
@@ -44,16 +48,24 @@ def rope_table(positions, rot, device="cuda"):
 class Layer:
     """One attention layer and a head, with a paged cache for a batch."""
 
-    def __init__(self, B, V, d, q_heads, kv_heads, D, positions, dtype, gen, window=0, sinks=0, causal=True):
+    def __init__(self, B, V, d, q_heads, kv_heads, D, positions, dtype, gen, window=0, sinks=0, causal=True, cache="same"):
         w = lambda o, i: (torch.randn((o, i), generator=gen, device="cuda") / i**0.5).to(dtype)  # noqa: E731
         self.shape = (q_heads, kv_heads, D)
         self.qkv, self.o, self.head = w((q_heads + 2 * kv_heads) * D, d), w(d, q_heads * D), w(V, d)
         pages = -(-positions // PAGE)
         # each sequence's pages, in any order
         table = torch.randperm(B * pages, generator=gen, device="cuda").to(torch.int32).view(B, pages)
-        k, v = (torch.empty((B * pages, PAGE, kv_heads, D), dtype=dtype, device="cuda") for _ in range(2))
-        self.cache = rt.KvCache(k, v, table)
-        self.ws = rt.AttendWorkspace(q_heads, kv_heads, D, dtype)
+        kept = dtype if cache == "same" else torch.float8_e4m3fn
+        k, v = (torch.empty((B * pages, PAGE, kv_heads, D), dtype=kept, device="cuda") for _ in range(2))
+        if cache == "same":
+            self.cache, self.pool = rt.KvCache(k, v, table), None
+            self.calls = rt.retrace_kv_append, rt.retrace_attend
+        else:
+            self.pool = rt.PagePool.of(B * pages, PAGE, B, pages)
+            units = (torch.zeros((B * pages, kv_heads), dtype=torch.int8, device="cuda") for _ in range(2))
+            self.cache = rt.KvCacheFp8(k, v, self.pool.page_table, *units)
+            self.calls = rt.retrace_kv_append_fp8, rt.retrace_attend_fp8
+        self.ws = rt.AttendWorkspace(q_heads, kv_heads, D, kept)
         self.rope = rope_table(positions, D)
         self.mask = {"window": window, "sinks": sinks, "causal": causal}
 
@@ -62,32 +74,38 @@ class Layer:
         y = (x @ self.qkv.T).view(-1, q_heads + 2 * kv_heads, D)
         return y.split([q_heads, kv_heads, kv_heads], 1)
 
+    def reserve(self, length, new):
+        """Pages for `new` tokens after `length` of them; those behind are given back."""
+        if self.pool is not None:
+            rt.retrace_kv_reserve(length, new, self.pool)
+
     def append(self, x, length):
         """The keys and values of x [B, n, d] at positions length, length + 1, ..."""
         _, k, v = self._project(x)
-        rt.retrace_kv_append(None, k, v, self.cache, length, self.rope)
+        self.calls[0](None, k, v, self.cache, length, self.rope)
 
     def states(self, x, length):
         """The states of x [B, n, d], whose keys and values enter the cache."""
         q, k, v = self._project(x)
         turned = torch.empty_like(q, memory_format=torch.contiguous_format)
-        rt.retrace_kv_append(q, k, v, self.cache, length, self.rope, turned)
+        self.calls[0](q, k, v, self.cache, length, self.rope, turned)
         out = torch.empty_like(turned)
-        rt.retrace_attend(turned, self.cache, length, out, self.ws, **self.mask)
+        self.calls[1](turned, self.cache, length, out, self.ws, **self.mask)
         return x + (out.view(*x.shape[:2], -1) @ self.o.T)
 
 
 class Decoder:
     """A target, a drafter and the state of a batch of sequences."""
 
-    def __init__(self, B=4, K=8, V=1024, d=256, dtype=torch.bfloat16, positions=512, seed=0, temperature=1.0, top_k=1, top_p=1.0):
+    def __init__(self, B=4, K=8, V=1024, d=256, dtype=torch.bfloat16, positions=512, seed=0, temperature=1.0, top_k=1, top_p=1.0,
+                 cache="same"):
         gen = torch.Generator(device="cuda").manual_seed(seed)
         self.B, self.K, self.V, self.d, self.dtype, self.gen = B, K, V, d, dtype, gen
         self.setting = (float(temperature), int(top_k), float(top_p))
         self.embed = torch.randn((V, d), generator=gen, device="cuda").to(dtype)
-        self.target = Layer(B, V, d, 4, 2, 64, positions, dtype, gen)
+        self.target = Layer(B, V, d, 4, 2, 64, positions, dtype, gen, cache=cache)
         # the drafter is the target seen through a window, so that it is often right
-        self.drafter = Layer(B, V, d, 4, 2, 64, positions, dtype, gen, window=64, sinks=4, causal=False)
+        self.drafter = Layer(B, V, d, 4, 2, 64, positions, dtype, gen, window=64, sinks=4, causal=False, cache=cache)
         self.drafter.qkv, self.drafter.o, self.drafter.head = self.target.qkv, self.target.o, self.target.head
         w = lambda i: (torch.randn((d, i), generator=gen, device="cuda") * 0.02).to(dtype)  # noqa: E731
         self.weights = (w(2 * d), w(d), w(2 * d))
@@ -98,6 +116,7 @@ class Decoder:
         # state: the anchor, tokens before it, the drafter's next inputs, tokens not in its cache yet
         self.anchor = torch.randint(0, V, (B,), generator=gen, device="cuda")
         self.length = torch.zeros(B, dtype=torch.int32, device="cuda")
+        self.block, self.nothing = full(K + 1, torch.int32), full(0, torch.int32)
         self.inputs = self.mask_input.expand(B, K, d).contiguous()
         self.fresh, self.fresh_at = None, None
 
@@ -105,6 +124,8 @@ class Decoder:
         """One round; returns the committed tokens [B, K + 1] (-1 after the last) and their number."""
         B, K, V, d = self.B, self.K, self.V, self.d
         anchor = self.embed[self.anchor][:, None]
+        for layer in (self.drafter, self.target):
+            layer.reserve(self.length, self.block)
         if self.fresh is not None:  # the tokens of the round before, over the drafts it left
             self.drafter.append(self.embed[self.fresh], self.fresh_at)
         h = self.drafter.states(torch.cat([anchor, self.inputs], 1), self.length)
@@ -124,6 +145,8 @@ class Decoder:
         # the drafter has the anchor; it lacks the committed tokens but the last, which is the next anchor
         self.fresh, self.fresh_at = out.committed.clamp(min=0).long(), self.length + 1
         self.anchor, self.length, self.inputs = out.bonus.long(), self.length + count, out.e_out
+        for layer in (self.drafter, self.target):
+            layer.reserve(self.length, self.nothing)
         return out.committed, count
 
 
@@ -133,9 +156,10 @@ def main():
     ap.add_argument("--batch", type=int, default=4)
     ap.add_argument("--dtype", choices=["bf16", "f32"], default="bf16")
     ap.add_argument("--top-k", type=int, default=1)
+    ap.add_argument("--cache", choices=["same", "fp8"], default="same", help="elements of the caches")
     args = ap.parse_args()
     dec = Decoder(B=args.batch, dtype=torch.bfloat16 if args.dtype == "bf16" else torch.float32, top_k=args.top_k,
-                  positions=2 * args.tokens + 64)
+                  positions=2 * args.tokens + 64, cache=args.cache)
     rounds, total = [], torch.zeros(args.batch, dtype=torch.int64, device="cuda")
     t0 = time.perf_counter()
     while len(rounds) < args.tokens and (not rounds or int(total.min()) < args.tokens):

@@ -42,8 +42,11 @@ constexpr unsigned long long kDrainNs = 20ull * 1000ull * 1000ull;
 constexpr int kInfoTiles = 16;  // ring of tiles' units: more than the tiles between loading and softmax
 constexpr int kMostBoxes = 16;  // of a tile: pages of 8 slots
 constexpr float kFirstTop = 4.f, kMostTop = 15.f;
-constexpr float kNone = 1e30f;     // in place of the reference of a row that has seen nothing
-constexpr float kFar = 4194304.f;  // 2^22: references up to it are whole numbers, and sums of two are exact
+constexpr float kNone = 3.402823466e38f;  // in place of the reference of a row that has seen nothing
+constexpr float kFar = 4194304.f;         // 2^22: references up to it are whole numbers, and sums of two are exact
+// Exponents of 2^10 and more lose places of a weight.  From 2^28 on what the rounding left is not counted: neighbouring
+// scores are 32 apart there.
+constexpr float kLarge = 1024.f, kHuge = 268435456.f;
 
 struct TcParams {
   AttendArgs a;
@@ -720,20 +723,23 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
             const float4 x = *reinterpret_cast<const float4*>(from);
             return Four{make_float2(x.x, x.y), make_float2(x.z, x.w)};
           };
-          // The product with the factor rounded before the reference is taken off, for references far from
-          // zero; `fresh`: rows that have none keep their exponents.
+          // For references far from zero: the product with the factor rounded, the reference taken off, and then
+          // what the rounding left added.  `fresh`: rows without a reference keep their exponents.
           auto exact = [&](bool fresh) {
-            scores([&](int r, const float2& x0, const float2& x1) {
-              const Four factors = four(factor + r), rest = four(ct.rest[h] + r);
-              Four ref = four(ct.minus[h] + r);
+            auto one = [&](const float2& x, const float2& factor, float2 ref, const float2& rest) {
               if (fresh) {
-                if (ref.p.x == kNone) ref.p.x = 0.f;
-                if (ref.p.y == kNone) ref.p.y = 0.f;
-                if (ref.q.x == kNone) ref.q.x = 0.f;
-                if (ref.q.y == kNone) ref.q.y = 0.f;
+                if (ref.x == kNone) ref.x = 0.f;
+                if (ref.y == kNone) ref.y = 0.f;
               }
-              put(r, add2(add2(add2(mul2(mul2(x0, unit2), factors.p), ref.p), v2), rest.p),
-                  add2(add2(add2(mul2(mul2(x1, unit2), factors.q), ref.q), v2), rest.q));
+              const float2 t = mul2(x, unit2), m = mul2(t, factor);
+              float2 left = fma2(t, factor, make_float2(-m.x, -m.y));
+              if (fabsf(ref.x) >= kHuge) left.x = 0.f;
+              if (fabsf(ref.y) >= kHuge) left.y = 0.f;
+              return add2(add2(add2(m, ref), left), add2(v2, rest));
+            };
+            scores([&](int r, const float2& x0, const float2& x1) {
+              const Four factors = four(factor + r), rest = four(ct.rest[h] + r), ref = four(ct.minus[h] + r);
+              put(r, one(x0, factors.p, ref.p, rest.p), one(x1, factors.q, ref.q, rest.q));
             });
           };
           auto exponents = [&]() {
@@ -779,20 +785,22 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
             maxima();
             float old = 0.f, old_rest = 0.f, now = 0.f, now_rest = 0.f, move = 0.f;
             bool pending = false;
+            const float aim = fresh ? first_top : kFirstTop;
             if (key < R) {
               old = now = ct.minus[h][key];
               old_rest = now_rest = ct.rest[h][key];
-              const float most = most_of(key), by = floorf((fresh ? first_top : kFirstTop) - most);
+              const float most = most_of(key), by = floorf(aim - most);
               if (old == kNone ? most > -INFINITY : most > kMostTop) {
                 const float from_zero = old == kNone ? 0.f : old;
-                if (fabsf(from_zero) >= kFar) {
+                if (fabsf(from_zero) >= kFar && fabsf(old_rest + by) < kFar) {
                   now_rest = old_rest + by;
                   move = by;
-                } else if (fabsf(from_zero + by) < kFar) {
+                } else if (fabsf(from_zero) < kFar && fabsf(from_zero + by) < kFar) {
                   now = from_zero + by;
                   move = by;
                 } else {  // the maximum itself, and what is left of it over the tile
-                  now = from_zero - most;
+                  now = (from_zero + old_rest) - most;
+                  now_rest = 0.f;
                   pending = true;
                 }
                 ct.minus[h][key] = now;
@@ -800,15 +808,23 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
               }
               ct.move[h][key] = move;
             }
-            const bool again = any_of_group(h, pending);
+            const bool again = any_of_group(h, pending || fabsf(move) >= kLarge);
             if (again) {
-              exact(false);
-              maxima();
-              if (pending) {
-                now_rest = floorf((fresh ? first_top : kFirstTop) - most_of(key));
-                ct.rest[h][key] = now_rest;
-              }
               far = true;
+              // (a maximum that moves by more than its own places takes another turn)
+              for (int turn = 0;; ++turn) {
+                exact(false);
+                maxima();
+                if (pending) {
+                  const float most = most_of(key);
+                  pending = fabsf(most) >= kFar && turn < 2;
+                  if (pending)
+                    ct.minus[h][key] = now -= most;
+                  else
+                    ct.rest[h][key] = now_rest = floorf(aim - most);
+                }
+                if (!any_of_group(h, pending)) break;
+              }
             }
             if (key < R) ct.scale[h][key] = old == kNone ? 0.f : exp2_fast((now - old) + (now_rest - old_rest));
             group_barrier(h);

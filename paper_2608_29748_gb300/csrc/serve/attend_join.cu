@@ -80,7 +80,8 @@ __global__ void __launch_bounds__(kThreads) attend_join_kernel(const __grid_cons
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             if (i0 + i >= unit.pieces) break;
-            if (st[i].x == -INFINITY) continue;  // the part's keys are hidden from this row
+            // the part's keys are hidden from this row (a sum that is no number has no maximum)
+            if (a.k_exp ? st[i].y == 0.f : st[i].x == -INFINITY) continue;
             const float up = fmaxf(top, st[i].x), f = power(top - up, part.scale2), g = power(st[i].x - up, part.scale2);
             top = up;
             sum = sum * f + st[i].y * g;

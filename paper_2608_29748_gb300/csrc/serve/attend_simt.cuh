@@ -513,9 +513,10 @@ __global__ void __launch_bounds__(FewShape<C, DP>::kThreads, FewShape<C, DP>::kP
 #pragma unroll
       for (int x = 0; x < kWarps; ++x) {
         const float2 st = sm.stat[x][row];
-        const float g = st.x == -INFINITY ? 0.f : expf(st.x - top);
+        const bool hidden = sizeof(C) == 1 ? st.y == 0.f : st.x == -INFINITY;  // a sum that is no number has no maximum
+        const float g = hidden ? 0.f : expf(st.x - top);
         sum += st.y * g;
-        o += st.x == -INFINITY ? 0.f : sm.k[x][row][col] * g;
+        o += hidden ? 0.f : sm.k[x][row][col] * g;
       }
       if (whole) {
         if (col < D) row_out<T>(a, pc, w, row)[col] = from_f32<T>(sum == 0.f ? 0.f : o / sum);

@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(kListThreads) kv_slots_kernel(const __grid_con
 
 cudaError_t launch_kv_reserve(const ReserveArgs& a, cudaStream_t stream) {
   // One small CTA where its threads have a few tokens and pages each.  In one graph, a call that takes and a call
-  // that gives back: 8 sequences of 17 tokens 6.5 us on one CTA of 512 (8.0 on eight of 1024), 256 sequences of 17 tokens
+  // that gives back: 8 sequences of a token 6.5 us on one CTA of 512 (8.0 on eight of 1024), 256 sequences of 17 tokens
   // 15.1 (9.8), 2048 prompts of 1000 tokens 148 (30.6).
   const bool few = a.B <= 128 && (!a.slots || a.T <= 4096);
   const bool listed = a.slots && a.T > kListTokens;
