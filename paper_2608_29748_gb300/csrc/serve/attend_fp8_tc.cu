@@ -781,7 +781,10 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
             raise = any_of_group(h, top > kMostTop);
           }
           if (__builtin_expect(raise, false)) {
-            exact(true);
+            if (fresh && !far)
+              scores([&](int r, const float2& x0, const float2& x1) { put(r, fma2(x0, factor2, v2), fma2(x1, factor2, v2)); });
+            else
+              exact(true);
             maxima();
             float old = 0.f, old_rest = 0.f, now = 0.f, now_rest = 0.f, move = 0.f;
             bool pending = false;
