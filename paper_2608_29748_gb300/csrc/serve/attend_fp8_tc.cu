@@ -112,9 +112,8 @@ struct Control {
   long long sum[20];
   uint32_t tmem;
   int abort;
-  PieceWalk walk[kGroups];  // of the softmax groups
-  Piece piece[kGroups][2];  // this one and the next
-  int more[kGroups][2];
+  Piece piece[2];  // of the softmax, with its queries
+  int more[2];     // 0: no piece, the end
   BoxUnits units[kInfoTiles][kMostBoxes];
   int2 q_range[2][4];  // largest and smallest exponent of the rows of a warp
   int even[2];         // the rows have one unit
@@ -473,14 +472,30 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
       // A lane has 16 elements of a row.
       constexpr int kLanes = DP / 16, kAtOnce = 32 / kLanes;
       const int which = warp - 2 - kProducts, D = a.cache.head_dim, col = lane % kLanes * 16;
-      uint32_t pieces = 0;
-      while (ok && walk.next<kKeys, false, true>(P.shape, plan, &pc)) {
-        if (pc.k1 == pc.k0) continue;
+      for (uint32_t pieces = 0;; ++pieces) {
+        bool more;
+        int rows;
+        while ((more = walk.next<kKeys, true, true>(P.shape, plan, &pc))) {
+          rows = (pc.i1 - pc.i0) * P.group;
+          if (pc.k1 > pc.k0) break;
+          for (int i = which * 32 + lane; i < rows * D; i += 32 * kQueries) {  // nothing is visible
+            const int r = i / D, token = P.by_group(r);
+            static_cast<__nv_bfloat16*>(a.out)[(long long)(pc.row0 + pc.i0 + token) * a.out_token +
+                                               (pc.head * P.group + r - token * P.group) * (long long)a.out_head + i % D] = __float2bfloat16_rn(0.f);
+          }
+        }
         const uint32_t buffer = pieces & 1u;
         ok = warp_wait_quick(&ct.q_empty[buffer], (pieces >> 1 & 1u) ^ 1u, abort);
         if (!ok) break;
-        ++pieces;
-        const int rows = (pc.i1 - pc.i0) * P.group;
+        if (lane == 0 && which == 0) {
+          ct.piece[buffer] = pc;
+          ct.more[buffer] = more;
+        }
+        if (!more) {
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&ct.q_full[buffer]));
+          break;
+        }
         uint8_t* to = smem + Sh::kQAt + buffer * Sh::kQBytes;
         uint4 raw[2];
         uint32_t top;  // the row's largest magnitude, as bits: infinities and NaN are the largest
@@ -592,37 +607,22 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
         if (lane == 0) raise_abort(abort, a.status);
       }
     };
-    // One thread of the group walks, a piece ahead; the pieces stay in shared memory.
-    const bool walker = key == 96;
-    if (walker) {
-      ct.walk[h].start(plan);
-      ct.more[h][0] = ct.walk[h].template next<kKeys, true, true>(P.shape, plan, &ct.piece[h][0]);
-    }
-    for (int np = 0;; np ^= 1) {
-      group_barrier(h);
-      if (!ct.more[h][np]) break;
-      if (walker) ct.more[h][np ^ 1] = ct.walk[h].template next<kKeys, true, true>(P.shape, plan, &ct.piece[h][np ^ 1]);
-      const Piece& pc = ct.piece[h][np];
-      const int nt = pc.k1 - pc.k0, rows = (pc.i1 - pc.i0) * G;
-      if (nt == 0) {  // nothing is visible
-        for (int i = h * 128 + key; i < Sh::kRows * D; i += 128 * Sh::kGroups) {
-          const int r = i / D, token = P.by_group(r);
-          if (r < rows)
-            static_cast<__nv_bfloat16*>(a.out)[(long long)(pc.row0 + pc.i0 + token) * a.out_token +
-                                               (pc.head * G + r - token * G) * (long long)a.out_head + i % D] = __float2bfloat16_rn(0.f);
-        }
-        continue;
-      }
+    for (;;) {
       const uint32_t buffer = pieces & 1u;
+      const Piece& pc = ct.piece[buffer];
       wait(&ct.q_full[buffer], pieces >> 1 & 1u);
-      ++pieces;
-      const float* factor = ct.factor[buffer] + r0;
+      const bool more = ok && ct.more[buffer];
+      const int rows = more ? (pc.i1 - pc.i0) * G : 0;
       // A row of the tile that holds no token refers to a number that no weight comes near.
       if (key < R) {
         ct.minus[h][key] = r0 + key < rows ? kNone : -kNone;
         ct.rest[h][key] = 0.f;
       }
-      group_barrier(h);
+      // (after an expired wait the group leaves together)
+      if (any_of_group(h, !more)) break;
+      const int nt = pc.k1 - pc.k0;
+      ++pieces;
+      const float* factor = ct.factor[buffer] + r0;
       float2 l[R / 2];  // sums of this thread's keys
 #pragma unroll
       for (int i = 0; i < R / 2; ++i) l[i] = make_float2(0.f, 0.f);
@@ -950,10 +950,10 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
           put_rows(r0 + 16 * c, o, n);
         });
       }
+      if (!whole && h == 0 && pc.k0 == 0) unit = JoinUnit{pc.pieces, rows, rows, pc.row0 + pc.i0, pc.head * G, G, {0, 0}};
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&ct.q_empty[buffer]));
-      if (!whole && h == 0 && pc.k0 == 0) unit = JoinUnit{pc.pieces, rows, rows, pc.row0 + pc.i0, pc.head * G, G, {0, 0}};
     }
     if (tid == kBase) a.units[blockIdx.x] = unit;
   }

@@ -55,6 +55,8 @@ class Cta:
                 yield f"q_empty{n & 1}", (n >> 1) - 1
                 self.bars[f"q_full{n & 1}"].arrive()
                 n += 1
+        yield f"q_empty{n & 1}", (n >> 1) - 1  # the end
+        self.bars[f"q_full{n & 1}"].arrive()
 
     def scores(self, g, flight):
         b, slot = g & 1, g % self.rings[0]
@@ -102,7 +104,6 @@ class Cta:
             return f"group{h}", meets - 1
 
         for nt, clears, raises in self.pieces:
-            yield meet()
             if nt == 0:
                 continue
             yield f"q_full{n & 1}", n >> 1
@@ -124,6 +125,8 @@ class Cta:
             yield f"pv_done{tiles - 1 & 1}", tiles - 1 >> 1
             self.bars[f"q_empty{n & 1}"].arrive()
             n += 1
+        yield f"q_full{n & 1}", n >> 1
+        yield meet()
 
     def run(self, rng):
         roles = {"copy k": self.copies(0), "copy v": self.copies(1)}
