@@ -69,12 +69,12 @@ struct TcShape {
   static constexpr int kRows = R * kGroups;
   static constexpr int kChunks = (R + 15) / 16;
   __host__ __device__ static constexpr int rows_of(int chunk) { return R - 16 * chunk < 16 ? R - 16 * chunk : 16; }
-  // Columns of S: 2 a row, the two parts of a chunk's queries side by side, group after group.
-  static constexpr int kSGroup = 2 * R, kSColumns = kSGroup * kGroups;
+  // Columns of S: one a row, group after group, to a whole number of 16.
+  static constexpr int kSColumns = (kRows + 15) / 16 * 16;
   // Columns of O (and of P): 3 a row; all groups' first chunks, then all second ones.
   __host__ __device__ static constexpr int o_column(int group, int chunk) { return 48 * kGroups * chunk + 3 * rows_of(chunk) * group; }
   static constexpr int kOColumns = (3 * kRows + 15) / 16 * 16;
-  static_assert(kSColumns % 16 == 0 && kOColumns <= 256, "columns of a product");
+  static_assert(kSColumns <= 256 && kOColumns <= 256, "columns of a product");
   static constexpr int kOAt = 2 * kSColumns, kTmem = 512 / kPerSm;
   static_assert(kOAt + kOColumns <= kTmem, "columns of TMEM");
   // Registers of a thread: what the softmax takes of the others' of the launch.
@@ -84,7 +84,7 @@ struct TcShape {
   static constexpr int kTileBytes = kKeys * DP;
   static constexpr int kPWidth = kOColumns == 96 ? 32 : kOColumns > 64 ? 128 : kOColumns > 32 ? 64 : 32;  // bytes of a key's columns of P side by side
   static constexpr int kPBytes = (kOColumns + kPWidth - 1) / kPWidth * kKeys * kPWidth;
-  static constexpr int kQBytes = (kSColumns * DP + 1023) / 1024 * 1024;
+  static constexpr int kQPart = kSColumns * DP, kQBytes = (2 * kQPart + 1023) / 1024 * 1024;
   static constexpr int kControlBytes = kFew ? 7 * 1024 : 12 * 1024;
   static constexpr int kRoom = ((kFew ? 113 : 227) * 1024 - kControlBytes - 2 * kPBytes - 2 * kQBytes) / kTileBytes;
   static constexpr int kRingV = (kRoom + 1) / 2 < 8 ? (kRoom + 1) / 2 : 8, kRingK = kRoom / 2 < 8 ? kRoom / 2 : 8;
@@ -412,7 +412,10 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
         if (elect_one()) {
           const uint64_t kd = rows_desc<DP>(base + slot * Sh::kTileBytes, 16), qd = rows_desc<DP>(base + Sh::kQAt + (pieces & 1u) * Sh::kQBytes, 16);
 #pragma unroll
-          for (int k = 0; k < DP / 32; ++k) tc_mma_8bit(tmem + b * Sh::kSColumns, kd + 2 * k, qd + 2 * k, kDesc, k > 0);
+          for (int k = 0; k < DP / 16; ++k) {  // the queries' leading parts, then what is left of them
+            const int at = k % (DP / 32), part = k / (DP / 32);
+            tc_mma_8bit(tmem + b * Sh::kSColumns, kd + 2 * at, qd + part * (Sh::kQPart >> 4) + 2 * at, kDesc, k > 0);
+          }
           tc_commit(smem_u32(&ct.s_full[b]));
           tc_commit(smem_u32(&ct.empty[0][slot]));
         }
@@ -557,16 +560,14 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
               const uint32_t c = to_e4m3x2(x, y);
               const float2 f = e4m3_floats(c);
               lead[i] |= c << (16 * k);
-              rest[i] |= to_e4m3x2((x - f.x) * 16.f, (y - f.y) * 16.f) << (16 * k);
+              rest[i] |= to_e4m3x2(x - f.x, y - f.y) << (16 * k);
             }
             if (top >= 0x7F800000u) lead[i] = 0x7F7F7F7Fu;  // an infinity or a NaN: NaN throughout, as its scores are
           }
           if (r < Sh::kRows) {
-            // the columns of the row's two parts
-            const int group = r / R, in = r % R, chunk = in / 16, size = min(16, R - 16 * chunk), n = group * Sh::kSGroup + 32 * chunk + in % 16;
-            auto at = [&](int n) { return to + n * DP + ((col / 16) ^ (DP == 128 ? n & 7 : n >> 1 & 3)) * 16; };
-            *reinterpret_cast<uint4*>(at(n)) = make_uint4(lead[0], lead[1], lead[2], lead[3]);
-            *reinterpret_cast<uint4*>(at(n + size)) = make_uint4(rest[0], rest[1], rest[2], rest[3]);
+            uint8_t* at = to + r * DP + ((col / 16) ^ (DP == 128 ? r & 7 : r >> 1 & 3)) * 16;
+            *reinterpret_cast<uint4*>(at) = make_uint4(lead[0], lead[1], lead[2], lead[3]);
+            *reinterpret_cast<uint4*>(at + Sh::kQPart) = make_uint4(rest[0], rest[1], rest[2], rest[3]);
             if (col == 0) {
               const int token = P.by_group(r);
               ct.factor[buffer][r] = P.scale2 * power_of_two(e);
@@ -677,8 +678,8 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
           }
         }
         if (!idle) {
-          const uint32_t t_s = tmem + lanes + b * Sh::kSColumns + h * Sh::kSGroup;
-          const float2 sixteenth = make_float2(0.0625f, 0.0625f), unit2 = make_float2(u.k, u.k), v2 = make_float2(u.v, u.v);
+          const uint32_t t_s = tmem + lanes + b * Sh::kSColumns + r0;
+          const float2 unit2 = make_float2(u.k, u.k), v2 = make_float2(u.v, u.v);
           const float2 factor2 = make_float2(u.k * one_factor, u.k * one_factor);
           float y[R];  // exponents of the weights, then the weights
           auto hide = [&]() {
@@ -689,25 +690,14 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
           };
           // Scores, four rows at a time: f(row, two of them, two of them).
           auto scores = [&](auto&& f) {
-            float s[2 * R];
+            float s[R];
             each_chunk<Sh::kChunks>([&](auto chunk) {
               constexpr int c = decltype(chunk)::value;
-              tmem_load<2 * Sh::rows_of(c)>(t_s + 32 * c, s + 32 * c);
+              tmem_load<Sh::rows_of(c)>(t_s + 16 * c, s + 16 * c);
             });
             tmem_wait_ld();
-            each_chunk<Sh::kChunks>([&](auto chunk) {
-              constexpr int c = decltype(chunk)::value, n = Sh::rows_of(c);
 #pragma unroll
-              for (int i = 0; i < n; i += 4) {
-                float2 x[2];
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                  const int at = 32 * c + i + 2 * k;
-                  x[k] = fma2(make_float2(s[at + n], s[at + n + 1]), sixteenth, make_float2(s[at], s[at + 1]));
-                }
-                f(16 * c + i, x[0], x[1]);
-              }
-            });
+            for (int r = 0; r < R; r += 4) f(r, make_float2(s[r], s[r + 1]), make_float2(s[r + 2], s[r + 3]));
             hide();
           };
           auto put = [&](int r, const float2& p, const float2& q) {
