@@ -204,13 +204,13 @@ __device__ __forceinline__ TokenPlace place_token(const AppendArgs& a, int unifo
       x.b = t0 < from ? 0 : a.B;
       x.first = from;
     }
-    x.end = x.b < a.B ? min(a.q_start[x.b + 1], a.T) : 0;
-    while (x.b < a.B && t >= x.end) {
-      x.first = x.end;
-      ++x.b;
-      if (x.b < a.B) x.end = min(a.q_start[x.b + 1], a.T);
+    const bool inside = x.b < a.B && t >= x.first && t < min(a.q_start[a.B], a.T);
+    if (inside && t >= a.q_start[x.b + 1]) {
+      x.b = sequence_from(a.q_start, a.B, x.b, t);
+      x.first = a.q_start[x.b];
     }
-    if (x.b >= a.B || t < x.first || t >= a.T) x.b = -1;
+    if (!inside || x.first < 0 || t < x.first) x.b = -1;
+    x.end = x.b >= 0 ? min(a.q_start[x.b + 1], a.T) : 0;
   }
   x.pos = x.b < 0 ? -2 : cached_tokens(a.cache_len, x.b) + (t - x.first);
   if (x.b >= 0 && (x.pos < 0 || (a.rope && x.pos >= a.rope_positions))) x.pos = -1;

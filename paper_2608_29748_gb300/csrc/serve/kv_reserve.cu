@@ -203,10 +203,9 @@ __global__ void __launch_bounds__(kListThreads) kv_slots_kernel(const __grid_con
       long long slot = -1;
       if (b >= 0 && t < total) {
         if (t >= next) {
-          do {  // t < total: it ends
-            first = next;
-            next = a.q_start[++b + 1];
-          } while (t >= next);
+          b = sequence_from(a.q_start, a.B, b, t);
+          first = a.q_start[b];
+          next = a.q_start[b + 1];
           cached = cached_tokens(a.cache_len, b);
         }
         const int p = cached + (t - first);

@@ -62,6 +62,21 @@ __device__ __forceinline__ int sequence_of(const int32_t* q_start, int B, int un
   return t >= q_start[b + 1] || *first < 0 ? -1 : b;  // a token of no sequence
 }
 
+// The sequence of token t, before q_start[B], that lies in b or behind it: among the next ones, or by halving
+// (a batch may have any number of sequences without tokens).
+__device__ __forceinline__ int sequence_from(const int32_t* q_start, int B, int b, int t) {
+  for (int i = 0; i < 4; ++i, ++b)
+    if (t < q_start[b + 1]) return b;
+  for (int hi = B; hi - b > 1;) {  // t is before the start of hi
+    const int mid = b + (hi - b) / 2;
+    if (t < q_start[mid])
+      hi = mid;
+    else
+      b = mid;
+  }
+  return b;
+}
+
 // Lengths outside (-2^30, 2^30) are taken as the nearest end, so that positions
 // stay in 32 bits (a sequence has at most 2^30 places).
 __device__ __forceinline__ int cached_tokens(const int32_t* cache_len, int b) {

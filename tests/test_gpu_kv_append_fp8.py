@@ -56,6 +56,13 @@ def test_heads_and_rotations(rt, dtype, interleaved, D, rot):
     check(Batch8([(3, 5), (1, 0), (7, 30)], 6, 2, D, 8, dtype, seed=D + rot), rt, rot, interleaved, 64)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_few_sequences_among_many(rt, dtype):
+    """Long runs of sequences without tokens; rows behind the last sequence."""
+    lens = [(0, 3)] * 300 + [(5, 14), (0, 0), (2, 7)] + [(0, 9)] * 400 + [(20, 1)] + [(1, 5)] * 40 + [(0, 2)] * 333
+    check(Batch8(lens, 4, 2, 64, 16, dtype, seed=5), rt, 32, False, 64)
+
+
 @pytest.mark.parametrize("Hq, Hkv", [(1, 1), (7, 1), (32, 8), (71, 71)])
 def test_head_counts(rt, Hq, Hkv):
     check(Batch8([(5, 9), (2, 0)], Hq, Hkv, 64, 16, BF16, seed=Hq), rt, 64, False, 32)

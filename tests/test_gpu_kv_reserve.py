@@ -49,7 +49,7 @@ class Pages:
         return out
 
 
-@pytest.mark.parametrize("B", [1, 3, 33, 200, 600, 1500])
+@pytest.mark.parametrize("B", [1, 3, 33, 200, 600, 1500, 5000])
 @pytest.mark.parametrize("page", [1, 16, 100])
 def test_rounds(rt, B, page):
     """Blocks reserved, some tokens committed, pages given back, sequences that end and begin."""
@@ -80,7 +80,15 @@ def test_a_long_list_of_tokens(rt):
         x.call([5] * 70, new, T=T)
 
 
-@pytest.mark.parametrize("B", [5, 800])
+def test_a_long_list_of_few_sequences_among_many(rt):
+    """Long runs of sequences without tokens, before, between and behind those that have some."""
+    new = np.zeros(3000, int)
+    new[[700, 701, 2100]] = [9000, 3, 9000]
+    x = Pages(rt, 3000, 16, 3000, 600, seed=6)
+    x.call(np.where(np.arange(3000) % 7 == 0, 5, 0), new)
+
+
+@pytest.mark.parametrize("B", [5, 800, 4500])
 def test_too_few_pages(rt, B):
     """The first sequences get theirs; the others try again when there are more."""
     x = Pages(rt, 4 * B, 4, B, 12, seed=1)
