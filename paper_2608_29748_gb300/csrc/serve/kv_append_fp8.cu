@@ -74,7 +74,8 @@ struct Chunk<__nv_bfloat16, 8> {
 
 // Lanes of a rotated head: first the chunks that rotate with a partner chunk (halves; single
 // elements also when interleaved), then those whose pairs lie inside (interleaved), then
-// those that are copied.  Lane i of a head of v has the chunks i and i + lanes.
+// those that are copied.  Without a rotation a head's halves are chunks and their partners, and nothing is
+// turned.  Lane i of a head of v has the chunks i and i + lanes.
 struct HeadShape {
   int pairs, inside, copies, lanes;  // lanes: their sum
   int step;                          // from a chunk to its partner, elements
@@ -241,12 +242,12 @@ template <typename T, int N>
 __device__ __forceinline__ void rotate_queries(const AppendArgs& a, const HeadShape& s, Shared& sm, int t0, int tokens) {
   const int tid = threadIdx.x, L = s.lanes, group = tid / L, i = tid % L, each = kThreads / L / s.per_token;
   if (group >= each * s.per_token) return;
-  const Place at = place_of<N>(s, a.rot, i);
+  const Place at = place_of<N>(s, a.rot, i), turns{at.pair && a.rot > 0, at.inside, at.at};
   for (int k = group / s.per_token; k < tokens; k += each) {
     const int pos = sm.pos[k], t = t0 + k;
     if (pos == -2) continue;
     float cs[2 * N];
-    if (pos >= 0 && a.rope) load_angles<N>(cs, a.rope, pos, a.rot, at, i);
+    if (pos >= 0) load_angles<N>(cs, a.rope, pos, a.rot, turns, i);
     for (int h0 = group % s.per_token; h0 < a.q_heads; h0 += kHeadsEach * s.per_token) {
       Chunk<T, N> x[kHeadsEach], y[kHeadsEach];
 #pragma unroll
@@ -263,12 +264,12 @@ __device__ __forceinline__ void rotate_queries(const AppendArgs& a, const HeadSh
         if (h >= a.q_heads) break;
         T* to = static_cast<T*>(a.q_out) + (long long)t * a.qo_token + h * a.qo_head + at.at;
         float fx[N], fy[N];
-        turned(x[u], y[u], cs, at, fx, fy);
+        turned(x[u], y[u], cs, turns, fx, fy);
         if (pos < 0) {
 #pragma unroll
           for (int j = 0; j < N; ++j) fx[j] = fy[j] = 0.f;
         }
-        if (at.pair || (N > 1 && at.inside) || pos < 0) {  // else copied as it is
+        if (turns.pair || (N > 1 && at.inside) || pos < 0) {  // else copied as it is
           x[u].from(fx);
           y[u].from(fy);
         }
@@ -374,7 +375,7 @@ __device__ __forceinline__ void fill_pages(const AppendArgs& a, const HeadShape&
       asm volatile("" ::: "memory");  // an item's angles at a time: all at once do not fit the registers
       x[u].to(fx[u]);
       y[u].to(fy[u]);
-      if (!value && a.rope) {
+      if (!value && a.rot > 0) {
         float cs[2 * N];
         if (there) load_angles<N>(cs, a.rope, p.pos + lane_token + u * apart, a.rot, at, i);
         turn_chunks(fx[u], fy[u], cs, at);
@@ -467,8 +468,8 @@ __device__ __forceinline__ void fill_pages_twice(const AppendArgs& a, const Head
           const Chunks w = item_chunks(q + u);
           if (t >= p.count) break;
           float cs[2 * N], fx[N], fy[N];
-          if (!value && a.rope) load_angles<N>(cs, a.rope, p.pos + t, a.rot, w.at, item_chunk(q + u));
-          turned(x[u], y[u], cs, w.at, fx, fy);
+          if (!value && a.rot > 0) load_angles<N>(cs, a.rope, p.pos + t, a.rot, w.at, item_chunk(q + u));
+          turned(x[u], y[u], cs, !value && a.rot > 0 ? w.at : Place{false, false, 0}, fx, fy);
           f(t, w, fx, fy);
         }
       }
@@ -528,6 +529,12 @@ __global__ void __launch_bounds__(kThreads, kCtasPerSm) kv_append_fp8_kernel(con
   }
 }
 
+// Nothing is turned, and the heads have two halves of whole chunks.
+template <int N>
+bool halves_of(const AppendArgs& a) {
+  return N > 1 && a.rot == 0 && a.cache.head_dim % (2 * N) == 0;
+}
+
 template <typename T, int N>
 cudaError_t launch(const AppendArgs& a, cudaStream_t stream) {
   HeadShape s{};
@@ -537,6 +544,11 @@ cudaError_t launch(const AppendArgs& a, cudaStream_t stream) {
   s.inside = halves ? 0 : a.rot / N;
   s.copies = (D - a.rot) / N;
   s.step = a.interleaved ? 1 : a.rot / 2;
+  if (halves_of<N>(a)) {
+    s.pairs = D / 2 / N;
+    s.copies = 0;
+    s.step = D / 2;
+  }
   s.lanes = s.pairs + s.inside + s.copies;
   s.by_lanes = FastDivide::of(s.lanes);
   const int groups = kThreads / s.lanes, share = (a.q_heads + kHeadsEach - 1) / kHeadsEach;
@@ -581,7 +593,7 @@ cudaError_t launch_typed(const AppendArgs& a, cudaStream_t stream) {
     vec = vec && whole(a.q_token) && whole(a.q_head) && whole(a.qo_token) && whole(a.qo_head) && aligned(a.q, 16) &&
           aligned(a.q_out, 16);
   // A head's lanes fit a warp (256 numbers in fp32 need 64 where they are copied: element by element).
-  const int pairs = a.interleaved ? 0 : a.rot / 2, lanes = (a.interleaved ? a.rot : pairs) / N + (c.head_dim - a.rot) / N;
+  const int pairs = a.interleaved ? 0 : a.rot / 2, lanes = halves_of<N>(a) ? c.head_dim / 2 / N : (a.interleaved ? a.rot : pairs) / N + (c.head_dim - a.rot) / N;
   return vec && lanes <= 32 ? launch<T, N>(a, stream) : launch<T, 1>(a, stream);
 }
 

@@ -63,6 +63,25 @@ def test_few_sequences_among_many(rt, dtype):
     check(Batch8(lens, 4, 2, 64, 16, dtype, seed=5), rt, 32, False, 64)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [8, 16, 24, 33, 64, 80, 128, 200, 256])
+def test_without_a_rotation(rt, dtype, D):
+    """Copied as they are, the bits of what is no number among them; zeros where a token has no position."""
+    x = Batch8([(3, 5), (1, 0), (7, 30), (20, 0), (2, -1)], 6, 2, D, 8, dtype, seed=D)
+    bits = torch.int16 if dtype == BF16 else torch.int32
+    x.q.view(bits)[3, 1, D // 2] = 0x7FA5 if dtype == BF16 else 0x7FA12345
+    x.q[4, 2, 0] = -0.0
+    q = x.q.clone()
+    q[31] = 0  # at position -1
+    x.q[3, 1, D // 2], save = 0, x.q.view(bits)[3, 1, D // 2].clone()
+    y_k, y_v, e_k, e_v = (t.clone() for t in (x.k, x.v, x.k_exp, x.v_exp))
+    check(x, rt, None, False, 0)
+    x.k.copy_(y_k), x.v.copy_(y_v), x.k_exp.copy_(e_k), x.v_exp.copy_(e_v)
+    x.q.view(bits)[3, 1, D // 2] = save
+    rt.retrace_kv_append_fp8(x.q, x.nk, x.nv, x.cache(rt), x.cache_len, None, x.out, q_start=x.q_start)
+    assert torch.equal(x.out.view(bits), q.view(bits))
+
+
 @pytest.mark.parametrize("Hq, Hkv", [(1, 1), (7, 1), (32, 8), (71, 71)])
 def test_head_counts(rt, Hq, Hkv):
     check(Batch8([(5, 9), (2, 0)], Hq, Hkv, 64, 16, BF16, seed=Hq), rt, 64, False, 32)
