@@ -19,7 +19,7 @@
 // 72 rows, and the softmax does 128 rows exponentials: with few rows on the N side all of
 // it scales with the rows that there are.
 // A tile of D = 128 and 16-slot pages takes an SM 730 ns with 4 to 32 rows (6.8 TB/s: bound by HBM), 1125 ns with
-// 68 (4.5 TB/s): there the issue slots are 54 % taken and the tensor cores 28 %; a third of the warps' time is
+// 68 (4.4 TB/s): there the issue slots are 54 % taken and the tensor cores 28 %; a third of the warps' time is
 // the chain of a tile (scores from TMEM, the group's agreement, exponentials, parts) without another one to fill it.
 // A unit costs 2 us (8 rows) to 7 us (68) besides its tiles.
 //
@@ -478,6 +478,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
       // ---- queries: rows of 128 or 64 bytes, each a sum of two e4m3 numbers times a unit ----
       // A lane has 16 elements of a row.
       constexpr int kLanes = DP / 16, kAtOnce = 32 / kLanes;
+      constexpr int kSteps = (Sh::kRows + kQueries * kAtOnce - 1) / (kQueries * kAtOnce);
       const int which = warp - 2 - kProducts, D = a.cache.head_dim, col = lane % kLanes * 16;
       for (uint32_t pieces = 0;; ++pieces) {
         bool more;
@@ -504,15 +505,19 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
           break;
         }
         uint8_t* to = smem + Sh::kQAt + buffer * Sh::kQBytes;
-        uint4 raw[2];
-        uint32_t top;  // the row's largest magnitude, as bits: infinities and NaN are the largest
-        auto load = [&](int r) {
+        auto row_of = [&](int step) { return (step * kQueries + which) * kAtOnce + lane / kLanes; };
+        // Where the two parts of this lane's elements of row r go, and until then the elements themselves.
+        auto place = [&](int r) { return to + r * DP + ((col / 16) ^ (DP == 128 ? r & 7 : r >> 1 & 3)) * 16; };
+        auto load = [&](int r, uint4 (&raw)[2]) {
           const int token = P.by_group(r);
           const __nv_bfloat16* from = static_cast<const __nv_bfloat16*>(a.q) + (long long)(pc.row0 + pc.i0 + token) * a.q_token +
                                       (pc.head * P.group + r - token * P.group) * a.q_head + col;
           raw[0] = raw[1] = make_uint4(0u, 0u, 0u, 0u);
           if (r < rows && col < D) raw[0] = *reinterpret_cast<const uint4*>(from);
           if (r < rows && col + 8 < D) raw[1] = *reinterpret_cast<const uint4*>(from + 8);
+        };
+        // The row's largest magnitude, as bits: infinities and NaN are the largest.
+        auto top_of = [&](const uint4 (&raw)[2]) {
           constexpr uint32_t kMagnitude = 0x7FFF7FFFu;
           uint32_t most = 0u;
 #pragma unroll
@@ -520,18 +525,26 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
             most = __vmaxu2(__vmaxu2(most, __vmaxu2(raw[i].x & kMagnitude, raw[i].y & kMagnitude)), __vmaxu2(raw[i].z & kMagnitude, raw[i].w & kMagnitude));
 #pragma unroll
           for (int o = 1; o < kLanes; o <<= 1) most = __vmaxu2(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
-          top = max(most & 0xFFFFu, most >> 16) << 16;
+          return max(most & 0xFFFFu, most >> 16) << 16;
         };
         // The least exponent with a magnitude <= 448 times its power of two.
         auto exponent_of = [](uint32_t t) { return min(max((int)(t >> 23) - 127 - 8 + ((t & 0x7FFFFFu) > 0x600000u), -120), 120); };
         // The rows have the largest row's unit, and then the softmax one factor for all; where a row is much
         // smaller (2^-6, of some 2^-17 that its elements may be off in that unit), each has its own.
         int high = -120, low = 120;
-        for (int r0 = which * kAtOnce; r0 < rows; r0 += kQueries * kAtOnce) {
-          load(r0 + lane / kLanes);
+#pragma unroll 1
+        for (int step = 0; step < kSteps; ++step) {
+          uint4 raw[2];
+          const int r = row_of(step);
+          load(r, raw);
+          const uint32_t top = top_of(raw);
           const bool counts = top != 0u && top < 0x7F800000u;
           high = max(high, __reduce_max_sync(0xFFFFFFFFu, counts ? exponent_of(top) : -120));
           low = min(low, __reduce_min_sync(0xFFFFFFFFu, counts ? exponent_of(top) : 120));
+          if (r < Sh::kRows) {
+            *reinterpret_cast<uint4*>(place(r)) = raw[0];
+            *reinterpret_cast<uint4*>(place(r) + Sh::kQPart) = raw[1];
+          }
         }
         if constexpr (kQueries > 1) {
           if (lane == 0) ct.q_range[buffer][which] = make_int2(high, low);
@@ -547,9 +560,15 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
           ct.even[buffer] = even;
           ct.one_factor[buffer] = P.scale2 * power_of_two(high);
         }
-        for (int r0 = which * kAtOnce; r0 < Sh::kRows; r0 += kQueries * kAtOnce) {
-          const int r = r0 + lane / kLanes;
-          load(r);
+#pragma unroll 1
+        for (int step = 0; step < kSteps; ++step) {
+          const int r = row_of(step);
+          uint4 raw[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
+          if (r < Sh::kRows) {
+            raw[0] = *reinterpret_cast<const uint4*>(place(r));
+            raw[1] = *reinterpret_cast<const uint4*>(place(r) + Sh::kQPart);
+          }
+          const uint32_t top = top_of(raw);
           const int e = even ? high : exponent_of(top);
           const float down = power_of_two(-e);
           uint32_t lead[4], rest[4];
@@ -569,7 +588,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
             if (top >= 0x7F800000u) lead[i] = 0x7F7F7F7Fu;  // an infinity or a NaN: NaN throughout, as its scores are
           }
           if (r < Sh::kRows) {
-            uint8_t* at = to + r * DP + ((col / 16) ^ (DP == 128 ? r & 7 : r >> 1 & 3)) * 16;
+            uint8_t* at = place(r);
             *reinterpret_cast<uint4*>(at) = make_uint4(lead[0], lead[1], lead[2], lead[3]);
             *reinterpret_cast<uint4*>(at + Sh::kQPart) = make_uint4(rest[0], rest[1], rest[2], rest[3]);
             if (col == 0) {
