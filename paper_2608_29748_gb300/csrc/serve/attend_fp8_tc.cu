@@ -205,6 +205,21 @@ __device__ __forceinline__ bool any_of_group(int group, bool mine) {
       : "memory");
   return p != 0;
 }
+// The query warps' agreement on whether all of them say so.  Each finds for itself whether a wait has expired, and
+// they meet again behind it: one that left alone would be waited for without a limit.
+template <int kWarps>
+__device__ __forceinline__ bool all_of_queries(bool mine) {
+  uint32_t p = mine;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.b32 p, %0, 0;\n\t"
+      "barrier.cta.red.and.pred q, 5, %1, p;\n\t"
+      "selp.u32 %0, 1, 0, q;\n\t}"
+      : "+r"(p)
+      : "n"(32 * kWarps)
+      : "memory");
+  return p != 0;
+}
 __device__ __forceinline__ void group_barrier(int group) { asm volatile("bar.sync %0, 128;" ::"r"(2 + group) : "memory"); }
 
 // Registers from the copies, products and queries to the softmax.
@@ -494,6 +509,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
         }
         const uint32_t buffer = pieces & 1u;
         ok = warp_wait_quick(&ct.q_empty[buffer], (pieces >> 1 & 1u) ^ 1u, abort);
+        if constexpr (kQueries > 1) ok = all_of_queries<kQueries>(ok);
         if (!ok) break;
         if (lane == 0 && which == 0) {
           ct.piece[buffer] = pc;
