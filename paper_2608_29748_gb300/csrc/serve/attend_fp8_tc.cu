@@ -119,10 +119,7 @@ struct Control {
   Piece piece[2];  // of the softmax, with its queries
   int more[2];     // 0: no piece, the end
   BoxUnits units[kInfoTiles][kMostBoxes];
-  int2 q_range[2][4];  // largest and smallest exponent of the rows of a warp
-  int even[2];         // the rows have one unit
-  float one_factor[2];                        // scale log2(e) times it
-  alignas(16) float factor[2][R * kGroups];   // and times a row's own
+  alignas(16) float factor[2][R * kGroups];   // scale log2(e) times a row's unit
   long long out[2][R * kGroups];              // where a row goes, elements
   // Of a group's rows: what is added to exponents (minus the reference), and, where that is far from
   // zero, added to the difference; how the reference moves; what sums, and at the end O, are multiplied by.
@@ -202,21 +199,6 @@ __device__ __forceinline__ bool any_of_group(int group, bool mine) {
       "selp.u32 %0, 1, 0, q;\n\t}"
       : "+r"(p)
       : "r"(2 + group)
-      : "memory");
-  return p != 0;
-}
-// The query warps' agreement on whether all of them say so.  Each finds for itself whether a wait has expired, and
-// they meet again behind it: one that left alone would be waited for without a limit.
-template <int kWarps>
-__device__ __forceinline__ bool all_of_queries(bool mine) {
-  uint32_t p = mine;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
-      "setp.ne.b32 p, %0, 0;\n\t"
-      "barrier.cta.red.and.pred q, 5, %1, p;\n\t"
-      "selp.u32 %0, 1, 0, q;\n\t}"
-      : "+r"(p)
-      : "n"(32 * kWarps)
       : "memory");
   return p != 0;
 }
@@ -509,7 +491,6 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
         }
         const uint32_t buffer = pieces & 1u;
         ok = warp_wait_quick(&ct.q_empty[buffer], (pieces >> 1 & 1u) ^ 1u, abort);
-        if constexpr (kQueries > 1) ok = all_of_queries<kQueries>(ok);
         if (!ok) break;
         if (lane == 0 && which == 0) {
           ct.piece[buffer] = pc;
@@ -522,16 +503,8 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
         }
         uint8_t* to = smem + Sh::kQAt + buffer * Sh::kQBytes;
         auto row_of = [&](int step) { return (step * kQueries + which) * kAtOnce + lane / kLanes; };
-        // Where the two parts of this lane's elements of row r go, and until then the elements themselves.
+        // Where the two parts of this lane's elements of row r go.
         auto place = [&](int r) { return to + r * DP + ((col / 16) ^ (DP == 128 ? r & 7 : r >> 1 & 3)) * 16; };
-        auto load = [&](int r, uint4 (&raw)[2]) {
-          const int token = P.by_group(r);
-          const __nv_bfloat16* from = static_cast<const __nv_bfloat16*>(a.q) + (long long)(pc.row0 + pc.i0 + token) * a.q_token +
-                                      (pc.head * P.group + r - token * P.group) * a.q_head + col;
-          raw[0] = raw[1] = make_uint4(0u, 0u, 0u, 0u);
-          if (r < rows && col < D) raw[0] = *reinterpret_cast<const uint4*>(from);
-          if (r < rows && col + 8 < D) raw[1] = *reinterpret_cast<const uint4*>(from + 8);
-        };
         // The row's largest magnitude, as bits: infinities and NaN are the largest.
         auto top_of = [&](const uint4 (&raw)[2]) {
           constexpr uint32_t kMagnitude = 0x7FFF7FFFu;
@@ -545,47 +518,18 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
         };
         // The least exponent with a magnitude <= 448 times its power of two.
         auto exponent_of = [](uint32_t t) { return min(max((int)(t >> 23) - 127 - 8 + ((t & 0x7FFFFFu) > 0x600000u), -120), 120); };
-        // The rows have the largest row's unit, and then the softmax one factor for all; where a row is much
-        // smaller (2^-6, of some 2^-17 that its elements may be off in that unit), each has its own.
-        int high = -120, low = 120;
+        // A row's unit is its own: in a larger row's, 2^6 above it, elements 2^-5 of the row's largest would be
+        // off by 2^-7 of themselves, and what a token gets would depend on what else is in its unit.
 #pragma unroll 1
         for (int step = 0; step < kSteps; ++step) {
-          uint4 raw[2];
-          const int r = row_of(step);
-          load(r, raw);
-          const uint32_t top = top_of(raw);
-          const bool counts = top != 0u && top < 0x7F800000u;
-          high = max(high, __reduce_max_sync(0xFFFFFFFFu, counts ? exponent_of(top) : -120));
-          low = min(low, __reduce_min_sync(0xFFFFFFFFu, counts ? exponent_of(top) : 120));
-          if (r < Sh::kRows) {
-            *reinterpret_cast<uint4*>(place(r)) = raw[0];
-            *reinterpret_cast<uint4*>(place(r) + Sh::kQPart) = raw[1];
-          }
-        }
-        if constexpr (kQueries > 1) {
-          if (lane == 0) ct.q_range[buffer][which] = make_int2(high, low);
-          named_barrier<5, 32 * kQueries>();
-#pragma unroll
-          for (int i = 0; i < kQueries; ++i) {
-            high = max(high, ct.q_range[buffer][i].x);
-            low = min(low, ct.q_range[buffer][i].y);
-          }
-        }
-        const bool even = high - low <= 6;
-        if (lane == 0 && which == 0) {
-          ct.even[buffer] = even;
-          ct.one_factor[buffer] = P.scale2 * power_of_two(high);
-        }
-#pragma unroll 1
-        for (int step = 0; step < kSteps; ++step) {
-          const int r = row_of(step);
+          const int r = row_of(step), token = P.by_group(r);
           uint4 raw[2] = {make_uint4(0u, 0u, 0u, 0u), make_uint4(0u, 0u, 0u, 0u)};
-          if (r < Sh::kRows) {
-            raw[0] = *reinterpret_cast<const uint4*>(place(r));
-            raw[1] = *reinterpret_cast<const uint4*>(place(r) + Sh::kQPart);
-          }
+          const __nv_bfloat16* from = static_cast<const __nv_bfloat16*>(a.q) + (long long)(pc.row0 + pc.i0 + token) * a.q_token +
+                                      (pc.head * P.group + r - token * P.group) * a.q_head + col;
+          if (r < rows && col < D) raw[0] = *reinterpret_cast<const uint4*>(from);
+          if (r < rows && col + 8 < D) raw[1] = *reinterpret_cast<const uint4*>(from + 8);
           const uint32_t top = top_of(raw);
-          const int e = even ? high : exponent_of(top);
+          const int e = exponent_of(top);
           const float down = power_of_two(-e);
           uint32_t lead[4], rest[4];
 #pragma unroll
@@ -608,7 +552,6 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
             *reinterpret_cast<uint4*>(at) = make_uint4(lead[0], lead[1], lead[2], lead[3]);
             *reinterpret_cast<uint4*>(at + Sh::kQPart) = make_uint4(rest[0], rest[1], rest[2], rest[3]);
             if (col == 0) {
-              const int token = P.by_group(r);
               ct.factor[buffer][r] = P.scale2 * power_of_two(e);
               ct.out[buffer][r] = (pc.row0 + pc.i0 + token) * a.out_token + (pc.head * P.group + r - token * P.group) * a.out_head;
             }
@@ -666,8 +609,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
       float2 l[R / 2];  // sums of this thread's keys
 #pragma unroll
       for (int i = 0; i < R / 2; ++i) l[i] = make_float2(0.f, 0.f);
-      bool far = !ct.even[buffer];  // factors differ, or some row's reference is far from zero
-      const float one_factor = ct.one_factor[buffer];
+      bool far = false;  // some row's reference is far from zero
       const UnitKeys keys = pc.keys;
       const int first = pc.c + pc.i0, k0 = pc.k0;  // position of the unit's first token
       const bool idle = r0 >= rows;
@@ -719,7 +661,6 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
         if (!idle) {
           const uint32_t t_s = tmem + lanes + b * Sh::kSColumns + r0;
           const float2 unit2 = make_float2(u.k, u.k), v2 = make_float2(u.v, u.v);
-          const float2 factor2 = make_float2(u.k * one_factor, u.k * one_factor);
           float y[R];  // exponents of the weights, then the weights
           auto hide = [&]() {
             if (inner) return;
@@ -776,8 +717,8 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
               exact(false);
             else
               scores([&](int r, const float2& x0, const float2& x1) {
-                const Four ref = four(ct.minus[h] + r);
-                put(r, add2(fma2(x0, factor2, ref.p), v2), add2(fma2(x1, factor2, ref.q), v2));
+                const Four factors = four(factor + r), ref = four(ct.minus[h] + r);
+                put(r, add2(fma2(x0, mul2(factors.p, unit2), ref.p), v2), add2(fma2(x1, mul2(factors.q, unit2), ref.q), v2));
               });
           };
           // The rows' maxima, to ct.part.
@@ -811,7 +752,10 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
           }
           if (__builtin_expect(raise, false)) {
             if (fresh && !far)
-              scores([&](int r, const float2& x0, const float2& x1) { put(r, fma2(x0, factor2, v2), fma2(x1, factor2, v2)); });
+              scores([&](int r, const float2& x0, const float2& x1) {
+                const Four factors = four(factor + r);
+                put(r, fma2(x0, mul2(factors.p, unit2), v2), fma2(x1, mul2(factors.q, unit2), v2));
+              });
             else
               exact(true);
             maxima();
