@@ -608,11 +608,11 @@ retrace_status retrace_kv_append_fp8(const void* q, int64_t q_token_stride, int6
  * `dtype`.
  * bf16: products on tensor cores in 8 bits with fp32 accumulation, the softmax in fp32.  A query is the
  * sum of two e4m3 numbers times a power of two of its row (an element is off by at most 2^-17 of the row's
- * largest, and exact above 2^-9 of it), a weight the sum of three e5m2 numbers: off by at most 2^-9 of it, or by 2^-26 of the row's largest weight (2^-19
- * where the row's first keys are few).  out is rounded once.  That needs head_dim <= 128 a multiple of 8,
- * page_size a multiple of 8, at most 72 query heads per key/value head, q strides that are multiples of 8 and cache
- * strides that are multiples of 16 elements, and 16-byte aligned bases.  Other shapes, and fp32, run on FFMA with the
- * weights kept in fp32.  An infinity or NaN in q or in a visible key makes the rows that meet it NaN (or, from
+ * largest, and exact above 2^-9 of it), a weight the sum of three e5m2 numbers: off by at most 2^-9 of it, or by
+ * 2^-24 of the row's largest weight.  out is rounded once.  That needs head_dim <= 128 a multiple of 8, page_size a
+ * multiple of 8, at most 72 query heads per key/value head, q strides that are multiples of 8 and cache strides that
+ * are multiples of 16 elements, and 16-byte aligned bases.  Other shapes, and fp32, run on FFMA with the weights kept
+ * in fp32.  An infinity or NaN in q or in a visible key makes the rows that meet it NaN (or, from
  * an infinity in fp32, what its scores give); a NaN in v at a position that only some tokens of
  * a call see may reach the others, as in retrace_attend.  One stream, no host synchronisation; the same inputs
  * on the same device give the same bits. */

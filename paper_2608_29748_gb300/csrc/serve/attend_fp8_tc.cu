@@ -10,9 +10,12 @@
 //                      bits each, in columns of their own.
 // e5m2 is the upper byte of an fp16 number, so the first part of a weight is a byte of it and the second
 // a byte of what is left, times 4; the last, times 32, is rounded: 9 bits in all, where a bf16 weight has 8,
-// down to 2^-13, and within 2^-22 below.  m puts the largest weight of a row's first tile at 2^4 (lower if
-// the tile shows few keys) and is raised, O and l rescaled, when a weight passes 2^15.  So a weight is off by
-// at most 2^-9 of it, or by 2^-26 of the row's largest (2^-19 from few keys).
+// down to 2^-13, and within 2^-22 below.  m puts the largest weight of a row's first tile at 2^3 to 2^4 and is
+// raised, O and l rescaled, when a weight passes 2^15.  So a weight is off by at most 2^-9 of it, or by 2^-24 of the
+// row's largest.  (From few keys, a window's sinks, m could be set lower, as larger scores may follow: window-tokens
+// took 83 us with up to 2^7 and takes 100.  But sinks are kept because they have most of the weight, and what is
+// lost of the others below them counts: 3 % of all weight under one sink 12.5 above 8192 equal scores.  At 2^7 more rows
+// are raised later: block-16k 424 us where 2^4 takes 377.)
 // Nothing is converted but the queries, once, and the weights: keys and values go from HBM to shared
 // memory to the tensor core, 256 D bytes a tile, 1400 cycles of an SM's share of HBM at D = 128.  The
 // products are 4 (2 rows + 3 rows) cycles at D = 128, shared memory moves some 1100 cycles' worth at
@@ -618,13 +621,6 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
       // the last token's first key.
       const int inner_hi = min(keys.hi, a.causal ? first : pc.c + pc.n - 1) - (kKeys - 1);
       const int inner_lo = a.window > 0 ? pc.c + pc.i1 - a.window : 0;
-      // Where the largest weight of a row's first tile goes: lower if the unit sees few of its keys (sinks,
-      // a window's edge) and others follow, which are likely to have larger scores.
-      float first_top = kFirstTop;
-      if (nt > 1) {
-        const int a0 = keys.tile(k0) * kKeys, seen = min(a0 + kKeys, keys.hi + 1) - max(a0, keys.lo), sinks = min(a.sinks, a0 + kKeys) - a0;
-        first_top -= (float)min(max(__clz(max(max(seen, sinks), 1)) - 24, 0), 7);
-      }
 
       for (int j = 0; j < nt; ++j) {
         const uint32_t g = tiles + j, b = g & 1u;
@@ -761,11 +757,10 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
             maxima();
             float old = 0.f, old_rest = 0.f, now = 0.f, now_rest = 0.f, move = 0.f;
             bool pending = false;
-            const float aim = fresh ? first_top : kFirstTop;
             if (key < R) {
               old = now = ct.minus[h][key];
               old_rest = now_rest = ct.rest[h][key];
-              const float most = most_of(key), by = floorf(aim - most);
+              const float most = most_of(key), by = floorf(kFirstTop - most);
               if (old == kNone ? most > -INFINITY : most > kMostTop) {
                 const float from_zero = old == kNone ? 0.f : old;
                 if (fabsf(from_zero) >= kFar && fabsf(old_rest + by) < kFar) {
@@ -797,7 +792,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
                   if (pending)
                     ct.minus[h][key] = now -= most;
                   else
-                    ct.rest[h][key] = now_rest = floorf(aim - most);
+                    ct.rest[h][key] = now_rest = floorf(kFirstTop - most);
                 }
                 if (!any_of_group(h, pending)) break;
               }
