@@ -122,6 +122,7 @@ struct Control {
   Piece piece[2];  // of the softmax, with its queries
   int more[2];     // 0: no piece, the end
   BoxUnits units[kInfoTiles][kMostBoxes];
+  int holes[kInfoTiles];  // some boxes of the tile have no page
   alignas(16) float factor[2][R * kGroups];   // scale log2(e) times a row's unit
   long long out[2][R * kGroups];              // where a row goes, elements
   // Of a group's rows: what is added to exponents (minus the reference), and, where that is far from
@@ -380,6 +381,10 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
             const int ve = clamp_exponent(now.ve);
             ct.units[tiles % kInfoTiles][box] = now.page < a.cache.num_pages ? BoxUnits{power_of_two(clamp_exponent(now.ke)), (float)ve, power_of_two(-ve), 0.f}
                                                                              : BoxUnits{1.f, -INFINITY, 1.f, 0.f};
+          }
+          if (keys) {
+            const bool holes = __any_sync(0xFFFFFFFFu, active && now.page >= a.cache.num_pages);
+            if (lane == 0) ct.holes[tiles % kInfoTiles] = holes;
           }
           __syncwarp();
           if (lane == 0) mbar_arrive_expect_tx(bar, Sh::kTileBytes);
@@ -641,6 +646,9 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
         wait(&ct.s_full[b], g >> 1 & 1u);
         tc_fence_after();
         const BoxUnits u = ct.units[g % kInfoTiles][my_box];
+        // No row sees a key without a page (its score is zero times the query, which need not be a number).
+        const bool hides = !inner || ct.holes[g % kInfoTiles];
+        if (u.v == -INFINITY) to = 0;
         // A row of V that no row of the unit sees holds anything, and 0 times that need not be 0:
         // cleared before the product.
         if (!inner && h == 0 && (j0 < keys.lo || j0 + kKeys - 1 > keys.hi)) {
@@ -659,7 +667,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
           const float2 unit2 = make_float2(u.k, u.k), v2 = make_float2(u.v, u.v);
           float y[R];  // exponents of the weights, then the weights
           auto hide = [&]() {
-            if (inner) return;
+            if (!hides) return;
 #pragma unroll
             for (int r = 0; r < R; ++r)
               if (r < from || r >= to) y[r] = -INFINITY;
