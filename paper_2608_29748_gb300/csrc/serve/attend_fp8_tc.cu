@@ -4,8 +4,8 @@
 // heads of a group) a CTA computes, all products in 8 bits with fp32 accumulation,
 //     S^T = K Q^T      [keys, rows]: K as it lies in the cache; a query is the sum of two e4m3 numbers
 //                      (its leading 4 bits and the other 4), products of their own into the same sum;
-//     t = scale S 2^ke, p = 2^(t + ve - m), l += p 2^-ve       a key's exponents ke and ve are its
-//                      thread's: one thread per key and 8 to 32 rows;
+//     t = scale S 2^ke, p = 2^(t + ve - m), l += p 2^-ve       a key's exponents ke and ve (from the
+//                      unit that O counts in) are its thread's: one thread per key and 8 to 32 rows;
 //     O^T += V^T P^T   [head dim, rows]: V as it lies; a weight is the sum of three e5m2 numbers of 3
 //                      bits each, in columns of their own.
 // e5m2 is the upper byte of an fp16 number, so the first part of a weight is a byte of it and the second
@@ -13,9 +13,16 @@
 // down to 2^-13, and within 2^-22 below.  m puts the largest weight of a row's first tile at 2^3 to 2^4 and is
 // raised, O and l rescaled, when a weight passes 2^15.  So a weight is off by at most 2^-9 of it, or by 2^-24 of the
 // row's largest.  (From few keys, a window's sinks, m could be set lower, as larger scores may follow: window-tokens
-// took 83 us with up to 2^7 and takes 100.  But sinks are kept because they have most of the weight, and what is
+// took 83 us with up to 2^7 and takes 106.  But sinks are kept because they have most of the weight, and what is
 // lost of the others below them counts: 3 % of all weight under one sink 12.5 above 8192 equal scores.  At 2^7 more rows
 // are raised later: block-16k 424 us where 2^4 takes 377.)
+// One page in a much larger unit would push all other pages' weights out of that range, whatever it holds: one
+// rejected token of huge values makes such a page.  So the product has the pages within 2^3 of the unit that O counts in
+// (2^-24 becomes 2^-18 at its ends); it moves to where most pages of a tile are.  The keys of others count in sums of their
+// own, in fp32 on the CUDA cores, a column of TMEM to a row.  64 blocks of 17 over 4096, 32 / 8 heads of 128: 183 us, with one
+// page apart in each sequence 240, one in each tile 860; all pages anywhere within 2^17 1940.  Tiles of the second kind, which
+// also look for pages that are missing, have code of their own: inside the usual tile's it made that slower
+// (window-tokens 106 -> 123 us).
 // Nothing is converted but the queries, once, and the weights: keys and values go from HBM to shared
 // memory to the tensor core, 256 D bytes a tile, 1400 cycles of an SM's share of HBM at D = 128.  The
 // products are 4 (2 rows + 3 rows) cycles at D = 128, shared memory moves some 1100 cycles' worth at
@@ -54,6 +61,9 @@ constexpr float kFar = 4194304.f;         // 2^22: references up to it are whole
 // Exponents of 2^10 and more lose places of a weight.  From 2^28 on what the rounding left is not counted: neighbouring
 // scores are 32 apart there.
 constexpr float kLarge = 1024.f, kHuge = 268435456.f;
+constexpr int kNoPage = -1000;  // in place of a box's exponent
+// Values whose exponent is within [unit - kBelow, unit + kAbove] are in the product.
+constexpr int kBelow = 3, kAbove = 3;
 
 struct TcParams {
   AttendArgs a;
@@ -83,7 +93,8 @@ struct TcShape {
   static constexpr int kOColumns = (3 * kRows + 15) / 16 * 16;
   static_assert(kSColumns <= 256 && kOColumns <= 256, "columns of a product");
   static constexpr int kOAt = 2 * kSColumns, kTmem = 512 / kPerSm;
-  static_assert(kOAt + kOColumns <= kTmem, "columns of TMEM");
+  static constexpr int kApartAt = kOAt + kOColumns;  // a column a row: what is not in the product
+  static_assert(kApartAt + kRows <= kTmem, "columns of TMEM");
   // Registers of a thread: what the softmax takes of the others' of the launch.
   static constexpr int kFewer = kFew ? 64 : 56, kMore = kFew ? 192 : 120;
   static_assert(kBase * kFewer + 128 * kGroups * kMore <= kThreads * (65536 / (kThreads * kPerSm) / 8 * 8), "registers of a CTA");
@@ -101,10 +112,10 @@ struct TcShape {
   static constexpr int kPart = kRows * (DP + 2);  // floats of a part
 };
 
-// A box's keys: scores are multiplied by k, weights are 2^(.. + v), sums take them times inv.  Without a
-// page v is minus infinity.
+// A box's keys: scores are multiplied by k, values by 2^v.  Where no row sees the box, or it has no page, v is kNoPage.
 struct BoxUnits {
-  float k, v, inv, unused;
+  float k;
+  int v;
 };
 
 template <int R, int kGroups>
@@ -122,13 +133,14 @@ struct Control {
   Piece piece[2];  // of the softmax, with its queries
   int more[2];     // 0: no piece, the end
   BoxUnits units[kInfoTiles][kMostBoxes];
-  int holes[kInfoTiles];  // some boxes of the tile have no page
+  int2 span[kInfoTiles];  // largest and smallest v of the tile's boxes that are seen; the latter kNoPage if one has no page
   alignas(16) float factor[2][R * kGroups];   // scale log2(e) times a row's unit
   long long out[2][R * kGroups];              // where a row goes, elements
   // Of a group's rows: what is added to exponents (minus the reference), and, where that is far from
   // zero, added to the difference; how the reference moves; what sums, and at the end O, are multiplied by.
   alignas(16) float minus[kGroups][R], rest[kGroups][R], move[kGroups][R], scale[kGroups][R];
-  float part[kGroups][4][R];  // per warp: a row's maximum, or sum
+  float part[kGroups][4][R];  // per warp: a row's maximum, or sum; of four keys: their weights
+  uint32_t others[kGroups];   // boxes that are not in the product
 };
 
 // ---- instructions -------------------------------------------------------------
@@ -243,8 +255,8 @@ __device__ __forceinline__ uint32_t to_e5m2x4(uint32_t a, uint32_t b) {
   return y;
 }
 // The three parts of four weights, none negative, a byte each; the second times 4, the third times 32.
-__device__ __forceinline__ void take_apart(const float (&w)[4], uint32_t& first, uint32_t& second, uint32_t& third) {
-  const uint32_t a = halves(w[0], w[1]), b = halves(w[2], w[3]);
+__device__ __forceinline__ void take_apart(const float2& w0, const float2& w1, uint32_t& first, uint32_t& second, uint32_t& third) {
+  const uint32_t a = halves(w0.x, w0.y), b = halves(w1.x, w1.y);
   const uint32_t a1 = times<4>(minus_halves(a, a & 0xFF00FF00u)), b1 = times<4>(minus_halves(b, b & 0xFF00FF00u));
   const uint32_t a2 = minus_halves(a1, a1 & 0xFF00FF00u), b2 = minus_halves(b1, b1 & 0xFF00FF00u);
   first = __byte_perm(a, b, 0x7531);
@@ -338,10 +350,11 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
         int head, slot;  // slot: within the page
         int page;
         int ke, ve;
+        bool seen;  // by a row of the unit
       };
       int nt = 0, k = 0;
       auto pages = [&]() {  // of the next batch
-        Batch x{0, 0, 0, -1, 0, 0};
+        Batch x{0, 0, 0, -1, 0, 0, false};
         while (k >= nt) {
           if (!walk.next<kKeys, false, true>(P.shape, plan, &pc)) return x;
           nt = pc.k1 - pc.k0;
@@ -352,6 +365,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
         if (my_tile < x.count) {
           const int j = pc.keys.tile(pc.k0 + k + my_tile) * kKeys + box * P.kv_box, i = P.page_size(j);
           x.slot = j - i * P.page_size.by;
+          x.seen = j <= pc.keys.hi && (j + P.kv_box > pc.keys.lo || j < a.sinks);
           if (i < a.cache.max_pages) x.page = a.cache.page_table[pc.b * a.cache.table_stride + i];
         }
         k += batch;
@@ -377,14 +391,13 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
           if (!ok) break;
           const uint32_t bar = smem_u32(&ct.full[!keys][slot]);
           const bool active = my_tile == t;
-          if (keys && active) {
-            const int ve = clamp_exponent(now.ve);
-            ct.units[tiles % kInfoTiles][box] = now.page < a.cache.num_pages ? BoxUnits{power_of_two(clamp_exponent(now.ke)), (float)ve, power_of_two(-ve), 0.f}
-                                                                             : BoxUnits{1.f, -INFINITY, 1.f, 0.f};
-          }
           if (keys) {
-            const bool holes = __any_sync(0xFFFFFFFFu, active && now.page >= a.cache.num_pages);
-            if (lane == 0) ct.holes[tiles % kInfoTiles] = holes;
+            const bool there = active && now.page < a.cache.num_pages;
+            const int v = there && now.seen ? clamp_exponent(now.ve) : kNoPage;
+            if (active) ct.units[tiles % kInfoTiles][box] = BoxUnits{there ? power_of_two(clamp_exponent(now.ke)) : 1.f, v};
+            const int hi = __reduce_max_sync(0xFFFFFFFFu, max(v, -kMostExponent));
+            const int lo = __reduce_min_sync(0xFFFFFFFFu, active && now.seen ? v : kMostExponent);
+            if (lane == 0) ct.span[tiles % kInfoTiles] = make_int2(hi, lo);
           }
           __syncwarp();
           if (lane == 0) mbar_arrive_expect_tx(bar, Sh::kTileBytes);
@@ -582,7 +595,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
     // ---- softmax: group h, one thread per key ----
     const int h = (warp - kBase / 32) / 4, key = tid & 127, quarter = warp & 3, r0 = h * R;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    const uint32_t t_o = tmem + lanes + Sh::kOAt;
+    const uint32_t t_o = tmem + lanes + Sh::kOAt, t_apart = tmem + lanes + Sh::kApartAt + r0;
     // This key's weights, with the swizzle of its row: a column of 16 bytes is one exclusive or away.
     const uint32_t my_weights = (base + Sh::kPAt + key * Sh::kPWidth) ^
                                 (Sh::kPWidth == 128 ? key & 7 : Sh::kPWidth == 64 ? key >> 1 & 3 : key >> 2 & 1) * 16;
@@ -618,6 +631,8 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
 #pragma unroll
       for (int i = 0; i < R / 2; ++i) l[i] = make_float2(0.f, 0.f);
       bool far = false;  // some row's reference is far from zero
+      int o_unit = 0;      // O counts in 2^o_unit
+      bool apart = false;  // something was not in the product
       const UnitKeys keys = pc.keys;
       const int first = pc.c + pc.i0, k0 = pc.k0;  // position of the unit's first token
       const bool idle = r0 >= rows;
@@ -627,7 +642,9 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
       const int inner_hi = min(keys.hi, a.causal ? first : pc.c + pc.n - 1) - (kKeys - 1);
       const int inner_lo = a.window > 0 ? pc.c + pc.i1 - a.window : 0;
 
-      for (int j = 0; j < nt; ++j) {
+      // A tile; false: it needs care, and nothing has been done with it.
+      auto tile = [&](auto care, int j) {
+        constexpr bool kCare = decltype(care)::value;
         const uint32_t g = tiles + j, b = g & 1u;
         const int j0 = keys.tile(k0 + j) * kKeys;
         const bool inner = j0 >= inner_lo && j0 <= inner_hi;  // every row sees every key that has a page
@@ -645,15 +662,41 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
         }
         wait(&ct.s_full[b], g >> 1 & 1u);
         tc_fence_after();
+        const bool fresh = j == 0;
         const BoxUnits u = ct.units[g % kInfoTiles][my_box];
-        // No row sees a key without a page (its score is zero times the query, which need not be a number).
-        const bool hides = !inner || ct.holes[g % kInfoTiles];
-        if (u.v == -INFINITY) to = 0;
+        const int2 span = ct.span[g % kInfoTiles];
+        int now_unit = fresh ? span.x : o_unit;
+        const bool wide = span.x > now_unit + kAbove || span.y < now_unit - kBelow;
+        bool hides = !inner;
+        uint32_t others = 0u;  // boxes that are not in the product
+        if (kCare && wide) {
+          // No row sees a key without a page (its score is zero times the query, which need not be a number).
+          if (span.y == kNoPage) {
+            hides = true;
+            if (u.v == kNoPage) to = 0;
+          }
+          // The unit that most boxes fit; this one, if it is one of several.
+          const int v = lane < kKeys / P.kv_box ? ct.units[g % kInfoTiles][lane].v : kNoPage;
+          auto fitting = [&](int x) { return __ballot_sync(0xFFFFFFFFu, v != kNoPage && v <= x + kAbove && v >= x - kBelow); };
+          uint32_t in = fitting(now_unit);
+          for (int i = 0; i < kKeys / P.kv_box; ++i) {
+            const int x = __shfl_sync(0xFFFFFFFFu, v, i);
+            const uint32_t then = fitting(x);
+            if (__popc(then) > __popc(in)) {
+              in = then;
+              now_unit = x;
+            }
+          }
+          others = __ballot_sync(0xFFFFFFFFu, v != kNoPage) & ~in;
+        }
+        // Exponents of this key's weights: they are in the product as they are then, so that it counts in 2^now_unit.
+        const int above = u.v - now_unit, shift = above <= kAbove ? max(above, -2 * kMostExponent) : 0;
         // A row of V that no row of the unit sees holds anything, and 0 times that need not be 0:
         // cleared before the product.
-        if (!inner && h == 0 && (j0 < keys.lo || j0 + kKeys - 1 > keys.hi)) {
-          // (the slot's phase before is over: the scores of this tile waited for a later product)
-          wait(&ct.full[1][g % Sh::kRingV], g / Sh::kRingV & 1u);
+        const bool clears = !inner && h == 0 && (j0 < keys.lo || j0 + kKeys - 1 > keys.hi);
+        // (the slot's phase before is over: the scores of this tile waited for a later product)
+        if (clears || (kCare && others != 0u)) wait(&ct.full[1][g % Sh::kRingV], g / Sh::kRingV & 1u);
+        if (clears) {
           const int at = j0 + key;
           if (at > keys.hi || (at < keys.lo && at >= a.sinks)) {
             uint8_t* v = smem + Sh::kVAt + (g % Sh::kRingV) * Sh::kTileBytes + key * DP;
@@ -664,7 +707,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
         }
         if (!idle) {
           const uint32_t t_s = tmem + lanes + b * Sh::kSColumns + r0;
-          const float2 unit2 = make_float2(u.k, u.k), v2 = make_float2(u.v, u.v);
+          const float2 unit2 = make_float2(u.k, u.k), shift2 = make_float2((float)shift, (float)shift);
           float y[R];  // exponents of the weights, then the weights
           auto hide = [&]() {
             if (!hides) return;
@@ -709,7 +752,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
               float2 left = fma2(t, factor, make_float2(-m.x, -m.y));
               if (fabsf(ref.x) >= kHuge) left.x = 0.f;
               if (fabsf(ref.y) >= kHuge) left.y = 0.f;
-              return add2(add2(add2(m, ref), left), add2(v2, rest));
+              return add2(add2(add2(m, ref), left), add2(shift2, rest));
             };
             scores([&](int r, const float2& x0, const float2& x1) {
               const Four factors = four(factor + r), rest = four(ct.rest[h] + r), ref = four(ct.minus[h] + r);
@@ -722,7 +765,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
             else
               scores([&](int r, const float2& x0, const float2& x1) {
                 const Four factors = four(factor + r), ref = four(ct.minus[h] + r);
-                put(r, add2(fma2(x0, mul2(factors.p, unit2), ref.p), v2), add2(fma2(x1, mul2(factors.q, unit2), ref.q), v2));
+                put(r, add2(fma2(x0, mul2(factors.p, unit2), ref.p), shift2), add2(fma2(x1, mul2(factors.q, unit2), ref.q), shift2));
               });
           };
           // The rows' maxima, to ct.part.
@@ -742,7 +785,8 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
           // The first tile sets the references.  After it a weight may outgrow its own, or a row may see
           // its first keys: then, too, the rows' maxima over the tile, new references (whole numbers,
           // so that they are the same however often they move), and what was summed so far in the new unit.
-          const bool fresh = j == 0;
+          // So does another unit of the values; and a tile that needs care, or has boxes that are not in the product, comes
+          // by here, because the group agrees on it: after an expired wait its warps may have read different units.
           bool raise = fresh;
           if (!fresh) {
             exponents();
@@ -752,17 +796,24 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
             // (the weights do not wait for the answer: exponents are worked out again where they move)
 #pragma unroll
             for (int r = 0; r < R; ++r) y[r] = exp2_fast(y[r]);
-            raise = any_of_group(h, top > kMostTop);
+            raise = any_of_group(h, top > kMostTop || (kCare ? now_unit != o_unit || others != 0u : wide));
           }
+          bool some_apart = false;
           if (__builtin_expect(raise, false)) {
+            if (key == 0) ct.others[h] = kCare ? others : wide;
             if (fresh && !far)
               scores([&](int r, const float2& x0, const float2& x1) {
                 const Four factors = four(factor + r);
-                put(r, fma2(x0, mul2(factors.p, unit2), v2), fma2(x1, mul2(factors.q, unit2), v2));
+                put(r, fma2(x0, mul2(factors.p, unit2), shift2), fma2(x1, mul2(factors.q, unit2), shift2));
               });
             else
               exact(true);
             maxima();
+            some_apart = ct.others[h] != 0u;
+            if (!kCare && some_apart) {
+              group_barrier(h);  // all have read it
+              return false;
+            }
             float old = 0.f, old_rest = 0.f, now = 0.f, now_rest = 0.f, move = 0.f;
             bool pending = false;
             if (key < R) {
@@ -810,6 +861,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
             if (!fresh) {
 #pragma unroll
               for (int r = 0; r < R; r += 2) l[r / 2] = mul2(l[r / 2], *reinterpret_cast<const float2*>(ct.scale[h] + r));
+              const float carry = kCare ? power_of_two(o_unit - now_unit) : 1.f;
               const uint32_t before = g - 1;
               wait(&ct.pv_done[before & 1u], before >> 1 & 1u);
               tc_fence_after();
@@ -822,11 +874,22 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
                   tmem_load<n>(column, o);
                   tmem_wait_ld();
 #pragma unroll
-                  for (int i = 0; i < n; ++i) o[i] *= ct.scale[h][16 * c + i];
+                  for (int i = 0; i < n; ++i) o[i] *= ct.scale[h][16 * c + i] * carry;
 #pragma unroll
                   for (int i = 0; i < n; i += 4) tmem_store4(column + i, o + i);
                 }
               });
+              if (kCare && apart)
+#pragma unroll 1
+                for (int r = 0; r < R; r += 8) {
+                  float o[8];
+                  tmem_load<8>(t_apart + r, o);
+                  tmem_wait_ld();
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) o[i] *= ct.scale[h][r + i];
+                  tmem_store4(t_apart + r, o);
+                  tmem_store4(t_apart + r + 4, o + 4);
+                }
               tmem_wait_st();
             }
             if (again) {
@@ -843,17 +906,10 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
           }
 
           const uint32_t weights = my_weights + b * Sh::kPBytes;
-          const float2 inv2 = make_float2(u.inv, u.inv);
-          each_chunk<Sh::kChunks>([&](auto chunk) {
+          const float inv = power_of_two(-shift);
+          const float2 inv2 = make_float2(inv, inv);
+          auto put_weights = [&](auto chunk, const uint32_t* w) {
             constexpr int c = decltype(chunk)::value, n = Sh::rows_of(c);
-            uint32_t w[3 * n / 4];
-#pragma unroll
-            for (int i = 0; i < n; i += 4) {
-              const float e[4] = {y[16 * c + i], y[16 * c + i + 1], y[16 * c + i + 2], y[16 * c + i + 3]};
-              l[(16 * c + i) / 2] = fma2(make_float2(e[0], e[1]), inv2, l[(16 * c + i) / 2]);
-              l[(16 * c + i) / 2 + 1] = fma2(make_float2(e[2], e[3]), inv2, l[(16 * c + i) / 2 + 1]);
-              take_apart(e, w[i / 4], w[n / 4 + i / 4], w[2 * (n / 4) + i / 4]);
-            }
             const int column = Sh::o_column(h, c);
 #pragma unroll
             for (int i = 0; i < 3; ++i) {
@@ -864,13 +920,84 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
               else
                 st_shared(at_w, w[2 * i], w[2 * i + 1]);
             }
+          };
+          each_chunk<Sh::kChunks>([&](auto chunk) {
+            constexpr int c = decltype(chunk)::value, n = Sh::rows_of(c);
+            uint32_t w[3 * n / 4];
+#pragma unroll
+            for (int i = 0; i < n; i += 4) {
+              const float2 p = make_float2(y[16 * c + i], y[16 * c + i + 1]), q = make_float2(y[16 * c + i + 2], y[16 * c + i + 3]);
+              l[(16 * c + i) / 2] = fma2(p, inv2, l[(16 * c + i) / 2]);
+              l[(16 * c + i) / 2 + 1] = fma2(q, inv2, l[(16 * c + i) / 2 + 1]);
+              take_apart(p, q, w[i / 4], w[n / 4 + i / 4], w[2 * (n / 4) + i / 4]);
+            }
+            put_weights(chunk, w);
           });
+
+          // Keys that are not in the product, four at a time: their weights through shared memory, and this thread's
+          // element of their values, in fp32.
+          if (kCare && some_apart) {
+            if (ct.others[h] >> my_box & 1u)
+              each_chunk<Sh::kChunks>([&](auto chunk) {
+                const uint32_t none[12] = {};
+                put_weights(chunk, none);
+              });
+            if (!apart) {
+              const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int r = 0; r < R; r += 4) tmem_store4(t_apart + r, zero);
+              tmem_wait_st();
+              apart = true;
+            }
+            const uint8_t* values = smem + Sh::kVAt + (g % Sh::kRingV) * Sh::kTileBytes;
+            const int element = key % DP;
+#pragma unroll 1
+            for (uint32_t left = ct.others[h]; left != 0u; left &= left - 1u) {
+              const int box = __ffs(left) - 1;
+              const float value_unit = power_of_two(ct.units[g % kInfoTiles][box].v);
+#pragma unroll 1
+              for (int four_at = box * P.kv_box; four_at < (box + 1) * P.kv_box; four_at += 4) {
+                if (key / 4 == four_at / 4) {
+#pragma unroll
+                  for (int r = 0; r < R; ++r) ct.part[h][key % 4][r] = y[r] * inv;
+                }
+                group_barrier(h);
+                float v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const int k = four_at + i, at = j0 + k;
+                  const bool seen = at <= keys.hi && (at >= keys.lo || at < a.sinks);
+                  const uint32_t code = values[k * DP + ((element / 16) ^ (DP == 128 ? k & 7 : k >> 1 & 3)) * 16 + element % 16];
+                  v[i] = seen ? e4m3_floats(code).x * value_unit : 0.f;
+                }
+#pragma unroll 1
+                for (int r = 0; r < R; r += 8) {
+                  float o[8];
+                  tmem_load<8>(t_apart + r, o);
+                  tmem_wait_ld();
+#pragma unroll
+                  for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) o[x] += ct.part[h][i][r + x] * v[i];
+                  tmem_store4(t_apart + r, o);
+                  tmem_store4(t_apart + r + 4, o + 4);
+                }
+                tmem_wait_st();
+                group_barrier(h);
+              }
+            }
+          }
         }
+        o_unit = now_unit;
         fence_proxy_async_shared();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&ct.p_full[b]));
-      }
+        return true;
+      };
+      int j = 0;
+      while (j < nt && tile(Index<0>{}, j)) ++j;
+      for (; j < nt; ++j) tile(Index<1>{}, j);
       tiles += nt;
 
       // The rows' sums over the group's threads.
@@ -890,7 +1017,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
         // What O is multiplied by, so that it refers to m: to a number, where minus and rest are two.
         const float m = -(ct.minus[h][key] + ct.rest[h][key]);
         const float f = exp2_fast(-((ct.minus[h][key] + m) + ct.rest[h][key])), sum = sum_of(h, key) * f;
-        ct.scale[h][key] = whole ? (sum == 0.f ? 0.f : f / sum) : f;
+        ct.scale[h][key] = (whole ? (sum == 0.f ? 0.f : f / sum) : f) * power_of_two(o_unit);
         if (!whole && ok && r0 + key < rows)
           *reinterpret_cast<float2*>(part + Sh::kRows * DP + (r0 + key) * 2) = make_float2(sum == 0.f ? -INFINITY : m, sum);
       }
@@ -922,7 +1049,16 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
           for (int p = 0; p < 3; ++p) tmem_load<n>(t_o + Sh::o_column(h, c) + p * n, o + p * n);
           tmem_wait_ld();
 #pragma unroll
-          for (int i = 0; i < n; ++i) o[i] = (o[i] + (o[n + i] * 0.25f + o[2 * n + i] * 0.03125f)) * ct.scale[h][16 * c + i];
+          for (int i = 0; i < n; ++i) o[i] = o[i] + (o[n + i] * 0.25f + o[2 * n + i] * 0.03125f);
+          if (apart) {
+            const float down = power_of_two(-o_unit);
+            tmem_load<n>(t_apart + 16 * c, o + n);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < n; ++i) o[i] += o[n + i] * down;
+          }
+#pragma unroll
+          for (int i = 0; i < n; ++i) o[i] *= ct.scale[h][16 * c + i];
           put_rows(r0 + 16 * c, o, n);
         });
       }
