@@ -61,6 +61,9 @@ constexpr float kFar = 4194304.f;         // 2^22: references up to it are whole
 // Exponents of 2^10 and more lose places of a weight.  From 2^28 on what the rounding left is not counted: neighbouring
 // scores are 32 apart there.
 constexpr float kLarge = 1024.f, kHuge = 268435456.f;
+// A factor times the largest unit of keys would leave fp32, and a score of zero times that is no number: the factor is
+// multiplied by last.
+constexpr float kLargeFactor = 1.2e24f;  // 2^80
 constexpr int kNoPage = -1000;  // in place of a box's exponent
 // Values whose exponent is within [unit - kBelow, unit + kAbove] are in the product.
 constexpr int kBelow = 3, kAbove = 3;
@@ -134,6 +137,7 @@ struct Control {
   int more[2];     // 0: no piece, the end
   BoxUnits units[kInfoTiles][kMostBoxes];
   int2 span[kInfoTiles];  // largest and smallest v of the tile's boxes that are seen; the latter kNoPage if one has no page
+  int large[2][4];     // some factor of a query warp's rows is
   alignas(16) float factor[2][R * kGroups];   // scale log2(e) times a row's unit
   long long out[2][R * kGroups];              // where a row goes, elements
   // Of a group's rows: what is added to exponents (minus the reference), and, where that is far from
@@ -541,6 +545,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
         auto exponent_of = [](uint32_t t) { return min(max((int)(t >> 23) - 127 - 8 + ((t & 0x7FFFFFu) > 0x600000u), -120), 120); };
         // A row's unit is its own: in a larger row's, 2^6 above it, elements 2^-5 of the row's largest would be
         // off by 2^-7 of themselves, and what a token gets would depend on what else is in its unit.
+        bool large = false;
 #pragma unroll 1
         for (int step = 0; step < kSteps; ++step) {
           const int r = row_of(step), token = P.by_group(r);
@@ -573,11 +578,15 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
             *reinterpret_cast<uint4*>(at) = make_uint4(lead[0], lead[1], lead[2], lead[3]);
             *reinterpret_cast<uint4*>(at + Sh::kQPart) = make_uint4(rest[0], rest[1], rest[2], rest[3]);
             if (col == 0) {
-              ct.factor[buffer][r] = P.scale2 * power_of_two(e);
+              const float factor = fminf(fmaxf(P.scale2 * power_of_two(e), -kNone), kNone);
+              ct.factor[buffer][r] = factor;
+              large |= fabsf(factor) >= kLargeFactor;
               ct.out[buffer][r] = (pc.row0 + pc.i0 + token) * a.out_token + (pc.head * P.group + r - token * P.group) * a.out_head;
             }
           }
         }
+        large = __any_sync(0xFFFFFFFFu, large);
+        if (lane == 0) ct.large[buffer][which] = large;
         fence_proxy_async_shared();
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&ct.q_full[buffer]));
@@ -630,7 +639,9 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
       float2 l[R / 2];  // sums of this thread's keys
 #pragma unroll
       for (int i = 0; i < R / 2; ++i) l[i] = make_float2(0.f, 0.f);
-      bool far = false;  // some row's reference is far from zero
+      bool far = false;  // some row's reference is far from zero, or its factor large
+#pragma unroll
+      for (int i = 0; i < kQueries; ++i) far |= ct.large[buffer][i] != 0;
       int o_unit = 0;      // O counts in 2^o_unit
       bool apart = false;  // something was not in the product
       const UnitKeys keys = pc.keys;
@@ -1141,7 +1152,7 @@ cudaError_t launch_attend_fp8_tc(const AttendArgs& a, cudaStream_t stream) {
   p.by_group = FastDivide::of(p.group);
   p.page_size = FastDivide::of(c.page_size);
   p.kv_box = gcd(c.page_size, kKeys);
-  p.scale2 = a.scale * 1.4426950408889634f;
+  p.scale2 = std::min(std::max(a.scale * 1.4426950408889634f, -kNone), kNone);  // finite, as scale is
   p.shape.q_start = a.q_start;
   p.shape.cache_len = a.cache_len;
   p.shape.B = a.B;
