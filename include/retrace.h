@@ -608,9 +608,9 @@ retrace_status retrace_kv_append_fp8(const void* q, int64_t q_token_stride, int6
  * `dtype`.
  * bf16: products on tensor cores in 8 bits with fp32 accumulation, the softmax in fp32.  A query is the
  * sum of two e4m3 numbers times a power of two of its row (an element is off by at most 2^-17 of the row's
- * largest, and exact above 2^-9 of it), a weight the sum of three e5m2 numbers: off by at most 2^-9 of it, or by
- * 2^-24 of the row's largest weight (2^-18 where the powers of two of the values' pages differ: those within 2^3 of one
- * that most pages are near go to the tensor cores together, others' weights stay in fp32, which takes longer).  out is
+ * largest, and exact above 2^-9 of it), a weight the sum of three e5m2 numbers: off by at most 2^-9 + 2^-11 of
+ * it, or by 2^-24 of the row's largest weight (2^-18 where the powers of two of the values' pages differ: those within
+ * 2^3 of one that most pages are near go to the tensor cores together, others' weights stay in fp32, which takes longer).  out is
  * rounded once.  That needs head_dim <= 128 a multiple of 8, page_size a multiple of 8, at most 72 query heads per
  * key/value head, q strides that are multiples of 8 and cache strides that are multiples of 16 elements, and 16-byte
  * aligned bases.  Other shapes, and fp32, run on FFMA with the weights kept in fp32.  An infinity or NaN in q or in a

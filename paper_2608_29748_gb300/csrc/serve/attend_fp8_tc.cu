@@ -9,18 +9,18 @@
 //     O^T += V^T P^T   [head dim, rows]: V as it lies; a weight is the sum of three e5m2 numbers of 3
 //                      bits each, in columns of their own.
 // e5m2 is the upper byte of an fp16 number, so the first part of a weight is a byte of it and the second
-// a byte of what is left, times 4; the last, times 32, is rounded: 9 bits in all, where a bf16 weight has 8,
-// down to 2^-13, and within 2^-22 below.  m puts the largest weight of a row's first tile at 2^3 to 2^4 and is
-// raised, O and l rescaled, when a weight passes 2^15.  So a weight is off by at most 2^-9 of it, or by 2^-24 of the
-// row's largest.  (From few keys, a window's sinks, m could be set lower, as larger scores may follow: window-tokens
-// took 83 us with up to 2^7 and takes 106.  But sinks are kept because they have most of the weight, and what is
-// lost of the others below them counts: 3 % of all weight under one sink 12.5 above 8192 equal scores.  At 2^7 more rows
-// are raised later: block-16k 424 us where 2^4 takes 377.)
+// a byte of what is left, times 4; the last, times 32, is rounded: down to 2^-13 off by at most 2^-9 and 2^-11
+// of it (two roundings), and by 2^-21.8 below.  m puts the largest weight of a row's first tile at 2^3 to 2^4 and is
+// raised, O and l rescaled, when a weight passes 2^15: so that is 2^-24 of the row's largest.  (From few keys, a window's
+// sinks, m could be set lower, as larger scores may follow: window-tokens took 83 us with up to 2^7 and takes 106.
+// But sinks are kept because they have most of the weight, and what is lost of the others below them counts: 3 % of all
+// weight under one sink 12.5 above 8192 equal scores.  At 2^7 more rows are raised later: block-16k 424 us where 2^4
+// takes 377.)
 // One page in a much larger unit would push all other pages' weights out of that range, whatever it holds: one
 // rejected token of huge values makes such a page.  So the product has the pages within 2^3 of the unit that O counts in
 // (2^-24 becomes 2^-18 at its ends); it moves to where most pages of a tile are.  The keys of others count in sums of their
 // own, in fp32 on the CUDA cores, a column of TMEM to a row.  64 blocks of 17 over 4096, 32 / 8 heads of 128: 183 us, with one
-// page apart in each sequence 240, one in each tile 860; all pages anywhere within 2^17 1940.  Tiles of the second kind, which
+// page apart in each sequence 240, one in each tile 860; all pages anywhere within 2^17 1690.  Tiles of the second kind, which
 // also look for pages that are missing, have code of their own: inside the usual tile's it made that slower
 // (window-tokens 106 -> 123 us).
 // Nothing is converted but the queries, once, and the weights: keys and values go from HBM to shared
