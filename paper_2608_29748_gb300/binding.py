@@ -631,7 +631,7 @@ def retrace_kv_append_fp8(q, k, v, cache: KvCacheFp8, cache_len, rope, q_out=Non
         if rope.dtype != torch.float32 or rope.dim() != 3 or rope.shape[2] != 2 or not rope.is_contiguous() or not rope.is_cuda:
             raise ValueError("rope must be a contiguous float32 [positions, rot/2, 2] on the GPU")
         positions, half, _ = rope.shape
-        rot, rope_ptr = 2 * half, rope.data_ptr()
+        rot, rope_ptr = 2 * half, rope.data_ptr() or 16  # an empty table has no address, and no address means no table
     len_ptr, start_ptr = _lengths(cache, cache_len, q_start)
     status = _append_fp8(q_ptr, q_token, q_head, q_heads, k.data_ptr(), k_token, k_head, v.data_ptr(), v_token, v_head, _dtype_code(k),
                          start_ptr, len_ptr, cache.B, T, rope_ptr, positions, rot, interleaved, cache.ref, out_ptr, o_token, o_head,
