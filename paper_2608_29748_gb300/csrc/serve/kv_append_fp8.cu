@@ -79,7 +79,6 @@ struct Chunk<__nv_bfloat16, 8> {
 struct HeadShape {
   int pairs, inside, copies, lanes;  // lanes: their sum
   int step;                          // from a chunk to its partner, elements
-  FastDivide by_lanes;
   int page_ctas;             // the others have the queries
   int shares, share_tasks;   // of a chunk's heads (k and v apart)
   int tokens, query_tokens;  // of a CTA at a time
@@ -550,7 +549,6 @@ cudaError_t launch(const AppendArgs& a, cudaStream_t stream) {
     s.step = D / 2;
   }
   s.lanes = s.pairs + s.inside + s.copies;
-  s.by_lanes = FastDivide::of(s.lanes);
   const int groups = kThreads / s.lanes, share = (a.q_heads + kHeadsEach - 1) / kHeadsEach;
   s.per_token = share < 1 ? 1 : groups < share ? groups : share;
   // As many warps to a page's tokens as keep them.
