@@ -12,17 +12,17 @@
 // a byte of what is left, times 4; the last, times 32, is rounded: down to 2^-13 off by at most 2^-9 and 2^-11
 // of it (two roundings), and by 2^-21.8 below.  m puts the largest weight of a row's first tile at 2^3 to 2^4 and is
 // raised, O and l rescaled, when a weight passes 2^15: so that is 2^-24 of the row's largest.  (From few keys, a window's
-// sinks, m could be set lower, as larger scores may follow: window-tokens took 83 us with up to 2^7 and takes 106.
-// But sinks are kept because they have most of the weight, and what is lost of the others below them counts: 3 % of all
-// weight under one sink 12.5 above 8192 equal scores.  At 2^7 more rows are raised later: block-16k 424 us where 2^4
-// takes 377.)
+// sinks, m could be set lower, as larger scores may follow: window-tokens took 83 us with up to 2^7.  But sinks are
+// kept because they have most of the weight, and what is lost of the others below them counts: 3 % of all weight under
+// one sink 12.5 above 8192 equal scores.  Instead a window's sinks come last: 96 us, 107 with the sinks first.  At 2^7
+// more rows are raised later: block-16k 424 us where 2^4 takes 377.)
 // One page in a much larger unit would push all other pages' weights out of that range, whatever it holds: one
 // rejected token of huge values makes such a page.  So the product has the pages within 2^3 of the unit that O counts in
 // (2^-24 becomes 2^-18 at its ends); it moves to where most pages of a tile are.  The keys of others count in sums of their
 // own, in fp32 on the CUDA cores, a column of TMEM to a row.  64 blocks of 17 over 4096, 32 / 8 heads of 128: 183 us, with one
 // page apart in each sequence 240, one in each tile 860; all pages anywhere within 2^17 1690.  Tiles of the second kind, which
 // also look for pages that are missing, have code of their own: inside the usual tile's it made that slower
-// (window-tokens 106 -> 123 us).
+// (window-tokens, sinks first, 106 -> 123 us).
 // Nothing is converted but the queries, once, and the weights: keys and values go from HBM to shared
 // memory to the tensor core, 256 D bytes a tile, 1400 cycles of an SM's share of HBM at D = 128.  The
 // products are 4 (2 rows + 3 rows) cycles at D = 128, shared memory moves some 1100 cycles' worth at
@@ -275,6 +275,13 @@ __device__ __forceinline__ void st_shared(uint32_t at, uint32_t x, uint32_t y) {
   asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(at), "r"(x), "r"(y) : "memory");
 }
 
+// The tiles of a unit in this kernel's order: the window's first, then the sinks'.  The first tile sets the references, and
+// sinks show few keys.
+__device__ __forceinline__ int tile_of(const UnitKeys& keys, int k) {
+  const int window = keys.count - keys.sink_tiles;
+  return k < window ? keys.first + k : k - window;
+}
+
 template <int I>
 struct Index {
   static constexpr int value = I;
@@ -367,7 +374,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
         x.count = min(batch, nt - k);
         x.head = pc.head;
         if (my_tile < x.count) {
-          const int j = pc.keys.tile(pc.k0 + k + my_tile) * kKeys + box * P.kv_box, i = P.page_size(j);
+          const int j = tile_of(pc.keys, pc.k0 + k + my_tile) * kKeys + box * P.kv_box, i = P.page_size(j);
           x.slot = j - i * P.page_size.by;
           x.seen = j <= pc.keys.hi && (j + P.kv_box > pc.keys.lo || j < a.sinks);
           if (i < a.cache.max_pages) x.page = a.cache.page_table[pc.b * a.cache.table_stride + i];
@@ -657,7 +664,7 @@ __global__ void __launch_bounds__(TcShape<DP, R>::kThreads, TcShape<DP, R>::kPer
       auto tile = [&](auto care, int j) {
         constexpr bool kCare = decltype(care)::value;
         const uint32_t g = tiles + j, b = g & 1u;
-        const int j0 = keys.tile(k0 + j) * kKeys;
+        const int j0 = tile_of(keys, k0 + j) * kKeys;
         const bool inner = j0 >= inner_lo && j0 <= inner_hi;  // every row sees every key that has a page
         // Else the key is seen by the rows [from, to).
         int from = 0, to = R;
