@@ -10,7 +10,6 @@
 // in bf16: 15 us of HBM.  It takes 35: a CTA is a chain of waits (its tokens' places 2 us, then 2 us for each
 // team's next page and head), and the registers allow three CTAs.
 #include "fp8.cuh"
-#include "pairs.cuh"
 #include "tokens.cuh"
 
 namespace retrace {
@@ -122,7 +121,8 @@ __device__ __forceinline__ void load_angles(float (&cs)[2 * N], const float* rop
   }
 }
 
-// (v, w) turned by (c, s); the products are rounded before they are added.
+// (v, w) turned by (c, s); the products are rounded before they are added.  (As operations on two numbers at once the
+// assembler joins a product and a sum into one rounding, although both ask for their own.)
 __device__ __forceinline__ void turn(float& v, float& w, float c, float s) {
   const float a = __fsub_rn(__fmul_rn(v, c), __fmul_rn(w, s));
   w = __fadd_rn(__fmul_rn(w, c), __fmul_rn(v, s));
@@ -131,20 +131,8 @@ __device__ __forceinline__ void turn(float& v, float& w, float c, float s) {
 template <int N>
 __device__ __forceinline__ void turn_chunks(float (&fx)[N], float (&fy)[N], const float (&cs)[2 * N], const Place& p) {
   if (p.pair) {
-    if constexpr (N == 1) {
-      turn(fx[0], fy[0], cs[0], cs[1]);
-    } else {
 #pragma unroll
-      for (int k = 0; k < N; k += 2) {  // two at a time; minus the second product is exact
-        const float2 v = make_float2(fx[k], fx[k + 1]), w = make_float2(fy[k], fy[k + 1]);
-        const float2 c = make_float2(cs[2 * k], cs[2 * k + 2]), sn = make_float2(cs[2 * k + 1], cs[2 * k + 3]);
-        const float2 ws = mul2(w, sn), x = add2(mul2(v, c), make_float2(-ws.x, -ws.y)), y = add2(mul2(w, c), mul2(v, sn));
-        fx[k] = x.x;
-        fx[k + 1] = x.y;
-        fy[k] = y.x;
-        fy[k + 1] = y.y;
-      }
-    }
+    for (int k = 0; k < N; ++k) turn(fx[k], fy[k], cs[2 * k], cs[2 * k + 1]);
   } else if (N > 1 && p.inside) {
 #pragma unroll
     for (int k = 0; k + 1 < N; k += 2) turn(fx[k], fx[k + 1], cs[k], cs[k + 1]);
