@@ -645,7 +645,8 @@ retrace_status retrace_attend_fp8(const void* q, int64_t q_token_stride, int64_t
  *                as the other calls take it.  May be NULL if slots is.
  *   slots        [T] int64 out, optional: page * page_size + slot of each new token's
  *                position, -1 where it has no place, and behind the last sequence's
- *                tokens.
+ *                tokens.  For what the caller keeps by slot itself: the other calls
+ *                find places through the page table.
  * page_table, held and free_pages hold what a call leaves there; other values give
  * unspecified ones, within the arrays.  T is not read without slots and q_start. */
 retrace_status retrace_kv_reserve(const int32_t* cache_len, const int32_t* new_len, int B, int page_size,

@@ -28,10 +28,10 @@
 // products are 4 (2 rows + 3 rows) cycles at D = 128, shared memory moves some 1100 cycles' worth at
 // 72 rows, and the softmax does 128 rows exponentials: with few rows on the N side all of
 // it scales with the rows that there are.
-// A tile of D = 128 and 16-slot pages takes an SM 730 ns with 4 to 32 rows (6.8 TB/s: bound by HBM), 1125 ns with
-// 68 (4.4 TB/s): there the issue slots are 54 % taken and the tensor cores 28 %; a third of the warps' time is
-// the chain of a tile (scores from TMEM, the group's agreement, exponentials, parts) without another one to fill it.
-// A unit costs 2 us (8 rows) to 7 us (68) besides its tiles.
+// A tile of D = 128 and 16-slot pages takes an SM 705 ns with 4 or 8 rows, 730 with 16, 750 with 32 (7.0 to 6.6 TB/s:
+// bound by HBM), 980 ns with 48 and 1155 with 68 (4.3 TB/s): there the issue slots are 52 % taken and the tensor
+// cores 27 %; a third of the warps' time is the chain of a tile (scores from TMEM, the group's agreement, exponentials,
+// parts) without another one to fill it.  A unit costs 2.7 us (4 to 16 rows), 4.6 us (32) or 7 us (48, 68) besides its tiles.
 //
 // Warps of a CTA: copies of K and of V (TMA boxes of the slots of a page), the products, the queries
 // (taken apart a piece ahead), and the softmax in groups of four warps, a thread to a key.  Up to 32

@@ -1,4 +1,5 @@
-// Two fp32 operations as one instruction.
+// Two fp32 operations as one instruction.  The assembler may join a product and a sum that takes it into one rounding:
+// where each has to be rounded, __fmul_rn and __fadd_rn.
 #pragma once
 
 #include <stdint.h>
